@@ -295,7 +295,7 @@ def _prepare_logits(case, seed):
             x[r:r + 256].masked_fill_((token + shift[r:r + 256, None]) % V >= int(case["allowed"] * V), -math.inf)
     x[torch.arange(N, device="cuda"), target] = boost.to(x.dtype)
     st = dict(case=case, x=x, target=target, logp=torch.empty(N, device="cuda"), entropy=torch.empty(N, device="cuda"),
-              lse=torch.empty(N, device="cuda"))
+              lse=torch.empty(N, device="cuda"), stats=torch.empty(N, 2, device="cuda"))
     if case["kind"] == "train":
         st.update(d_logp=torch.randn(N, generator=g, device="cuda") / N, d_entropy=torch.full((N,), 0.01 / N, device="cuda"),
                   dx=torch.empty_like(x))
@@ -465,12 +465,12 @@ def _own(st):
         cp.cpes_pages_compact(st["cache"], st["pool"], st["packed"], st["ws"], moved=st["moved"])
         return {"table": st["table2"], "refs": st["refs2"], "lengths": st["lengths2"], "moved": st["moved"],
                 "k": st["k"], "v": st["v"]}
-    cp.cpes_logprobs(st["x"], st["target"], st["logp"], entropy=st["entropy"], lse=st["lse"], top_logp=st.get("top_logp"),
-                     top_ids=st.get("top_ids"), scale=case["scale"], workspace=st["ws"])
+    cp.cpes_logprobs(st["x"], st["target"], st["logp"], entropy=st["entropy"], lse=st["lse"], stats=st["stats"],
+                     top_logp=st.get("top_logp"), top_ids=st.get("top_ids"), scale=case["scale"], workspace=st["ws"])
     out = {"logp": st["logp"], "entropy": st["entropy"], "lse": st["lse"]}
     if kind == "score":
         return dict(out, top_logp=st["top_logp"], top_ids=st["top_ids"])
-    cp.cpes_logprobs_backward(st["x"], st["target"], st["lse"], st["entropy"], st["d_logp"], st["d_entropy"], st["dx"],
+    cp.cpes_logprobs_backward(st["x"], st["target"], st["stats"], st["entropy"], st["d_logp"], st["d_entropy"], st["dx"],
                               scale=case["scale"])
     return dict(out, dx=st["dx"])
 
