@@ -87,6 +87,9 @@ enum cpes_scale_mode { CPES_SCALE_ALPHA_OVER_N_SIGMA = 0, CPES_SCALE_ALPHA_OVER_
 #define CPES_MAX_PERMUTATION_K 256   /* subspaces of a CPES_PART_PERMUTATION partition */
 #define CPES_MAX_STEP_SUBSPACES 32   /* subspaces per cpes_update_step call */
 #define CPES_STATIC_MAX_CHUNKS (1 << 20) /* chunks per cpes_partition_chunks_static call */
+#define CPES_MAX_HEAD_DIM 256        /* head dimension of a cpes_cache */
+#define CPES_MAX_ALTERNATIVES 64     /* most likely tokens cpes_logprobs lists per row */
+#define CPES_MAX_SEQUENCES (1 << 20) /* sequences listed per cpes_pages_* call, rows per cpes_attend call */
 
 typedef struct cpes_subspace {
     int64_t offset;          /* first parameter (no map) or first map entry */
@@ -394,6 +397,237 @@ CPES_API int cpes_update_step32(void* w_dev, int64_t numel, int dtype, int32_t K
                                 const uint32_t* index32_dev, int32_t n, const uint64_t* seeds_host,
                                 const int8_t* signs_host, const int32_t* subspace_host, const float* rnorm_dev,
                                 float alpha, const float* sigma_host, int scale_mode, void* stream);
+
+/* ---------------- evaluating a member ----------------------------------- *
+ *
+ * Between a member's perturbation and its restore the perturbed model is
+ * evaluated: rollouts are generated token by token and their tokens scored.
+ * The calls below are that evaluation's operators next to the model's plain
+ * matrix products.  The conventions are those above; in addition:
+ *   - sequence lengths, page tables and reference counts live in device
+ *     memory and are read there when the work runs, so a captured graph can be
+ *     replayed as sequences grow.  Nothing on the device is trusted to address
+ *     memory: page ids outside [0, pages), sequence ids outside [0, sequences)
+ *     and lengths beyond the table are caught there, as each call says.
+ *   - tensors start at any element; only cpes_cache has a rule for its rows. */
+
+/*
+ * Keys and values of `layers` layers in pages of `page_size` tokens.  Element d
+ * of token t of head h in page p of layer l is at
+ *   l * layer_stride + p * page_stride + h * head_stride + t * token_stride + d
+ * (in elements, the same for keys and values), so pages may be head-major,
+ * token-major or hold keys beside values.  head_dim: a multiple of 8 up to
+ * CPES_MAX_HEAD_DIM; strides not negative.  Different (l, p, h, t) must not
+ * overlap.
+ */
+typedef struct cpes_cache {
+    void* k_dev;
+    void* v_dev;
+    int64_t layer_stride;
+    int64_t page_stride;
+    int64_t head_stride;
+    int64_t token_stride;
+    int32_t layers;
+    int32_t pages;
+    int32_t heads;          /* key-value heads */
+    int32_t page_size;      /* tokens per page, any number >= 1 */
+    int32_t head_dim;
+    int32_t dtype;          /* CPES_BF16 or CPES_F32 */
+} cpes_cache;
+
+/*
+ * The pages of `sequences` sequences: token j of sequence s lies in slot j %
+ * page_size of page table[s * table_stride + j / page_size], j < lengths[s].
+ * refs[p] counts the sequences that hold page p; a page is free while it is
+ * not positive.  Entries of the table behind a sequence's last page mean
+ * nothing.  A page held by several sequences is full: only the last, partly
+ * filled page of a sequence is ever written to, and cpes_pages_fork copies it.
+ */
+typedef struct cpes_pool {
+    int32_t* table_dev;     /* int32[sequences * table_stride] */
+    int32_t* lengths_dev;   /* int32[sequences] */
+    int32_t* refs_dev;      /* int32[pages]; NULL for calls that only read the cache through the table */
+    int64_t table_stride;   /* >= width */
+    int32_t sequences;
+    int32_t width;          /* pages a sequence can hold */
+    int32_t pages;
+    int32_t page_size;
+} cpes_pool;
+
+/* What the page calls report in status_dev (NULL, or a device int32). */
+enum cpes_pages_status {
+    CPES_PAGES_OK = 0,
+    CPES_PAGES_SHORT = 1,       /* not enough free pages: nothing was changed */
+    CPES_PAGES_BAD_SEQUENCE = 2 /* a sequence id, length or state the call does not allow: nothing was changed */
+};
+
+/* Workspace bytes of cpes_pages_reserve, cpes_pages_fork and cpes_pages_compact
+ * on a pool of `pages` pages; 0 for pages < 1. */
+CPES_API size_t cpes_pages_workspace_bytes(int32_t pages);
+
+/*
+ * cpes_pages_reserve -- room for the next tokens: sequence seqs[i] grows to
+ * new_lengths[i] tokens (device int32[n] each).  The pages it lacks are the
+ * free pages of lowest id, handed out in the order of the list; a length not
+ * above the present one leaves the sequence as it is.  All or nothing: too few
+ * free pages give status CPES_PAGES_SHORT, a sequence id out of range or listed
+ * twice, or a length that is negative or beyond the table's width,
+ * CPES_PAGES_BAD_SEQUENCE, and then nothing has changed.
+ * Errors: null pointers, n < 0, n > sequences -> CPES_ERR_INVALID_ARGUMENT; n above
+ *   CPES_MAX_SEQUENCES -> CPES_ERR_UNSUPPORTED; workspace too small or not 16-byte
+ *   aligned -> CPES_ERR_WORKSPACE.
+ */
+CPES_API int cpes_pages_reserve(const cpes_pool* pool, int32_t n, const int32_t* seqs_dev,
+                                const int32_t* new_lengths_dev, void* workspace_dev, size_t workspace_bytes,
+                                int32_t* status_dev, void* stream);
+
+/*
+ * cpes_pages_fork -- children[i], an empty sequence (length 0), becomes a copy of
+ * parents[i] (device int32[n] each; a parent may occur many times): full pages
+ * are shared and their reference counts raised, a partly filled last page is
+ * copied, in every layer of the cache, to the free page of lowest id, handed
+ * out in the order of the list.  All or nothing, as cpes_pages_reserve: a child
+ * that is not empty or listed twice, or an id out of range, gives
+ * CPES_PAGES_BAD_SEQUENCE.  A listed child is no parent in the same call (it
+ * counts as empty).
+ * Errors: as cpes_pages_reserve; a cache that does not fit the pool (pages,
+ *   page size) or breaks the rules of cpes_cache -> CPES_ERR_INVALID_ARGUMENT.
+ */
+CPES_API int cpes_pages_fork(const cpes_cache* cache, const cpes_pool* pool, int32_t n, const int32_t* parents_dev,
+                             const int32_t* children_dev, void* workspace_dev, size_t workspace_bytes,
+                             int32_t* status_dev, void* stream);
+
+/*
+ * cpes_pages_free -- sequences seqs[i] (device int32[n]) give their pages up: each
+ * page's reference count falls by one, their table entries become -1, their
+ * lengths 0.  A sequence listed twice is freed once; ids out of range are
+ * skipped and give CPES_PAGES_BAD_SEQUENCE.
+ * Errors: null pointers, n < 0 -> CPES_ERR_INVALID_ARGUMENT; n above
+ *   CPES_MAX_SEQUENCES -> CPES_ERR_UNSUPPORTED.
+ */
+CPES_API int cpes_pages_free(const cpes_pool* pool, int32_t n, const int32_t* seqs_dev, int32_t* status_dev,
+                             void* stream);
+
+/*
+ * cpes_pages_copy -- page dst[i] of every layer becomes a copy of page src[i]
+ * (device int32[n] each).  Pairs with an id outside [0, pages) are skipped; a
+ * page that is both a source and a destination, or a destination twice, has
+ * undefined contents.
+ * Errors: null pointers, n < 0, a bad cache -> CPES_ERR_INVALID_ARGUMENT.
+ */
+CPES_API int cpes_pages_copy(const cpes_cache* cache, int32_t n, const int32_t* src_dev, const int32_t* dst_dev,
+                             void* stream);
+
+/*
+ * cpes_pages_compact -- the L live pages (refs > 0) move to page ids below L, so
+ * that the rest of the cache can be used for something else (the next weight
+ * backup).  Live pages with ids >= L move, in ascending order, into the free
+ * ids below L in ascending order; all others stay.  `packed` receives the
+ * table, lengths and reference counts with the new ids; its tensors may be
+ * those of `pool` (in place).  moved_dev: NULL, or a device int32 that receives
+ * the number of pages moved.
+ * Errors: null pointers, `packed` of another shape than `pool`, a cache that
+ *   does not fit -> CPES_ERR_INVALID_ARGUMENT; workspace as cpes_pages_reserve.
+ */
+CPES_API int cpes_pages_compact(const cpes_cache* cache, const cpes_pool* pool, const cpes_pool* packed,
+                                void* workspace_dev, size_t workspace_bytes, int32_t* moved_dev, void* stream);
+
+/*
+ * cpes_cache_append -- the keys and values of n new tokens enter their pages in
+ * one layer: token i belongs to sequence seqs[i] (device int32[n]; NULL: i) and
+ * position positions[i] (device int32[n]); element d of head h of token i is
+ * k_new[i * new_stride + h * new_head_stride + d], and the same of v_new.  Bit
+ * copies.  Tokens whose sequence or position is out of range, or whose table
+ * entry names no page, are skipped.  Two tokens at one place leave either.
+ * Errors: null pointers, n < 0, a layer out of range, negative strides, a bad
+ *   cache or a pool that does not fit it -> CPES_ERR_INVALID_ARGUMENT.
+ */
+CPES_API int cpes_cache_append(const cpes_cache* cache, int32_t layer, const cpes_pool* pool, int32_t n,
+                               const int32_t* seqs_dev, const int32_t* positions_dev, const void* k_new_dev,
+                               const void* v_new_dev, int64_t new_stride, int64_t new_head_stride, void* stream);
+
+/* Workspace bytes of cpes_attend for `rows` rows (0 for invalid arguments). */
+CPES_API size_t cpes_attend_workspace_bytes(int32_t rows, int32_t q_heads, int32_t kv_heads, int32_t head_dim);
+
+/*
+ * cpes_attend -- attention of one new token per row over the paged cache of one
+ * layer.  Row r asks for sequence s = seqs[r] (device int32[rows]; NULL: r),
+ * whose newest token, at position n - 1 with n = lengths[s], is the one asking
+ * (its own key and value are in the cache).  It sees the positions
+ *   j < n,  and with window > 0 only  j >= n - window  or  j < sinks.
+ * Query head i of key-value head h = i / (q_heads / heads), q at
+ * q[r * q_stride + i * q_head_stride + d]:
+ *   x_j = scale * sum_d q_d k_j,d;  out_d = sum_j e^(x_j) v_j,d / sum_j e^(x_j);
+ *   lse = ln sum_j e^(x_j)  (lse_dev: NULL, or device float32[rows * q_heads]).
+ * One pass over the keys and values with a running maximum; the maximum, the
+ * sums and the output are held in fp32, and the weights of bf16 values carry 16
+ * bits of mantissa into the matrix instructions.  out has the cache's dtype:
+ * element d of head i of row r at out[r * out_stride + i * out_head_stride + d].
+ * A row that sees nothing (an empty sequence, an id out of range) gets out = 0
+ * and lse = -inf, as does one whose scores are all -inf; positions whose table
+ * entry names no page are not seen.  The result does not depend on the
+ * contents of unseen positions, nor on the run.
+ * workspace: as cpes_attend_workspace_bytes, 16-byte aligned; needs no
+ * particular contents, and calls that overlap in time need their own.
+ * Errors: null pointers, rows < 0, q_heads not a positive multiple of the
+ *   cache's heads, a layer out of range, window or sinks negative, scale not
+ *   finite, negative strides, a bad cache or a pool that does not fit it ->
+ *   CPES_ERR_INVALID_ARGUMENT; rows above CPES_MAX_SEQUENCES ->
+ *   CPES_ERR_UNSUPPORTED; workspace -> CPES_ERR_WORKSPACE.
+ */
+CPES_API int cpes_attend(const cpes_cache* cache, int32_t layer, const cpes_pool* pool, int32_t rows,
+                         const int32_t* seqs_dev, const void* q_dev, int64_t q_stride, int64_t q_head_stride,
+                         int32_t q_heads, float scale, int32_t window, int32_t sinks, void* out_dev,
+                         int64_t out_stride, int64_t out_head_stride, float* lse_dev, void* workspace_dev,
+                         size_t workspace_bytes, void* stream);
+
+/* Workspace bytes of cpes_logprobs (0 for invalid arguments). */
+CPES_API size_t cpes_logprobs_workspace_bytes(int32_t rows, int32_t vocab, int32_t top);
+
+/*
+ * cpes_logprobs -- scores of given tokens under rows of logits x (`dtype`, row r
+ * at x + r * stride, `vocab` entries), with z = scale * x (scale = 1 /
+ * temperature):
+ *   lse = ln sum_v e^(z_v);  logp = z_target - lse;  entropy = -sum_v p_v ln p_v,
+ *   p_v = e^(z_v - lse);
+ *   alternatives: the `top` tokens of largest x in descending order, ties by the
+ *   lowest token, and their log probabilities.
+ * targets_dev: device int64[rows]; a target outside [0, vocab) scores 0.
+ * logp_dev, entropy_dev, lse_dev: NULL, or device float32[rows].
+ * stats_dev: NULL, or device float32[2 * rows]: max x and ln sum_v e^(z_v - scale
+ *   max x), what cpes_logprobs_backward needs.
+ * top_logp_dev / top_ids_dev: device float32 / int64[rows * top] (NULL with top
+ *   = 0); entries behind the vocabulary's end are -inf and -1.
+ * Each logit is read once.  Sums are fp32 within a thread and a workgroup.
+ * Logits of -inf have probability 0; a row of nothing but -inf has lse = -inf,
+ * entropy 0 and log probabilities -inf.  A NaN or +inf makes the row's numbers
+ * NaN and its alternatives -1.
+ * Errors: x NULL, rows < 0, vocab < 1, stride < vocab with more than one row,
+ *   scale not positive and finite, logp without targets, top outside [0,
+ *   CPES_MAX_ALTERNATIVES] or without both outputs -> CPES_ERR_INVALID_ARGUMENT;
+ *   workspace -> CPES_ERR_WORKSPACE.
+ */
+CPES_API int cpes_logprobs(const void* x_dev, int dtype, int32_t rows, int32_t vocab, int64_t stride, float scale,
+                           const int64_t* targets_dev, float* logp_dev, float* entropy_dev, float* lse_dev,
+                           float* stats_dev, int32_t top, float* top_logp_dev, int64_t* top_ids_dev,
+                           void* workspace_dev, size_t workspace_bytes, void* stream);
+
+/*
+ * cpes_logprobs_backward -- the gradient of cpes_logprobs' logp and entropy with
+ * respect to the logits:
+ *   dx_v = scale * (d_logp * ([v = target] - p_v) - d_entropy * p_v (ln p_v + entropy)),
+ * from the forward call's stats and entropy and the upstream gradients d_logp,
+ * d_entropy (device float32[rows]; either may be NULL, for zero).  dx has the
+ * dtype of x, row r at dx + r * dx_stride, and may be x itself.  The targets
+ * of rows outside [0, vocab) give no gradient of logp, a row of nothing but -inf
+ * gives 0.  Computed in fp32, rounded once.
+ * Errors: null pointers (targets needed with d_logp, entropy with d_entropy),
+ *   sizes and scale as cpes_logprobs -> CPES_ERR_INVALID_ARGUMENT.
+ */
+CPES_API int cpes_logprobs_backward(const void* x_dev, int dtype, int32_t rows, int32_t vocab, int64_t stride,
+                                    float scale, const int64_t* targets_dev, const float* stats_dev,
+                                    const float* entropy_dev, const float* d_logp_dev, const float* d_entropy_dev,
+                                    void* dx_dev, int64_t dx_stride, void* stream);
 
 /* ---------------- test hooks and measurement utilities ------------------ */
 

@@ -23,12 +23,17 @@ NORM_Z, NORM_RANK = 0, 1
 SCALE_ALPHA_OVER_N_SIGMA, SCALE_ALPHA_OVER_N = 0, 1
 SUB_ASCENDING = 1
 MAX_MEMBERS, MAX_REWARDS, MAX_GROUPS, MAX_PERMUTATION_K, MAX_STEP_SUBSPACES = 256, 4096, 1024, 256, 32
+MAX_HEAD_DIM, MAX_ALTERNATIVES, MAX_SEQUENCES = 256, 64, 1 << 20
+PAGES_OK, PAGES_SHORT, PAGES_BAD_SEQUENCE = 0, 1, 2
 
 EXPORTED = (
     "cpes_partition", "cpes_partition32", "cpes_partition_workspace_bytes", "cpes_partition_chunks",
     "cpes_partition_chunks_workspace_bytes", "cpes_partition_chunks_static", "cpes_perturb", "cpes_restore", "cpes_backup",
     "cpes_backup_to_host", "cpes_restore_from_host", "cpes_stage_master", "cpes_normalize_rewards",
-    "cpes_update", "cpes_update_step", "cpes_update_step32", "cpes_debug_philox", "cpes_debug_normals", "cpes_debug_bm_grid",
+    "cpes_update", "cpes_update_step", "cpes_update_step32", "cpes_pages_workspace_bytes", "cpes_pages_reserve",
+    "cpes_pages_fork", "cpes_pages_free", "cpes_pages_copy", "cpes_pages_compact", "cpes_cache_append",
+    "cpes_attend_workspace_bytes", "cpes_attend", "cpes_logprobs_workspace_bytes", "cpes_logprobs",
+    "cpes_logprobs_backward", "cpes_debug_philox", "cpes_debug_normals", "cpes_debug_bm_grid",
     "cpes_debug_prp", "cpes_rng_probe", "cpes_probe_map_copy", "cpes_probe_copy", "cpes_fill_normal",
     "cpes_last_error", "cpes_abi_version",
 )
@@ -46,6 +51,19 @@ class Subspace(ctypes.Structure):
                 ("flags", ctypes.c_int64)]
 
 
+class Cache(ctypes.Structure):
+    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("layer_stride", ctypes.c_int64),
+                ("page_stride", ctypes.c_int64), ("head_stride", ctypes.c_int64), ("token_stride", ctypes.c_int64),
+                ("layers", ctypes.c_int32), ("pages", ctypes.c_int32), ("heads", ctypes.c_int32),
+                ("page_size", ctypes.c_int32), ("head_dim", ctypes.c_int32), ("dtype", ctypes.c_int32)]
+
+
+class Pool(ctypes.Structure):
+    _fields_ = [("table", ctypes.c_void_p), ("lengths", ctypes.c_void_p), ("refs", ctypes.c_void_p),
+                ("table_stride", ctypes.c_int64), ("sequences", ctypes.c_int32), ("width", ctypes.c_int32),
+                ("pages", ctypes.c_int32), ("page_size", ctypes.c_int32)]
+
+
 _lib = None
 
 
@@ -59,7 +77,7 @@ def load(path: str = LIB_PATH) -> ctypes.CDLL:
     L = ctypes.CDLL(path)
     vp, i64, u64, i32, u32, f32 = (ctypes.c_void_p, ctypes.c_int64, ctypes.c_uint64, ctypes.c_int32,
                                    ctypes.c_uint32, ctypes.c_float)
-    sp = ctypes.POINTER(Subspace)
+    sp, kc, pp, size = ctypes.POINTER(Subspace), ctypes.POINTER(Cache), ctypes.POINTER(Pool), ctypes.c_size_t
     sig = {
         "cpes_partition": [i32, i64, i32, u64, vp, vp, vp, vp, ctypes.c_size_t, vp, vp],
         "cpes_partition32": [i64, i32, u64, vp, vp, vp, ctypes.c_size_t, vp, vp],
@@ -77,6 +95,18 @@ def load(path: str = LIB_PATH) -> ctypes.CDLL:
         "cpes_update": [vp, i64, i32, sp, vp, i32, vp, vp, vp, f32, f32, i32, vp],
         "cpes_update_step": [vp, i64, i32, i32, vp, vp, i64, vp, i32, vp, vp, vp, vp, f32, vp, i32, vp],
         "cpes_update_step32": [vp, i64, i32, i32, vp, vp, i32, vp, vp, vp, vp, f32, vp, i32, vp],
+        "cpes_pages_workspace_bytes": [i32],
+        "cpes_pages_reserve": [pp, i32, vp, vp, vp, size, vp, vp],
+        "cpes_pages_fork": [kc, pp, i32, vp, vp, vp, size, vp, vp],
+        "cpes_pages_free": [pp, i32, vp, vp, vp],
+        "cpes_pages_copy": [kc, i32, vp, vp, vp],
+        "cpes_pages_compact": [kc, pp, pp, vp, size, vp, vp],
+        "cpes_cache_append": [kc, i32, pp, i32, vp, vp, vp, vp, i64, i64, vp],
+        "cpes_attend_workspace_bytes": [i32, i32, i32, i32],
+        "cpes_attend": [kc, i32, pp, i32, vp, vp, i64, i64, i32, f32, i32, i32, vp, i64, i64, vp, vp, size, vp],
+        "cpes_logprobs_workspace_bytes": [i32, i32, i32],
+        "cpes_logprobs": [vp, i32, i32, i32, i64, f32, vp, vp, vp, vp, vp, i32, vp, vp, vp, size, vp],
+        "cpes_logprobs_backward": [vp, i32, i32, i32, i64, f32, vp, vp, vp, vp, vp, vp, i64, vp],
         "cpes_debug_philox": [u64, u32, u64, i64, vp, vp],
         "cpes_debug_normals": [u64, i64, i64, vp, vp],
         "cpes_debug_bm_grid": [u32, i64, vp, vp, vp, vp],
@@ -92,8 +122,9 @@ def load(path: str = LIB_PATH) -> ctypes.CDLL:
         fn = getattr(L, name)
         fn.argtypes = args
         fn.restype = ctypes.c_int
-    L.cpes_partition_workspace_bytes.restype = ctypes.c_size_t
-    L.cpes_partition_chunks_workspace_bytes.restype = ctypes.c_size_t
+    for name in sig:
+        if name.endswith("_workspace_bytes"):
+            getattr(L, name).restype = ctypes.c_size_t
     L.cpes_last_error.restype = ctypes.c_char_p
     _lib = L
     return L
@@ -411,6 +442,211 @@ def cpes_update_step(w, offsets: Sequence[int], seeds: Sequence[int], signs: Seq
     _check((_lib or load()).cpes_update_step(_dev_ptr(w, "w"), w.numel(), _dtype_code(w), K, co, _dev_ptr(index, "index"),
                                    int(chunk), cl, n, cs, cg, ck, _dev_ptr(rnorm, "rnorm"), alpha, csg, scale_mode,
                                    _stream(stream)))
+
+
+# ------------------------------------------------------ evaluating a member --
+
+def paged_cache(k, v) -> Cache:
+    """A key-value cache in pages: k and v of shape [layers, pages, heads,
+    page_size, head_dim], bfloat16 or float32, with the same strides and the
+    last dimension contiguous (token-major pages are a transposed view)."""
+    if k.dim() != 5 or k.shape != v.shape or k.dtype != v.dtype or k.stride() != v.stride():
+        raise ValueError("keys and values must be [layers, pages, heads, page_size, head_dim] of one shape, dtype and strides")
+    if not (k.is_cuda and v.is_cuda):
+        raise ValueError("keys and values must be GPU tensors")
+    if k.stride(4) != 1 and k.shape[4] > 1:
+        raise ValueError("the head dimension must be contiguous")
+    st = k.stride()
+    cache = Cache(k.data_ptr(), v.data_ptr(), st[0], st[1], st[2], st[3], *k.shape, _dtype_code(k))
+    cache._tensors = (k, v)     # the descriptor holds raw pointers: keep the storage alive with it
+    cache._dtype = k.dtype
+    return cache
+
+
+def page_pool(table, lengths, page_size: int, refs=None) -> Pool:
+    """The pages of sequences: ``table`` int32 [sequences, width] (rows may be
+    further apart), ``lengths`` int32 [sequences], and for the calls that hand
+    pages out or take them back ``refs`` int32 [pages]."""
+    torch = _torch()
+    if table.dim() != 2 or (table.stride(1) != 1 and table.shape[1] > 1):
+        raise ValueError("the page table must be [sequences, width] with contiguous rows")
+    if not table.is_cuda:
+        raise ValueError("the page table must be a GPU tensor")
+    for t, what, n in ((table, "page table", 0), (lengths, "lengths", table.shape[0]), (refs, "refs", 0)):
+        _need(t, what, n, torch.int32)
+    pool = Pool(table.data_ptr(), _dev_ptr(lengths, "lengths"), _dev_ptr(refs, "refs"),
+                max(table.stride(0), table.shape[1]) if table.shape[0] == 1 else table.stride(0), table.shape[0],
+                table.shape[1], 0 if refs is None else refs.numel(), int(page_size))
+    pool._tensors = (table, lengths, refs)
+    return pool
+
+
+def _int32_list(t, what: str, n: Optional[int] = None) -> Optional[int]:
+    """Device pointer of an int32 list (of n entries)."""
+    if t is None:
+        return None
+    if t.dtype != _torch().int32:
+        raise TypeError(f"{what} must have dtype torch.int32, not {t.dtype}")
+    if n is not None and t.numel() < n:
+        raise ValueError(f"{what} holds {t.numel()} elements, {n} needed")
+    return _dev_ptr(t, what)
+
+
+def _floats(t, what: str, n: int) -> Optional[int]:
+    """Device pointer of a float32 tensor of n elements at least, or None."""
+    if t is None:
+        return None
+    _need(t, what, n, _torch().float32)
+    return _dev_ptr(t, what)
+
+
+def _workspace(t):
+    return (None, 0) if t is None else (_dev_ptr(t, "workspace"), t.numel() * t.element_size())
+
+
+def _rows(t, what: str, shape, dtype):
+    """(pointer, row stride, head stride) of a [rows, heads, dim] tensor whose rows and heads may be apart."""
+    if t.dtype != dtype:
+        raise TypeError(f"{what} must have dtype {dtype}, not {t.dtype}")
+    if not t.is_cuda:
+        raise ValueError(f"{what} must be a GPU tensor")
+    if t.shape != shape:
+        raise ValueError(f"{what} has shape {tuple(t.shape)}, {tuple(shape)} needed")
+    st = t.stride()
+    if st[2] != 1 and shape[2] > 1:
+        raise ValueError(f"{what} must be contiguous in its last dimension")
+    return t.data_ptr(), st[0], st[1]
+
+
+def cpes_pages_workspace_bytes(pages: int) -> int:
+    return int(load().cpes_pages_workspace_bytes(pages))
+
+
+def cpes_pages_reserve(pool: Pool, seqs, new_lengths, workspace, status=None, stream=None) -> None:
+    """Sequences seqs[i] grow to new_lengths[i] tokens (all or nothing; ``status``
+    receives PAGES_OK, PAGES_SHORT or PAGES_BAD_SEQUENCE)."""
+    n = seqs.numel()
+    ws, size = _workspace(workspace)
+    _check((_lib or load()).cpes_pages_reserve(ctypes.byref(pool), n, _int32_list(seqs, "seqs"),
+                                               _int32_list(new_lengths, "new_lengths", n), ws, size,
+                                               _int32_list(status, "status", 1), _stream(stream)))
+
+
+def cpes_pages_fork(cache: Cache, pool: Pool, parents, children, workspace, status=None, stream=None) -> None:
+    """Empty sequences children[i] become copies of parents[i]: full pages are
+    shared, a partly filled last page is copied in every layer."""
+    n = children.numel()
+    ws, size = _workspace(workspace)
+    _check((_lib or load()).cpes_pages_fork(ctypes.byref(cache), ctypes.byref(pool), n,
+                                            _int32_list(parents, "parents", n), _int32_list(children, "children"), ws,
+                                            size, _int32_list(status, "status", 1), _stream(stream)))
+
+
+def cpes_pages_free(pool: Pool, seqs, status=None, stream=None) -> None:
+    """Sequences seqs[i] give their pages up."""
+    _check((_lib or load()).cpes_pages_free(ctypes.byref(pool), seqs.numel(), _int32_list(seqs, "seqs"),
+                                            _int32_list(status, "status", 1), _stream(stream)))
+
+
+def cpes_pages_copy(cache: Cache, src, dst, stream=None) -> None:
+    """Page dst[i] of every layer becomes a copy of page src[i]."""
+    n = dst.numel()
+    _check((_lib or load()).cpes_pages_copy(ctypes.byref(cache), n, _int32_list(src, "src", n), _int32_list(dst, "dst"),
+                                            _stream(stream)))
+
+
+def cpes_pages_compact(cache: Cache, pool: Pool, packed: Pool, workspace, moved=None, stream=None) -> None:
+    """The live pages move to the front of the cache; ``packed`` (``pool`` itself,
+    or a pool of the same shape) receives table, lengths and reference counts."""
+    ws, size = _workspace(workspace)
+    _check((_lib or load()).cpes_pages_compact(ctypes.byref(cache), ctypes.byref(pool), ctypes.byref(packed), ws, size,
+                                               _int32_list(moved, "moved", 1), _stream(stream)))
+
+
+def cpes_cache_append(cache: Cache, layer: int, pool: Pool, k_new, v_new, positions, seqs=None, stream=None) -> None:
+    """Keys and values of new tokens ([tokens, heads, head_dim], rows may be apart)
+    enter the pages of sequences seqs[i] (None: i) at positions[i]."""
+    shape = (k_new.shape[0], cache.heads, cache.head_dim)
+    k, row, head = _rows(k_new, "k_new", shape, cache._dtype)
+    v, v_row, v_head = _rows(v_new, "v_new", shape, cache._dtype)
+    if (v_row, v_head) != (row, head):
+        raise ValueError("k_new and v_new must have the same strides")
+    _check((_lib or load()).cpes_cache_append(ctypes.byref(cache), layer, ctypes.byref(pool), shape[0],
+                                              _int32_list(seqs, "seqs", shape[0]),
+                                              _int32_list(positions, "positions", shape[0]), k, v, row, head,
+                                              _stream(stream)))
+
+
+def cpes_attend_workspace_bytes(rows: int, q_heads: int, kv_heads: int, head_dim: int) -> int:
+    return int(load().cpes_attend_workspace_bytes(rows, q_heads, kv_heads, head_dim))
+
+
+def cpes_attend(cache: Cache, layer: int, pool: Pool, q, out, lse=None, seqs=None, scale: Optional[float] = None,
+                window: int = 0, sinks: int = 0, workspace=None, stream=None) -> None:
+    """Attention of the newest token of sequences seqs[r] (None: r) over the cache:
+    q and out are [rows, q_heads, head_dim] (rows and heads may be apart), lse
+    float32 [rows, q_heads]; scale defaults to head_dim ** -0.5."""
+    if q.dim() != 3 or q.shape[2] != cache.head_dim:
+        raise ValueError(f"q must be [rows, q_heads, {cache.head_dim}], not {tuple(q.shape)}")
+    rows, heads = q.shape[0], q.shape[1]
+    qp, q_row, q_head = _rows(q, "q", q.shape, cache._dtype)
+    op, o_row, o_head = _rows(out, "out", q.shape, cache._dtype)
+    ws, size = _workspace(workspace)
+    _check((_lib or load()).cpes_attend(ctypes.byref(cache), layer, ctypes.byref(pool), rows,
+                                        _int32_list(seqs, "seqs", rows), qp, q_row, q_head, heads,
+                                        cache.head_dim ** -0.5 if scale is None else scale, window, sinks, op, o_row,
+                                        o_head, _floats(lse, "lse", rows * heads), ws, size, _stream(stream)))
+
+
+def _logits(x, what: str = "logits"):
+    """(pointer, rows, vocabulary, row stride) of a [rows, vocabulary] tensor whose rows may be apart."""
+    if x.dim() != 2 or (x.stride(1) != 1 and x.shape[1] > 1):
+        raise ValueError(f"{what} must be [rows, vocabulary] with contiguous rows")
+    if not x.is_cuda:
+        raise ValueError(f"{what} must be a GPU tensor")
+    return x.data_ptr(), x.shape[0], x.shape[1], max(x.stride(0), x.shape[1]) if x.shape[0] < 2 else x.stride(0)
+
+
+def cpes_logprobs_workspace_bytes(rows: int, vocab: int, top: int = 0) -> int:
+    return int(load().cpes_logprobs_workspace_bytes(rows, vocab, top))
+
+
+def cpes_logprobs(logits, targets, logp, entropy=None, lse=None, stats=None, top_logp=None, top_ids=None,
+                  scale: float = 1.0, workspace=None, stream=None) -> None:
+    """Scores of tokens targets[r] (int64) under logits [rows, vocabulary] times
+    ``scale``: float32 [rows] log probabilities, entropies and normalisers, the
+    float32 [rows, 2] ``stats`` for cpes_logprobs_backward, and the most likely
+    alternatives in float32 / int64 [rows, k] ``top_logp`` and ``top_ids``."""
+    torch = _torch()
+    x, rows, vocab, stride = _logits(logits)
+    _need(targets, "targets", rows, torch.int64)
+    top = 0
+    if top_ids is not None or top_logp is not None:
+        if top_ids is None or top_logp is None or top_ids.dim() != 2 or top_ids.shape[0] != rows or top_logp.shape != top_ids.shape:
+            raise ValueError("top_logp and top_ids must both be [rows, k]")
+        top = top_ids.shape[1]
+        _need(top_ids, "top_ids", rows * top, torch.int64)
+    ws, size = _workspace(workspace)
+    _check((_lib or load()).cpes_logprobs(x, _dtype_code(logits), rows, vocab, stride, scale, _dev_ptr(targets, "targets"),
+                                          _floats(logp, "logp", rows), _floats(entropy, "entropy", rows),
+                                          _floats(lse, "lse", rows), _floats(stats, "stats", 2 * rows), top,
+                                          _floats(top_logp, "top_logp", rows * top), _dev_ptr(top_ids, "top_ids"), ws,
+                                          size, _stream(stream)))
+
+
+def cpes_logprobs_backward(logits, targets, stats, entropy, d_logp, d_entropy, d_logits, scale: float = 1.0,
+                           stream=None) -> None:
+    """d_logits (dtype of the logits, may be them) from the upstream gradients
+    d_logp and d_entropy (float32 [rows], either may be None)."""
+    x, rows, vocab, stride = _logits(logits)
+    dx, d_rows, d_vocab, d_stride = _logits(d_logits, "d_logits")
+    if (d_rows, d_vocab) != (rows, vocab) or d_logits.dtype != logits.dtype:
+        raise ValueError("d_logits must have the shape and dtype of the logits")
+    _need(targets, "targets", rows, _torch().int64)
+    _check((_lib or load()).cpes_logprobs_backward(x, _dtype_code(logits), rows, vocab, stride, scale,
+                                                   _dev_ptr(targets, "targets"), _floats(stats, "stats", 2 * rows),
+                                                   _floats(entropy, "entropy", rows), _floats(d_logp, "d_logp", rows),
+                                                   _floats(d_entropy, "d_entropy", rows), dx, d_stride, _stream(stream)))
 
 
 def cpes_debug_philox(seed: int, domain: int, q0: int, nblocks: int, out, stream=None) -> None:

@@ -10,7 +10,8 @@ ROOT = os.path.dirname(PKG)
 CSRC = os.path.join(PKG, "csrc")
 INCLUDE = os.path.join(ROOT, "include")
 LIB = os.path.join(PKG, "libcpes.so")
-SOURCES = ["cpes_api.hip", "cpes_kernels.hip"]
+SOURCES = ["cpes_api.hip", "cpes_kernels.hip", "cpes_eval_api.hip", "cpes_pages.hip", "cpes_attend.hip",
+           "cpes_logprobs.hip"]
 ARCH = "gfx950"
 
 HIPCC_FLAGS = [

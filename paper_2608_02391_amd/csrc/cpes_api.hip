@@ -9,22 +9,30 @@
 #include <cstdio>
 #include <cstring>
 #include <mutex>
-#include <string>
 
+#include "cpes_host.hpp"
 #include "cpes_launch.hpp"
 
 namespace {
 
-thread_local std::string g_error;
+// A fixed buffer: reporting an error cannot throw across the C boundary.
+thread_local char g_error[512];
+
+}  // namespace
+
+namespace cpes {
+
+void clear_error()
+{
+    g_error[0] = 0;
+}
 
 int fail(int code, const char* fmt, ...)
 {
-    char buf[512];
     va_list ap;
     va_start(ap, fmt);
-    std::vsnprintf(buf, sizeof buf, fmt, ap);
+    std::vsnprintf(g_error, sizeof g_error, fmt, ap);
     va_end(ap);
-    g_error = buf;
     return code;
 }
 
@@ -34,10 +42,13 @@ int hip_status(hipError_t e, const char* what)
     return CPES_OK;
 }
 
-bool aligned16(const void* p)
-{
-    return (reinterpret_cast<uintptr_t>(p) & 15u) == 0;
-}
+}  // namespace cpes
+
+namespace {
+
+using cpes::aligned16;
+using cpes::fail;
+using cpes::hip_status;
 
 size_t elem_size(int dtype)
 {
@@ -330,7 +341,7 @@ extern "C" {
 
 const char* cpes_last_error(void)
 {
-    return g_error.c_str();
+    return g_error;
 }
 
 int cpes_abi_version(void)
@@ -350,7 +361,7 @@ size_t cpes_partition_workspace_bytes(int mode, int64_t d, int32_t K)
 int cpes_partition(int mode, int64_t d, int32_t K, uint64_t seed, const int64_t* bounds_host, int64_t* offsets_host,
                    int64_t* index_dev, void* workspace_dev, size_t workspace_bytes, int32_t* status_dev, void* stream)
 {
-    g_error.clear();
+    cpes::clear_error();
     const char* fn = "cpes_partition";
     if (mode != CPES_PART_CONTIGUOUS && mode != CPES_PART_PERMUTATION)
         return fail(CPES_ERR_INVALID_ARGUMENT, "%s: unknown mode %d", fn, mode);
@@ -379,7 +390,7 @@ int cpes_partition(int mode, int64_t d, int32_t K, uint64_t seed, const int64_t*
 int cpes_partition32(int64_t d, int32_t K, uint64_t seed, int64_t* offsets_host, uint32_t* index_dev,
                      void* workspace_dev, size_t workspace_bytes, int32_t* status_dev, void* stream)
 {
-    g_error.clear();
+    cpes::clear_error();
     const char* fn = "cpes_partition32";
     if (d < 1 || d > ((int64_t)1 << 32))
         return fail(CPES_ERR_INVALID_ARGUMENT, "%s: d %lld not in [1, 2^32]", fn, (long long)d);
@@ -401,7 +412,7 @@ int cpes_partition_chunks(int64_t d, int64_t chunk, int32_t K, uint64_t seed, in
                           int64_t* lengths_host, int64_t* chunks_dev, void* workspace_dev, size_t workspace_bytes,
                           int32_t* status_dev, void* stream)
 {
-    g_error.clear();
+    cpes::clear_error();
     const char* fn = "cpes_partition_chunks";
     int rc = check_chunk_partition(d, chunk, K, list_offsets_host, lengths_host, fn);
     if (rc) return rc;
@@ -412,7 +423,7 @@ int cpes_partition_chunks(int64_t d, int64_t chunk, int32_t K, uint64_t seed, in
 int cpes_partition_chunks_static(int64_t d, int64_t chunk, int32_t K, uint64_t seed, int64_t* list_offsets_host,
                                  int64_t* lengths_host, int64_t* chunks_dev, int32_t* status_dev, void* stream)
 {
-    g_error.clear();
+    cpes::clear_error();
     const char* fn = "cpes_partition_chunks_static";
     int rc = check_chunk_partition(d, chunk, K, list_offsets_host, lengths_host, fn);
     if (rc) return rc;
@@ -454,8 +465,9 @@ int chunk_partition(int64_t d, int64_t chunk, int32_t K, uint64_t seed, int64_t*
     int rc = cpes_partition(CPES_PART_PERMUTATION, n_chunks, K, seed, nullptr, list_offsets_host, chunks_dev,
                             workspace_dev, workspace_bytes, status_dev, stream);
     if (rc) {
-        const std::string msg = g_error;
-        return fail(rc, "%s: %s", fn, msg.c_str());
+        char msg[sizeof g_error];
+        std::memcpy(msg, g_error, sizeof msg);
+        return fail(rc, "%s: %s", fn, msg);
     }
     for (int32_t k = 0; k < K; ++k) lengths_host[k] = (list_offsets_host[k + 1] - list_offsets_host[k]) * chunk;
     const int64_t short_by = n_chunks * chunk - d;
@@ -476,7 +488,7 @@ extern "C" {
 int cpes_perturb(void* w_dev, int64_t numel, int dtype, const cpes_subspace* s, float sigma, uint64_t seed,
                  int32_t sign, void* aux_dev, int aux_mode, void* stream)
 {
-    g_error.clear();
+    cpes::clear_error();
     const char* fn = "cpes_perturb";
     int rc = check_subspace(w_dev, numel, dtype, s, fn);
     if (rc) return rc;
@@ -497,7 +509,7 @@ int cpes_perturb(void* w_dev, int64_t numel, int dtype, const cpes_subspace* s, 
 int cpes_restore(void* w_dev, int64_t numel, int dtype, const cpes_subspace* s, float sigma, uint64_t seed,
                  int32_t sign, const void* aux_dev, int aux_mode, void* stream)
 {
-    g_error.clear();
+    cpes::clear_error();
     const char* fn = "cpes_restore";
     int rc = check_subspace(w_dev, numel, dtype, s, fn);
     if (rc) return rc;
@@ -526,7 +538,7 @@ int cpes_restore(void* w_dev, int64_t numel, int dtype, const cpes_subspace* s, 
 int cpes_backup_to_host(const void* w_dev, int64_t numel, int dtype, const cpes_subspace* s, void* backup_host,
                         void* stream)
 {
-    g_error.clear();
+    cpes::clear_error();
     return host_backup_copy(const_cast<void*>(w_dev), numel, dtype, s, backup_host, true, stream,
                             "cpes_backup_to_host");
 }
@@ -534,14 +546,14 @@ int cpes_backup_to_host(const void* w_dev, int64_t numel, int dtype, const cpes_
 int cpes_restore_from_host(void* w_dev, int64_t numel, int dtype, const cpes_subspace* s, const void* backup_host,
                            void* stream)
 {
-    g_error.clear();
+    cpes::clear_error();
     return host_backup_copy(w_dev, numel, dtype, s, const_cast<void*>(backup_host), false, stream,
                             "cpes_restore_from_host");
 }
 
 int cpes_backup(const void* w_dev, int64_t numel, int dtype, const cpes_subspace* s, void* backup_dev, void* stream)
 {
-    g_error.clear();
+    cpes::clear_error();
     const char* fn = "cpes_backup";
     int rc = check_subspace(w_dev, numel, dtype, s, fn);
     if (rc) return rc;
@@ -554,7 +566,7 @@ int cpes_backup(const void* w_dev, int64_t numel, int dtype, const cpes_subspace
 int cpes_stage_master(const void* w_dev, int64_t numel, int dtype, const cpes_subspace* s, float* master_dev,
                       void* stream)
 {
-    g_error.clear();
+    cpes::clear_error();
     const char* fn = "cpes_stage_master";
     int rc = check_subspace(w_dev, numel, dtype, s, fn);
     if (rc) return rc;
@@ -567,7 +579,7 @@ int cpes_stage_master(const void* w_dev, int64_t numel, int dtype, const cpes_su
 int cpes_normalize_rewards(const float* r_dev, int32_t n, int mode, const int32_t* group_dev, int32_t n_groups,
                            float* out_dev, int32_t* status_dev, void* stream)
 {
-    g_error.clear();
+    cpes::clear_error();
     const char* fn = "cpes_normalize_rewards";
     if (!r_dev || !out_dev) return fail(CPES_ERR_INVALID_ARGUMENT, "%s: null reward or output pointer", fn);
     if (n < 1 || n > CPES_MAX_REWARDS) return fail(CPES_ERR_INVALID_ARGUMENT, "%s: n %d not in [1, %d]", fn, n, CPES_MAX_REWARDS);
@@ -593,7 +605,7 @@ int cpes_update(void* w_dev, int64_t numel, int dtype, const cpes_subspace* s, f
                 const uint64_t* seeds_host, const int8_t* signs_host, const float* rnorm_dev, float alpha, float sigma,
                 int scale_mode, void* stream)
 {
-    g_error.clear();
+    cpes::clear_error();
     const char* fn = "cpes_update";
     int rc = check_subspace(w_dev, numel, dtype, s, fn);
     if (rc) return rc;
@@ -740,7 +752,7 @@ int cpes_update_step(void* w_dev, int64_t numel, int dtype, int32_t K, const int
                      const int32_t* subspace_host, const float* rnorm_dev, float alpha, const float* sigma_host,
                      int scale_mode, void* stream)
 {
-    g_error.clear();
+    cpes::clear_error();
     return update_step_impl(w_dev, numel, dtype, K, offsets_host, index_dev, false, chunk, lengths_host, n,
                             seeds_host, signs_host, subspace_host, rnorm_dev, alpha, sigma_host, scale_mode, stream,
                             "cpes_update_step");
@@ -751,7 +763,7 @@ int cpes_update_step32(void* w_dev, int64_t numel, int dtype, int32_t K, const i
                        const int32_t* subspace_host, const float* rnorm_dev, float alpha, const float* sigma_host,
                        int scale_mode, void* stream)
 {
-    g_error.clear();
+    cpes::clear_error();
     if (!index32_dev) return fail(CPES_ERR_INVALID_ARGUMENT, "cpes_update_step32: index32 map is null");
     return update_step_impl(w_dev, numel, dtype, K, offsets_host, index32_dev, true, 0, nullptr, n, seeds_host,
                             signs_host, subspace_host, rnorm_dev, alpha, sigma_host, scale_mode, stream,
@@ -760,7 +772,7 @@ int cpes_update_step32(void* w_dev, int64_t numel, int dtype, int32_t K, const i
 
 int cpes_fill_normal(void* w_dev, int64_t n, int dtype, uint64_t seed, uint32_t domain, float stddev, void* stream)
 {
-    g_error.clear();
+    cpes::clear_error();
     const char* fn = "cpes_fill_normal";
     if (dtype != CPES_BF16 && dtype != CPES_F32) return fail(CPES_ERR_INVALID_ARGUMENT, "%s: unknown dtype %d", fn, dtype);
     if (n < 0) return fail(CPES_ERR_INVALID_ARGUMENT, "%s: n %lld is negative", fn, (long long)n);
@@ -773,7 +785,7 @@ int cpes_fill_normal(void* w_dev, int64_t n, int dtype, uint64_t seed, uint32_t 
 
 int cpes_debug_philox(uint64_t seed, uint32_t domain, uint64_t q0, int64_t nblocks, uint32_t* out_dev, void* stream)
 {
-    g_error.clear();
+    cpes::clear_error();
     if (!out_dev || nblocks < 0) return fail(CPES_ERR_INVALID_ARGUMENT, "cpes_debug_philox: bad output or count");
     if (nblocks == 0) return CPES_OK;
     return hip_status(cpes::launch_debug_philox(seed, domain, q0, nblocks, out_dev, (hipStream_t)stream), "cpes_debug_philox");
@@ -781,7 +793,7 @@ int cpes_debug_philox(uint64_t seed, uint32_t domain, uint64_t q0, int64_t nbloc
 
 int cpes_debug_normals(uint64_t seed, int64_t j0, int64_t n, float* out_dev, void* stream)
 {
-    g_error.clear();
+    cpes::clear_error();
     if (!out_dev || n < 0 || j0 < 0) return fail(CPES_ERR_INVALID_ARGUMENT, "cpes_debug_normals: bad output, j0 or count");
     if (n == 0) return CPES_OK;
     return hip_status(cpes::launch_debug_normals(seed, j0, n, out_dev, (hipStream_t)stream), "cpes_debug_normals");
@@ -789,7 +801,7 @@ int cpes_debug_normals(uint64_t seed, int64_t j0, int64_t n, float* out_dev, voi
 
 int cpes_debug_bm_grid(uint32_t m0, int64_t n, double* rho_dev, double* cos_dev, double* sin_dev, void* stream)
 {
-    g_error.clear();
+    cpes::clear_error();
     if (n < 0 || m0 < 1 || (int64_t)m0 + n - 1 > ((int64_t)1 << 24))
         return fail(CPES_ERR_INVALID_ARGUMENT, "cpes_debug_bm_grid: grid outside [1, 2^24]");
     if (n == 0) return CPES_OK;
@@ -799,7 +811,7 @@ int cpes_debug_bm_grid(uint32_t m0, int64_t n, double* rho_dev, double* cos_dev,
 int cpes_debug_prp(uint64_t seed, int64_t d, int32_t K, int64_t i0, int64_t n, int64_t* perm_dev, int32_t* bucket_dev,
                    void* stream)
 {
-    g_error.clear();
+    cpes::clear_error();
     if (d < 1 || d >= ((int64_t)1 << 55) || K < 1 || K > CPES_MAX_PERMUTATION_K || (int64_t)K > d || i0 < 0 || n < 0 ||
         i0 + n > d)
         return fail(CPES_ERR_INVALID_ARGUMENT, "cpes_debug_prp: bad d, K or range");
@@ -812,7 +824,7 @@ int cpes_debug_prp(uint64_t seed, int64_t d, int32_t K, int64_t i0, int64_t n, i
 int cpes_probe_map_copy(void* w_dev, int64_t numel, int dtype, const cpes_subspace* s, void* buf_dev, int direction,
                         void* stream)
 {
-    g_error.clear();
+    cpes::clear_error();
     const char* fn = "cpes_probe_map_copy";
     int rc = check_subspace(w_dev, numel, dtype, s, fn);
     if (rc) return rc;
@@ -828,7 +840,7 @@ int cpes_probe_map_copy(void* w_dev, int64_t numel, int dtype, const cpes_subspa
 
 int cpes_probe_copy(const void* src_dev, void* dst_dev, int64_t bytes, int nontemporal, void* stream)
 {
-    g_error.clear();
+    cpes::clear_error();
     const char* fn = "cpes_probe_copy";
     if (!src_dev || !dst_dev) return fail(CPES_ERR_INVALID_ARGUMENT, "%s: null pointer", fn);
     if (bytes < 0 || (bytes & 15) != 0)
@@ -841,7 +853,7 @@ int cpes_probe_copy(const void* src_dev, void* dst_dev, int64_t bytes, int nonte
 
 int cpes_rng_probe(uint64_t seed, int64_t n, uint32_t* sink_dev, void* stream)
 {
-    g_error.clear();
+    cpes::clear_error();
     if (!sink_dev || n < 0) return fail(CPES_ERR_INVALID_ARGUMENT, "cpes_rng_probe: bad sink or count");
     return hip_status(cpes::launch_rng_probe(seed, n, sink_dev, (hipStream_t)stream), "cpes_rng_probe");
 }

@@ -1,0 +1,616 @@
+// cpes_attend.hip -- gfx950 kernels of the attention of one new token per row
+// over a paged key-value cache.
+//
+// Mathematics.  For the heads i of one key-value head, with x_ij = scale q_i k_j:
+//   m_i = max_j x_ij,  l_i = sum_j e^(x_ij - m_i),  o_i = sum_j e^(x_ij - m_i) v_j,
+// kept for the positions seen so far and rescaled by e^(m_old - m_new) when the
+// maximum grows; pieces (m, l, o) of any split of the positions join the same
+// way, out = o / l and lse = m + ln l.
+//
+// What bounds it: every key and value is read once, 2 D elements for 4 D
+// operations per query head, far below what the matrix instructions do; the
+// kernel is a stream from HBM, so the work is arranged for many wide loads in
+// flight and none of it waits on another wave.
+//
+// Tiles.  A wave takes 32 positions (16 in fp32), about 16 KiB at D = 128.
+// Scores come out of the matrix instructions transposed, S^T = K Q^T with the
+// positions as rows: lane l then holds, for query head l % 16, positions
+// 4 (l / 16) .. + 3 of each 16, which is just where the second product
+// O^T = V^T P^T wants its right operand, whose inner index may be numbered at
+// will as long as V's rows are numbered alike.  So the weights never leave their
+// lane, and m, l and the rescaling are per lane.  A lane loads 16 bytes of keys
+// (rows of 64 bytes per load and position) and whole 16-byte pieces of its
+// positions' values, dims D/16 (l % 16) .., and in bf16 pairs two positions'
+// values with one byte permutation per two elements: no shared memory and no
+// transposition anywhere in the loop.  The weights of a bf16 cache go in as a
+// bf16 value and its bf16 remainder, 16 bits of mantissa for one more matrix
+// instruction in a kernel that has them to spare; scores, maxima, sums and
+// outputs are fp32.
+//
+// Split.  All rows' tiles, for every key-value head, form one line, cut into equal
+// shares, one per workgroup, whatever the lengths: a workgroup's share may end
+// one row and begin others.  A row (and head) that lies in one share is written
+// by its workgroup; otherwise each workgroup leaves its piece, and a second
+// launch joins the pieces in order, so the result does not depend on timing.
+#include <algorithm>
+#include <type_traits>
+
+#include "cpes_eval.hpp"
+
+namespace cpes {
+
+namespace {
+
+typedef unsigned int V4u __attribute__((ext_vector_type(4)));
+typedef unsigned int V2u __attribute__((ext_vector_type(2)));
+typedef float V4f __attribute__((ext_vector_type(4)));
+typedef __bf16 V8bf __attribute__((ext_vector_type(8)));
+typedef V4u V4uAnywhere __attribute__((aligned(2)));          // caches and queries start at any element
+typedef V2u V2uAnywhere __attribute__((aligned(2)));
+
+constexpr int kWaves = 4;
+constexpr int kThreads = 64 * kWaves;
+constexpr float kLog2e = 1.44269504088896340736f;
+
+template <typename T> struct Tile;
+template <> struct Tile<uint16_t> { static constexpr int n = 32; };
+template <> struct Tile<float> { static constexpr int n = 16; };
+
+// Tiles of one row: [0, sinks_tiles) from position 0 on, the rest from `from`.
+struct Row {
+    int32_t n;            // its tokens
+    int32_t sink_tiles;
+    int32_t from;
+    int32_t tiles;        // at least one: an empty row is written too
+    int32_t seq;
+};
+
+template <int TILE>
+__device__ __forceinline__ Row row_at(const AttendArgs& a, int32_t r)
+{
+    Row x;
+    x.seq = a.seqs ? a.seqs[r] : r;
+    x.n = 0;
+    if (x.seq >= 0 && x.seq < a.sequences) {
+        const int64_t cap = (int64_t)a.width * a.page_size;
+        const int32_t most = cap > INT32_MAX - 64 ? INT32_MAX - 64 : (int32_t)cap;
+        x.n = min(max(a.lengths[x.seq], 0), most);
+    }
+    x.sink_tiles = 0;
+    x.from = 0;
+    if (a.window > 0 && x.n > a.window) {
+        const int32_t begin = (x.n - a.window) / TILE, sinks = min((a.sinks - 1) / TILE + (a.sinks > 0), begin);
+        // where the sinks reach the window's first tile there is nothing to leave out
+        if (sinks < begin) {
+            x.sink_tiles = sinks;
+            x.from = begin * TILE;
+        }
+    }
+    x.tiles = max(1, x.sink_tiles + (x.n - x.from + TILE - 1) / TILE);
+    return x;
+}
+
+// e^x for x <= 0: the hardware's 2^x.  Scores and maxima stay in natural units,
+// so that lse loses nothing on a way through base 2.
+__device__ __forceinline__ float exp_hw(float x) { return __builtin_amdgcn_exp2f(x * kLog2e); }
+
+// The larger of the four lanes that hold one query head's scores.
+__device__ __forceinline__ float max_over_lanes(float x)
+{
+    x = fmaxf(x, __shfl_xor(x, 16));
+    return fmaxf(x, __shfl_xor(x, 32));
+}
+__device__ __forceinline__ float sum_over_lanes(float x)
+{
+    x += __shfl_xor(x, 16);
+    return x + __shfl_xor(x, 32);
+}
+
+// (page, slot) of a position; page -1 where the table has none.
+__device__ __forceinline__ int32_t page_at(const AttendArgs& a, const int32_t* table, int32_t pos, int32_t* slot)
+{
+    const int32_t at = a.page_shift >= 0 ? pos >> a.page_shift : pos / a.page_size;
+    *slot = pos - at * a.page_size;
+    const int32_t page = at < a.width ? table[at] : -1;
+    return page < a.pages ? page : -1;
+}
+
+// Where the positions of one tile lie: element offsets of their rows from the
+// head's first, and which are seen (bit j: position j of the tile).
+//   kWhole: 16 positions share a page (its size is a multiple of 16), so a lane's
+//   rows are a wave's base plus a fixed offset; otherwise each lane keeps the
+//   rows of positions l % 16 and 16 + l % 16 and asks other lanes for the rest.
+// Positions that are not seen point at some row of the cache, so that every
+// load is inside it.
+template <typename T, bool kWhole> struct Places {
+    static constexpr int SUB = Tile<T>::n / 16;
+    int64_t base[SUB];
+    uint32_t seen;
+};
+
+template <typename T, bool kWhole>
+__device__ __forceinline__ Places<T, kWhole> places(const AttendArgs& a, const Row& row, const int32_t* table,
+                                                    int32_t pos0, int lane)
+{
+    Places<T, kWhole> p;
+    p.seen = 0;
+#pragma unroll
+    for (int u = 0; u < Places<T, kWhole>::SUB; ++u) {
+        if constexpr (kWhole) {
+            const int32_t pos = pos0 + 16 * u;
+            int32_t slot = 0, page = -1;
+            if (pos < row.n) page = page_at(a, table, pos, &slot);
+            page = __builtin_amdgcn_readfirstlane(page);
+            slot = __builtin_amdgcn_readfirstlane(slot);
+            p.base[u] = max(page, 0) * a.page_stride + slot * a.token_stride;
+            if (page >= 0) p.seen |= 0xFFFFu << (16 * u);
+        } else {
+            const int32_t pos = pos0 + 16 * u + (lane & 15);
+            int32_t slot = 0, page = -1;
+            if (pos < row.n) page = page_at(a, table, pos, &slot);
+            p.base[u] = max(page, 0) * a.page_stride + slot * a.token_stride;
+            p.seen |= (uint32_t)(__ballot(page >= 0) & 0xFFFF) << (16 * u);
+        }
+    }
+    const int32_t left = row.n - pos0;
+    if (left < 32) p.seen &= left > 0 ? (1u << left) - 1u : 0u;
+    if (a.window > 0) {
+        // seen: before `sinks`, or from n - window on
+        const int32_t skip = row.n - a.window - pos0, sinks = a.sinks - pos0;
+        uint32_t keep = skip <= 0 ? ~0u : skip >= 32 ? 0u : ~0u << skip;
+        if (sinks > 0) keep |= sinks >= 32 ? ~0u : (1u << sinks) - 1u;
+        p.seen &= keep;
+    }
+    return p;
+}
+
+template <typename T, int DP> struct Layout;
+// bf16: 8 elements of a key row per load; a lane's part of a value row
+template <int DP> struct Layout<uint16_t, DP> {
+    static constexpr int KV = DP / 32;            // key loads of 16 bytes per 16 positions
+    static constexpr int VE = DP / 16;            // value elements of a lane's positions
+    static constexpr int VD = DP / 32;            // their dwords
+};
+template <int DP> struct Layout<float, DP> {
+    static constexpr int KV = DP / 16;
+    static constexpr int VE = DP / 16;
+    static constexpr int VD = DP / 16;
+};
+
+// One wave's state over the positions it has seen.
+template <int DP> struct State {
+    float m, l;              // of query head lane % 16; l is this lane's share
+    V4f o[DP / 16];          // o[b][r]: dim DP/16 * (4 (lane / 16) + r) + b
+};
+
+template <typename T, int DP, bool kWhole> struct Work {
+    typedef Layout<T, DP> L;
+    static constexpr int TILE = Tile<T>::n, SUB = TILE / 16, VROWS = TILE / 4;
+
+    V4u key[SUB][L::KV];
+    uint32_t val[VROWS][L::VD];
+
+    // Row offset of value row j of this lane: position 4 (lane / 16) + j % 4 of the tile's 16 j / 4.
+    static __device__ __forceinline__ int64_t value_row(const AttendArgs& a, const Places<T, kWhole>& p, int j, int lane)
+    {
+        const int in16 = 4 * (lane >> 4) + (j & 3);
+        if constexpr (kWhole) return p.base[j >> 2] + in16 * a.token_stride;
+        const uint64_t x = (uint64_t)p.base[j >> 2];
+        const uint32_t lo = __shfl((uint32_t)x, in16), hi = __shfl((uint32_t)(x >> 32), in16);
+        return (int64_t)(((uint64_t)hi << 32) | lo);
+    }
+
+    __device__ __forceinline__ void load_keys(const AttendArgs& a, const T* head, const Places<T, kWhole>& p, int lane)
+    {
+        constexpr int E = 16 / sizeof(T);
+        const int d0 = E * (lane >> 4);
+#pragma unroll
+        for (int u = 0; u < SUB; ++u) {
+            const T* q = head + p.base[u] + (kWhole ? (lane & 15) * a.token_stride : 0);
+#pragma unroll
+            for (int i = 0; i < L::KV; ++i) {
+                const int d = d0 + 4 * E * i;
+                key[u][i] = *reinterpret_cast<const V4uAnywhere*>(q + (d < a.dim ? d : 0));
+            }
+        }
+        if (a.dim != DP) {
+            // dims the head does not have: zero against the query's zero, whatever the cache holds
+#pragma unroll
+            for (int i = 0; i < L::KV; ++i)
+#pragma unroll
+                for (int u = 0; u < SUB; ++u)
+                    if (d0 + 4 * E * i >= a.dim) key[u][i] = V4u{0, 0, 0, 0};
+        }
+    }
+
+    __device__ __forceinline__ void load_values(const AttendArgs& a, const T* head, const Places<T, kWhole>& p, int lane)
+    {
+        constexpr int E = 16 / sizeof(T);
+        const int d0 = L::VE * (lane & 15);
+#pragma unroll
+        for (int j = 0; j < VROWS; ++j) {
+            const T* q = head + value_row(a, p, j, lane);
+            if constexpr (L::VD == 2) {
+                const V2u x = *reinterpret_cast<const V2uAnywhere*>(q + (d0 < a.dim ? d0 : 0));
+                val[j][0] = x[0];
+                val[j][1] = x[1];
+            } else {
+#pragma unroll
+                for (int i = 0; i < L::VD / 4; ++i) {
+                    const V4u x = *reinterpret_cast<const V4uAnywhere*>(q + (d0 + E * i < a.dim ? d0 + E * i : 0));
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) val[j][4 * i + e] = x[e];
+                }
+            }
+        }
+    }
+
+    // Values of positions that are not seen may be anything, and 0 times that is not 0.
+    __device__ __forceinline__ void drop_unseen_values(uint32_t seen, int lane)
+    {
+#pragma unroll
+        for (int j = 0; j < VROWS; ++j)
+            if (!(seen >> (16 * (j >> 2) + 4 * (lane >> 4) + (j & 3)) & 1)) {
+#pragma unroll
+                for (int i = 0; i < L::VD; ++i) val[j][i] = 0;
+            }
+    }
+
+    // Scores of the tile, unseen ones -inf: x[4 u + r] is position 16 u + 4 (lane / 16) + r.
+    __device__ __forceinline__ void scores(const AttendArgs& a, const V4u* q, uint32_t seen, int lane, float x[VROWS])
+    {
+#pragma unroll
+        for (int u = 0; u < SUB; ++u) {
+            V4f s = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int i = 0; i < L::KV; ++i) {
+                if constexpr (std::is_same<T, uint16_t>::value) {
+                    s = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(V8bf, key[u][i]),
+                                                                __builtin_bit_cast(V8bf, q[i]), s, 0, 0, 0);
+                } else {
+                    const V4f k4 = __builtin_bit_cast(V4f, key[u][i]), q4 = __builtin_bit_cast(V4f, q[i]);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) s = __builtin_amdgcn_mfma_f32_16x16x4f32(k4[e], q4[e], s, 0, 0, 0);
+                }
+            }
+#pragma unroll
+            for (int r = 0; r < 4; ++r) x[4 * u + r] = s[r] * a.scale;
+        }
+        if (seen != (TILE == 32 ? ~0u : 0xFFFFu)) {
+#pragma unroll
+            for (int j = 0; j < VROWS; ++j)
+                if (!(seen >> (16 * (j >> 2) + 4 * (lane >> 4) + (j & 3)) & 1)) x[j] = -__builtin_inff();
+        }
+    }
+
+    // Folds the tile's values, with weights e^x, into the state.
+    __device__ __forceinline__ void fold(State<DP>& st, float x[VROWS])
+    {
+        float top = x[0];
+#pragma unroll
+        for (int j = 1; j < VROWS; ++j) top = fmaxf(top, x[j]);
+        const float m = fmaxf(st.m, max_over_lanes(top));
+        // nothing seen yet: any finite base gives weights of 0
+        const float base = m == -__builtin_inff() ? 0.f : m;
+        const float keep = exp_hw(st.m - base);
+        float l = 0.f;
+#pragma unroll
+        for (int j = 0; j < VROWS; ++j) {
+            x[j] = exp_hw(x[j] - base);
+            l += x[j];
+        }
+        st.l = st.l * keep + l;
+        st.m = m;
+        if (__any(keep != 1.f)) {
+#pragma unroll
+            for (int b = 0; b < DP / 16; ++b) st.o[b] *= keep;
+        }
+        if constexpr (std::is_same<T, uint16_t>::value) {
+            V8bf hi, lo;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                hi[j] = (__bf16)x[j];
+                lo[j] = (__bf16)(x[j] - (float)hi[j]);
+            }
+#pragma unroll
+            for (int b = 0; b < DP / 16; ++b) {
+                V4u v;
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    v[i] = __builtin_amdgcn_perm(val[2 * i + 1][b >> 1], val[2 * i][b >> 1],
+                                                 b & 1 ? 0x07060302u : 0x05040100u);
+                const V8bf v8 = __builtin_bit_cast(V8bf, v);
+                st.o[b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v8, hi, st.o[b], 0, 0, 0);
+                st.o[b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v8, lo, st.o[b], 0, 0, 0);
+            }
+        } else {
+#pragma unroll
+            for (int b = 0; b < DP / 16; ++b)
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                    st.o[b] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(val[j][b]), x[j], st.o[b], 0, 0, 0);
+        }
+    }
+};
+
+template <typename T> __device__ __forceinline__ T rounded(float x);
+template <> __device__ __forceinline__ float rounded<float>(float x) { return x; }
+template <> __device__ __forceinline__ uint16_t rounded<uint16_t>(float x)
+{
+    return __builtin_bit_cast(uint16_t, (__bf16)x);
+}
+
+// The heads of one job: kAttendHeads of the group, or what is left of it.
+__device__ __forceinline__ int heads_of(const AttendArgs& a, int block)
+{
+    return min(kAttendHeads, a.group - block * kAttendHeads);
+}
+
+template <typename T>
+__device__ __forceinline__ void write_row(const AttendArgs& a, int32_t row, int32_t head, int d, float o, float l)
+{
+    T* const out = static_cast<T*>(a.out) + (int64_t)row * a.out_stride + head * a.out_head_stride;
+    out[d] = rounded<T>(l == 0.f ? 0.f : o / l);
+}
+
+__device__ __forceinline__ void write_lse(const AttendArgs& a, int32_t row, int32_t head, float m, float l)
+{
+    if (a.lse) a.lse[(int64_t)row * a.heads * a.group + head] = l == 0.f ? -__builtin_inff() : m + logf(l);
+}
+
+// First unit of a workgroup's share.
+__device__ __forceinline__ int64_t share_begin(int64_t units, int64_t groups, int64_t w)
+{
+    return (int64_t)((unsigned __int128)units * w / groups);
+}
+
+template <typename T, int DP, bool kWhole>
+__global__ __launch_bounds__(kThreads, DP == 256 ? 1 : 2) void k_attend(AttendArgs a)
+{
+    typedef Work<T, DP, kWhole> W;
+    constexpr int TILE = Tile<T>::n;
+    constexpr int PAD = DP + 4;
+    __shared__ float s_o[kWaves][kAttendHeads][PAD];
+    __shared__ float s_m[kWaves][kAttendHeads], s_l[kWaves][kAttendHeads];
+    __shared__ int64_t s_sum[kWaves];
+    __shared__ int64_t s_before;
+    __shared__ int32_t s_row;
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+
+    // every row's tiles, and this workgroup's share of their line
+    const int32_t each = (a.rows + kThreads - 1) / kThreads, r0 = min(a.rows, tid * each), r1 = min(a.rows, r0 + each);
+    int64_t mine = 0;
+    for (int32_t r = r0; r < r1; ++r) mine += row_at<TILE>(a, r).tiles;
+    int64_t upto = mine;
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) {
+        const int64_t y = __shfl_up(upto, d);
+        if (lane >= d) upto += y;
+    }
+    if (lane == 63) s_sum[wave] = upto;
+    __syncthreads();
+    int64_t tiles = 0;
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) {
+        if (w < wave) upto += s_sum[w];
+        tiles += s_sum[w];
+    }
+    const int64_t units = tiles * a.heads * a.blocks;
+    const int64_t groups = max((int64_t)1, min((int64_t)a.groups, units / kWaves));
+    const int64_t me = blockIdx.x;
+    if (tid == 0) a.joins[me].x = -1;
+    if (me >= groups) return;
+    int64_t at = share_begin(units, groups, me);
+    const int64_t end = share_begin(units, groups, me + 1);
+    int32_t hh = (int32_t)(at / tiles);
+    int64_t t = at - hh * tiles;              // tile of the line of one head
+    if (t >= upto - mine && t < upto) {
+        int64_t before = upto - mine;
+        int32_t r = r0;
+        for (; r < r1; ++r) {
+            const int32_t n = row_at<TILE>(a, r).tiles;
+            if (t < before + n) break;
+            before += n;
+        }
+        s_row = r;
+        s_before = before;
+    }
+    __syncthreads();
+    int32_t r = __builtin_amdgcn_readfirstlane(s_row);
+    int64_t before = s_before;
+
+    while (at < end) {
+        const Row row = row_at<TILE>(a, r);
+        const int32_t kv = hh / a.blocks, block = hh - kv * a.blocks, heads = heads_of(a, block);
+        const int32_t head0 = kv * a.group + block * kAttendHeads;
+        const int32_t first = __builtin_amdgcn_readfirstlane((int32_t)(t - before));
+        const int32_t last = __builtin_amdgcn_readfirstlane((int32_t)min((int64_t)row.tiles, first + (end - at)));
+        const int32_t* const table = a.table + (int64_t)max(row.seq, 0) * a.table_stride;
+        const T* const keys = static_cast<const T*>(a.k) + kv * a.head_stride;
+        const T* const values = static_cast<const T*>(a.v) + kv * a.head_stride;
+        const int head = lane & 15;
+
+        // the queries, as the right operand of the first product
+        V4u q[W::L::KV];
+        {
+            constexpr int E = 16 / sizeof(T);
+            const T* const p = static_cast<const T*>(a.q) + (int64_t)r * a.q_stride + (head0 + min(head, heads - 1)) * a.q_head_stride;
+#pragma unroll
+            for (int i = 0; i < W::L::KV; ++i) {
+                const int d = E * (lane >> 4) + 4 * E * i;
+                q[i] = *reinterpret_cast<const V4uAnywhere*>(p + (d < a.dim ? d : 0));
+                if (d >= a.dim || head >= heads) q[i] = V4u{0, 0, 0, 0};
+            }
+        }
+
+        State<DP> st;
+        st.m = -__builtin_inff();
+        st.l = 0.f;
+#pragma unroll
+        for (int b = 0; b < DP / 16; ++b) st.o[b] = V4f{0.f, 0.f, 0.f, 0.f};
+
+        // this wave's tiles: keys of the next one are on their way while the values of one are folded
+        auto begin_of = [&](int32_t i) { return i < row.sink_tiles ? i * TILE : row.from + (i - row.sink_tiles) * TILE; };
+        int32_t i = first + wave;
+        if (i < last) {
+            W w;
+            Places<T, kWhole> p = places<T, kWhole>(a, row, table, begin_of(i), lane);
+            w.load_keys(a, keys, p, lane);
+            w.load_values(a, values, p, lane);
+            while (true) {
+                const int32_t next = i + kWaves;
+                const bool more = next < last;
+                Places<T, kWhole> pn = p;
+                if (more) pn = places<T, kWhole>(a, row, table, begin_of(next), lane);
+                float x[W::VROWS];
+                w.scores(a, q, p.seen, lane, x);
+                if (more) w.load_keys(a, keys, pn, lane);
+                if (p.seen != (TILE == 32 ? ~0u : 0xFFFFu)) w.drop_unseen_values(p.seen, lane);
+                w.fold(st, x);
+                if (!more) break;
+                w.load_values(a, values, pn, lane);
+                p = pn;
+                i = next;
+            }
+        }
+
+        // the waves' pieces join
+        const float l = sum_over_lanes(st.l);
+        if (lane < 16) {
+            s_m[wave][lane] = st.m;
+            s_l[wave][lane] = l;
+        }
+        if (head < heads) {
+#pragma unroll
+            for (int b = 0; b < DP / 16; ++b)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) s_o[wave][head][DP / 16 * (4 * (lane >> 4) + e) + b] = st.o[b][e];
+        }
+        __syncthreads();
+        const bool begins = first == 0, ends = last == row.tiles;
+        float* part = nullptr;
+        if (!(begins && ends)) part = a.parts + (2 * me + (begins ? 1 : 0)) * attend_part_floats(a.dim);
+        for (int x = tid; x < heads * a.dim; x += kThreads) {
+            const int g = x / a.dim, d = x - g * a.dim;
+            float m = s_m[0][g];
+#pragma unroll
+            for (int w = 1; w < kWaves; ++w) m = fmaxf(m, s_m[w][g]);
+            const float base = m == -__builtin_inff() ? 0.f : m;
+            float sum = 0.f, o = 0.f;
+#pragma unroll
+            for (int w = 0; w < kWaves; ++w) {
+                const float f = exp_hw(s_m[w][g] - base);
+                sum += f * s_l[w][g];
+                o += f * s_o[w][g][d];
+            }
+            if (!part) {
+                write_row<T>(a, r, head0 + g, d, o, sum);
+                if (d == 0) write_lse(a, r, head0 + g, m, sum);
+            } else {
+                part[2 * kAttendHeads + (int64_t)g * a.dim + d] = o;
+                if (d == 0) {
+                    part[g] = m;
+                    part[kAttendHeads + g] = sum;
+                }
+            }
+        }
+        if (tid == 0 && begins && !ends) {
+            // the workgroup that holds the job's last unit
+            const int64_t stop = at + row.tiles;
+            a.joins[me] = int4{r, hh, (int32_t)(((unsigned __int128)stop * groups - 1) / units), 0};
+        }
+        __syncthreads();
+        at += last - first;
+        t += last - first;
+        if (last == row.tiles) {
+            before += row.tiles;
+            if (++r == a.rows) {
+                r = 0;
+                before = t = 0;
+                ++hh;
+            }
+        }
+    }
+}
+
+// Joins the pieces of the job that workgroup blockIdx.x began and did not end:
+// its own second part and the first parts of the ones behind it.
+template <typename T>
+__global__ __launch_bounds__(kThreads) void k_attend_join(AttendArgs a)
+{
+    __shared__ float s_f[kAttendMaxGroups];
+    __shared__ float s_red[2][kWaves];
+    const int4 job = a.joins[blockIdx.x];
+    if (job.x < 0) return;
+    const int32_t kv = job.y / a.blocks, block = job.y - kv * a.blocks, heads = heads_of(a, block);
+    const int32_t pieces = job.z - blockIdx.x + 1, tid = threadIdx.x;
+    const int64_t size = attend_part_floats(a.dim);
+    const float* const first = a.parts + (2 * (int64_t)blockIdx.x + 1) * size;
+    for (int g = blockIdx.y; g < heads; g += gridDim.y) {
+        auto piece = [&](int i) { return i == 0 ? first : first + (2 * (int64_t)i - 1) * size; };
+        float m = -__builtin_inff();
+        for (int i = tid; i < pieces; i += kThreads) {
+            s_f[i] = piece(i)[g];
+            m = fmaxf(m, s_f[i]);
+        }
+#pragma unroll
+        for (int d = 1; d < 64; d <<= 1) m = fmaxf(m, __shfl_xor(m, d));
+        if ((tid & 63) == 0) s_red[0][tid >> 6] = m;
+        __syncthreads();
+#pragma unroll
+        for (int w = 0; w < kWaves; ++w) m = fmaxf(m, s_red[0][w]);
+        const float base = m == -__builtin_inff() ? 0.f : m;
+        float l = 0.f;
+        for (int i = tid; i < pieces; i += kThreads) {
+            s_f[i] = exp_hw(s_f[i] - base);
+            l += s_f[i] * piece(i)[kAttendHeads + g];
+        }
+#pragma unroll
+        for (int d = 1; d < 64; d <<= 1) l += __shfl_xor(l, d);
+        if ((tid & 63) == 0) s_red[1][tid >> 6] = l;
+        __syncthreads();
+        l = 0.f;
+#pragma unroll
+        for (int w = 0; w < kWaves; ++w) l += s_red[1][w];
+        const int32_t head = kv * a.group + block * kAttendHeads + g;
+        for (int d = tid; d < a.dim; d += kThreads) {
+            float o = 0.f;
+#pragma unroll 8
+            for (int i = 0; i < pieces; ++i) o += s_f[i] * piece(i)[2 * kAttendHeads + (int64_t)g * a.dim + d];
+            write_row<T>(a, job.x, head, d, o, l);
+        }
+        if (tid == 0) write_lse(a, job.x, head, m, l);
+        __syncthreads();
+    }
+}
+
+template <typename T, int DP>
+hipError_t attend_dim(const AttendArgs& a, hipStream_t s)
+{
+    const dim3 grid((unsigned)a.groups), block(kThreads);
+    if (a.page_size % 16 == 0)
+        hipLaunchKernelGGL((k_attend<T, DP, true>), grid, block, 0, s, a);
+    else
+        hipLaunchKernelGGL((k_attend<T, DP, false>), grid, block, 0, s, a);
+    hipError_t e = hipGetLastError();
+    if (e != hipSuccess || a.groups == 1) return e;      // one share has no pieces
+    hipLaunchKernelGGL(k_attend_join<T>, dim3((unsigned)a.groups, (unsigned)std::min(a.group, kAttendHeads)), block, 0, s, a);
+    return hipGetLastError();
+}
+
+template <typename T>
+hipError_t attend_t(const AttendArgs& a, hipStream_t s)
+{
+    if (a.dim <= 64) return attend_dim<T, 64>(a, s);
+    if (a.dim <= 128) return attend_dim<T, 128>(a, s);
+    return attend_dim<T, 256>(a, s);
+}
+
+}  // namespace
+
+hipError_t launch_attend(int dtype, const AttendArgs& a, hipStream_t s)
+{
+    return dtype == 0 ? attend_t<uint16_t>(a, s) : attend_t<float>(a, s);
+}
+
+}  // namespace cpes

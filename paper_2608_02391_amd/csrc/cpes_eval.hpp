@@ -1,0 +1,123 @@
+// cpes_eval.hpp -- argument blocks and launchers of the operators that evaluate
+// a member (cache pages, attention, token scores), shared by the host runtime
+// (cpes_eval_api.hip) and the kernels.  Internal to the library.
+#pragma once
+
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+namespace cpes {
+
+// Pages and sequences of a pool, as include/cpes.h describes them.
+struct PoolArgs {
+    int32_t* table;
+    int32_t* lengths;
+    int32_t* refs;
+    int64_t table_stride;
+    int32_t sequences, width, pages, page_size;
+};
+
+// One page as `runs` pieces of `run` consecutive 16-byte units: layer, keys or
+// values, and the outer and inner of heads and tokens that do not join up.
+struct PageArgs {
+    char* k;
+    char* v;
+    int64_t page_bytes, layer_bytes, outer_bytes, inner_bytes;   // strides
+    int32_t layers, outers, inners;
+    uint32_t run;                // units of a run
+    uint32_t units;              // units of a page: 2 * layers * outers * inners * run
+};
+
+constexpr int kPlanBlock = 1024;         // the bookkeeping kernels are one workgroup
+constexpr int kPagesHeader = 16;         // int32 words in front of a workspace's lists
+
+struct AppendArgs {
+    PoolArgs pool;
+    char* k;                     // of the layer
+    char* v;
+    const char* k_new;
+    const char* v_new;
+    const int32_t* seqs;
+    const int32_t* positions;
+    int64_t page_bytes, head_bytes, token_bytes, new_bytes, new_head_bytes;   // strides
+    int32_t n, heads;
+    uint32_t run;                // 16-byte units of one head of one token
+};
+
+constexpr int kAttendHeads = 16;         // query heads of a workgroup: the columns of a matrix instruction
+constexpr int kAttendMaxGroups = 1024;   // workgroups of an attention launch at most
+
+struct AttendArgs {
+    const void* k;               // of the layer
+    const void* v;
+    const void* q;
+    void* out;
+    float* lse;
+    const int32_t* seqs;
+    const int32_t* table;
+    const int32_t* lengths;
+    float* parts;                // partial results, two per workgroup
+    int4* joins;                 // per workgroup: the job it began and did not end
+    int64_t page_stride, head_stride, token_stride, table_stride;
+    int64_t q_stride, q_head_stride, out_stride, out_head_stride;
+    int32_t rows, heads, group, blocks;      // q_heads = heads * group, in `blocks` blocks of kAttendHeads
+    int32_t dim, page_size, page_shift, pages, width, sequences;   // page_shift < 0: no power of two
+    int32_t window, sinks;
+    int32_t groups;              // workgroups launched
+    float scale;
+};
+
+// One partial result: kAttendHeads maxima, as many sums, then the output rows.
+inline __host__ __device__ int64_t attend_part_floats(int dim)
+{
+    return 2 * kAttendHeads + (int64_t)kAttendHeads * dim;
+}
+
+constexpr int kMaxSlices = 64;           // workgroups of one row of logits at most
+
+struct LogprobArgs {
+    const void* x;
+    const int64_t* targets;
+    float* logp;
+    float* entropy;
+    float* lse;
+    float* stats;
+    float* top_logp;
+    int64_t* top_ids;
+    float4* parts;               // [rows][slices]: maximum, sum, weighted sum
+    unsigned long long* keys;    // [rows][slices][top]
+    int64_t stride;
+    int32_t rows, vocab, top;
+    int32_t slices, per_slice;   // per_slice: a multiple of the vector
+    float scale;
+};
+
+struct LogprobGradArgs {
+    const void* x;
+    void* dx;
+    const int64_t* targets;
+    const float* stats;
+    const float* entropy;
+    const float* d_logp;
+    const float* d_entropy;
+    int64_t stride, dx_stride;
+    int32_t rows, vocab;
+    float scale;
+};
+
+hipError_t launch_pages_reserve(const PoolArgs& p, int32_t n, const int32_t* seqs, const int32_t* new_lengths,
+                                int32_t* ws, int32_t* status, hipStream_t s);
+hipError_t launch_pages_fork(const PageArgs& c, const PoolArgs& p, int32_t n, const int32_t* parents,
+                             const int32_t* children, int32_t* ws, int32_t* status, hipStream_t s);
+hipError_t launch_pages_free(const PoolArgs& p, int32_t n, const int32_t* seqs, int32_t* status, hipStream_t s);
+hipError_t launch_pages_copy(const PageArgs& c, int32_t pages, int32_t n, const int32_t* src, const int32_t* dst,
+                             hipStream_t s);
+hipError_t launch_pages_compact(const PageArgs& c, const PoolArgs& p, const PoolArgs& packed, int32_t* ws,
+                                int32_t* moved, hipStream_t s);
+hipError_t launch_append(const AppendArgs& a, hipStream_t s);
+hipError_t launch_attend(int dtype, const AttendArgs& a, hipStream_t s);
+int logprob_slices(int32_t rows, int32_t vocab, int dtype, int32_t* per_slice);
+hipError_t launch_logprobs(int dtype, const LogprobArgs& a, hipStream_t s);
+hipError_t launch_logprobs_backward(int dtype, const LogprobGradArgs& a, hipStream_t s);
+
+}  // namespace cpes

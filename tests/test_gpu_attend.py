@@ -1,0 +1,353 @@
+"""Attention of one new token over the paged cache, and the entry of tokens into
+it, against a plain implementation in 64 bits.  Everything a row does not see --
+other slots of its last page, positions outside its window, pages nobody holds --
+holds NaN or infinities."""
+import math
+
+import pytest
+import torch
+
+import eval_helpers as H
+import paper_2608_02391_amd as cp
+
+pytestmark = pytest.mark.gpu
+BF16, F32 = torch.bfloat16, torch.float32
+
+
+class Case:
+    """A cache of given sequences in scattered pages, in one layer of `layers`."""
+
+    def __init__(self, lens, kv_heads, dim, page, dtype, order="hnd", layers=2, layer=1, window=0, sinks=0, seed=0,
+                 spare=3, width=None):
+        g = torch.Generator().manual_seed(seed)
+        self.lens, self.kv, self.dim, self.page, self.dtype, self.layer = lens, kv_heads, dim, page, dtype, layer
+        self.window, self.sinks = window, sinks
+        counts = [-(-n // page) for n in lens]
+        self.pages = sum(counts) + spare
+        self.width = width or max(1, max(counts) + 1)
+        ids = torch.randperm(self.pages, generator=g)
+        shape = (layers, self.pages, kv_heads, page, dim)
+        if order == "nhd":
+            host = [torch.empty(layers, self.pages, page, kv_heads, dim, dtype=dtype).transpose(2, 3) for _ in range(2)]
+        else:
+            host = [torch.empty(shape, dtype=dtype) for _ in range(2)]
+        poison = torch.tensor([math.nan, math.inf, -math.inf, 3e38])
+        for t in host:
+            t.copy_(poison[torch.randint(0, 4, shape, generator=g)].to(dtype))
+        self.table = torch.full((len(lens), self.width), -1, dtype=torch.int32)
+        self.keys, self.values, at = [], [], 0
+        for s, n in enumerate(lens):
+            own = ids[at:at + counts[s]]
+            at += counts[s]
+            self.table[s, :counts[s]] = own.int()
+            k, v = (torch.randn(n, kv_heads, dim, generator=g).to(dtype) for _ in range(2))
+            seen = H.visible(n, window, sinks)
+            j = torch.arange(n)[seen]
+            for t, x in zip(host, (k, v)):
+                t[layer][own[j // page], :, j % page] = x[seen]
+            self.keys.append(k)
+            self.values.append(v)
+        self.k, self.v = (t.cuda() if order == "hnd" else t.transpose(2, 3).contiguous().cuda().transpose(2, 3) for t in host)
+        self.lengths = torch.tensor(lens, dtype=torch.int32)
+        self.bind()
+
+    def bind(self):
+        self.cache = cp.paged_cache(self.k, self.v)
+        self.dtable, self.dlengths = self.table.cuda(), self.lengths.cuda()
+        self.pool = cp.page_pool(self.dtable, self.dlengths, self.page)
+
+    def queries(self, q_heads, rows=None, seed=1):
+        g = torch.Generator().manual_seed(seed)
+        return (torch.randn(rows or len(self.lens), q_heads, self.dim, generator=g) * 2).to(self.dtype)
+
+    def run(self, q, seqs=None, scale=None, stream=None, out=None, lse=True):
+        rows, heads = q.shape[0], q.shape[1]
+        dq = q if q.is_cuda else q.cuda()
+        ws = torch.full((cp.cpes_attend_workspace_bytes(rows, heads, self.kv, self.dim),), 0xFF, dtype=torch.uint8, device="cuda")
+        out = torch.full(q.shape, math.nan, dtype=self.dtype, device="cuda") if out is None else out
+        dl = torch.full((rows, heads), math.nan, device="cuda") if lse else None
+        cp.cpes_attend(self.cache, self.layer, self.pool, dq, out, lse=dl, seqs=None if seqs is None else seqs.cuda(),
+                       scale=scale, window=self.window, sinks=self.sinks, workspace=ws, stream=stream)
+        return out, dl
+
+    def check(self, q, out, lse, seqs=None, scale=None, hidden=()):
+        """hidden: (sequence, position) pairs without a page."""
+        scale = self.dim ** -0.5 if scale is None else scale
+        out, lse = out.float().cpu(), lse.cpu()
+        group = q.shape[1] // self.kv
+        for r in range(q.shape[0]):
+            s = r if seqs is None else int(seqs[r])
+            known = 0 <= s < len(self.lens)
+            n = self.lens[s] if known else 0
+            seen = H.visible(n, self.window, self.sinks)
+            for hs, j in hidden:
+                if hs == s:
+                    seen[j] = False
+            for i in range(q.shape[1]):
+                k, v = (x[s][:, i // group] if known else torch.zeros(0, self.dim) for x in (self.keys, self.values))
+                ref, ref_lse, tol, tol_lse = H.attend(q[r, i].cpu(), k, v, seen, scale)
+                got = out[r, i].double()
+                assert torch.isfinite(got).all(), (r, i, s, n)
+                off = (got - ref).abs() - (tol + H.rounding(self.dtype) * (ref.abs() + tol) + 1e-38)
+                assert float(off.max()) <= 0, (r, i, n, float(off.max()), float((got - ref).abs().max()))
+                if ref_lse == -math.inf:
+                    assert float(lse[r, i]) == -math.inf and not bool(got.any())
+                else:
+                    assert abs(float(lse[r, i]) - ref_lse) <= tol_lse, (r, i, n, float(lse[r, i]), ref_lse)
+
+
+LENGTHS = [0, 1, 15, 16, 17, 31, 32, 33, 64, 100, 257, 600]
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32], ids=["bf16", "fp32"])
+@pytest.mark.parametrize("dim", [8, 40, 64, 80, 128, 136, 256])
+@pytest.mark.parametrize("page", [16, 7])
+def test_head_dims(dtype, dim, page):
+    print(f"attend dim={dim} page={page} {dtype}", flush=True)
+    c = Case(LENGTHS, 2, dim, page, dtype, seed=dim)
+    q = c.queries(6)
+    c.check(q, *c.run(q))
+
+
+@pytest.mark.parametrize("page", [1, 2, 8, 16, 24, 32, 48, 64, 100, 128])
+@pytest.mark.parametrize("order", ["hnd", "nhd"])
+def test_page_sizes(page, order):
+    print(f"attend page={page} {order}", flush=True)
+    c = Case(LENGTHS, 2, 64, page, BF16, order=order, seed=page)
+    q = c.queries(8)
+    c.check(q, *c.run(q))
+
+
+@pytest.mark.parametrize("kv,group", [(1, 1), (3, 1), (2, 5), (1, 16), (2, 17), (1, 33)])
+@pytest.mark.parametrize("dtype", [BF16, F32], ids=["bf16", "fp32"])
+def test_head_groups(kv, group, dtype):
+    print(f"attend kv={kv} group={group} {dtype}", flush=True)
+    c = Case([1, 33, 700, 0, 95], kv, 128, 16, dtype, seed=group)
+    q = c.queries(kv * group)
+    c.check(q, *c.run(q))
+
+
+@pytest.mark.parametrize("window,sinks", [(1, 0), (1, 1), (16, 4), (33, 0), (100, 37), (64, 200), (5000, 4), (300, 31)])
+@pytest.mark.parametrize("dtype,page", [(BF16, 16), (F32, 16), (BF16, 5), (F32, 24)])
+def test_windows_and_sinks(window, sinks, dtype, page):
+    print(f"attend window={window} sinks={sinks} {dtype} page={page}", flush=True)
+    c = Case([0, 1, 2, 17, 36, 40, 101, 138, 333, 900], 2, 64, page, dtype, window=window, sinks=sinks, seed=window)
+    q = c.queries(4)
+    c.check(q, *c.run(q))
+
+
+@pytest.mark.parametrize("lens", [[40000], [1] * 300, [9000, 1, 1, 0, 5000, 3], [20000] * 3 + [100] * 50],
+                         ids=["one_long", "many_short", "mixed", "few_long"])
+@pytest.mark.parametrize("dtype", [BF16, F32], ids=["bf16", "fp32"])
+def test_splits(lens, dtype):
+    """Long rows over many workgroups, many rows in one, and mixtures."""
+    print(f"attend lens={lens[:4]} {dtype}", flush=True)
+    c = Case(lens, 2, 64, 16, dtype, layers=1, layer=0, seed=len(lens))
+    q = c.queries(4)
+    c.check(q, *c.run(q))
+
+
+def test_listed_sequences_strides_and_order():
+    """Rows that ask for any sequence, twice or for none; queries and outputs inside wider tensors."""
+    c = Case([50, 700, 3, 129], 2, 64, 16, BF16, seed=5)
+    seqs = torch.tensor([3, 1, -1, 1, 0, 4, 2], dtype=torch.int32)
+    fused = torch.randn(7, 4 + 2 * 2, 64, generator=torch.Generator().manual_seed(2)).to(BF16).cuda()
+    wide = torch.full((7, 9, 72), math.nan, dtype=BF16, device="cuda")
+    q, out = fused[:, :4], wide[:, 2:6, 3:67]
+    _, lse = c.run(q, seqs=seqs, out=out)
+    c.check(q, out, lse, seqs=seqs)
+    rest = wide.clone()
+    rest[:, 2:6, 3:67] = math.nan
+    assert bool(torch.isnan(rest).all())                  # nothing else was written
+    out2 = torch.empty(7, 4, 64, dtype=BF16, device="cuda")
+    c.run(q, seqs=seqs, out=out2, lse=False)
+    assert torch.equal(out2, out)
+
+
+def test_unaligned_tensors():
+    """Cache, queries and outputs that start at odd elements."""
+    c = Case([77, 300], 2, 64, 16, BF16, layers=1, layer=0, seed=6)
+    def shifted(t, by):
+        flat = torch.full((t.numel() + by,), math.nan, dtype=t.dtype, device="cuda")
+        flat[by:] = t.reshape(-1)
+        return flat[by:].view(t.shape)
+    c.k, c.v = shifted(c.k, 1), shifted(c.v, 3)
+    c.bind()
+    q = shifted(c.queries(4).cuda(), 5)
+    out = torch.full((q.numel() + 7,), math.nan, dtype=BF16, device="cuda")[7:].view(q.shape)
+    _, lse = c.run(q, out=out)
+    c.check(q, out, lse)
+
+
+def test_positions_without_a_page_are_not_seen():
+    """Table entries of -1, beyond the cache, and lengths beyond the table."""
+    c = Case([200, 200, 64], 2, 64, 16, BF16, seed=7)
+    hidden = []
+    for s, entry, bad in ((0, 2, -1), (0, 11, c.pages), (1, 0, -7), (1, 12, 2 ** 31 - 1)):
+        c.table[s, entry] = bad
+        hidden += [(s, j) for j in range(16 * entry, min(16 * entry + 16, c.lens[s]))]
+    c.table[2, :] = -1
+    hidden += [(2, j) for j in range(64)]
+    c.bind()
+    q = c.queries(4)
+    c.check(q, *c.run(q), hidden=hidden)
+    # a length beyond the table sees what the table holds; a negative one nothing
+    c = Case([64, 64], 1, 64, 16, BF16, seed=8, width=4)
+    c.lengths = torch.tensor([1000, -5], dtype=torch.int32)
+    c.bind()
+    c.lens, c.keys[1], c.values[1] = [64, 0], c.keys[1][:0], c.values[1][:0]
+    q = c.queries(2)
+    c.check(q, *c.run(q))
+
+
+def test_extreme_scores():
+    """Scores far apart, equal ones, and a row whose scores are all -inf."""
+    c = Case([65, 65, 40], 1, 64, 16, F32, layers=1, layer=0, seed=9)
+    c.keys[0] *= 40.0
+    c.keys[1][:] = 0.25
+    c.keys[2][:] = 0.0
+    c.keys[2][:, 0, 0] = -math.inf
+    for s in range(3):
+        j = torch.arange(c.lens[s])
+        c.k[0][c.table[s].long()[j // 16].cuda(), :, (j % 16).cuda()] = c.keys[s].cuda()
+    q = c.queries(2)
+    q[2] = 0.0
+    q[2, :, 0] = 1.0
+    out, lse = c.run(q)
+    assert bool((lse[2] == -math.inf).all()) and not bool(out[2].any())
+    c.lens[2], c.keys[2], c.values[2] = 0, c.keys[2][:0], c.values[2][:0]
+    c.check(q, out, lse)
+
+
+@pytest.mark.parametrize("scale", [0.0, -0.3, 1.0])
+def test_scales(scale):
+    c = Case([129, 30], 2, 64, 16, BF16, seed=10)
+    q = c.queries(4)
+    c.check(q, *c.run(q, scale=scale), scale=scale)
+
+
+def test_same_result_on_every_run_and_stream():
+    c = Case([5000, 17, 900], 4, 128, 16, BF16, layers=1, layer=0, seed=11)
+    q = c.queries(16).cuda()
+    out, lse = c.run(q)
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    for _ in range(3):
+        side.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(side):
+            o2, l2 = c.run(q)
+        side.synchronize()
+        assert torch.equal(out, o2) and torch.equal(lse, l2)
+
+
+def test_offsets_beyond_32_bits():
+    """A cache of more than 2^32 elements: pages at its far end."""
+    page, kv, dim = 16, 2, 64
+    pages = 2 ** 32 // (page * kv * dim) + 40
+    k = torch.empty(1, pages, kv, page, dim, dtype=BF16, device="cuda")
+    v = torch.empty_like(k)
+    n, far = 100, [pages - 1, 3, pages - 20, pages // 2 + 1, pages - 7, 0, pages - 2]
+    g = torch.Generator(device="cuda").manual_seed(3)
+    c = Case([n], kv, dim, page, BF16, layers=1, layer=0)
+    for i, p in enumerate(far):
+        for t, own in ((k, c.keys), (v, c.values)):
+            t[0, p] = 3e38
+            take = own[0][16 * i:16 * i + 16].transpose(0, 1).cuda()
+            t[0, p, :, :take.shape[1]] = take
+    c.k, c.v, c.pages = k, v, pages
+    c.table = torch.full((1, 8), -1, dtype=torch.int32)
+    c.table[0, :7] = torch.tensor(far, dtype=torch.int32)
+    c.bind()
+    q = c.queries(4)
+    c.check(q, *c.run(q))
+    new = torch.randn(1, kv, dim, generator=g, device="cuda").to(BF16)
+    cp.cpes_cache_append(c.cache, 0, c.pool, new, new, torch.tensor([3], dtype=torch.int32, device="cuda"))
+    assert torch.equal(k[0, pages - 1, :, 3], new[0]) and torch.equal(v[0, pages - 1, :, 3], new[0])
+
+
+def test_captured_steps_follow_growing_lengths():
+    """A graph of append and attention, replayed as the sequences grow."""
+    lens = [40, 3, 130]
+    c = Case([n + 8 for n in lens], 2, 64, 16, BF16, layers=1, layer=0, seed=12)
+    full = [n + 8 for n in lens]
+    q, q_host = torch.empty(3, 4, 64, dtype=BF16, device="cuda"), [c.queries(4, seed=50 + t) for t in range(8)]
+    k_new, v_new = (torch.empty(3, 2, 64, dtype=BF16, device="cuda") for _ in range(2))
+    pos = torch.tensor(lens, dtype=torch.int32, device="cuda")
+    out, lse = torch.empty_like(q), torch.empty(3, 4, device="cuda")
+    ws = torch.empty(cp.cpes_attend_workspace_bytes(3, 4, 2, 64), dtype=torch.uint8, device="cuda")
+    kv_ref = [[x.clone() for x in t] for t in (c.keys, c.values)]
+
+    def step():
+        cp.cpes_cache_append(c.cache, 0, c.pool, k_new, v_new, pos)
+        cp.cpes_attend(c.cache, 0, c.pool, q, out, lse=lse, workspace=ws)
+
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.stream(side):
+        graph.capture_begin()
+        step()
+        graph.capture_end()
+    torch.cuda.current_stream().wait_stream(side)
+    for t in range(8):
+        now = [n + t for n in lens]
+        q.copy_(q_host[t])
+        for s in range(3):
+            k_new[s].copy_(kv_ref[0][s][now[s]])
+            v_new[s].copy_(kv_ref[1][s][now[s]])
+        pos.copy_(torch.tensor(now, dtype=torch.int32))
+        c.dlengths.copy_(torch.tensor([n + 1 for n in now], dtype=torch.int32))
+        # the page's place of the new token holds nothing useful before the replay
+        graph.replay()
+        torch.cuda.synchronize()
+        c.lens = [n + 1 for n in now]
+        c.keys, c.values = ([x[s][:now[s] + 1] for s in range(3)] for x in kv_ref)
+        c.check(q_host[t], out, lse)
+    assert [n + 1 for n in now] == full
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32], ids=["bf16", "fp32"])
+@pytest.mark.parametrize("order", ["hnd", "nhd"])
+@pytest.mark.parametrize("heads,dim,page,tokens", [(1, 8, 1, 5), (3, 40, 7, 100), (8, 128, 16, 1300), (2, 256, 64, 3)])
+def test_append(dtype, order, heads, dim, page, tokens):
+    print(f"append {dtype} {order} {heads}x{dim} page={page} tokens={tokens}", flush=True)
+    g = torch.Generator().manual_seed(tokens)
+    seqs_n, width = 4, -(-(tokens + 3) // page)
+    pages = seqs_n * width + 2
+    shape = (3, pages, heads, page, dim)
+    k, v = (torch.randn(shape, generator=g).to(dtype).cuda() for _ in range(2))
+    if order == "nhd":
+        k, v = (t.transpose(2, 3).contiguous().transpose(2, 3) for t in (k, v))
+    k0, v0 = k.clone(), v.clone()
+    table = torch.randperm(pages, generator=g)[:seqs_n * width].view(seqs_n, width).int()
+    table[2, 0] = -1
+    table[3, 0] = pages
+    pool = cp.page_pool(table.cuda(), torch.zeros(seqs_n, dtype=torch.int32, device="cuda"), page)
+    # every place at most once; sequences and positions out of range among them
+    places = [(s, j) for s in range(seqs_n) for j in range(tokens)]
+    places = [places[i] for i in torch.randperm(len(places), generator=g)[:tokens].tolist()] + [(-1, 0), (seqs_n, 1), (0, -1), (1, width * page)]
+    n = len(places)
+    fused = torch.randn(n, 3 * heads, dim, generator=g).to(dtype).cuda()
+    k_new, v_new = fused[:, :heads], fused[:, 2 * heads:]
+    seqs, pos = (torch.tensor([p[i] for p in places], dtype=torch.int32, device="cuda") for i in (0, 1))
+    cp.cpes_cache_append(cp.paged_cache(k, v), 1, pool, k_new, v_new, pos, seqs=seqs)
+    for i, (s, j) in enumerate(places):
+        if 0 <= s < seqs_n and 0 <= j < width * page:
+            p = int(table[s, j // page])
+            if 0 <= p < pages:
+                k0[1, p, :, j % page], v0[1, p, :, j % page] = k_new[i], v_new[i]
+    assert torch.equal(k, k0) and torch.equal(v, v0)
+
+
+def test_append_without_list_and_without_tokens():
+    k, v = (torch.zeros(1, 4, 1, 4, 8, dtype=BF16, device="cuda") for _ in range(2))
+    pool = cp.page_pool(torch.arange(4, dtype=torch.int32, device="cuda").view(2, 2), torch.zeros(2, dtype=torch.int32, device="cuda"), 4)
+    cache = cp.paged_cache(k, v)
+    new = torch.ones(2, 1, 8, dtype=BF16, device="cuda")
+    cp.cpes_cache_append(cache, 0, pool, new, 2 * new, torch.tensor([5, 0], dtype=torch.int32, device="cuda"))
+    assert float(k[0, 1, 0, 1].sum()) == 8 and float(v[0, 2, 0, 0].sum()) == 16 and float(k.sum()) == 16
+    cp.cpes_cache_append(cache, 0, pool, new[:0], new[:0], torch.empty(0, dtype=torch.int32, device="cuda"))
+    ws = torch.empty(cp.cpes_attend_workspace_bytes(0, 1, 1, 8), dtype=torch.uint8, device="cuda")
+    cp.cpes_attend(cache, 0, pool, new[:0], new[:0].clone(), workspace=ws)
+    torch.cuda.synchronize()
+    assert float(k.sum()) == 16
