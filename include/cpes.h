@@ -603,7 +603,7 @@ CPES_API size_t cpes_logprobs_workspace_bytes(int32_t rows, int32_t vocab, int32
  * entropy 0 and log probabilities -inf.  A NaN or +inf makes the row's numbers
  * NaN and its alternatives -1.
  * Errors: x NULL, rows < 0, vocab < 1, stride < vocab with more than one row,
- *   scale not positive and finite, logp without targets, top outside [0,
+ *   scale not positive or above FLT_MAX / 2, logp without targets, top outside [0,
  *   CPES_MAX_ALTERNATIVES] or without both outputs -> CPES_ERR_INVALID_ARGUMENT;
  *   workspace -> CPES_ERR_WORKSPACE.
  */

@@ -91,8 +91,11 @@ __device__ __forceinline__ Row row_at(const AttendArgs& a, int32_t r)
 }
 
 // e^x for x <= 0: the hardware's 2^x.  Scores and maxima stay in natural units,
-// so that lse loses nothing on a way through base 2.
-__device__ __forceinline__ float exp_hw(float x) { return __builtin_amdgcn_exp2f(x * kLog2e); }
+// so that lse loses nothing on a way through base 2.  The product's rounding
+// is |x| 2^-24 of the weight, which an fp32 cache's outputs would show.
+template <typename T> __device__ __forceinline__ float weight(float x);
+template <> __device__ __forceinline__ float weight<uint16_t>(float x) { return __builtin_amdgcn_exp2f(x * kLog2e); }
+template <> __device__ __forceinline__ float weight<float>(float x) { return expf(x); }
 
 // The larger of the four lanes that hold one query head's scores.
 __device__ __forceinline__ float max_over_lanes(float x)
@@ -261,17 +264,25 @@ template <typename T, int DP, bool kWhole> struct Work {
     {
 #pragma unroll
         for (int u = 0; u < SUB; ++u) {
-            V4f s = {0.f, 0.f, 0.f, 0.f};
+            V4f s;
+            if constexpr (std::is_same<T, uint16_t>::value) {
+                s = V4f{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-            for (int i = 0; i < L::KV; ++i) {
-                if constexpr (std::is_same<T, uint16_t>::value) {
+                for (int i = 0; i < L::KV; ++i)
                     s = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(V8bf, key[u][i]),
                                                                 __builtin_bit_cast(V8bf, q[i]), s, 0, 0, 0);
-                } else {
+            } else {
+                // four sums: a quarter of the roundings in line, and of the instructions that wait for each other
+                V4f part[4];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) part[e] = V4f{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int i = 0; i < L::KV; ++i) {
                     const V4f k4 = __builtin_bit_cast(V4f, key[u][i]), q4 = __builtin_bit_cast(V4f, q[i]);
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) s = __builtin_amdgcn_mfma_f32_16x16x4f32(k4[e], q4[e], s, 0, 0, 0);
+                    for (int e = 0; e < 4; ++e) part[e] = __builtin_amdgcn_mfma_f32_16x16x4f32(k4[e], q4[e], part[e], 0, 0, 0);
                 }
+                s = (part[0] + part[1]) + (part[2] + part[3]);
             }
 #pragma unroll
             for (int r = 0; r < 4; ++r) x[4 * u + r] = s[r] * a.scale;
@@ -292,11 +303,11 @@ template <typename T, int DP, bool kWhole> struct Work {
         const float m = fmaxf(st.m, max_over_lanes(top));
         // nothing seen yet: any finite base gives weights of 0
         const float base = m == -__builtin_inff() ? 0.f : m;
-        const float keep = exp_hw(st.m - base);
+        const float keep = weight<T>(st.m - base);
         float l = 0.f;
 #pragma unroll
         for (int j = 0; j < VROWS; ++j) {
-            x[j] = exp_hw(x[j] - base);
+            x[j] = weight<T>(x[j] - base);
             l += x[j];
         }
         st.l = st.l * keep + l;
@@ -499,7 +510,7 @@ __global__ __launch_bounds__(kThreads, DP == 256 ? 1 : 2) void k_attend(AttendAr
             float sum = 0.f, o = 0.f;
 #pragma unroll
             for (int w = 0; w < kWaves; ++w) {
-                const float f = exp_hw(s_m[w][g] - base);
+                const float f = weight<T>(s_m[w][g] - base);
                 sum += f * s_l[w][g];
                 o += f * s_o[w][g][d];
             }
@@ -562,7 +573,7 @@ __global__ __launch_bounds__(kThreads) void k_attend_join(AttendArgs a)
         const float base = m == -__builtin_inff() ? 0.f : m;
         float l = 0.f;
         for (int i = tid; i < pieces; i += kThreads) {
-            s_f[i] = exp_hw(s_f[i] - base);
+            s_f[i] = weight<T>(s_f[i] - base);
             l += s_f[i] * piece(i)[kAttendHeads + g];
         }
 #pragma unroll

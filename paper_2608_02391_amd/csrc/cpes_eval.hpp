@@ -90,6 +90,8 @@ struct LogprobArgs {
     int32_t rows, vocab, top;
     int32_t slices, per_slice;   // per_slice: a multiple of the vector
     float scale;
+    float c;                     // scale log2 e
+    float excess;                // (c / (scale log2 e) - 1) ln 2
 };
 
 struct LogprobGradArgs {

@@ -5,6 +5,7 @@
 #include "cpes.h"
 
 #include <algorithm>
+#include <cfloat>
 #include <cmath>
 
 #include "cpes_eval.hpp"
@@ -172,8 +173,8 @@ int check_logits(const void* x, int dtype, int32_t rows, int32_t vocab, int64_t 
     if (!x && rows > 0) return fail(CPES_ERR_INVALID_ARGUMENT, "%s: logits are null", fn);
     if (rows > 1 && stride < vocab)
         return fail(CPES_ERR_INVALID_ARGUMENT, "%s: row stride %lld below the %d logits of a row", fn, (long long)stride, vocab);
-    if (!std::isfinite(scale) || !(scale > 0.f))
-        return fail(CPES_ERR_INVALID_ARGUMENT, "%s: scale %g must be finite and > 0", fn, (double)scale);
+    if (!(scale > 0.f) || !(scale <= FLT_MAX / 2))
+        return fail(CPES_ERR_INVALID_ARGUMENT, "%s: scale %g is not positive or above FLT_MAX / 2", fn, (double)scale);
     return CPES_OK;
 }
 
@@ -416,6 +417,9 @@ int cpes_logprobs(const void* x_dev, int dtype, int32_t rows, int32_t vocab, int
     a.vocab = vocab;
     a.top = top;
     a.scale = scale;
+    const double c = (double)scale * M_LOG2E;
+    a.c = (float)c;
+    a.excess = (float)(((double)a.c / c - 1.0) * M_LN2);
     return hip_status(cpes::launch_logprobs(dtype, a, (hipStream_t)stream), fn);
 }
 

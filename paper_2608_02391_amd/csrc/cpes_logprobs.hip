@@ -2,11 +2,13 @@
 // logits: log probability, entropy, the most likely alternatives, and the
 // gradient of the first two.
 //
-// Mathematics.  With z = scale x, M = max z and d_v = z_v - M <= 0:
-//   s = sum e^(d_v),  u = sum d_v e^(d_v),
-//   lse = M + ln s,  ln p_v = d_v - ln s,  entropy = ln s - u / s
-// (both terms of the entropy are positive: nothing cancels).  Pieces (M, s, u) of
-// a row join by e^(M_old - M_new), u moving by s (M_old - M_new) as well.
+// Mathematics.  With z = scale x, M = max z, c = scale log2 e and t_v = c (x_v - max x) <= 0:
+//   s = sum 2^(t_v),  u = sum t_v 2^(t_v),
+//   lse = M + ln s,  ln p_v = z_v - M - ln s,  entropy = ln s - ln 2 u / s
+// (both terms of the entropy are positive: nothing cancels).  Pieces (max, s, u) of
+// a row join by 2^(t of the smaller maximum), u moving by s times that exponent as
+// well.  c rounded to fp32 is c (1 + r): to first order that adds r ln 2 u to s, which
+// is taken back at the end.
 //   dx_v = scale (g ([v = t] - p_v) - h p_v (ln p_v + entropy)).
 //
 // What bounds it: a logit is read once (and its gradient written once) for about
@@ -18,12 +20,14 @@
 // Split.  A row is one workgroup's where there are rows for the GPU; few rows are cut
 // into slices, joined by a second launch in slice order.
 //
-// Alternatives.  A thread keeps, with its running maximum, the step it first met it
-// in.  The k-th largest of the 256 threads' maxima bounds the row's k-th largest
-// from below, and exactly k threads hold anything from it on, so only their
-// logits, k / 256 of the row, are looked at again (from the caches).  Order: value
-// descending, then token ascending, as one 64-bit key, so no two are equal and the
-// result does not depend on who writes first.
+// Alternatives.  Order: value descending, then token ascending, as one 64-bit key,
+// so no two are equal and the result does not depend on who writes first.  A
+// thread keeps, with its running maximum, the step it first met it in, so the
+// maximum's key lies between those of the step's last and first token.  The k-th
+// largest of the 256 threads' lower ends bounds the row's k-th largest key from
+// below, and only threads whose upper end reaches that bound can hold a key from
+// there on: k of them, and a few that tie, whose logits, about k / 256 of the row,
+// are looked at again (from the caches).
 #include <algorithm>
 #include <type_traits>
 
@@ -39,11 +43,12 @@ typedef unsigned long long Key;
 
 constexpr int kThreads = 256;
 constexpr float kLog2e = 1.44269504088896340736f;
+constexpr float kLn2 = 0.69314718055994530942f;
 constexpr float kFar = -1e4f;            // stands in for what is below, -inf too: its exponential is 0, and 0 times it
 
 template <typename T> struct Vec { static constexpr int n = 16 / sizeof(T); };
 
-__device__ __forceinline__ float exp_hw(float x) { return __builtin_amdgcn_exp2f(x * kLog2e); }
+__device__ __forceinline__ float exp2_hw(float x) { return __builtin_amdgcn_exp2f(x); }
 
 template <typename T> __device__ __forceinline__ float value_of(T x);
 template <> __device__ __forceinline__ float value_of<float>(float x) { return x; }
@@ -80,15 +85,15 @@ __device__ __forceinline__ uint32_t key_token(Key k) { return ~(uint32_t)k; }
 
 // Sums of a piece of a row.
 struct Sums {
-    float m, s, u;       // largest logit, sum e^d, sum d e^d with d = scale (x - m)
+    float m, s, u;       // largest logit, sum 2^t, sum t 2^t with t = c (x - m)
 };
 
-__device__ __forceinline__ Sums join(Sums a, Sums b, float scale)
+__device__ __forceinline__ Sums join(Sums a, Sums b, float c)
 {
     const float m = fmaxf(a.m, b.m);
     // a piece of nothing but -inf has s = u = 0 and moves nothing
-    const float da = a.m == m ? 0.f : fmaxf(scale * (a.m - m), kFar), db = b.m == m ? 0.f : fmaxf(scale * (b.m - m), kFar);
-    const float fa = exp_hw(da), fb = exp_hw(db);
+    const float da = a.m == m ? 0.f : fmaxf(c * (a.m - m), kFar), db = b.m == m ? 0.f : fmaxf(c * (b.m - m), kFar);
+    const float fa = exp2_hw(da), fb = exp2_hw(db);
     return Sums{m, fa * a.s + fb * b.s, fa * (a.u + da * a.s) + fb * (b.u + db * b.s)};
 }
 
@@ -99,6 +104,7 @@ __device__ __forceinline__ void finish(const LogprobArgs& a, int64_t row, Sums t
     const float nan = __builtin_nanf("");
     const bool empty = t.s == 0.f;        // nothing but -inf
     *broken = !(t.s >= 0.f) || t.m == __builtin_inff();
+    t.s -= a.excess * t.u;
     *logsum = *broken ? nan : empty ? 0.f : logf(t.s);
     if (threadIdx.x != 0) return;
     if (a.logp) {
@@ -110,7 +116,7 @@ __device__ __forceinline__ void finish(const LogprobArgs& a, int64_t row, Sums t
         }
         a.logp[row] = x;
     }
-    if (a.entropy) a.entropy[row] = empty ? 0.f : *logsum - t.u / t.s;
+    if (a.entropy) a.entropy[row] = empty ? 0.f : *logsum - t.u / t.s * kLn2;
     if (a.lse) a.lse[row] = *broken ? nan : a.scale * t.m + *logsum;
     if (a.stats) {
         a.stats[2 * row] = t.m;
@@ -162,7 +168,7 @@ __global__ __launch_bounds__(kThreads) void k_logprobs(LogprobArgs a)
     constexpr uint32_t kNone = std::is_same<T, float>::value ? 0xFF800000u : 0xFF80FF80u;   // -inf
     __shared__ Sums s_sums[kThreads / 64];
     __shared__ Key s_keys[kCandidates], s_best[kMaxTop];
-    __shared__ int32_t s_owner[kMaxTop], s_count;
+    __shared__ int32_t s_owner[kThreads], s_count, s_owners;
     const int tid = threadIdx.x;
     for (int64_t job = blockIdx.x; job < (int64_t)a.rows * a.slices; job += gridDim.x) {
         const int64_t row = job / a.slices;
@@ -202,7 +208,7 @@ __global__ __launch_bounds__(kThreads) void k_logprobs(LogprobArgs a)
 #pragma unroll
             for (int j = 0; j < kUnroll * N; ++j) top = fmaxf(top, x[j]);
             if (top > t.m) {
-                const float d = t.s == 0.f ? 0.f : fmaxf(a.scale * (t.m - top), kFar), f = exp_hw(d);
+                const float d = t.s == 0.f ? 0.f : fmaxf(a.c * (t.m - top), kFar), f = exp2_hw(d);
                 t.u = f * (t.u + d * t.s);
                 t.s *= f;
                 t.m = top;
@@ -211,7 +217,7 @@ __global__ __launch_bounds__(kThreads) void k_logprobs(LogprobArgs a)
             const float base = t.m == -__builtin_inff() ? 0.f : t.m;
 #pragma unroll
             for (int j = 0; j < kUnroll * N; ++j) {
-                const float d = a.scale * (x[j] - base), e = exp_hw(d);
+                const float d = a.c * (x[j] - base), e = exp2_hw(d);
                 t.s += e;
                 t.u += e * fmaxf(d, kFar);
             }
@@ -220,20 +226,22 @@ __global__ __launch_bounds__(kThreads) void k_logprobs(LogprobArgs a)
         const float mine = t.m;
 #pragma unroll
         for (int d = 1; d < 64; d <<= 1)
-            t = join(t, Sums{__shfl_xor(t.m, d), __shfl_xor(t.s, d), __shfl_xor(t.u, d)}, a.scale);
+            t = join(t, Sums{__shfl_xor(t.m, d), __shfl_xor(t.s, d), __shfl_xor(t.u, d)}, a.c);
         if ((tid & 63) == 0) s_sums[tid >> 6] = t;
-        if (a.top > 0 && tid == 0) s_count = 0;
-        Key bound = 0;
+        if (a.top > 0 && tid == 0) s_count = s_owners = 0;
+        Key low = 0, high = 0;            // no more and no less than the key of this thread's maximum
         if (a.top > 0) {
-            // not after the token of the thread's maximum
-            const int64_t last = begin + ((int64_t)(met * kUnroll + kUnroll - 1) * kThreads + tid) * N + N - 1;
-            if (tid < vecs) bound = key_of(mine, (uint32_t)last);
-            s_keys[tid] = bound;
+            const int64_t first = begin + ((int64_t)(met * kUnroll) * kThreads + tid) * N;
+            if (tid < vecs) {
+                low = key_of(mine, (uint32_t)(first + (kUnroll - 1) * kThreads * N + N - 1));
+                high = key_of(mine, (uint32_t)first);
+            }
+            s_keys[tid] = low;
         }
         __syncthreads();
         t = s_sums[0];
 #pragma unroll
-        for (int w = 1; w < kThreads / 64; ++w) t = join(t, s_sums[w], a.scale);
+        for (int w = 1; w < kThreads / 64; ++w) t = join(t, s_sums[w], a.c);
         float logsum = 0.f;
         bool broken = false;
         if (a.slices == 1)
@@ -242,16 +250,17 @@ __global__ __launch_bounds__(kThreads) void k_logprobs(LogprobArgs a)
             a.parts[job] = float4{t.m, t.s, t.u, 0.f};
 
         if (a.top > 0) {
-            // the threads that hold the k largest maxima, and the least of these
+            // the k-th largest lower end, and the threads that reach it
             int place = 0;
-            for (int j = 0; j < kThreads; ++j) place += s_keys[j] > bound;
-            if (bound && place < a.top) s_owner[place] = tid;
-            const int owners = min(a.top, min(vecs, kThreads));
+            for (int j = 0; j < kThreads; ++j) place += s_keys[j] > low;
             if (tid == 0) s_best[0] = 1;
             __syncthreads();
-            if (bound && place == a.top - 1) s_best[0] = bound;
+            if (low && place == a.top - 1) s_best[0] = low;
             __syncthreads();
             Key least = s_best[0];
+            if (high >= least) s_owner[atomicAdd(&s_owners, 1)] = tid;
+            __syncthreads();
+            const int owners = s_owners;
             // their logits from there on
             const int32_t per = steps * kUnroll, items = owners * per;
             for (int32_t item0 = 0; item0 < items; item0 += kThreads) {
@@ -307,7 +316,7 @@ __global__ __launch_bounds__(kThreads) void k_logprobs_join(LogprobArgs a)
     }
 #pragma unroll
     for (int d = 1; d < 64; d <<= 1)
-        t = join(t, Sums{__shfl_xor(t.m, d), __shfl_xor(t.s, d), __shfl_xor(t.u, d)}, a.scale);
+        t = join(t, Sums{__shfl_xor(t.m, d), __shfl_xor(t.s, d), __shfl_xor(t.u, d)}, a.c);
     t = Sums{__shfl(t.m, 0), __shfl(t.s, 0), __shfl(t.u, 0)};
     float logsum;
     bool broken;
@@ -377,7 +386,7 @@ __global__ __launch_bounds__(kThreads) void k_logprobs_backward(LogprobGradArgs 
         const float gp = valid ? g : 0.f;
         const bool empty = m == -__builtin_inff() && logsum == 0.f;
         auto gradient = [&](float x, int64_t v) {
-            const float logp = a.scale * (x - m) - logsum, p = exp_hw(logp);
+            const float logp = a.scale * (x - m) - logsum, p = exp2_hw(logp * kLog2e);
             // p = 0: no gradient, whatever ln p is
             float d = p == 0.f || empty ? 0.f : -p * (gp + h * (logp + entropy));
             if (v == target) d += empty ? 0.f : gp;

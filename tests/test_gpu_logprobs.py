@@ -112,6 +112,21 @@ def test_alternatives_on_awkward_rows(rows, kind):
     assert all(torch.equal(y[0], y[-1]) for y in o.values())
 
 
+@pytest.mark.parametrize("rows,V,dtype", [(3, 70000, BF16), (800, 70000, BF16), (800, 3001, F32)])
+@pytest.mark.parametrize("levels", [3, 40, 1000])
+def test_alternatives_among_many_ties(rows, V, dtype, levels):
+    """Random logits of few values: the k-th largest ties with others all over the row."""
+    print(f"ties rows={rows} V={V} levels={levels}", flush=True)
+    top = 20
+    g = torch.Generator(device="cuda").manual_seed(levels)
+    x = torch.randn(rows, V, generator=g, device="cuda")
+    x = ((x * levels / 8).round() * (8.0 / levels)).to(dtype)
+    t = torch.zeros(rows, dtype=torch.int64)
+    o = score(x, t, top=top)
+    order = torch.sort(x, dim=-1, descending=True, stable=True).indices[:, :top]
+    assert torch.equal(o["top_ids"], order)
+
+
 @pytest.mark.parametrize("rows", [4, 1000])
 def test_masked_rows(rows):
     """-inf in most places, in all but one, in all; the type's lowest value everywhere; a target outside."""
