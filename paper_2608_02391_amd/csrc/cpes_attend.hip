@@ -28,10 +28,12 @@
 // outputs are fp32.
 //
 // Split.  All rows' tiles, for every key-value head, form one line, cut into equal
-// shares, one per workgroup, whatever the lengths: a workgroup's share may end
-// one row and begin others.  A row (and head) that lies in one share is written
-// by its workgroup; otherwise each workgroup leaves its piece, and a second
-// launch joins the pieces in order, so the result does not depend on timing.
+// shares, one per wave, whatever the lengths: a share may end one row and begin
+// others, and its loads run on across them.  A row (and head) that lies in one
+// share is written by its wave; otherwise each wave leaves its piece, and a
+// second launch joins the pieces in order, so the result does not depend on
+// timing.  Where no row can have more than a few tiles, a workgroup takes a row
+// (and head), its waves join in shared memory, and there is one launch.
 #include <algorithm>
 #include <type_traits>
 
@@ -48,8 +50,11 @@ typedef __bf16 V8bf __attribute__((ext_vector_type(8)));
 typedef V4u V4uAnywhere __attribute__((aligned(2)));          // caches and queries start at any element
 typedef V2u V2uAnywhere __attribute__((aligned(2)));
 
-constexpr int kWaves = 4;
+constexpr int kWaves = kAttendWaves;
 constexpr int kThreads = 64 * kWaves;
+constexpr int kShareTiles = 2;            // tiles of a wave's share at least
+constexpr int kShortTiles = 16;           // tiles of a row up to which a workgroup takes the row
+constexpr int64_t kMaxGrid = 1 << 20;     // workgroups of the short and the join launch
 constexpr float kLog2e = 1.44269504088896340736f;
 
 template <typename T> struct Tile;
@@ -63,6 +68,12 @@ struct Row {
     int32_t from;
     int32_t tiles;        // at least one: an empty row is written too
     int32_t seq;
+
+    // First position of tile i.
+    __device__ __forceinline__ int32_t begin(int32_t i, int tile) const
+    {
+        return i < sink_tiles ? i * tile : from + (i - sink_tiles) * tile;
+    }
 };
 
 template <int TILE>
@@ -109,15 +120,6 @@ __device__ __forceinline__ float sum_over_lanes(float x)
     return x + __shfl_xor(x, 32);
 }
 
-// (page, slot) of a position; page -1 where the table has none.
-__device__ __forceinline__ int32_t page_at(const AttendArgs& a, const int32_t* table, int32_t pos, int32_t* slot)
-{
-    const int32_t at = a.page_shift >= 0 ? pos >> a.page_shift : pos / a.page_size;
-    *slot = pos - at * a.page_size;
-    const int32_t page = at < a.width ? table[at] : -1;
-    return page < a.pages ? page : -1;
-}
-
 // Where the positions of one tile lie: element offsets of their rows from the
 // head's first, and which are seen (bit j: position j of the tile).
 //   kWhole: 16 positions share a page (its size is a multiple of 16), so a lane's
@@ -131,41 +133,50 @@ template <typename T, bool kWhole> struct Places {
     uint32_t seen;
 };
 
-template <typename T, bool kWhole>
-__device__ __forceinline__ Places<T, kWhole> places(const AttendArgs& a, const Row& row, const int32_t* table,
-                                                    int32_t pos0, int lane)
-{
-    Places<T, kWhole> p;
-    p.seen = 0;
+// The page ids of a tile's positions, asked for long before they are needed.
+template <typename T, bool kWhole> struct Pages {
+    static constexpr int SUB = Tile<T>::n / 16;
+    int32_t id[SUB], slot[SUB];
+
+    __device__ __forceinline__ void ask(const AttendArgs& a, const Row& row, const int32_t* table, int32_t pos0, int lane)
+    {
 #pragma unroll
-    for (int u = 0; u < Places<T, kWhole>::SUB; ++u) {
-        if constexpr (kWhole) {
-            const int32_t pos = pos0 + 16 * u;
-            int32_t slot = 0, page = -1;
-            if (pos < row.n) page = page_at(a, table, pos, &slot);
-            page = __builtin_amdgcn_readfirstlane(page);
-            slot = __builtin_amdgcn_readfirstlane(slot);
-            p.base[u] = max(page, 0) * a.page_stride + slot * a.token_stride;
-            if (page >= 0) p.seen |= 0xFFFFu << (16 * u);
-        } else {
-            const int32_t pos = pos0 + 16 * u + (lane & 15);
-            int32_t slot = 0, page = -1;
-            if (pos < row.n) page = page_at(a, table, pos, &slot);
-            p.base[u] = max(page, 0) * a.page_stride + slot * a.token_stride;
-            p.seen |= (uint32_t)(__ballot(page >= 0) & 0xFFFF) << (16 * u);
+        for (int u = 0; u < SUB; ++u) {
+            const int32_t pos = pos0 + 16 * u + (kWhole ? 0 : lane & 15);
+            const int32_t at = a.page_shift >= 0 ? pos >> a.page_shift : pos / a.page_size;
+            slot[u] = pos - at * a.page_size;
+            id[u] = -1;
+            if (pos < row.n) id[u] = table[at];          // row.n is at most what the table holds
         }
     }
-    const int32_t left = row.n - pos0;
-    if (left < 32) p.seen &= left > 0 ? (1u << left) - 1u : 0u;
-    if (a.window > 0) {
-        // seen: before `sinks`, or from n - window on
-        const int32_t skip = row.n - a.window - pos0, sinks = a.sinks - pos0;
-        uint32_t keep = skip <= 0 ? ~0u : skip >= 32 ? 0u : ~0u << skip;
-        if (sinks > 0) keep |= sinks >= 32 ? ~0u : (1u << sinks) - 1u;
-        p.seen &= keep;
+
+    __device__ __forceinline__ Places<T, kWhole> places(const AttendArgs& a, const Row& row, int32_t pos0)
+    {
+        Places<T, kWhole> p;
+        p.seen = 0;
+#pragma unroll
+        for (int u = 0; u < SUB; ++u) {
+            int32_t page = id[u], at = slot[u];
+            if constexpr (kWhole) page = __builtin_amdgcn_readfirstlane(page);
+            const bool there = page >= 0 && page < a.pages;
+            p.base[u] = there ? page * a.page_stride + at * a.token_stride : 0;
+            if constexpr (kWhole)
+                p.seen |= there ? 0xFFFFu << (16 * u) : 0u;
+            else
+                p.seen |= (uint32_t)(__ballot(there) & 0xFFFF) << (16 * u);
+        }
+        const int32_t left = row.n - pos0;
+        if (left < 32) p.seen &= left > 0 ? (1u << left) - 1u : 0u;
+        if (a.window > 0) {
+            // seen: before `sinks`, or from n - window on
+            const int32_t skip = row.n - a.window - pos0, sinks = a.sinks - pos0;
+            uint32_t keep = skip <= 0 ? ~0u : skip >= 32 ? 0u : ~0u << skip;
+            if (sinks > 0) keep |= sinks >= 32 ? ~0u : (1u << sinks) - 1u;
+            p.seen &= keep;
+        }
+        return p;
     }
-    return p;
-}
+};
 
 template <typename T, int DP> struct Layout;
 // bf16: 8 elements of a key row per load; a lane's part of a value row
@@ -184,6 +195,14 @@ template <int DP> struct Layout<float, DP> {
 template <int DP> struct State {
     float m, l;              // of query head lane % 16; l is this lane's share
     V4f o[DP / 16];          // o[b][r]: dim DP/16 * (4 (lane / 16) + r) + b
+
+    __device__ __forceinline__ void clear()
+    {
+        m = -__builtin_inff();
+        l = 0.f;
+#pragma unroll
+        for (int b = 0; b < DP / 16; ++b) o[b] = V4f{0.f, 0.f, 0.f, 0.f};
+    }
 };
 
 template <typename T, int DP, bool kWhole> struct Work {
@@ -351,17 +370,40 @@ template <> __device__ __forceinline__ uint16_t rounded<uint16_t>(float x)
     return __builtin_bit_cast(uint16_t, (__bf16)x);
 }
 
-// The heads of one job: kAttendHeads of the group, or what is left of it.
-__device__ __forceinline__ int heads_of(const AttendArgs& a, int block)
+// A key-value head with kAttendHeads of its query heads, or what is left of them.
+struct Job {
+    int32_t kv, head0, heads;
+};
+
+__device__ __forceinline__ Job job_at(const AttendArgs& a, int32_t hh)
 {
-    return min(kAttendHeads, a.group - block * kAttendHeads);
+    Job j;
+    j.kv = hh / a.blocks;
+    const int32_t block = hh - j.kv * a.blocks;
+    j.head0 = j.kv * a.group + block * kAttendHeads;
+    j.heads = min(kAttendHeads, a.group - block * kAttendHeads);
+    return j;
+}
+
+// The queries of a row, as the right operand of the first product.
+template <typename T, int DP>
+__device__ __forceinline__ void load_queries(const AttendArgs& a, int32_t r, const Job& job, int lane, V4u* q)
+{
+    constexpr int E = 16 / sizeof(T);
+    const int head = lane & 15;
+    const T* const p = static_cast<const T*>(a.q) + (int64_t)r * a.q_stride + (job.head0 + min(head, job.heads - 1)) * a.q_head_stride;
+#pragma unroll
+    for (int i = 0; i < Layout<T, DP>::KV; ++i) {
+        const int d = E * (lane >> 4) + 4 * E * i;
+        q[i] = *reinterpret_cast<const V4uAnywhere*>(p + (d < a.dim ? d : 0));
+        if (d >= a.dim || head >= job.heads) q[i] = V4u{0, 0, 0, 0};
+    }
 }
 
 template <typename T>
-__device__ __forceinline__ void write_row(const AttendArgs& a, int32_t row, int32_t head, int d, float o, float l)
+__device__ __forceinline__ T* out_row(const AttendArgs& a, int32_t row, int32_t head)
 {
-    T* const out = static_cast<T*>(a.out) + (int64_t)row * a.out_stride + head * a.out_head_stride;
-    out[d] = rounded<T>(l == 0.f ? 0.f : o / l);
+    return static_cast<T*>(a.out) + (int64_t)row * a.out_stride + head * a.out_head_stride;
 }
 
 __device__ __forceinline__ void write_lse(const AttendArgs& a, int32_t row, int32_t head, float m, float l)
@@ -369,26 +411,64 @@ __device__ __forceinline__ void write_lse(const AttendArgs& a, int32_t row, int3
     if (a.lse) a.lse[(int64_t)row * a.heads * a.group + head] = l == 0.f ? -__builtin_inff() : m + logf(l);
 }
 
-// First unit of a workgroup's share.
-__device__ __forceinline__ int64_t share_begin(int64_t units, int64_t groups, int64_t w)
+// Four consecutive output values.
+template <typename T> __device__ __forceinline__ void store4(T* p, V4f x);
+template <> __device__ __forceinline__ void store4<float>(float* p, V4f x)
 {
-    return (int64_t)((unsigned __int128)units * w / groups);
+    *reinterpret_cast<V4uAnywhere*>(p) = __builtin_bit_cast(V4u, x);
 }
+template <> __device__ __forceinline__ void store4<uint16_t>(uint16_t* p, V4f x)
+{
+    typedef __bf16 V4bf __attribute__((ext_vector_type(4)));
+    V4bf h;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) h[e] = (__bf16)x[e];
+    *reinterpret_cast<V2uAnywhere*>(p) = __builtin_bit_cast(V2u, h);
+}
+
+// First unit of a wave's share: floor(units w / waves) without its product.
+__device__ __forceinline__ int64_t share_begin(int64_t units, int32_t waves, int32_t w)
+{
+    const int64_t q = units / waves;
+    return q * w + (int64_t)((int32_t)(units - q * waves) * w / waves);       // both factors below 2^12
+}
+
+// The share that holds a unit.
+__device__ int32_t share_of(int64_t units, int32_t waves, int64_t unit)
+{
+    int32_t w = min(waves - 1, (int32_t)((double)unit * waves / (double)units));
+    while (share_begin(units, waves, w) > unit) --w;
+    while (w + 1 < waves && share_begin(units, waves, w + 1) <= unit) ++w;
+    return w;
+}
+
+// A tile of the line: row, key-value head and block, and its place in the row.
+struct Cursor {
+    Row row;
+    int32_t r, hh, i;
+
+    template <int TILE> __device__ __forceinline__ void next(const AttendArgs& a)
+    {
+        if (++i < row.tiles) return;
+        i = 0;
+        if (++r == a.rows) {
+            r = 0;
+            ++hh;
+        }
+        row = row_at<TILE>(a, r);
+    }
+};
 
 template <typename T, int DP, bool kWhole>
 __global__ __launch_bounds__(kThreads, DP == 256 ? 1 : 2) void k_attend(AttendArgs a)
 {
     typedef Work<T, DP, kWhole> W;
     constexpr int TILE = Tile<T>::n;
-    constexpr int PAD = DP + 4;
-    __shared__ float s_o[kWaves][kAttendHeads][PAD];
-    __shared__ float s_m[kWaves][kAttendHeads], s_l[kWaves][kAttendHeads];
-    __shared__ int64_t s_sum[kWaves];
-    __shared__ int64_t s_before;
-    __shared__ int32_t s_row;
+    __shared__ int64_t s_sum[kWaves], s_before[kWaves];
+    __shared__ int32_t s_row[kWaves];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
 
-    // every row's tiles, and this workgroup's share of their line
+    // every row's tiles, and where this workgroup's waves begin on their line
     const int32_t each = (a.rows + kThreads - 1) / kThreads, r0 = min(a.rows, tid * each), r1 = min(a.rows, r0 + each);
     int64_t mine = 0;
     for (int32_t r = r0; r < r1; ++r) mine += row_at<TILE>(a, r).tiles;
@@ -407,206 +487,298 @@ __global__ __launch_bounds__(kThreads, DP == 256 ? 1 : 2) void k_attend(AttendAr
         tiles += s_sum[w];
     }
     const int64_t units = tiles * a.heads * a.blocks;
-    const int64_t groups = max((int64_t)1, min((int64_t)a.groups, units / kWaves));
-    const int64_t me = blockIdx.x;
-    if (tid == 0) a.joins[me].x = -1;
-    if (me >= groups) return;
-    int64_t at = share_begin(units, groups, me);
-    const int64_t end = share_begin(units, groups, me + 1);
-    int32_t hh = (int32_t)(at / tiles);
-    int64_t t = at - hh * tiles;              // tile of the line of one head
-    if (t >= upto - mine && t < upto) {
-        int64_t before = upto - mine;
-        int32_t r = r0;
-        for (; r < r1; ++r) {
-            const int32_t n = row_at<TILE>(a, r).tiles;
-            if (t < before + n) break;
-            before += n;
+    const int32_t waves = (int32_t)max((int64_t)1, min((int64_t)a.groups * kWaves, units / kShareTiles));
+    const int32_t w0 = blockIdx.x * kWaves;
+    if (w0 >= waves) return;
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) {
+        if (w0 + w >= waves) break;
+        const int64_t t = share_begin(units, waves, w0 + w) % tiles;
+        if (t >= upto - mine && t < upto) {
+            int64_t before = upto - mine;
+            int32_t r = r0;
+            for (; r < r1; ++r) {
+                const int32_t n = row_at<TILE>(a, r).tiles;
+                if (t < before + n) break;
+                before += n;
+            }
+            s_row[w] = r;
+            s_before[w] = before;
         }
-        s_row = r;
-        s_before = before;
     }
     __syncthreads();
-    int32_t r = __builtin_amdgcn_readfirstlane(s_row);
-    int64_t before = s_before;
+    const int32_t me = w0 + wave;
+    if (me >= waves) return;
+    const int64_t at = share_begin(units, waves, me);
+    const int32_t share = __builtin_amdgcn_readfirstlane((int32_t)(share_begin(units, waves, me + 1) - at));
+    int32_t left = share;
+    if (left == 0) return;
 
-    while (at < end) {
-        const Row row = row_at<TILE>(a, r);
-        const int32_t kv = hh / a.blocks, block = hh - kv * a.blocks, heads = heads_of(a, block);
-        const int32_t head0 = kv * a.group + block * kAttendHeads;
-        const int32_t first = __builtin_amdgcn_readfirstlane((int32_t)(t - before));
-        const int32_t last = __builtin_amdgcn_readfirstlane((int32_t)min((int64_t)row.tiles, first + (end - at)));
-        const int32_t* const table = a.table + (int64_t)max(row.seq, 0) * a.table_stride;
-        const T* const keys = static_cast<const T*>(a.k) + kv * a.head_stride;
-        const T* const values = static_cast<const T*>(a.v) + kv * a.head_stride;
-        const int head = lane & 15;
+    Cursor cur;
+    cur.r = __builtin_amdgcn_readfirstlane(s_row[wave]);
+    cur.hh = __builtin_amdgcn_readfirstlane((int32_t)(at / tiles));
+    cur.i = __builtin_amdgcn_readfirstlane((int32_t)(at % tiles - s_before[wave]));
+    cur.row = row_at<TILE>(a, cur.r);
 
-        // the queries, as the right operand of the first product
-        V4u q[W::L::KV];
-        {
-            constexpr int E = 16 / sizeof(T);
-            const T* const p = static_cast<const T*>(a.q) + (int64_t)r * a.q_stride + (head0 + min(head, heads - 1)) * a.q_head_stride;
-#pragma unroll
-            for (int i = 0; i < W::L::KV; ++i) {
-                const int d = E * (lane >> 4) + 4 * E * i;
-                q[i] = *reinterpret_cast<const V4uAnywhere*>(p + (d < a.dim ? d : 0));
-                if (d >= a.dim || head >= heads) q[i] = V4u{0, 0, 0, 0};
+    // Three tiles are under way: the scores and values of one, the keys and values
+    // of the next, the page ids of the one behind.
+    W work;
+    State<DP> st;
+    V4u q[W::L::KV], q_next[W::L::KV];
+    Pages<T, kWhole> pages;
+    auto table_of = [&](const Row& row) { return a.table + (int64_t)max(row.seq, 0) * a.table_stride; };
+    auto keys_of = [&](int32_t hh) { return static_cast<const T*>(a.k) + hh / a.blocks * a.head_stride; };
+    auto values_of = [&](int32_t hh) { return static_cast<const T*>(a.v) + hh / a.blocks * a.head_stride; };
+
+    load_queries<T, DP>(a, cur.r, job_at(a, cur.hh), lane, q);
+    pages.ask(a, cur.row, table_of(cur.row), cur.row.begin(cur.i, TILE), lane);
+    Places<T, kWhole> p = pages.places(a, cur.row, cur.row.begin(cur.i, TILE));
+    work.load_keys(a, keys_of(cur.hh), p, lane);
+    work.load_values(a, values_of(cur.hh), p, lane);
+    Cursor nxt = cur;
+    if (left > 1) {
+        nxt.next<TILE>(a);
+        pages.ask(a, nxt.row, table_of(nxt.row), nxt.row.begin(nxt.i, TILE), lane);
+    }
+    st.clear();
+    int32_t first = cur.i;                // of this row in this share
+    while (true) {
+        const bool more = left > 1, turns = cur.i + 1 == cur.row.tiles;
+        Places<T, kWhole> pn = p;
+        Cursor far = nxt;
+        if (more) {
+            pn = pages.places(a, nxt.row, nxt.row.begin(nxt.i, TILE));
+            if (turns) load_queries<T, DP>(a, nxt.r, job_at(a, nxt.hh), lane, q_next);
+            if (left > 2) {
+                far.next<TILE>(a);
+                pages.ask(a, far.row, table_of(far.row), far.row.begin(far.i, TILE), lane);
             }
         }
+        float x[W::VROWS];
+        work.scores(a, q, p.seen, lane, x);
+        if (more) work.load_keys(a, keys_of(nxt.hh), pn, lane);
+        if (p.seen != (TILE == 32 ? ~0u : 0xFFFFu)) work.drop_unseen_values(p.seen, lane);
+        work.fold(st, x);
+        if (more) work.load_values(a, values_of(nxt.hh), pn, lane);
 
-        State<DP> st;
-        st.m = -__builtin_inff();
-        st.l = 0.f;
-#pragma unroll
-        for (int b = 0; b < DP / 16; ++b) st.o[b] = V4f{0.f, 0.f, 0.f, 0.f};
-
-        // this wave's tiles: keys of the next one are on their way while the values of one are folded
-        auto begin_of = [&](int32_t i) { return i < row.sink_tiles ? i * TILE : row.from + (i - row.sink_tiles) * TILE; };
-        int32_t i = first + wave;
-        if (i < last) {
-            W w;
-            Places<T, kWhole> p = places<T, kWhole>(a, row, table, begin_of(i), lane);
-            w.load_keys(a, keys, p, lane);
-            w.load_values(a, values, p, lane);
-            while (true) {
-                const int32_t next = i + kWaves;
-                const bool more = next < last;
-                Places<T, kWhole> pn = p;
-                if (more) pn = places<T, kWhole>(a, row, table, begin_of(next), lane);
-                float x[W::VROWS];
-                w.scores(a, q, p.seen, lane, x);
-                if (more) w.load_keys(a, keys, pn, lane);
-                if (p.seen != (TILE == 32 ? ~0u : 0xFFFFu)) w.drop_unseen_values(p.seen, lane);
-                w.fold(st, x);
-                if (!more) break;
-                w.load_values(a, values, pn, lane);
-                p = pn;
-                i = next;
+        if (turns || !more) {
+            // the row, or this share of it, is done
+            const Job job = job_at(a, cur.hh);
+            const int head = lane & 15;
+            const bool begins = first == 0;
+            const float l = sum_over_lanes(st.l);
+            const int64_t index = (int64_t)cur.r * (a.heads * a.blocks) + cur.hh;
+            if (begins && lane == 0) {
+                // which shares hold the rest of it
+                const int64_t stop = at + (share - left) - cur.i + cur.row.tiles - 1;
+                a.joins[index] = int2{me, turns ? me : share_of(units, waves, stop)};
             }
-        }
-
-        // the waves' pieces join
-        const float l = sum_over_lanes(st.l);
-        if (lane < 16) {
-            s_m[wave][lane] = st.m;
-            s_l[wave][lane] = l;
-        }
-        if (head < heads) {
+            if (head < job.heads) {
+                const int d0 = DP / 16 * 4 * (lane >> 4);
+                if (begins && turns) {
+                    T* const out = out_row<T>(a, cur.r, job.head0 + head);
+                    const float f = l == 0.f ? 0.f : 1.f / l;
 #pragma unroll
-            for (int b = 0; b < DP / 16; ++b)
+                    for (int e = 0; e < 4; ++e)
 #pragma unroll
-                for (int e = 0; e < 4; ++e) s_o[wave][head][DP / 16 * (4 * (lane >> 4) + e) + b] = st.o[b][e];
-        }
-        __syncthreads();
-        const bool begins = first == 0, ends = last == row.tiles;
-        float* part = nullptr;
-        if (!(begins && ends)) part = a.parts + (2 * me + (begins ? 1 : 0)) * attend_part_floats(a.dim);
-        for (int x = tid; x < heads * a.dim; x += kThreads) {
-            const int g = x / a.dim, d = x - g * a.dim;
-            float m = s_m[0][g];
+                        for (int b = 0; b < DP / 16; b += 4) {
+                            const int d = d0 + DP / 16 * e + b;
+                            if (d < a.dim)
+                                store4<T>(out + d, l == 0.f ? V4f{0.f, 0.f, 0.f, 0.f}
+                                                            : V4f{st.o[b][e], st.o[b + 1][e], st.o[b + 2][e], st.o[b + 3][e]} * f);
+                        }
+                    if (lane < 16) write_lse(a, cur.r, job.head0 + head, st.m, l);
+                } else {
+                    float* const part = a.parts + (2 * (int64_t)me + (begins ? 1 : 0)) * attend_part_floats(a.dim);
 #pragma unroll
-            for (int w = 1; w < kWaves; ++w) m = fmaxf(m, s_m[w][g]);
-            const float base = m == -__builtin_inff() ? 0.f : m;
-            float sum = 0.f, o = 0.f;
+                    for (int e = 0; e < 4; ++e)
 #pragma unroll
-            for (int w = 0; w < kWaves; ++w) {
-                const float f = weight<T>(s_m[w][g] - base);
-                sum += f * s_l[w][g];
-                o += f * s_o[w][g][d];
-            }
-            if (!part) {
-                write_row<T>(a, r, head0 + g, d, o, sum);
-                if (d == 0) write_lse(a, r, head0 + g, m, sum);
-            } else {
-                part[2 * kAttendHeads + (int64_t)g * a.dim + d] = o;
-                if (d == 0) {
-                    part[g] = m;
-                    part[kAttendHeads + g] = sum;
+                        for (int b = 0; b < DP / 16; b += 4) {
+                            const int d = d0 + DP / 16 * e + b;
+                            if (d < a.dim)
+                                *reinterpret_cast<V4f*>(part + 2 * kAttendHeads + head * a.dim + d) =
+                                    V4f{st.o[b][e], st.o[b + 1][e], st.o[b + 2][e], st.o[b + 3][e]};
+                        }
+                    if (lane < 16) {
+                        part[head] = st.m;
+                        part[kAttendHeads + head] = l;
+                    }
                 }
             }
+            if (!more) break;
+            st.clear();
+            first = 0;
+#pragma unroll
+            for (int i = 0; i < W::L::KV; ++i) q[i] = q_next[i];
         }
-        if (tid == 0 && begins && !ends) {
-            // the workgroup that holds the job's last unit
-            const int64_t stop = at + row.tiles;
-            a.joins[me] = int4{r, hh, (int32_t)(((unsigned __int128)stop * groups - 1) / units), 0};
+        p = pn;
+        cur = nxt;
+        nxt = far;
+        --left;
+    }
+}
+
+// A workgroup to a row and key-value head: its waves take every fourth tile, and
+// their pieces join in shared memory.
+template <typename T, int DP, bool kWhole>
+__global__ __launch_bounds__(kThreads, DP == 256 ? 1 : 2) void k_attend_short(AttendArgs a)
+{
+    typedef Work<T, DP, kWhole> W;
+    constexpr int TILE = Tile<T>::n;
+    __shared__ float s_o[kWaves][kAttendHeads][DP + 4];
+    __shared__ float s_m[kWaves][kAttendHeads], s_l[kWaves][kAttendHeads];
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, head = lane & 15;
+    const int32_t each = a.heads * a.blocks, r = blockIdx.x / each, hh = blockIdx.x - r * each;
+    const Job job = job_at(a, hh);
+    V4u q[W::L::KV];
+    load_queries<T, DP>(a, r, job, lane, q);
+    Row row = row_at<TILE>(a, r);
+    const int32_t* const table = a.table + (int64_t)max(row.seq, 0) * a.table_stride;
+    const T* const keys = static_cast<const T*>(a.k) + job.kv * a.head_stride;
+    const T* const values = static_cast<const T*>(a.v) + job.kv * a.head_stride;
+    State<DP> st;
+    st.clear();
+    for (int32_t i = wave; i < row.tiles; i += kWaves) {
+        W work;
+        Pages<T, kWhole> pages;
+        pages.ask(a, row, table, row.begin(i, TILE), lane);
+        const Places<T, kWhole> p = pages.places(a, row, row.begin(i, TILE));
+        work.load_keys(a, keys, p, lane);
+        work.load_values(a, values, p, lane);
+        float x[W::VROWS];
+        work.scores(a, q, p.seen, lane, x);
+        if (p.seen != (TILE == 32 ? ~0u : 0xFFFFu)) work.drop_unseen_values(p.seen, lane);
+        work.fold(st, x);
+    }
+    const float l = sum_over_lanes(st.l);
+    if (lane < 16) {
+        s_m[wave][lane] = st.m;
+        s_l[wave][lane] = l;
+    }
+    if (head < job.heads) {
+#pragma unroll
+        for (int b = 0; b < DP / 16; ++b)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) s_o[wave][head][DP / 16 * (4 * (lane >> 4) + e) + b] = st.o[b][e];
+    }
+    __syncthreads();
+    for (int x = tid; x < job.heads * a.dim; x += kThreads) {
+        const int g = x / a.dim, d = x - g * a.dim;
+        float m = s_m[0][g];
+#pragma unroll
+        for (int w = 1; w < kWaves; ++w) m = fmaxf(m, s_m[w][g]);
+        const float base = m == -__builtin_inff() ? 0.f : m;
+        float sum = 0.f, o = 0.f;
+#pragma unroll
+        for (int w = 0; w < kWaves; ++w) {
+            const float f = weight<T>(s_m[w][g] - base);
+            sum += f * s_l[w][g];
+            o += f * s_o[w][g][d];
         }
-        __syncthreads();
-        at += last - first;
-        t += last - first;
-        if (last == row.tiles) {
-            before += row.tiles;
-            if (++r == a.rows) {
-                r = 0;
-                before = t = 0;
-                ++hh;
+        out_row<T>(a, r, job.head0 + g)[d] = rounded<T>(sum == 0.f ? 0.f : o / sum);
+        if (d == 0) write_lse(a, r, job.head0 + g, m, sum);
+    }
+}
+
+// Joins the pieces of a row and head that lie in more than one share: the second
+// part of the share it begins in and the first parts of the ones behind it.
+// Eight groups of threads sum every eighth piece, four dims a thread.
+constexpr int kJoinGroups = 8;
+constexpr int kMaxDim = 256;
+constexpr int kJoinPieces = 512;          // factors kept at once
+
+template <typename T>
+__global__ __launch_bounds__(kThreads) void k_attend_join(AttendArgs a)
+{
+    __shared__ float s_f[kJoinPieces];
+    __shared__ float s_m[kWaves], s_l[kWaves];
+    __shared__ V4f s_o[kJoinGroups][kMaxDim / 4];
+    const int32_t each = a.heads * a.blocks, tid = threadIdx.x;
+    const int64_t size = attend_part_floats(a.dim);
+    for (int64_t index = blockIdx.x; index < (int64_t)a.rows * each; index += gridDim.x) {
+        const int2 held = a.joins[index];
+        const int32_t pieces = held.y - held.x + 1;
+        if (pieces == 1) continue;
+        const int32_t r = (int32_t)(index / each);
+        const Job job = job_at(a, (int32_t)(index - (int64_t)r * each));
+        const float* const first = a.parts + (2 * (int64_t)held.x + 1) * size;
+        auto piece = [&](int32_t i) { return i == 0 ? first : first + (2 * (int64_t)i - 1) * size; };
+        for (int g = blockIdx.y; g < job.heads; g += gridDim.y) {
+            float m = -__builtin_inff(), l = 0.f;
+            for (int32_t i = tid; i < pieces; i += kThreads) {
+                const float mi = piece(i)[g], li = piece(i)[kAttendHeads + g], top = fmaxf(m, mi);
+                const float base = top == -__builtin_inff() ? 0.f : top;
+                l = l * weight<T>(m - base) + li * weight<T>(mi - base);
+                m = top;
             }
+#pragma unroll
+            for (int d = 1; d < 64; d <<= 1) {
+                const float mi = __shfl_xor(m, d), li = __shfl_xor(l, d), top = fmaxf(m, mi);
+                const float base = top == -__builtin_inff() ? 0.f : top;
+                l = l * weight<T>(m - base) + li * weight<T>(mi - base);
+                m = top;
+            }
+            if ((tid & 63) == 0) {
+                s_m[tid >> 6] = m;
+                s_l[tid >> 6] = l;
+            }
+            __syncthreads();
+            m = s_m[0];
+#pragma unroll
+            for (int w = 1; w < kWaves; ++w) m = fmaxf(m, s_m[w]);
+            const float base = m == -__builtin_inff() ? 0.f : m;
+            l = 0.f;
+#pragma unroll
+            for (int w = 0; w < kWaves; ++w) l += s_l[w] * weight<T>(s_m[w] - base);
+
+            const int quads = a.dim / 4, group = tid / quads, d4 = tid - group * quads;
+            const int groups = min(kJoinGroups, kThreads / quads);
+            V4f o = {0.f, 0.f, 0.f, 0.f};
+            for (int32_t from = 0; from < pieces; from += kJoinPieces) {
+                const int32_t here = min(kJoinPieces, pieces - from);
+                __syncthreads();
+                for (int32_t i = tid; i < here; i += kThreads) s_f[i] = weight<T>(piece(from + i)[g] - base);
+                __syncthreads();
+                if (group < groups)
+#pragma unroll 4
+                    for (int32_t i = group; i < here; i += groups)
+                        o += s_f[i] * *reinterpret_cast<const V4f*>(piece(from + i) + 2 * kAttendHeads + g * a.dim + 4 * d4);
+            }
+            if (group < groups) s_o[group][d4] = o;
+            __syncthreads();
+            if (tid < quads) {
+                for (int i = 1; i < groups; ++i) o += s_o[i][tid];
+                const float f = l == 0.f ? 0.f : 1.f / l;
+                store4<T>(out_row<T>(a, r, job.head0 + g) + 4 * tid, l == 0.f ? V4f{0.f, 0.f, 0.f, 0.f} : o * f);
+            }
+            if (tid == 0) write_lse(a, r, job.head0 + g, m, l);
+            __syncthreads();
         }
     }
 }
 
-// Joins the pieces of the job that workgroup blockIdx.x began and did not end:
-// its own second part and the first parts of the ones behind it.
-template <typename T>
-__global__ __launch_bounds__(kThreads) void k_attend_join(AttendArgs a)
+template <typename T, int DP, bool kWhole>
+hipError_t attend_as(const AttendArgs& a, hipStream_t s)
 {
-    __shared__ float s_f[kAttendMaxGroups];
-    __shared__ float s_red[2][kWaves];
-    const int4 job = a.joins[blockIdx.x];
-    if (job.x < 0) return;
-    const int32_t kv = job.y / a.blocks, block = job.y - kv * a.blocks, heads = heads_of(a, block);
-    const int32_t pieces = job.z - blockIdx.x + 1, tid = threadIdx.x;
-    const int64_t size = attend_part_floats(a.dim);
-    const float* const first = a.parts + (2 * (int64_t)blockIdx.x + 1) * size;
-    for (int g = blockIdx.y; g < heads; g += gridDim.y) {
-        auto piece = [&](int i) { return i == 0 ? first : first + (2 * (int64_t)i - 1) * size; };
-        float m = -__builtin_inff();
-        for (int i = tid; i < pieces; i += kThreads) {
-            s_f[i] = piece(i)[g];
-            m = fmaxf(m, s_f[i]);
-        }
-#pragma unroll
-        for (int d = 1; d < 64; d <<= 1) m = fmaxf(m, __shfl_xor(m, d));
-        if ((tid & 63) == 0) s_red[0][tid >> 6] = m;
-        __syncthreads();
-#pragma unroll
-        for (int w = 0; w < kWaves; ++w) m = fmaxf(m, s_red[0][w]);
-        const float base = m == -__builtin_inff() ? 0.f : m;
-        float l = 0.f;
-        for (int i = tid; i < pieces; i += kThreads) {
-            s_f[i] = weight<T>(s_f[i] - base);
-            l += s_f[i] * piece(i)[kAttendHeads + g];
-        }
-#pragma unroll
-        for (int d = 1; d < 64; d <<= 1) l += __shfl_xor(l, d);
-        if ((tid & 63) == 0) s_red[1][tid >> 6] = l;
-        __syncthreads();
-        l = 0.f;
-#pragma unroll
-        for (int w = 0; w < kWaves; ++w) l += s_red[1][w];
-        const int32_t head = kv * a.group + block * kAttendHeads + g;
-        for (int d = tid; d < a.dim; d += kThreads) {
-            float o = 0.f;
-#pragma unroll 8
-            for (int i = 0; i < pieces; ++i) o += s_f[i] * piece(i)[2 * kAttendHeads + (int64_t)g * a.dim + d];
-            write_row<T>(a, job.x, head, d, o, l);
-        }
-        if (tid == 0) write_lse(a, job.x, head, m, l);
-        __syncthreads();
+    const dim3 block(kThreads);
+    const int64_t jobs = (int64_t)a.rows * a.heads * a.blocks;
+    const int64_t most = ((int64_t)a.width * a.page_size + Tile<T>::n - 1) / Tile<T>::n;      // tiles of a row
+    if (most <= kShortTiles && jobs <= kMaxGrid) {
+        hipLaunchKernelGGL((k_attend_short<T, DP, kWhole>), dim3((unsigned)jobs), block, 0, s, a);
+        return hipGetLastError();
     }
+    hipLaunchKernelGGL((k_attend<T, DP, kWhole>), dim3((unsigned)a.groups), block, 0, s, a);
+    hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+    hipLaunchKernelGGL(k_attend_join<T>, dim3((unsigned)std::min(jobs, kMaxGrid), (unsigned)std::min(a.group, kAttendHeads)),
+                       block, 0, s, a);
+    return hipGetLastError();
 }
 
 template <typename T, int DP>
 hipError_t attend_dim(const AttendArgs& a, hipStream_t s)
 {
-    const dim3 grid((unsigned)a.groups), block(kThreads);
-    if (a.page_size % 16 == 0)
-        hipLaunchKernelGGL((k_attend<T, DP, true>), grid, block, 0, s, a);
-    else
-        hipLaunchKernelGGL((k_attend<T, DP, false>), grid, block, 0, s, a);
-    hipError_t e = hipGetLastError();
-    if (e != hipSuccess || a.groups == 1) return e;      // one share has no pieces
-    hipLaunchKernelGGL(k_attend_join<T>, dim3((unsigned)a.groups, (unsigned)std::min(a.group, kAttendHeads)), block, 0, s, a);
-    return hipGetLastError();
+    return a.page_size % 16 == 0 ? attend_as<T, DP, true>(a, s) : attend_as<T, DP, false>(a, s);
 }
 
 template <typename T>

@@ -45,7 +45,7 @@ struct AppendArgs {
 };
 
 constexpr int kAttendHeads = 16;         // query heads of a workgroup: the columns of a matrix instruction
-constexpr int kAttendMaxGroups = 1024;   // workgroups of an attention launch at most
+constexpr int kAttendWaves = 4;          // of a workgroup, each with a share of the tiles
 
 struct AttendArgs {
     const void* k;               // of the layer
@@ -56,8 +56,8 @@ struct AttendArgs {
     const int32_t* seqs;
     const int32_t* table;
     const int32_t* lengths;
-    float* parts;                // partial results, two per workgroup
-    int4* joins;                 // per workgroup: the job it began and did not end
+    float* parts;                // partial results, two per share
+    int2* joins;                 // per row and head block: the shares it begins and ends in
     int64_t page_stride, head_stride, token_stride, table_stride;
     int64_t q_stride, q_head_stride, out_stride, out_head_stride;
     int32_t rows, heads, group, blocks;      // q_heads = heads * group, in `blocks` blocks of kAttendHeads

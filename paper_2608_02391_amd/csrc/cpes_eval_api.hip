@@ -155,10 +155,20 @@ int attend_groups(int32_t head_dim)
     return head_dim > 128 ? 256 : 512;
 }
 
-size_t attend_bytes(int32_t head_dim)
+int32_t head_blocks(int32_t group)
 {
-    const size_t groups = attend_groups(head_dim);
-    return groups * sizeof(int4) + 2 * groups * (size_t)cpes::attend_part_floats(head_dim) * sizeof(float);
+    return (group + cpes::kAttendHeads - 1) / cpes::kAttendHeads;
+}
+
+// Two partial results a share, then the shares of every row and head block.
+size_t attend_parts_bytes(int32_t head_dim)
+{
+    return 2 * (size_t)attend_groups(head_dim) * cpes::kAttendWaves * cpes::attend_part_floats(head_dim) * sizeof(float);
+}
+
+size_t attend_bytes(int32_t rows, int32_t q_heads, int32_t kv_heads, int32_t head_dim)
+{
+    return round16(attend_parts_bytes(head_dim) + (size_t)rows * kv_heads * head_blocks(q_heads / kv_heads) * sizeof(int2));
 }
 
 size_t logprob_bytes(int32_t rows, int32_t slices, int32_t top)
@@ -312,7 +322,7 @@ size_t cpes_attend_workspace_bytes(int32_t rows, int32_t q_heads, int32_t kv_hea
     if (rows < 0 || rows > CPES_MAX_SEQUENCES || kv_heads < 1 || q_heads < 1 || q_heads % kv_heads != 0 || head_dim < 8 ||
         head_dim > CPES_MAX_HEAD_DIM || head_dim % 8 != 0)
         return 0;
-    return attend_bytes(head_dim);
+    return attend_bytes(rows, q_heads, kv_heads, head_dim);
 }
 
 int cpes_attend(const cpes_cache* cache, int32_t layer, const cpes_pool* pool, int32_t rows, const int32_t* seqs_dev,
@@ -334,7 +344,7 @@ int cpes_attend(const cpes_cache* cache, int32_t layer, const cpes_pool* pool, i
         rc = fail(CPES_ERR_INVALID_ARGUMENT, "%s: window %d or sinks %d negative", fn, window, sinks);
     if (!rc && (q_stride < 0 || q_head_stride < 0 || out_stride < 0 || out_head_stride < 0))
         rc = fail(CPES_ERR_INVALID_ARGUMENT, "%s: negative stride", fn);
-    if (!rc) rc = check_workspace(workspace_dev, workspace_bytes, attend_bytes(cache->head_dim), fn);
+    if (!rc) rc = check_workspace(workspace_dev, workspace_bytes, attend_bytes(rows, q_heads, cache->heads, cache->head_dim), fn);
     if (rc || rows == 0) return rc;
     cpes::AttendArgs a;
     a.k = at_layer(cache, cache->k_dev, layer);
@@ -346,8 +356,8 @@ int cpes_attend(const cpes_cache* cache, int32_t layer, const cpes_pool* pool, i
     a.table = pool->table_dev;
     a.lengths = pool->lengths_dev;
     a.groups = attend_groups(cache->head_dim);
-    a.joins = static_cast<int4*>(workspace_dev);
-    a.parts = reinterpret_cast<float*>(a.joins + a.groups);
+    a.parts = static_cast<float*>(workspace_dev);
+    a.joins = reinterpret_cast<int2*>(static_cast<char*>(workspace_dev) + attend_parts_bytes(cache->head_dim));
     a.page_stride = cache->page_stride;
     a.head_stride = cache->head_stride;
     a.token_stride = cache->token_stride;
@@ -359,7 +369,7 @@ int cpes_attend(const cpes_cache* cache, int32_t layer, const cpes_pool* pool, i
     a.rows = rows;
     a.heads = cache->heads;
     a.group = q_heads / cache->heads;
-    a.blocks = (a.group + cpes::kAttendHeads - 1) / cpes::kAttendHeads;
+    a.blocks = head_blocks(a.group);
     a.dim = cache->head_dim;
     a.page_size = cache->page_size;
     a.page_shift = -1;

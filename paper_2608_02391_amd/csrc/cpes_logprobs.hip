@@ -97,9 +97,19 @@ __device__ __forceinline__ Sums join(Sums a, Sums b, float c)
     return Sums{m, fa * a.s + fb * b.s, fa * (a.u + da * a.s) + fb * (b.u + db * b.s)};
 }
 
+// The logit of a row's target, if it has one.
+template <typename T> __device__ __forceinline__ float target_logit(const LogprobArgs& a, int64_t row, bool* valid)
+{
+    *valid = false;
+    if (!a.logp) return 0.f;
+    const int64_t v = a.targets[row];
+    *valid = v >= 0 && v < a.vocab;
+    return *valid ? value_of(static_cast<const T*>(a.x)[row * a.stride + v]) : 0.f;
+}
+
 // Writes a finished row's numbers; every thread gets what the alternatives need.
-template <typename T>
-__device__ __forceinline__ void finish(const LogprobArgs& a, int64_t row, Sums t, float* logsum, bool* broken)
+__device__ __forceinline__ void finish(const LogprobArgs& a, int64_t row, Sums t, float target, bool valid, float* logsum,
+                                       bool* broken)
 {
     const float nan = __builtin_nanf("");
     const bool empty = t.s == 0.f;        // nothing but -inf
@@ -107,15 +117,7 @@ __device__ __forceinline__ void finish(const LogprobArgs& a, int64_t row, Sums t
     t.s -= a.excess * t.u;
     *logsum = *broken ? nan : empty ? 0.f : logf(t.s);
     if (threadIdx.x != 0) return;
-    if (a.logp) {
-        const int64_t v = a.targets[row];
-        float x = 0.f;
-        if (v >= 0 && v < a.vocab) {
-            x = value_of(static_cast<const T*>(a.x)[row * a.stride + v]);
-            x = empty ? -__builtin_inff() : a.scale * (x - t.m) - *logsum;
-        }
-        a.logp[row] = x;
-    }
+    if (a.logp) a.logp[row] = !valid ? 0.f : empty ? -__builtin_inff() : a.scale * (target - t.m) - *logsum;
     if (a.entropy) a.entropy[row] = empty ? 0.f : *logsum - t.u / t.s * kLn2;
     if (a.lse) a.lse[row] = *broken ? nan : a.scale * t.m + *logsum;
     if (a.stats) {
@@ -157,18 +159,138 @@ __device__ void largest(const Key* keys, int n, int k, Key* best)
 
 constexpr int kUnroll = 4;                // 16-byte loads of a thread and step
 constexpr int kMaxTop = 64;
-constexpr int kSoft = 256;                // candidates from which on they are thinned out
-constexpr int kCandidates = kSoft + kThreads * 8;
+constexpr int kNoted = 32;                // steps whose maxima are kept
+constexpr int kItems = 512;               // of them looked at again
+constexpr int kRound = 64;                // threads that look at a vector each while candidates may have to be thinned out
+constexpr int kCandidates = 768;          // a key's room; kRound threads can add 8 each to 256
+constexpr int kManyOwners = 3 * kMaxTop / 2;
+constexpr float kHuge = 1e30f;
 
-// One slice of one row.
-template <typename T>
-__global__ __launch_bounds__(kThreads) void k_logprobs(LogprobArgs a)
+// A thread's sums while it reads.  Exponents are one fused multiply-add, c x - b
+// with b = c m rounded; what b lost is put right when the thread is done.  Where
+// b does not fit (nothing but -inf so far, or the type's lowest value) they are
+// c (x - m).
+struct Running {
+    float m, b, s, u;
+
+    __device__ __forceinline__ bool far() const { return !(fabsf(b) < kHuge); }
+
+    __device__ __forceinline__ void rise(float top, float c)
+    {
+        const float next = top * c;
+        const float d = s == 0.f ? 0.f : fmaxf(far() || !(fabsf(next) < kHuge) ? c * (m - top) : b - next, kFar);
+        const float f = exp2_hw(d);
+        u = f * (u + d * s);
+        s *= f;
+        m = top;
+        b = next;
+    }
+
+    // Adds N logits; true if one is a new maximum.  *most receives their own.
+    template <int N> __device__ __forceinline__ bool take(const float* x, float c, float* most)
+    {
+        float top = x[0], least = x[0];
+#pragma unroll
+        for (int j = 1; j < N; ++j) {
+            top = fmaxf(top, x[j]);
+            least = fminf(least, x[j]);
+        }
+        const bool rises = top > m;
+        *most = top;
+        if (rises) rise(top, c);
+        // 0 times an exponent of -inf is no number: such steps bound it
+        if (__all(!far() && fmaf(least, c, -b) > -kHuge)) {
+#pragma unroll
+            for (int j = 0; j < N; ++j) {
+                const float t = fmaf(x[j], c, -b), e = exp2_hw(t);
+                s += e;
+                u = fmaf(e, t, u);
+            }
+        } else {
+            const float base = m == -__builtin_inff() ? 0.f : m;
+            const bool apart = far();
+#pragma unroll
+            for (int j = 0; j < N; ++j) {
+                const float t = apart ? c * (x[j] - base) : fmaf(x[j], c, -b), e = exp2_hw(t);
+                s += e;
+                u = fmaf(e, fmaxf(t, kFar), u);
+            }
+        }
+        return rises;
+    }
+
+    __device__ __forceinline__ Sums done(float c) const
+    {
+        const float lost = far() ? 0.f : fmaf(m, c, -b), f = exp2_hw(-lost);
+        return Sums{m, f * s, f * (u - lost * s)};
+    }
+};
+
+// The least bf16 not below x.
+__device__ __forceinline__ uint16_t bf16_above(float x)
+{
+    const uint32_t u = __float_as_uint(x);
+    return (uint16_t)((u & 0x80000000u ? u : u + 0xFFFFu) >> 16);
+}
+
+// The key that at least `top` threads' maxima reach, and the threads that may hold
+// a key from there on, in s_owner; their number is returned.  low and high bound
+// the key of this thread's maximum (0: no logits).  Each wave ranks its own lanes;
+// the least of the waves' (top / waves)-th keys is reached by `top` of them.  All
+// threads.
+__device__ int bound_by_waves(Key low, Key high, int top, Key* s_wave, int32_t* s_owner, int32_t* s_owners, Key* least)
+{
+    constexpr int kWaves = kThreads / 64;
+    const int each = (top + kWaves - 1) / kWaves;
+    int place = 0;
+#pragma unroll 8
+    for (int j = 0; j < 64; ++j) {
+        const Key other = ((Key)(uint32_t)__builtin_amdgcn_readlane((int)(low >> 32), j) << 32) |
+                          (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)low, j);
+        place += other > low;
+    }
+    if (threadIdx.x == 0) *s_owners = 0;
+    if ((threadIdx.x & 63) == 0) s_wave[threadIdx.x >> 6] = 0;
+    __syncthreads();
+    if (low && place == each - 1) s_wave[threadIdx.x >> 6] = low;
+    __syncthreads();
+    Key bound = s_wave[0];
+#pragma unroll
+    for (int w = 1; w < kWaves; ++w) bound = min(bound, s_wave[w]);
+    *least = max(bound, (Key)1);          // fewer logits than that: all of them
+    if (high >= *least) s_owner[atomicAdd(s_owners, 1)] = threadIdx.x;
+    __syncthreads();
+    return *s_owners;
+}
+
+// The same exactly, from the exact keys of all threads' maxima: `top` owners, or all.
+__device__ int bound_exactly(Key key, int top, Key* s_keys, int32_t* s_owner, int32_t* s_owners, Key* least)
+{
+    s_keys[threadIdx.x] = key;
+    if (threadIdx.x == 0) *s_owners = 0;
+    __syncthreads();
+    int place = 0;
+    for (int j = 0; j < kThreads; ++j) place += s_keys[j] > key;
+    const bool mine = key && place < top;
+    if (mine) s_owner[place] = threadIdx.x;
+    if (mine) atomicAdd(s_owners, 1);
+    __syncthreads();
+    const int owners = *s_owners;
+    *least = owners == top ? s_keys[s_owner[top - 1]] : 1;
+    __syncthreads();
+    return owners;
+}
+
+// One slice of one row.  NT: the logits exceed the last-level cache, and are read
+// past the caches (622 million of bf16: 233 -> 206 us with 5 alternatives).
+template <typename T, bool NT>
+__global__ __launch_bounds__(kThreads, 5) void k_logprobs(LogprobArgs a)
 {
     constexpr int N = Vec<T>::n;
-    constexpr uint32_t kNone = std::is_same<T, float>::value ? 0xFF800000u : 0xFF80FF80u;   // -inf
     __shared__ Sums s_sums[kThreads / 64];
-    __shared__ Key s_keys[kCandidates], s_best[kMaxTop];
-    __shared__ int32_t s_owner[kThreads], s_count, s_owners;
+    __shared__ Key s_keys[kCandidates], s_best[kMaxTop], s_wave[kThreads / 64];
+    __shared__ int32_t s_owner[kThreads], s_count, s_owners, s_items;
+    __shared__ uint16_t s_most[kNoted][kThreads], s_item[kItems];
     const int tid = threadIdx.x;
     for (int64_t job = blockIdx.x; job < (int64_t)a.rows * a.slices; job += gridDim.x) {
         const int64_t row = job / a.slices;
@@ -178,118 +300,166 @@ __global__ __launch_bounds__(kThreads) void k_logprobs(LogprobArgs a)
         const T* const x0 = static_cast<const T*>(a.x) + row * a.stride + begin;
         const int32_t full = len / N, vecs = (len + N - 1) / N, steps = (vecs + kUnroll * kThreads - 1) / (kUnroll * kThreads);
 
-        auto vector_at = [&](int32_t i) {
-            if (i < full) return (V4u)*reinterpret_cast<const V4uAnywhere*>(x0 + (int64_t)i * N);
-            V4u w = {kNone, kNone, kNone, kNone};
-            if (i < vecs) {
-                T* const e = reinterpret_cast<T*>(&w);
-                for (int j = 0; j < N; ++j)
-                    if (i * N + j < len) e[j] = x0[(int64_t)i * N + j];
-            }
-            return w;
-        };
+        const int32_t whole = full / (kUnroll * kThreads);
 
-        Sums t = {-__builtin_inff(), 0.f, 0.f};
-        int32_t met = 0;                  // the step the maximum was first met in
-        for (int32_t step = 0; step < steps; ++step) {
-            V4u w[kUnroll];
-            const int32_t i0 = step * kUnroll * kThreads + tid;
-            if ((step + 1) * kUnroll * kThreads <= full) {
-#pragma unroll
-                for (int u = 0; u < kUnroll; ++u)
-                    w[u] = *reinterpret_cast<const V4uAnywhere*>(x0 + (int64_t)(i0 + u * kThreads) * N);
+        // Vector i as floats; -inf behind the slice's end.
+        auto floats_at = [&](int32_t i, float* x) {
+            if (i < full) {
+                unpack<T>(*reinterpret_cast<const V4uAnywhere*>(x0 + (int64_t)i * N), x);
             } else {
 #pragma unroll
-                for (int u = 0; u < kUnroll; ++u) w[u] = vector_at(i0 + u * kThreads);
+                for (int j = 0; j < N; ++j) {
+                    x[j] = -__builtin_inff();
+                    if (i < vecs && i * N + j < len) x[j] = value_of(x0[(int64_t)i * N + j]);
+                }
             }
-            float x[kUnroll * N], top = t.m;
+        };
+
+        bool valid = false;
+        float target = 0.f;
+        if (a.slices == 1 && tid == 0) target = target_logit<T>(a, row, &valid);
+        Running run = {-__builtin_inff(), -__builtin_inff(), 0.f, 0.f};
+        int32_t met = 0;                  // the step the maximum was first met in
+        float most;
+        V4u w[kUnroll];                   // the next step's, on their way while one is added
+        auto load = [&](int32_t step) {
+#pragma unroll
+            for (int u = 0; u < kUnroll; ++u) {
+                const V4uAnywhere* const q =
+                    reinterpret_cast<const V4uAnywhere*>(x0 + (int64_t)((step * kUnroll + u) * kThreads + tid) * N);
+                w[u] = NT ? __builtin_nontemporal_load(q) : *q;
+            }
+        };
+        if (whole > 0) load(0);
+        for (int32_t step = 0; step < whole; ++step) {
+            float x[kUnroll * N];
 #pragma unroll
             for (int u = 0; u < kUnroll; ++u) unpack<T>(w[u], x + u * N);
-#pragma unroll
-            for (int j = 0; j < kUnroll * N; ++j) top = fmaxf(top, x[j]);
-            if (top > t.m) {
-                const float d = t.s == 0.f ? 0.f : fmaxf(a.c * (t.m - top), kFar), f = exp2_hw(d);
-                t.u = f * (t.u + d * t.s);
-                t.s *= f;
-                t.m = top;
-                met = step;
-            }
-            const float base = t.m == -__builtin_inff() ? 0.f : t.m;
-#pragma unroll
-            for (int j = 0; j < kUnroll * N; ++j) {
-                const float d = a.c * (x[j] - base), e = exp2_hw(d);
-                t.s += e;
-                t.u += e * fmaxf(d, kFar);
-            }
+            if (step + 1 < whole) load(step + 1);
+            if (run.take<kUnroll * N>(x, a.c, &most)) met = step;
+            if (a.top > 0 && step < kNoted) s_most[step][tid] = bf16_above(most);
         }
-        // the threads' sums join, in a fixed order; the maximum a thread met stays its own
-        const float mine = t.m;
+        if (whole < steps) {
+            float all = -__builtin_inff();
+#pragma unroll 1
+            for (int u = 0; u < kUnroll; ++u) {
+                float x[N];
+                floats_at((whole * kUnroll + u) * kThreads + tid, x);
+                if (run.take<N>(x, a.c, &most)) met = whole;
+                all = fmaxf(all, most);
+            }
+            if (a.top > 0 && whole < kNoted) s_most[whole][tid] = bf16_above(all);
+        }
+        // the threads' sums join, in a fixed order
+        Sums t = run.done(a.c);
 #pragma unroll
         for (int d = 1; d < 64; d <<= 1)
             t = join(t, Sums{__shfl_xor(t.m, d), __shfl_xor(t.s, d), __shfl_xor(t.u, d)}, a.c);
         if ((tid & 63) == 0) s_sums[tid >> 6] = t;
-        if (a.top > 0 && tid == 0) s_count = s_owners = 0;
-        Key low = 0, high = 0;            // no more and no less than the key of this thread's maximum
-        if (a.top > 0) {
-            const int64_t first = begin + ((int64_t)(met * kUnroll) * kThreads + tid) * N;
-            if (tid < vecs) {
-                low = key_of(mine, (uint32_t)(first + (kUnroll - 1) * kThreads * N + N - 1));
-                high = key_of(mine, (uint32_t)first);
-            }
-            s_keys[tid] = low;
-        }
+        if (tid == 0) s_count = s_items = 0;
         __syncthreads();
         t = s_sums[0];
 #pragma unroll
-        for (int w = 1; w < kThreads / 64; ++w) t = join(t, s_sums[w], a.c);
+        for (int v = 1; v < kThreads / 64; ++v) t = join(t, s_sums[v], a.c);
         float logsum = 0.f;
         bool broken = false;
         if (a.slices == 1)
-            finish<T>(a, row, t, &logsum, &broken);
+            finish(a, row, t, target, valid, &logsum, &broken);
         else if (tid == 0)
             a.parts[job] = float4{t.m, t.s, t.u, 0.f};
 
         if (a.top > 0) {
-            // the k-th largest lower end, and the threads that reach it
-            int place = 0;
-            for (int j = 0; j < kThreads; ++j) place += s_keys[j] > low;
-            if (tid == 0) s_best[0] = 1;
-            __syncthreads();
-            if (low && place == a.top - 1) s_best[0] = low;
-            __syncthreads();
-            Key least = s_best[0];
-            if (high >= least) s_owner[atomicAdd(&s_owners, 1)] = tid;
-            __syncthreads();
-            const int owners = s_owners;
-            // their logits from there on
-            const int32_t per = steps * kUnroll, items = owners * per;
-            for (int32_t item0 = 0; item0 < items; item0 += kThreads) {
-                const int n = s_count;
-                __syncthreads();          // read by all before any candidate is added
-                if (n > kSoft) {
-                    largest(s_keys, n, a.top, s_best);
-                    if (tid < a.top) s_keys[tid] = s_best[tid];
-                    if (tid == 0) s_count = a.top;
-                    least = s_best[a.top - 1];
-                    __syncthreads();
-                }
-                const int32_t item = item0 + tid, o = item / per;
-                if (item < items) {
-                    const int32_t i = (item - o * per) * kThreads + s_owner[o];
-                    if (i < vecs) {
-                        const V4u w = vector_at(i);
+            const int32_t first = met * kUnroll * kThreads + tid;             // vectors of the step
+            auto token = [&](int32_t i, int j) { return (uint32_t)(begin + (int64_t)i * N + j); };
+            Key low = 0, high = 0, least;
+            if (tid < vecs) {
+                low = key_of(run.m, token(first + (kUnroll - 1) * kThreads, N - 1));
+                high = key_of(run.m, token(first, 0));
+            }
+            int owners = bound_by_waves(low, high, a.top, s_wave, s_owner, &s_owners, &least);
+            if (owners > kManyOwners) {
+                // many maxima tie: find where each was met
+                Key exact = 0;
+                if (tid < vecs)
+                    for (int u = kUnroll - 1; u >= 0; --u) {
                         float x[N];
-                        unpack<T>(w, x);
+                        floats_at(first + u * kThreads, x);
 #pragma unroll
-                        for (int j = 0; j < N; ++j) {
-                            const Key k = key_of(x[j], (uint32_t)(begin + (int64_t)i * N + j));
-                            if (i * N + j < len && k >= least) s_keys[atomicAdd(&s_count, 1)] = k;
-                        }
+                        for (int j = N - 1; j >= 0; --j)
+                            if (x[j] == run.m && (first + u * kThreads) * N + j < len)
+                                exact = key_of(run.m, token(first + u * kThreads, j));
+                    }
+                __syncthreads();
+                owners = bound_exactly(exact, a.top, s_keys, s_owner, &s_owners, &least);
+            }
+            // the owners' logits from the bound on
+            auto collect = [&](const float* x, int32_t i) {
+#pragma unroll
+                for (int j = 0; j < N; ++j) {
+                    const Key k = key_of(x[j], token(i, j));
+                    if (k >= least && i * N + j < len) {
+                        const int at = atomicAdd(&s_count, 1);
+                        if (at < kCandidates) s_keys[at] = k;
                     }
                 }
+            };
+            bool whole_owners = steps > kNoted;
+            if (!whole_owners) {
+                // only the steps of theirs that reach the bound
+                if (high >= least)
+                    for (int32_t step = 0; step < steps; ++step)
+                        if (value_of(s_most[step][tid]) >= key_value(least) || least == 1) {
+                            const int at = atomicAdd(&s_items, 1);
+                            if (at < kItems) s_item[at] = (uint16_t)(step * kThreads + tid);
+                        }
                 __syncthreads();
+                const int items = s_items;
+                whole_owners = items > kItems;
+                if (!whole_owners) {
+                    for (int at = tid; at < items * kUnroll; at += kThreads) {
+                        const int32_t x = s_item[at / kUnroll];
+                        const int32_t i = (x / kThreads * kUnroll + at % kUnroll) * kThreads + x % kThreads;
+                        if (i < vecs) {
+                            float v[N];
+                            floats_at(i, v);
+                            collect(v, i);
+                        }
+                    }
+                    __syncthreads();
+                    whole_owners = s_count > kCandidates;
+                }
             }
-            largest(s_keys, s_count, a.top, s_best);
+            int n = s_count;
+            if (whole_owners) {
+                // more than there is room for: all of theirs, a round at a time, with the bound raised by what is there
+                __syncthreads();
+                if (tid == 0) s_count = 0;
+                __syncthreads();
+                const int32_t per = steps * kUnroll, items = owners * per;
+                for (int32_t item0 = 0; item0 < items; item0 += kRound) {
+                    const int had = s_count;
+                    __syncthreads();      // read by all before any candidate is added
+                    if (had > kCandidates - 8 * kRound) {
+                        largest(s_keys, had, a.top, s_best);
+                        if (tid < a.top) s_keys[tid] = s_best[tid];
+                        if (tid == 0) s_count = a.top;
+                        least = s_best[a.top - 1];
+                        __syncthreads();
+                    }
+                    const int32_t item = item0 + tid, o = item / per;
+                    if (tid < kRound && item < items) {
+                        const int32_t i = (item - o * per) * kThreads + s_owner[o];
+                        if (i < vecs) {
+                            float x[N];
+                            floats_at(i, x);
+                            collect(x, i);
+                        }
+                    }
+                    __syncthreads();
+                }
+                n = s_count;
+            }
+            largest(s_keys, n, a.top, s_best);
             if (tid < a.top) {
                 if (a.slices == 1)
                     write_top(a, row, tid, s_best[tid], t.m, logsum, broken);
@@ -305,10 +475,12 @@ __global__ __launch_bounds__(kThreads) void k_logprobs(LogprobArgs a)
 template <typename T>
 __global__ __launch_bounds__(kThreads) void k_logprobs_join(LogprobArgs a)
 {
-    __shared__ Key s_keys[kMaxSlices * kMaxTop], s_head[kMaxSlices], s_best[kMaxTop], s_least;
+    __shared__ Key s_keys[kMaxSlices * kMaxTop], s_best[kMaxTop], s_least;
     __shared__ int32_t s_count;
     const int tid = threadIdx.x, lane = tid & 63;
     const int64_t row = blockIdx.x;
+    bool valid;
+    const float target = target_logit<T>(a, row, &valid);
     Sums t = {-__builtin_inff(), 0.f, 0.f};
     if (lane < a.slices) {
         const float4 p = a.parts[row * a.slices + lane];
@@ -320,20 +492,21 @@ __global__ __launch_bounds__(kThreads) void k_logprobs_join(LogprobArgs a)
     t = Sums{__shfl(t.m, 0), __shfl(t.s, 0), __shfl(t.u, 0)};
     float logsum;
     bool broken;
-    finish<T>(a, row, t, &logsum, &broken);
+    finish(a, row, t, target, valid, &logsum, &broken);
     if (a.top == 0) return;
-    // the k-th largest of the slices' first keys bounds what can be among the row's k largest
+    // the k-th largest of the slices' first few keys, twice as many as k, bounds what can be among the row's k largest
     const Key* const keys = a.keys + row * a.slices * a.top;
-    const Key head = tid < a.slices ? keys[tid * a.top] : 0;
-    if (tid < kMaxSlices) s_head[tid] = head;
+    const int few = min(a.top, 2 * ((a.top + a.slices - 1) / a.slices)), heads = a.slices * few;
+    for (int i = tid; i < heads; i += kThreads) s_keys[i] = keys[i / few * a.top + i % few];
     if (tid == 0) {
         s_count = 0;
         s_least = 1;
     }
     __syncthreads();
-    if (tid < a.slices) {
+    for (int i = tid; i < heads; i += kThreads) {
+        const Key head = s_keys[i];
         int place = 0;
-        for (int j = 0; j < a.slices; ++j) place += s_head[j] > head;
+        for (int j = 0; j < heads; ++j) place += s_keys[j] > head;
         if (place == a.top - 1 && head) s_least = head;
     }
     __syncthreads();
@@ -346,8 +519,8 @@ __global__ __launch_bounds__(kThreads) void k_logprobs_join(LogprobArgs a)
 }
 
 // --------------------------------------------------------------- gradient --
-constexpr int kGradUnroll = 2;
 constexpr int64_t kMaxGrid = 1 << 20;     // workgroups per launch; larger jobs loop
+constexpr double kCacheBytes = 256 << 20; // the last-level cache
 
 template <typename T> __device__ __forceinline__ V4u pack(const float* x);
 template <> __device__ __forceinline__ V4u pack<float>(const float* x)
@@ -366,9 +539,14 @@ template <> __device__ __forceinline__ V4u pack<uint16_t>(const float* x)
     return __builtin_bit_cast(V4u, h);
 }
 
-template <typename T>
+// Large gradients are written past the caches, and logits that exceed them read so
+// too, four vectors a thread then (622 million of bf16: 444 -> 402 us); logits that
+// the forward call has left in the caches are read from there (100 million: 72 ->
+// 60 us with the stores alone).
+template <typename T, bool kFarLoad, bool kFarStore>
 __global__ __launch_bounds__(kThreads) void k_logprobs_backward(LogprobGradArgs a)
 {
+    constexpr int kGradUnroll = kFarLoad ? 4 : 2;
     constexpr int N = Vec<T>::n;
     const int32_t vecs = (a.vocab + N - 1) / N, full = a.vocab / N;
     const int64_t chunks = (vecs + kGradUnroll * kThreads - 1) / (kGradUnroll * kThreads);
@@ -395,8 +573,10 @@ __global__ __launch_bounds__(kThreads) void k_logprobs_backward(LogprobGradArgs 
         V4u w[kGradUnroll];
 #pragma unroll
         for (int u = 0; u < kGradUnroll; ++u)
-            if (i0 + u * kThreads < full)
-                w[u] = *reinterpret_cast<const V4uAnywhere*>(x0 + (int64_t)(i0 + u * kThreads) * N);
+            if (i0 + u * kThreads < full) {
+                const V4uAnywhere* const q = reinterpret_cast<const V4uAnywhere*>(x0 + (int64_t)(i0 + u * kThreads) * N);
+                w[u] = kFarLoad ? __builtin_nontemporal_load(q) : *q;
+            }
 #pragma unroll
         for (int u = 0; u < kGradUnroll; ++u) {
             const int32_t i = i0 + u * kThreads;
@@ -405,7 +585,11 @@ __global__ __launch_bounds__(kThreads) void k_logprobs_backward(LogprobGradArgs 
                 unpack<T>(w[u], x);
 #pragma unroll
                 for (int j = 0; j < N; ++j) x[j] = gradient(x[j], (int64_t)i * N + j);
-                *reinterpret_cast<V4uAnywhere*>(d0 + (int64_t)i * N) = pack<T>(x);
+                V4uAnywhere* const q = reinterpret_cast<V4uAnywhere*>(d0 + (int64_t)i * N);
+                if (kFarStore)
+                    __builtin_nontemporal_store(pack<T>(x), q);
+                else
+                    *q = pack<T>(x);
             } else if (i < vecs) {
                 for (int64_t v = (int64_t)i * N; v < a.vocab; ++v) {
                     const float d = gradient(value_of(x0[v]), v);
@@ -423,18 +607,35 @@ template <typename T>
 hipError_t logprobs_t(const LogprobArgs& a, hipStream_t s)
 {
     const int64_t jobs = (int64_t)a.rows * a.slices;
-    hipLaunchKernelGGL(k_logprobs<T>, dim3((unsigned)std::min(jobs, kMaxGrid)), dim3(kThreads), 0, s, a);
+    const dim3 grid((unsigned)std::min(jobs, kMaxGrid)), block(kThreads);
+    if ((double)a.rows * a.vocab * sizeof(T) > kCacheBytes)
+        hipLaunchKernelGGL((k_logprobs<T, true>), grid, block, 0, s, a);
+    else
+        hipLaunchKernelGGL((k_logprobs<T, false>), grid, block, 0, s, a);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess || a.slices == 1) return e;
     hipLaunchKernelGGL(k_logprobs_join<T>, dim3((unsigned)a.rows), dim3(kThreads), 0, s, a);
     return hipGetLastError();
 }
 
+template <typename T, bool kFarLoad, bool kFarStore>
+void backward_as(const LogprobGradArgs& a, hipStream_t s)
+{
+    const int64_t per = (int64_t)(kFarLoad ? 4 : 2) * kThreads * Vec<T>::n, jobs = a.rows * ((a.vocab + per - 1) / per);
+    hipLaunchKernelGGL((k_logprobs_backward<T, kFarLoad, kFarStore>), dim3((unsigned)std::min(jobs, kMaxGrid)),
+                       dim3(kThreads), 0, s, a);
+}
+
 template <typename T>
 hipError_t backward_t(const LogprobGradArgs& a, hipStream_t s)
 {
-    const int64_t per = (int64_t)kGradUnroll * kThreads * Vec<T>::n, jobs = a.rows * ((a.vocab + per - 1) / per);
-    hipLaunchKernelGGL(k_logprobs_backward<T>, dim3((unsigned)std::min(jobs, kMaxGrid)), dim3(kThreads), 0, s, a);
+    const double bytes = (double)a.rows * a.vocab * sizeof(T);
+    if (bytes > kCacheBytes)
+        backward_as<T, true, true>(a, s);
+    else if (2 * bytes > kCacheBytes)
+        backward_as<T, false, true>(a, s);
+    else
+        backward_as<T, false, false>(a, s);
     return hipGetLastError();
 }
 
