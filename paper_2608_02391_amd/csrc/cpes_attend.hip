@@ -53,7 +53,12 @@ typedef V2u V2uAnywhere __attribute__((aligned(2)));
 constexpr int kWaves = kAttendWaves;
 constexpr int kThreads = 64 * kWaves;
 constexpr int kShareTiles = 2;            // tiles of a wave's share at least
-constexpr int kShortTiles = 16;           // tiles of a row up to which a workgroup takes the row
+// A workgroup of four waves takes a row where none has more than this many tiles,
+// or four times as many and rows and heads alone fill the GPU (64 rows of 700
+// positions, 8 heads: 42 us in shares, 31 so); of eight waves where none has more
+// than twice as many (one row of 600: 15.4 us in shares, 9.4 so; of 2,000: 15 and 22).
+constexpr int kShortTiles = 16;
+constexpr int64_t kManyJobs = 256;
 constexpr int64_t kMaxGrid = 1 << 20;     // workgroups of the short and the join launch
 constexpr float kLog2e = 1.44269504088896340736f;
 
@@ -245,6 +250,9 @@ template <typename T, int DP, bool kWhole> struct Work {
         }
     }
 
+    // Past the caches: a step reads each value once, and all layers' caches exceed
+    // them (3 GB: 504 -> 454 us; 134 MB that could have stayed there: 31.2 -> 32.1 us).
+    // A key row's line is completed by the next load, so keys take the usual way.
     __device__ __forceinline__ void load_values(const AttendArgs& a, const T* head, const Places<T, kWhole>& p, int lane)
     {
         constexpr int E = 16 / sizeof(T);
@@ -253,13 +261,14 @@ template <typename T, int DP, bool kWhole> struct Work {
         for (int j = 0; j < VROWS; ++j) {
             const T* q = head + value_row(a, p, j, lane);
             if constexpr (L::VD == 2) {
-                const V2u x = *reinterpret_cast<const V2uAnywhere*>(q + (d0 < a.dim ? d0 : 0));
+                const V2u x = __builtin_nontemporal_load(reinterpret_cast<const V2uAnywhere*>(q + (d0 < a.dim ? d0 : 0)));
                 val[j][0] = x[0];
                 val[j][1] = x[1];
             } else {
 #pragma unroll
                 for (int i = 0; i < L::VD / 4; ++i) {
-                    const V4u x = *reinterpret_cast<const V4uAnywhere*>(q + (d0 + E * i < a.dim ? d0 + E * i : 0));
+                    const V4u x = __builtin_nontemporal_load(
+                        reinterpret_cast<const V4uAnywhere*>(q + (d0 + E * i < a.dim ? d0 + E * i : 0)));
 #pragma unroll
                     for (int e = 0; e < 4; ++e) val[j][4 * i + e] = x[e];
                 }
@@ -426,21 +435,35 @@ template <> __device__ __forceinline__ void store4<uint16_t>(uint16_t* p, V4f x)
     *reinterpret_cast<V2uAnywhere*>(p) = __builtin_bit_cast(V2u, h);
 }
 
-// First unit of a wave's share: floor(units w / waves) without its product.
-__device__ __forceinline__ int64_t share_begin(int64_t units, int32_t waves, int32_t w)
+// floor(x / y) of counts below 2^53: a third of the integer sequence's instructions.
+__device__ __forceinline__ int64_t quotient(int64_t x, int64_t y)
 {
-    const int64_t q = units / waves;
-    return q * w + (int64_t)((int32_t)(units - q * waves) * w / waves);       // both factors below 2^12
+    int64_t q = (int64_t)((double)x / (double)y);
+    const int64_t r = x - q * y;
+    return r < 0 ? q - 1 : r >= y ? q + 1 : q;
 }
 
-// The share that holds a unit.
-__device__ int32_t share_of(int64_t units, int32_t waves, int64_t unit)
-{
-    int32_t w = min(waves - 1, (int32_t)((double)unit * waves / (double)units));
-    while (share_begin(units, waves, w) > unit) --w;
-    while (w + 1 < waves && share_begin(units, waves, w + 1) <= unit) ++w;
-    return w;
-}
+// The line of `units` tiles in `waves` shares: share w begins at floor(units w / waves).
+struct Shares {
+    int64_t units, q;
+    int32_t rest, waves;
+
+    __device__ __forceinline__ Shares(int64_t u, int32_t n) : units(u), q(quotient(u, n)), rest((int32_t)(u - q * n)), waves(n) {}
+
+    __device__ __forceinline__ int64_t begin(int32_t w) const
+    {
+        return q * w + (int64_t)((uint32_t)(rest * w) / (uint32_t)waves);     // both factors below 2^12
+    }
+
+    // The share that holds a unit.
+    __device__ int32_t of(int64_t unit) const
+    {
+        int32_t w = min(waves - 1, (int32_t)((double)unit * waves / (double)units));      // or a neighbour
+        while (begin(w) > unit) --w;
+        while (w + 1 < waves && begin(w + 1) <= unit) ++w;
+        return w;
+    }
+};
 
 // A tile of the line: row, key-value head and block, and its place in the row.
 struct Cursor {
@@ -468,8 +491,12 @@ __global__ __launch_bounds__(kThreads, DP == 256 ? 1 : 2) void k_attend(AttendAr
     __shared__ int32_t s_row[kWaves];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
 
-    // every row's tiles, and where this workgroup's waves begin on their line
-    const int32_t each = (a.rows + kThreads - 1) / kThreads, r0 = min(a.rows, tid * each), r1 = min(a.rows, r0 + each);
+    // Every row's tiles, and where this workgroup's waves begin on their line.  Up
+    // to 64 rows a wave finds its own place, a lane to a row; more are spread over
+    // the workgroup's threads.
+    const bool few = a.rows <= 64;
+    const int32_t threads = few ? 64 : kThreads, thread = few ? lane : tid;
+    const int32_t each = (a.rows + threads - 1) / threads, r0 = min(a.rows, thread * each), r1 = min(a.rows, r0 + each);
     int64_t mine = 0;
     for (int32_t r = r0; r < r1; ++r) mine += row_at<TILE>(a, r).tiles;
     int64_t upto = mine;
@@ -478,46 +505,60 @@ __global__ __launch_bounds__(kThreads, DP == 256 ? 1 : 2) void k_attend(AttendAr
         const int64_t y = __shfl_up(upto, d);
         if (lane >= d) upto += y;
     }
-    if (lane == 63) s_sum[wave] = upto;
-    __syncthreads();
-    int64_t tiles = 0;
+    int64_t tiles = __shfl(upto, 63);
+    if (!few) {
+        if (lane == 63) s_sum[wave] = upto;
+        __syncthreads();
+        tiles = 0;
 #pragma unroll
-    for (int w = 0; w < kWaves; ++w) {
-        if (w < wave) upto += s_sum[w];
-        tiles += s_sum[w];
+        for (int w = 0; w < kWaves; ++w) {
+            if (w < wave) upto += s_sum[w];
+            tiles += s_sum[w];
+        }
     }
     const int64_t units = tiles * a.heads * a.blocks;
     const int32_t waves = (int32_t)max((int64_t)1, min((int64_t)a.groups * kWaves, units / kShareTiles));
-    const int32_t w0 = blockIdx.x * kWaves;
+    const int32_t w0 = blockIdx.x * kWaves, me = w0 + wave;
     if (w0 >= waves) return;
-#pragma unroll
-    for (int w = 0; w < kWaves; ++w) {
-        if (w0 + w >= waves) break;
-        const int64_t t = share_begin(units, waves, w0 + w) % tiles;
-        if (t >= upto - mine && t < upto) {
-            int64_t before = upto - mine;
-            int32_t r = r0;
-            for (; r < r1; ++r) {
-                const int32_t n = row_at<TILE>(a, r).tiles;
-                if (t < before + n) break;
-                before += n;
+    const Shares shares(units, waves);
+    if (!few) {
+#pragma unroll 1
+        for (int w = 0; w < kWaves; ++w) {
+            if (w0 + w >= waves) break;
+            const int64_t at = shares.begin(w0 + w), t = at - quotient(at, tiles) * tiles;
+            if (t >= upto - mine && t < upto) {
+                int64_t before = upto - mine;
+                int32_t r = r0;
+                for (; r < r1; ++r) {
+                    const int32_t n = row_at<TILE>(a, r).tiles;
+                    if (t < before + n) break;
+                    before += n;
+                }
+                s_row[w] = r;
+                s_before[w] = before;
             }
-            s_row[w] = r;
-            s_before[w] = before;
         }
+        __syncthreads();
     }
-    __syncthreads();
-    const int32_t me = w0 + wave;
     if (me >= waves) return;
-    const int64_t at = share_begin(units, waves, me);
-    const int32_t share = __builtin_amdgcn_readfirstlane((int32_t)(share_begin(units, waves, me + 1) - at));
+    const int64_t at = shares.begin(me), hh = quotient(at, tiles), t = at - hh * tiles;
+    const int32_t share = __builtin_amdgcn_readfirstlane((int32_t)(shares.begin(me + 1) - at));
     int32_t left = share;
     if (left == 0) return;
 
     Cursor cur;
-    cur.r = __builtin_amdgcn_readfirstlane(s_row[wave]);
-    cur.hh = __builtin_amdgcn_readfirstlane((int32_t)(at / tiles));
-    cur.i = __builtin_amdgcn_readfirstlane((int32_t)(at % tiles - s_before[wave]));
+    int64_t before;
+    if (few) {
+        const int from = __ffsll(__ballot(t < upto)) - 1;    // the first row that ends behind it
+        cur.r = from;
+        before = __shfl(upto - mine, from);
+    } else {
+        cur.r = s_row[wave];
+        before = s_before[wave];
+    }
+    cur.r = __builtin_amdgcn_readfirstlane(cur.r);
+    cur.hh = __builtin_amdgcn_readfirstlane((int32_t)hh);
+    cur.i = __builtin_amdgcn_readfirstlane((int32_t)(t - before));
     cur.row = row_at<TILE>(a, cur.r);
 
     // Three tiles are under way: the scores and values of one, the keys and values
@@ -571,7 +612,7 @@ __global__ __launch_bounds__(kThreads, DP == 256 ? 1 : 2) void k_attend(AttendAr
             if (begins && lane == 0) {
                 // which shares hold the rest of it
                 const int64_t stop = at + (share - left) - cur.i + cur.row.tiles - 1;
-                a.joins[index] = int2{me, turns ? me : share_of(units, waves, stop)};
+                a.joins[index] = int2{me, turns ? me : shares.of(stop)};
             }
             if (head < job.heads) {
                 const int d0 = DP / 16 * 4 * (lane >> 4);
@@ -618,37 +659,52 @@ __global__ __launch_bounds__(kThreads, DP == 256 ? 1 : 2) void k_attend(AttendAr
     }
 }
 
-// A workgroup to a row and key-value head: its waves take every fourth tile, and
+// A workgroup to a row and key-value head: its waves take every WAVES-th tile, and
 // their pieces join in shared memory.
-template <typename T, int DP, bool kWhole>
-__global__ __launch_bounds__(kThreads, DP == 256 ? 1 : 2) void k_attend_short(AttendArgs a)
+template <typename T, int DP, bool kWhole, int WAVES>
+__global__ __launch_bounds__(64 * WAVES, DP == 256 || WAVES == 8 ? 1 : 2) void k_attend_short(AttendArgs a)
 {
     typedef Work<T, DP, kWhole> W;
     constexpr int TILE = Tile<T>::n;
-    __shared__ float s_o[kWaves][kAttendHeads][DP + 4];
-    __shared__ float s_m[kWaves][kAttendHeads], s_l[kWaves][kAttendHeads];
+    __shared__ float s_o[WAVES][kAttendHeads][DP + 4];
+    __shared__ float s_m[WAVES][kAttendHeads], s_l[WAVES][kAttendHeads];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, head = lane & 15;
     const int32_t each = a.heads * a.blocks, r = blockIdx.x / each, hh = blockIdx.x - r * each;
     const Job job = job_at(a, hh);
     V4u q[W::L::KV];
     load_queries<T, DP>(a, r, job, lane, q);
-    Row row = row_at<TILE>(a, r);
+    const Row row = row_at<TILE>(a, r);
     const int32_t* const table = a.table + (int64_t)max(row.seq, 0) * a.table_stride;
     const T* const keys = static_cast<const T*>(a.k) + job.kv * a.head_stride;
     const T* const values = static_cast<const T*>(a.v) + job.kv * a.head_stride;
     State<DP> st;
     st.clear();
-    for (int32_t i = wave; i < row.tiles; i += kWaves) {
+    int32_t i = __builtin_amdgcn_readfirstlane(wave);
+    if (i < row.tiles) {
         W work;
         Pages<T, kWhole> pages;
         pages.ask(a, row, table, row.begin(i, TILE), lane);
-        const Places<T, kWhole> p = pages.places(a, row, row.begin(i, TILE));
+        Places<T, kWhole> p = pages.places(a, row, row.begin(i, TILE));
         work.load_keys(a, keys, p, lane);
         work.load_values(a, values, p, lane);
-        float x[W::VROWS];
-        work.scores(a, q, p.seen, lane, x);
-        if (p.seen != (TILE == 32 ? ~0u : 0xFFFFu)) work.drop_unseen_values(p.seen, lane);
-        work.fold(st, x);
+        if (i + WAVES < row.tiles) pages.ask(a, row, table, row.begin(i + WAVES, TILE), lane);
+        while (true) {
+            const bool more = i + WAVES < row.tiles;
+            Places<T, kWhole> pn = p;
+            if (more) {
+                pn = pages.places(a, row, row.begin(i + WAVES, TILE));
+                if (i + 2 * WAVES < row.tiles) pages.ask(a, row, table, row.begin(i + 2 * WAVES, TILE), lane);
+            }
+            float x[W::VROWS];
+            work.scores(a, q, p.seen, lane, x);
+            if (more) work.load_keys(a, keys, pn, lane);
+            if (p.seen != (TILE == 32 ? ~0u : 0xFFFFu)) work.drop_unseen_values(p.seen, lane);
+            work.fold(st, x);
+            if (!more) break;
+            work.load_values(a, values, pn, lane);
+            p = pn;
+            i += WAVES;
+        }
     }
     const float l = sum_over_lanes(st.l);
     if (lane < 16) {
@@ -662,15 +718,15 @@ __global__ __launch_bounds__(kThreads, DP == 256 ? 1 : 2) void k_attend_short(At
             for (int e = 0; e < 4; ++e) s_o[wave][head][DP / 16 * (4 * (lane >> 4) + e) + b] = st.o[b][e];
     }
     __syncthreads();
-    for (int x = tid; x < job.heads * a.dim; x += kThreads) {
+    for (int x = tid; x < job.heads * a.dim; x += 64 * WAVES) {
         const int g = x / a.dim, d = x - g * a.dim;
         float m = s_m[0][g];
 #pragma unroll
-        for (int w = 1; w < kWaves; ++w) m = fmaxf(m, s_m[w][g]);
+        for (int w = 1; w < WAVES; ++w) m = fmaxf(m, s_m[w][g]);
         const float base = m == -__builtin_inff() ? 0.f : m;
         float sum = 0.f, o = 0.f;
 #pragma unroll
-        for (int w = 0; w < kWaves; ++w) {
+        for (int w = 0; w < WAVES; ++w) {
             const float f = weight<T>(s_m[w][g] - base);
             sum += f * s_l[w][g];
             o += f * s_o[w][g][d];
@@ -681,98 +737,97 @@ __global__ __launch_bounds__(kThreads, DP == 256 ? 1 : 2) void k_attend_short(At
 }
 
 // Joins the pieces of a row and head that lie in more than one share: the second
-// part of the share it begins in and the first parts of the ones behind it.
-// Eight groups of threads sum every eighth piece, four dims a thread.
+// part of the share it begins in and the first parts of the ones behind it.  Eight
+// groups of threads take every eighth piece, four dims a thread, each with a
+// running maximum of its own, and join in shared memory: two trips to memory.
 constexpr int kJoinGroups = 8;
 constexpr int kMaxDim = 256;
-constexpr int kJoinPieces = 512;          // factors kept at once
 
 template <typename T>
 __global__ __launch_bounds__(kThreads) void k_attend_join(AttendArgs a)
 {
-    __shared__ float s_f[kJoinPieces];
-    __shared__ float s_m[kWaves], s_l[kWaves];
+    __shared__ float s_m[kJoinGroups], s_l[kJoinGroups];
     __shared__ V4f s_o[kJoinGroups][kMaxDim / 4];
     const int32_t each = a.heads * a.blocks, tid = threadIdx.x;
     const int64_t size = attend_part_floats(a.dim);
+    const int quads = a.dim / 4, groups = min(kJoinGroups, kThreads / quads), group = tid / quads, d4 = tid - group * quads;
     for (int64_t index = blockIdx.x; index < (int64_t)a.rows * each; index += gridDim.x) {
         const int2 held = a.joins[index];
         const int32_t pieces = held.y - held.x + 1;
         if (pieces == 1) continue;
-        const int32_t r = (int32_t)(index / each);
+        const int32_t r = (int32_t)quotient(index, each);
         const Job job = job_at(a, (int32_t)(index - (int64_t)r * each));
         const float* const first = a.parts + (2 * (int64_t)held.x + 1) * size;
-        auto piece = [&](int32_t i) { return i == 0 ? first : first + (2 * (int64_t)i - 1) * size; };
         for (int g = blockIdx.y; g < job.heads; g += gridDim.y) {
             float m = -__builtin_inff(), l = 0.f;
-            for (int32_t i = tid; i < pieces; i += kThreads) {
-                const float mi = piece(i)[g], li = piece(i)[kAttendHeads + g], top = fmaxf(m, mi);
-                const float base = top == -__builtin_inff() ? 0.f : top;
-                l = l * weight<T>(m - base) + li * weight<T>(mi - base);
-                m = top;
-            }
-#pragma unroll
-            for (int d = 1; d < 64; d <<= 1) {
-                const float mi = __shfl_xor(m, d), li = __shfl_xor(l, d), top = fmaxf(m, mi);
-                const float base = top == -__builtin_inff() ? 0.f : top;
-                l = l * weight<T>(m - base) + li * weight<T>(mi - base);
-                m = top;
-            }
-            if ((tid & 63) == 0) {
-                s_m[tid >> 6] = m;
-                s_l[tid >> 6] = l;
-            }
-            __syncthreads();
-            m = s_m[0];
-#pragma unroll
-            for (int w = 1; w < kWaves; ++w) m = fmaxf(m, s_m[w]);
-            const float base = m == -__builtin_inff() ? 0.f : m;
-            l = 0.f;
-#pragma unroll
-            for (int w = 0; w < kWaves; ++w) l += s_l[w] * weight<T>(s_m[w] - base);
-
-            const int quads = a.dim / 4, group = tid / quads, d4 = tid - group * quads;
-            const int groups = min(kJoinGroups, kThreads / quads);
             V4f o = {0.f, 0.f, 0.f, 0.f};
-            for (int32_t from = 0; from < pieces; from += kJoinPieces) {
-                const int32_t here = min(kJoinPieces, pieces - from);
-                __syncthreads();
-                for (int32_t i = tid; i < here; i += kThreads) s_f[i] = weight<T>(piece(from + i)[g] - base);
-                __syncthreads();
-                if (group < groups)
+            if (group < groups)
 #pragma unroll 4
-                    for (int32_t i = group; i < here; i += groups)
-                        o += s_f[i] * *reinterpret_cast<const V4f*>(piece(from + i) + 2 * kAttendHeads + g * a.dim + 4 * d4);
+                for (int32_t i = group; i < pieces; i += groups) {
+                    const float* const part = i == 0 ? first : first + (2 * (int64_t)i - 1) * size;
+                    const float mi = part[g], li = part[kAttendHeads + g];
+                    const V4f oi = *reinterpret_cast<const V4f*>(part + 2 * kAttendHeads + g * a.dim + 4 * d4);
+                    const float top = fmaxf(m, mi), base = top == -__builtin_inff() ? 0.f : top;
+                    const float f = weight<T>(m - base), fi = weight<T>(mi - base);
+                    l = l * f + li * fi;
+                    o = o * f + oi * fi;
+                    m = top;
+                }
+            if (group < groups) {
+                s_o[group][d4] = o;
+                if (d4 == 0) {
+                    s_m[group] = m;
+                    s_l[group] = l;
+                }
             }
-            if (group < groups) s_o[group][d4] = o;
             __syncthreads();
             if (tid < quads) {
-                for (int i = 1; i < groups; ++i) o += s_o[i][tid];
+                for (int i = 1; i < groups; ++i) m = fmaxf(m, s_m[i]);
+                const float base = m == -__builtin_inff() ? 0.f : m;
+                l = 0.f;
+                o = V4f{0.f, 0.f, 0.f, 0.f};
+                for (int i = 0; i < groups; ++i) {
+                    const float f = weight<T>(s_m[i] - base);
+                    l += s_l[i] * f;
+                    o += s_o[i][tid] * f;
+                }
                 const float f = l == 0.f ? 0.f : 1.f / l;
                 store4<T>(out_row<T>(a, r, job.head0 + g) + 4 * tid, l == 0.f ? V4f{0.f, 0.f, 0.f, 0.f} : o * f);
+                if (tid == 0) write_lse(a, r, job.head0 + g, m, l);
             }
-            if (tid == 0) write_lse(a, r, job.head0 + g, m, l);
             __syncthreads();
         }
     }
 }
 
 template <typename T, int DP, bool kWhole>
-hipError_t attend_as(const AttendArgs& a, hipStream_t s)
+hipError_t attend_shares(const AttendArgs& a, int64_t jobs, hipStream_t s)
 {
     const dim3 block(kThreads);
-    const int64_t jobs = (int64_t)a.rows * a.heads * a.blocks;
-    const int64_t most = ((int64_t)a.width * a.page_size + Tile<T>::n - 1) / Tile<T>::n;      // tiles of a row
-    if (most <= kShortTiles && jobs <= kMaxGrid) {
-        hipLaunchKernelGGL((k_attend_short<T, DP, kWhole>), dim3((unsigned)jobs), block, 0, s, a);
-        return hipGetLastError();
-    }
     hipLaunchKernelGGL((k_attend<T, DP, kWhole>), dim3((unsigned)a.groups), block, 0, s, a);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
     hipLaunchKernelGGL(k_attend_join<T>, dim3((unsigned)std::min(jobs, kMaxGrid), (unsigned)std::min(a.group, kAttendHeads)),
                        block, 0, s, a);
     return hipGetLastError();
+}
+
+template <typename T, int DP, bool kWhole>
+hipError_t attend_as(const AttendArgs& a, hipStream_t s)
+{
+    const int64_t jobs = (int64_t)a.rows * a.heads * a.blocks;
+    const int64_t most = ((int64_t)a.width * a.page_size + Tile<T>::n - 1) / Tile<T>::n;      // tiles of a row
+    if (jobs <= kMaxGrid && (most <= kShortTiles || (most <= 4 * kShortTiles && jobs >= kManyJobs))) {
+        hipLaunchKernelGGL((k_attend_short<T, DP, kWhole, 4>), dim3((unsigned)jobs), dim3(256), 0, s, a);
+        return hipGetLastError();
+    }
+    if constexpr (DP <= 128) {            // eight waves of the widest heads would not fit the registers
+        if (jobs <= kMaxGrid && most <= 2 * kShortTiles) {
+            hipLaunchKernelGGL((k_attend_short<T, DP, kWhole, 8>), dim3((unsigned)jobs), dim3(512), 0, s, a);
+            return hipGetLastError();
+        }
+    }
+    return attend_shares<T, DP, kWhole>(a, jobs, s);
 }
 
 template <typename T, int DP>

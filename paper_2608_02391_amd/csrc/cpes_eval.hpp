@@ -17,14 +17,34 @@ struct PoolArgs {
     int32_t sequences, width, pages, page_size;
 };
 
+// Division of counts below 2^31 by a divisor known on the host: one multiplication.
+// With l = ceil(log2 d) and m = floor(2^(31 + l) / d) + 1, floor(n m / 2^(31 + l)) is
+// floor(n / d), since n (m - 2^(31 + l) / d) < 2^(31 + l) / d.
+struct Divisor {
+    uint32_t d, m, shift;
+
+    Divisor() = default;
+    explicit Divisor(uint32_t divisor) : d(divisor), m(0), shift(0)
+    {
+        int l = 0;
+        while (((uint64_t)1 << l) < d) ++l;
+        if (l > 0) {
+            m = (uint32_t)(((uint64_t)1 << (31 + l)) / d + 1);
+            shift = l - 1;
+        }
+    }
+
+    __device__ __forceinline__ uint32_t of(uint32_t n) const { return m ? __umulhi(n, m) >> shift : n; }
+};
+
 // One page as `runs` pieces of `run` consecutive 16-byte units: layer, keys or
 // values, and the outer and inner of heads and tokens that do not join up.
 struct PageArgs {
     char* k;
     char* v;
     int64_t page_bytes, layer_bytes, outer_bytes, inner_bytes;   // strides
-    int32_t layers, outers, inners;
-    uint32_t run;                // units of a run
+    Divisor outers, inners;
+    Divisor run;                 // units of a run
     uint32_t units;              // units of a page: 2 * layers * outers * inners * run
 };
 
@@ -41,7 +61,7 @@ struct AppendArgs {
     const int32_t* positions;
     int64_t page_bytes, head_bytes, token_bytes, new_bytes, new_head_bytes;   // strides
     int32_t n, heads;
-    uint32_t run;                // 16-byte units of one head of one token
+    Divisor run, token;          // 16-byte units of one head, and of all heads, of one token
 };
 
 constexpr int kAttendHeads = 16;         // query heads of a workgroup: the columns of a matrix instruction

@@ -135,10 +135,9 @@ int page_args(const cpes_cache* c, cpes::PageArgs* a, const char* fn)
     a->layer_bytes = c->layer_stride * e;
     a->outer_bytes = outer * e;
     a->inner_bytes = inner * e;
-    a->layers = c->layers;
-    a->outers = (int32_t)outers;
-    a->inners = (int32_t)inners;
-    a->run = (uint32_t)(run * e / 16);
+    a->outers = cpes::Divisor((uint32_t)outers);
+    a->inners = cpes::Divisor((uint32_t)inners);
+    a->run = cpes::Divisor((uint32_t)(run * e / 16));
     a->units = (uint32_t)units;
     return CPES_OK;
 }
@@ -313,7 +312,10 @@ int cpes_cache_append(const cpes_cache* cache, int32_t layer, const cpes_pool* p
     a.new_head_bytes = new_head_stride * e;
     a.n = n;
     a.heads = cache->heads;
-    a.run = (uint32_t)(cache->head_dim * e / 16);
+    const int64_t run = cache->head_dim * e / 16, token = run * cache->heads;
+    if (token >= ((int64_t)1 << 24)) return fail(CPES_ERR_UNSUPPORTED, "%s: a token of more than 256 MB", fn);
+    a.run = cpes::Divisor((uint32_t)run);
+    a.token = cpes::Divisor((uint32_t)token);
     return hip_status(cpes::launch_append(a, (hipStream_t)stream), fn);
 }
 

@@ -104,14 +104,15 @@ __device__ __forceinline__ void load_refs(const PoolArgs& p, int64_t first, int3
 }
 
 // The lowest `want` free pages, ascending, into list (fewer if there are not
-// that many); their number is returned.  All threads.
-__device__ int32_t lowest_free(const PoolArgs& p, int32_t want, int32_t* list)
+// that many); their number is returned.  r holds the counts of the first step's
+// pages, 16 a thread.  All threads.
+__device__ int32_t lowest_free(const PoolArgs& p, int32_t r[16], int32_t want, int32_t* list)
 {
     int32_t found = 0;
     for (int64_t base = 0; base < p.pages && found < want; base += 16 * kPlanBlock) {
         const int64_t first = base + 16 * (int64_t)threadIdx.x;
-        int32_t r[16], mine = 0, total;
-        load_refs(p, first, 1, r);
+        int32_t mine = 0, total;
+        if (base > 0) load_refs(p, first, 1, r);
 #pragma unroll
         for (int e = 0; e < 16; ++e) mine += r[e] <= 0;
         int32_t at = found + block_scan(mine, &total);
@@ -129,36 +130,66 @@ __device__ int32_t lowest_free(const PoolArgs& p, int32_t want, int32_t* list)
 
 // ---------------------------------------------------------------- reserve --
 // Claims every listed sequence, sums what they lack, takes that many of the
-// lowest free pages and hands them out, one wave per sequence at a time.
+// lowest free pages and hands them out, one wave per sequence at a time.  The
+// first 1,024 entries of the list stay in registers, and the first reference
+// counts are on their way while the sequences are claimed: the kernel is a chain
+// of trips to memory, and these are two of them.
 __global__ __launch_bounds__(kPlanBlock) void k_pages_reserve(PoolArgs p, int32_t n, const int32_t* seqs,
                                                               const int32_t* new_lengths, int32_t* ws, int32_t* status)
 {
     __shared__ int32_t s_seq[kPlanBlock], s_from[kPlanBlock], s_need[kPlanBlock], s_at[kPlanBlock];
     int32_t* const list = ws + kPagesHeader;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    int32_t r[16];
+    load_refs(p, 16 * (int64_t)tid, 1, r);
     bool bad = false;
+    int32_t seq0 = 0, len0 = 0, old0 = 0;               // of entry tid
     for (int32_t i = tid; i < n; i += kPlanBlock) {
         const int32_t s = seqs[i], len = new_lengths[i];
-        if (!known(p, s)) {
+        if (!known(p, s) || len < 0 || (int64_t)len > capacity(p)) {
             bad = true;
             continue;
         }
-        bad |= len < 0 || (int64_t)len > capacity(p) || atomicOr(&p.lengths[s], kClaim) < 0;
+        const int32_t old = atomicOr(&p.lengths[s], kClaim);
+        bad |= old < 0;
+        if (i == tid) {
+            seq0 = s;
+            len0 = len;
+            old0 = old & ~kClaim;
+        }
     }
     bad = __syncthreads_or(bad);
-    // pages lacking in all; two sums of 16 bits each, so that none overflows
-    int64_t want = 0;
-    for (int32_t base = 0; base < n && !bad; base += kPlanBlock) {
-        int32_t need = 0, lo, hi;
-        if (base + tid < n) {
-            const int32_t old = held_tokens(p, p.lengths[seqs[base + tid]] & ~kClaim);
-            need = max(0, pages_of(new_lengths[base + tid], p.page_size) - pages_of(old, p.page_size));
+    auto entry = [&](int32_t i, int32_t* s, int32_t* len, int32_t* old) {
+        if (i == tid) {
+            *s = seq0;
+            *len = len0;
+            *old = old0;
+        } else {
+            *s = seqs[i];
+            *len = new_lengths[i];
+            *old = p.lengths[*s] & ~kClaim;
         }
-        block_scan(need & 0xFFFF, &lo);
-        block_scan(need >> 16, &hi);
+        const int32_t from = pages_of(held_tokens(p, *old), p.page_size);
+        s_from[tid] = from;
+        return max(0, pages_of(*len, p.page_size) - from);
+    };
+    // pages lacking in all, and in front of this thread's first entry; two sums of 16 bits where one could overflow
+    const bool wide = p.width >= 1 << 20;
+    int64_t want = 0;
+    int32_t need0 = 0, at0 = 0;
+    for (int32_t base = 0; base < n && !bad; base += kPlanBlock) {
+        int32_t need = 0, lo, hi = 0, s, len, old;
+        if (base + tid < n) need = entry(base + tid, &s, &len, &old);
+        const int32_t at = block_scan(wide ? need & 0xFFFF : need, &lo);
+        if (wide) block_scan(need >> 16, &hi);
         want += ((int64_t)hi << 16) + lo;
+        if (base == 0) {
+            need0 = need;
+            at0 = at;
+        }
     }
-    const bool enough = !bad && want <= p.pages && lowest_free(p, (int32_t)want, list) == (int32_t)want;
+    const bool once = n <= kPlanBlock && !wide;          // then these are all there is to know
+    const bool enough = !bad && want <= p.pages && lowest_free(p, r, (int32_t)want, list) == (int32_t)want;
     if (!enough) {
         for (int32_t i = tid; i < n; i += kPlanBlock)
             if (known(p, seqs[i])) atomicAnd(&p.lengths[seqs[i]], ~kClaim);
@@ -167,17 +198,14 @@ __global__ __launch_bounds__(kPlanBlock) void k_pages_reserve(PoolArgs p, int32_
     }
     int32_t given = 0;
     for (int32_t base = 0; base < n; base += kPlanBlock) {
-        int32_t need = 0, from = 0, s = 0, total;
-        if (base + tid < n) {
-            s = seqs[base + tid];
-            const int32_t old = p.lengths[s] & ~kClaim, len = new_lengths[base + tid];
-            from = pages_of(held_tokens(p, old), p.page_size);
-            need = max(0, pages_of(len, p.page_size) - from);
-            p.lengths[s] = max(old, len);
+        int32_t need = need0, at = at0, total = 0, s = seq0, len = len0, old = old0;
+        if (!once) {
+            need = 0;
+            if (base + tid < n) need = entry(base + tid, &s, &len, &old);
+            at = given + block_scan(need, &total);
         }
-        const int32_t at = given + block_scan(need, &total);
+        if (base + tid < n) p.lengths[s] = max(old, len);
         s_seq[tid] = s;
-        s_from[tid] = from;
         s_need[tid] = need;
         s_at[tid] = at;
         __syncthreads();
@@ -201,24 +229,23 @@ __global__ __launch_bounds__(kPlanBlock) void k_pages_reserve(PoolArgs p, int32_
 // Byte offset of unit u of a page, and whether it belongs to the values.
 __device__ __forceinline__ int64_t unit_offset(const PageArgs& c, uint32_t u, bool* values)
 {
-    uint32_t run = u / c.run;
-    int64_t at = (int64_t)(u - run * c.run) * 16;
-    if (c.inners > 1) {
-        at += (int64_t)(run % c.inners) * c.inner_bytes;
-        run /= c.inners;
-    }
-    if (c.outers > 1) {
-        at += (int64_t)(run % c.outers) * c.outer_bytes;
-        run /= c.outers;
-    }
-    *values = run & 1;
-    return at + (int64_t)(run >> 1) * c.layer_bytes;
+    uint32_t run = c.run.of(u);
+    int64_t at = (int64_t)(u - run * c.run.d) * 16;
+    uint32_t rest = c.inners.of(run);
+    at += (int64_t)(run - rest * c.inners.d) * c.inner_bytes;
+    run = rest;
+    rest = c.outers.of(run);
+    at += (int64_t)(run - rest * c.outers.d) * c.outer_bytes;
+    *values = rest & 1;
+    return at + (int64_t)(rest >> 1) * c.layer_bytes;
 }
 
 constexpr int kCopyBlock = 256;
 constexpr int kCopyUnits = 4;             // 16-byte units a thread has in flight
 
-// Units [piece * kCopyBlock * kCopyUnits, ...) of page src to page dst.
+// Units [piece * kCopyBlock * kCopyUnits, ...) of page src to page dst.  NT: past
+// the caches, for copies that exceed them.
+template <bool NT>
 __device__ __forceinline__ void copy_piece(const PageArgs& c, int32_t src, int32_t dst, uint32_t piece)
 {
     const uint32_t u0 = piece * (kCopyBlock * kCopyUnits) + threadIdx.x;
@@ -232,13 +259,18 @@ __device__ __forceinline__ void copy_piece(const PageArgs& c, int32_t src, int32
             bool values;
             const int64_t at = unit_offset(c, u, &values);
             char* const base = (values ? c.v : c.k) + at;
-            x[i] = load16(base + from);
+            x[i] = NT ? __builtin_nontemporal_load(reinterpret_cast<const V4uAnywhere*>(base + from)) : load16(base + from);
             q[i] = base + to;
         }
     }
 #pragma unroll
     for (int i = 0; i < kCopyUnits; ++i)
-        if (u0 + i * kCopyBlock < c.units) store16(q[i], x[i]);
+        if (u0 + i * kCopyBlock < c.units) {
+            if (NT)
+                __builtin_nontemporal_store(x[i], reinterpret_cast<V4uAnywhere*>(q[i]));
+            else
+                store16(q[i], x[i]);
+        }
 }
 
 __device__ __host__ __forceinline__ uint32_t pieces_of(const PageArgs& c)
@@ -252,32 +284,48 @@ __global__ __launch_bounds__(kCopyBlock) void k_pages_copy(PageArgs c, int32_t p
     const uint32_t pieces = pieces_of(c);
     for (int64_t job = blockIdx.x; job < (int64_t)n * pieces; job += gridDim.x) {
         const int32_t i = (int32_t)(job / pieces), a = src[i], b = dst[i];
-        if (a >= 0 && a < pages && b >= 0 && b < pages) copy_piece(c, a, b, (uint32_t)(job - (int64_t)i * pieces));
+        if (a >= 0 && a < pages && b >= 0 && b < pages) copy_piece<false>(c, a, b, (uint32_t)(job - (int64_t)i * pieces));
     }
 }
 
 // ------------------------------------------------------------------- fork --
 // The plan claims the children (an empty one's length becomes the mark), takes
 // the lowest free page for each partly filled last page, writes it into the
-// child's table and sets the child's length; ws[0] says whether it went well.
+// child's table and sets the child's length; ws[0] says whether it went well.  As
+// in k_pages_reserve, the first entries and reference counts are in registers.
 __global__ __launch_bounds__(kPlanBlock) void k_pages_fork_plan(PoolArgs p, int32_t n, const int32_t* parents,
                                                                 const int32_t* children, int32_t* ws, int32_t* status)
 {
     int32_t* const list = ws + kPagesHeader;
     const int tid = threadIdx.x;
+    int32_t r[16];
+    load_refs(p, 16 * (int64_t)tid, 1, r);
     bool bad = false;
+    int32_t child0 = 0, len0 = 0;         // of entry tid
     for (int32_t i = tid; i < n; i += kPlanBlock) {
-        const int32_t c = children[i];
-        bad |= !known(p, parents[i]) || !known(p, c) || atomicCAS(&p.lengths[c], 0, kClaim) != 0;
+        const int32_t a = parents[i], c = children[i];
+        if (!known(p, a) || !known(p, c)) {
+            bad = true;
+            continue;
+        }
+        // a parent that is itself a child of this call is empty, or carries the mark: it counts as empty
+        const int32_t len = held_tokens(p, p.lengths[a]);
+        bad |= atomicCAS(&p.lengths[c], 0, kClaim) != 0;
+        if (i == tid) {
+            child0 = c;
+            len0 = len;
+        }
     }
     bad = __syncthreads_or(bad);
-    int32_t want = 0;
+    auto length = [&](int32_t i) { return i == tid ? len0 : held_tokens(p, p.lengths[parents[i]]); };
+    int32_t want = 0, at0 = 0;
     for (int32_t base = 0; base < n && !bad; base += kPlanBlock) {
         int32_t total;
-        block_scan(base + tid < n && held_tokens(p, p.lengths[parents[base + tid]]) % p.page_size != 0, &total);
+        const int32_t at = block_scan(base + tid < n && length(base + tid) % p.page_size != 0, &total);
+        if (base == 0) at0 = at;
         want += total;
     }
-    const bool enough = !bad && lowest_free(p, want, list) == want;
+    const bool enough = !bad && lowest_free(p, r, want, list) == want;
     if (!enough) {
         // only a child that was empty and claimed here carries the mark alone
         for (int32_t i = tid; i < n; i += kPlanBlock)
@@ -290,21 +338,27 @@ __global__ __launch_bounds__(kPlanBlock) void k_pages_fork_plan(PoolArgs p, int3
     }
     int32_t given = 0;
     for (int32_t base = 0; base < n; base += kPlanBlock) {
-        int32_t total, len = 0;
+        int32_t total = 0, len = 0, c = child0;
         const bool mine = base + tid < n;
-        if (mine) len = held_tokens(p, p.lengths[parents[base + tid]]);
-        const bool tail = len % p.page_size != 0;
-        const int32_t at = given + block_scan(tail, &total);
+        if (mine) {
+            len = length(base + tid);
+            if (base > 0) c = children[base + tid];
+        }
+        const int32_t last = len / p.page_size;
+        const bool tail = len - last * p.page_size != 0;
+        const int32_t at = n <= kPlanBlock ? at0 : given + block_scan(tail, &total);
         if (tail) {
-            row_of(p, children[base + tid])[len / p.page_size] = list[at];
+            row_of(p, c)[last] = list[at];
             p.refs[list[at]] = 1;
         }
-        // the mark stays on, so that a parent that is itself a child of this call counts as empty
-        if (mine) p.lengths[children[base + tid]] = len | kClaim;
+        // the mark stays on while entries behind may read this length as a parent's
+        if (mine) p.lengths[c] = n > kPlanBlock ? len | kClaim : len;
         given += total;
     }
-    __syncthreads();                      // every parent's length has been read
-    for (int32_t i = tid; i < n; i += kPlanBlock) p.lengths[children[i]] &= ~kClaim;
+    if (n > kPlanBlock) {
+        __syncthreads();                  // every parent's length has been read
+        for (int32_t i = tid; i < n; i += kPlanBlock) p.lengths[children[i]] &= ~kClaim;
+    }
     if (tid == 0) {
         ws[0] = 1;
         if (status) *status = kOk;
@@ -329,7 +383,7 @@ __global__ __launch_bounds__(kCopyBlock) void k_pages_fork(PageArgs c, PoolArgs 
     if (len % p.page_size == 0) return;
     const int32_t src = from[full], dst = to[full];
     if (src < 0 || src >= p.pages || dst < 0 || dst >= p.pages) return;
-    for (uint32_t piece = part; piece < pieces_of(c); piece += per) copy_piece(c, src, dst, piece);
+    for (uint32_t piece = part; piece < pieces_of(c); piece += per) copy_piece<false>(c, src, dst, piece);
 }
 
 // ------------------------------------------------------------------- free --
@@ -381,9 +435,10 @@ __device__ __host__ __forceinline__ CompactLists compact_lists(int32_t* ws, int3
 __global__ __launch_bounds__(kPlanBlock) void k_pages_compact_plan(PoolArgs p, int32_t* ws, int32_t* moved)
 {
     const CompactLists l = compact_lists(ws, p.pages);
-    int32_t live = 0;
+    const bool once = p.pages <= 16 * kPlanBlock;        // the counts of the one step stay in registers
+    int32_t live = 0, r[16];
     for (int64_t base = 0; base < p.pages; base += 16 * kPlanBlock) {
-        int32_t r[16], mine = 0, total;
+        int32_t mine = 0, total;
         load_refs(p, base + 16 * (int64_t)threadIdx.x, 0, r);
 #pragma unroll
         for (int e = 0; e < 16; ++e) mine += r[e] > 0;
@@ -393,8 +448,8 @@ __global__ __launch_bounds__(kPlanBlock) void k_pages_compact_plan(PoolArgs p, i
     int32_t holes = 0, movers = 0;
     for (int64_t base = 0; base < p.pages; base += 16 * kPlanBlock) {
         const int64_t first = base + 16 * (int64_t)threadIdx.x;
-        int32_t r[16], mine = 0, total;
-        load_refs(p, first, 0, r);
+        int32_t mine = 0, total;
+        if (!once) load_refs(p, first, 0, r);
         // both counts of a step fit 16 bits: one sum
 #pragma unroll
         for (int e = 0; e < 16; ++e) mine += first + e < live ? r[e] <= 0 : r[e] > 0 ? 1 << 16 : 0;
@@ -423,6 +478,7 @@ __global__ __launch_bounds__(kPlanBlock) void k_pages_compact_plan(PoolArgs p, i
 // Data, reference counts, tables and lengths.  In place, each count that
 // changes is written by one thread: the hole's and the mover's by the thread of
 // their pair; the thread of a page writes only what the page had.
+template <bool NT>
 __global__ __launch_bounds__(kCopyBlock) void k_pages_compact(PageArgs c, PoolArgs p, PoolArgs packed, int32_t* ws)
 {
     const CompactLists l = compact_lists(ws, p.pages);
@@ -430,7 +486,7 @@ __global__ __launch_bounds__(kCopyBlock) void k_pages_compact(PageArgs c, PoolAr
     const uint32_t pieces = pieces_of(c);
     for (int64_t job = blockIdx.x; job < (int64_t)moved * pieces; job += gridDim.x) {
         const int32_t i = (int32_t)(job / pieces);
-        copy_piece(c, l.src[i], l.dst[i], (uint32_t)(job - (int64_t)i * pieces));
+        copy_piece<NT>(c, l.src[i], l.dst[i], (uint32_t)(job - (int64_t)i * pieces));
     }
     const int64_t thread = (int64_t)blockIdx.x * kCopyBlock + threadIdx.x, threads = (int64_t)gridDim.x * kCopyBlock;
     for (int64_t page = thread; page < p.pages; page += threads) {
@@ -480,9 +536,9 @@ __global__ __launch_bounds__(kCopyBlock) void k_append(AppendArgs a, int32_t per
             s_to[threadIdx.x] = to;
         }
         __syncthreads();
-        const uint32_t token = (uint32_t)a.heads * a.run, all = token * here;
+        const uint32_t all = a.token.d * here;
         for (uint32_t u = threadIdx.x; u < all; u += kCopyBlock) {
-            const uint32_t t = u / token, h = (u - t * token) / a.run, x = u - t * token - h * a.run;
+            const uint32_t t = a.token.of(u), rest = u - t * a.token.d, h = a.run.of(rest), x = rest - h * a.run.d;
             const int64_t to = s_to[t];
             if (to < 0) continue;
             const int64_t from = (first + t) * a.new_bytes + h * a.new_head_bytes + x * 16;
@@ -497,6 +553,7 @@ __global__ __launch_bounds__(kCopyBlock) void k_append(AppendArgs a, int32_t per
 // Workgroups of a launch whose jobs are counted on the device, or are many.
 constexpr int kCopyGrid = 4096;
 constexpr int kAppendGrid = 1 << 20;
+constexpr double kCacheBytes = 256 << 20; // the last-level cache
 
 }  // namespace
 
@@ -543,14 +600,17 @@ hipError_t launch_pages_compact(const PageArgs& c, const PoolArgs& p, const Pool
     if (e != hipSuccess) return e;
     // half of the pages move at most
     const int64_t jobs = std::max<int64_t>((int64_t)(p.pages / 2) * pieces_of(c), p.sequences);
-    hipLaunchKernelGGL(k_pages_compact, dim3((unsigned)std::max<int64_t>(1, std::min<int64_t>(jobs, kCopyGrid))),
-                       dim3(kCopyBlock), 0, s, c, p, packed, ws);
+    const dim3 grid((unsigned)std::max<int64_t>(1, std::min<int64_t>(jobs, 4 * kCopyGrid))), block(kCopyBlock);
+    if ((double)p.pages * c.units * 16 > kCacheBytes)
+        hipLaunchKernelGGL(k_pages_compact<true>, grid, block, 0, s, c, p, packed, ws);
+    else
+        hipLaunchKernelGGL(k_pages_compact<false>, grid, block, 0, s, c, p, packed, ws);
     return hipGetLastError();
 }
 
 hipError_t launch_append(const AppendArgs& a, hipStream_t s)
 {
-    const int64_t token = (int64_t)a.heads * a.run;
+    const int64_t token = a.token.d;
     // one token a workgroup while they are few, then enough for every thread's units
     const int64_t full = std::max<int64_t>(1, std::min<int64_t>(kAppendTokens, kCopyBlock * kAppendUnits / token));
     const int32_t per = (int32_t)std::min<int64_t>(full, std::max(1, a.n / 1024));

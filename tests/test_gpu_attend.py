@@ -351,3 +351,36 @@ def test_append_without_list_and_without_tokens():
     cp.cpes_attend(cache, 0, pool, new[:0], new[:0].clone(), workspace=ws)
     torch.cuda.synchronize()
     assert float(k.sum()) == 16
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32], ids=["bf16", "fp32"])
+@pytest.mark.parametrize("dim,page,window,sinks", [(64, 16, 0, 0), (128, 48, 0, 0), (128, 7, 0, 0), (80, 64, 0, 0), (256, 16, 0, 0),
+                                                   (64, 16, 100, 37), (128, 5, 33, 4), (128, 32, 1, 0), (40, 24, 300, 31)])
+def test_rows_of_wide_tables(dtype, dim, page, window, sinks):
+    """Tables wide enough for long sequences, whatever their lengths: shares that end and begin anywhere."""
+    print(f"wide table dim={dim} page={page} window={window} {dtype}", flush=True)
+    c = Case([0, 1, 17, 2500, 36, 0, 40, 777, 33, 5000, 138, 5], 2, dim, page, dtype, width=70000 // page, window=window,
+             sinks=sinks, seed=dim)
+    q = c.queries(6)
+    c.check(q, *c.run(q))
+
+
+@pytest.mark.parametrize("rows", [63, 64, 65, 300, 1100])
+def test_many_rows_of_wide_tables(rows):
+    """Up to 64 rows every wave finds its own place among them, more are found by a workgroup."""
+    print(f"wide table rows={rows}", flush=True)
+    lens = [(37 * r) % 90 if r % 7 else 0 for r in range(rows)]
+    lens[rows // 2] = 1500
+    c = Case(lens, 1, 64, 16, BF16, layers=1, layer=0, width=5000, seed=rows)
+    q = c.queries(2)
+    c.check(q, *c.run(q))
+
+
+@pytest.mark.parametrize("rows,longest", [(2, 1000), (2, 2000), (150, 1000), (150, 2040), (150, 2100), (3, 500)])
+def test_every_launch_of_a_size(rows, longest):
+    """Row counts and table widths on either side of each rule that picks a launch."""
+    print(f"launch rows={rows} longest={longest}", flush=True)
+    lens = [longest if r == rows // 2 else 1 + (13 * r) % 40 for r in range(rows)]
+    c = Case(lens, 2, 64, 16, BF16, layers=1, layer=0, width=-(-longest // 16), seed=rows)
+    q = c.queries(4)
+    c.check(q, *c.run(q))
