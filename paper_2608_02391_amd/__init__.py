@@ -481,23 +481,25 @@ def page_pool(table, lengths, page_size: int, refs=None) -> Pool:
     return pool
 
 
-def _int32_list(t, what: str, n: Optional[int] = None) -> Optional[int]:
-    """Device pointer of an int32 list (of n entries)."""
+def _buffer(t, what: str, n: int, dtype) -> Optional[int]:
+    """Device pointer of a contiguous tensor of at least n elements of ``dtype``, or None.
+    One test for the usual case (0.4 us); what is wrong is found out behind it."""
     if t is None:
         return None
-    if t.dtype != _torch().int32:
-        raise TypeError(f"{what} must have dtype torch.int32, not {t.dtype}")
-    if n is not None and t.numel() < n:
-        raise ValueError(f"{what} holds {t.numel()} elements, {n} needed")
+    if t.dtype is dtype and t.is_cuda and t.numel() >= n and t.is_contiguous():
+        return t.data_ptr()
+    _need(t, what, n, dtype)
     return _dev_ptr(t, what)
+
+
+def _int32_list(t, what: str, n: int = 0) -> Optional[int]:
+    """Device pointer of an int32 list (of n entries)."""
+    return _buffer(t, what, n, _torch().int32)
 
 
 def _floats(t, what: str, n: int) -> Optional[int]:
     """Device pointer of a float32 tensor of n elements at least, or None."""
-    if t is None:
-        return None
-    _need(t, what, n, _torch().float32)
-    return _dev_ptr(t, what)
+    return _buffer(t, what, n, _torch().float32)
 
 
 def _workspace(t):
@@ -506,7 +508,7 @@ def _workspace(t):
 
 def _rows(t, what: str, shape, dtype):
     """(pointer, row stride, head stride) of a [rows, heads, dim] tensor whose rows and heads may be apart."""
-    if t.dtype != dtype:
+    if t.dtype is not dtype:
         raise TypeError(f"{what} must have dtype {dtype}, not {t.dtype}")
     if not t.is_cuda:
         raise ValueError(f"{what} must be a GPU tensor")
@@ -586,25 +588,28 @@ def cpes_attend(cache: Cache, layer: int, pool: Pool, q, out, lse=None, seqs=Non
     """Attention of the newest token of sequences seqs[r] (None: r) over the cache:
     q and out are [rows, q_heads, head_dim] (rows and heads may be apart), lse
     float32 [rows, q_heads]; scale defaults to head_dim ** -0.5."""
-    if q.dim() != 3 or q.shape[2] != cache.head_dim:
-        raise ValueError(f"q must be [rows, q_heads, {cache.head_dim}], not {tuple(q.shape)}")
-    rows, heads = q.shape[0], q.shape[1]
-    qp, q_row, q_head = _rows(q, "q", q.shape, cache._dtype)
-    op, o_row, o_head = _rows(out, "out", q.shape, cache._dtype)
+    shape, dtype = q.shape, cache._dtype
+    if len(shape) != 3 or shape[2] != cache.head_dim:
+        raise ValueError(f"q must be [rows, q_heads, {cache.head_dim}], not {tuple(shape)}")
+    rows, heads, dim = shape
+    qp, q_row, q_head = _rows(q, "q", shape, dtype)
+    op, o_row, o_head = _rows(out, "out", shape, dtype)
     ws, size = _workspace(workspace)
     _check((_lib or load()).cpes_attend(ctypes.byref(cache), layer, ctypes.byref(pool), rows,
                                         _int32_list(seqs, "seqs", rows), qp, q_row, q_head, heads,
-                                        cache.head_dim ** -0.5 if scale is None else scale, window, sinks, op, o_row,
+                                        dim ** -0.5 if scale is None else scale, window, sinks, op, o_row,
                                         o_head, _floats(lse, "lse", rows * heads), ws, size, _stream(stream)))
 
 
 def _logits(x, what: str = "logits"):
     """(pointer, rows, vocabulary, row stride) of a [rows, vocabulary] tensor whose rows may be apart."""
-    if x.dim() != 2 or (x.stride(1) != 1 and x.shape[1] > 1):
+    shape, strides = x.shape, x.stride()
+    if len(shape) != 2 or (strides[1] != 1 and shape[1] > 1):
         raise ValueError(f"{what} must be [rows, vocabulary] with contiguous rows")
     if not x.is_cuda:
         raise ValueError(f"{what} must be a GPU tensor")
-    return x.data_ptr(), x.shape[0], x.shape[1], max(x.stride(0), x.shape[1]) if x.shape[0] < 2 else x.stride(0)
+    rows, vocab = shape
+    return x.data_ptr(), rows, vocab, strides[0] if rows > 1 else max(strides[0], vocab)
 
 
 def cpes_logprobs_workspace_bytes(rows: int, vocab: int, top: int = 0) -> int:
@@ -617,21 +622,19 @@ def cpes_logprobs(logits, targets, logp, entropy=None, lse=None, stats=None, top
     ``scale``: float32 [rows] log probabilities, entropies and normalisers, the
     float32 [rows, 2] ``stats`` for cpes_logprobs_backward, and the most likely
     alternatives in float32 / int64 [rows, k] ``top_logp`` and ``top_ids``."""
-    torch = _torch()
     x, rows, vocab, stride = _logits(logits)
-    _need(targets, "targets", rows, torch.int64)
+    int64 = _torch().int64
     top = 0
     if top_ids is not None or top_logp is not None:
         if top_ids is None or top_logp is None or top_ids.dim() != 2 or top_ids.shape[0] != rows or top_logp.shape != top_ids.shape:
             raise ValueError("top_logp and top_ids must both be [rows, k]")
         top = top_ids.shape[1]
-        _need(top_ids, "top_ids", rows * top, torch.int64)
     ws, size = _workspace(workspace)
-    _check((_lib or load()).cpes_logprobs(x, _dtype_code(logits), rows, vocab, stride, scale, _dev_ptr(targets, "targets"),
-                                          _floats(logp, "logp", rows), _floats(entropy, "entropy", rows),
-                                          _floats(lse, "lse", rows), _floats(stats, "stats", 2 * rows), top,
-                                          _floats(top_logp, "top_logp", rows * top), _dev_ptr(top_ids, "top_ids"), ws,
-                                          size, _stream(stream)))
+    _check((_lib or load()).cpes_logprobs(x, _dtype_code(logits), rows, vocab, stride, scale,
+                                          _buffer(targets, "targets", rows, int64), _floats(logp, "logp", rows),
+                                          _floats(entropy, "entropy", rows), _floats(lse, "lse", rows),
+                                          _floats(stats, "stats", 2 * rows), top, _floats(top_logp, "top_logp", rows * top),
+                                          _buffer(top_ids, "top_ids", rows * top, int64), ws, size, _stream(stream)))
 
 
 def cpes_logprobs_backward(logits, targets, stats, entropy, d_logp, d_entropy, d_logits, scale: float = 1.0,
@@ -642,9 +645,8 @@ def cpes_logprobs_backward(logits, targets, stats, entropy, d_logp, d_entropy, d
     dx, d_rows, d_vocab, d_stride = _logits(d_logits, "d_logits")
     if (d_rows, d_vocab) != (rows, vocab) or d_logits.dtype != logits.dtype:
         raise ValueError("d_logits must have the shape and dtype of the logits")
-    _need(targets, "targets", rows, _torch().int64)
     _check((_lib or load()).cpes_logprobs_backward(x, _dtype_code(logits), rows, vocab, stride, scale,
-                                                   _dev_ptr(targets, "targets"), _floats(stats, "stats", 2 * rows),
+                                                   _buffer(targets, "targets", rows, _torch().int64), _floats(stats, "stats", 2 * rows),
                                                    _floats(entropy, "entropy", rows), _floats(d_logp, "d_logp", rows),
                                                    _floats(d_entropy, "d_entropy", rows), dx, d_stride, _stream(stream)))
 

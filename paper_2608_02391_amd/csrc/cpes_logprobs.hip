@@ -141,17 +141,34 @@ __device__ __forceinline__ void write_top(const LogprobArgs& a, int64_t row, int
     a.top_ids[row * a.top + j] = id;
 }
 
+// How many of the n keys in LDS are larger than x: eight loads at a time are on
+// their way.  Behind the n keys there is room, and 0, up to a multiple of eight.
+__device__ __forceinline__ int larger(const Key* keys, int n, Key x)
+{
+    int place = 0;
+    for (int j = 0; j < n; j += 8)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) place += keys[j + e] > x;
+    return place;
+}
+
+// 0 behind the n keys, up to a multiple of eight.
+__device__ __forceinline__ void pad(Key* keys, int n)
+{
+    if (threadIdx.x < 8 && (n & 7) && (int)threadIdx.x >= (n & 7)) keys[(n & ~7) + threadIdx.x] = 0;
+}
+
 // The k largest of the n keys in LDS, descending, into best (0 where there are
 // fewer): each key's place is the number of larger ones.  All threads; the keys
 // are distinct.
-__device__ void largest(const Key* keys, int n, int k, Key* best)
+__device__ void largest(Key* keys, int n, int k, Key* best)
 {
     for (int i = threadIdx.x; i < k; i += kThreads) best[i] = 0;
+    pad(keys, n);
     __syncthreads();
     for (int i = threadIdx.x; i < n; i += kThreads) {
         const Key x = keys[i];
-        int place = 0;
-        for (int j = 0; j < n; ++j) place += keys[j] > x;
+        const int place = larger(keys, n, x);
         if (place < k) best[place] = x;
     }
     __syncthreads();
@@ -269,8 +286,7 @@ __device__ int bound_exactly(Key key, int top, Key* s_keys, int32_t* s_owner, in
     s_keys[threadIdx.x] = key;
     if (threadIdx.x == 0) *s_owners = 0;
     __syncthreads();
-    int place = 0;
-    for (int j = 0; j < kThreads; ++j) place += s_keys[j] > key;
+    const int place = larger(s_keys, kThreads, key);
     const bool mine = key && place < top;
     if (mine) s_owner[place] = threadIdx.x;
     if (mine) atomicAdd(s_owners, 1);
@@ -341,12 +357,21 @@ __global__ __launch_bounds__(kThreads, 5) void k_logprobs(LogprobArgs a)
         }
         if (whole < steps) {
             float all = -__builtin_inff();
+            int32_t i = whole * kUnroll * kThreads + tid;
+#pragma unroll
+            for (int u = 0; u < kUnroll; ++u)
+                if (i + u * kThreads < full) w[u] = *reinterpret_cast<const V4uAnywhere*>(x0 + (int64_t)(i + u * kThreads) * N);
 #pragma unroll 1
-            for (int u = 0; u < kUnroll; ++u) {
+            for (int u = 0; u < kUnroll; ++u, i += kThreads) {
                 float x[N];
-                floats_at((whole * kUnroll + u) * kThreads + tid, x);
+                if (i < full)
+                    unpack<T>(w[0], x);
+                else
+                    floats_at(i, x);
                 if (run.take<N>(x, a.c, &most)) met = whole;
                 all = fmaxf(all, most);
+#pragma unroll
+                for (int v = 1; v < kUnroll; ++v) w[v - 1] = w[v];
             }
             if (a.top > 0 && whole < kNoted) s_most[whole][tid] = bf16_above(all);
         }
@@ -472,20 +497,25 @@ __global__ __launch_bounds__(kThreads, 5) void k_logprobs(LogprobArgs a)
 }
 
 // Joins the slices of a row.
+constexpr int kJoinKeys = kMaxSlices * kMaxTop;
+// Keys from the bound on: k of the lists' first few, and behind them only in lists whose
+// few, at least two, all are among these.
+constexpr int kJoinCandidates = kMaxTop + kMaxTop / 2 * kMaxTop;
+
 template <typename T>
 __global__ __launch_bounds__(kThreads) void k_logprobs_join(LogprobArgs a)
 {
-    __shared__ Key s_keys[kMaxSlices * kMaxTop], s_best[kMaxTop], s_least;
+    __shared__ Key s_all[kJoinKeys], s_keys[kJoinCandidates], s_best[kMaxTop], s_least;
     __shared__ int32_t s_count;
     const int tid = threadIdx.x, lane = tid & 63;
     const int64_t row = blockIdx.x;
+    float4 p = {-__builtin_inff(), 0.f, 0.f, 0.f};
+    if (lane < a.slices) p = a.parts[row * a.slices + lane];
+    const Key* const keys = a.keys + row * a.slices * a.top;
+    for (int i = tid; i < a.slices * a.top; i += kThreads) s_all[i] = keys[i];
     bool valid;
     const float target = target_logit<T>(a, row, &valid);
-    Sums t = {-__builtin_inff(), 0.f, 0.f};
-    if (lane < a.slices) {
-        const float4 p = a.parts[row * a.slices + lane];
-        t = Sums{p.x, p.y, p.z};
-    }
+    Sums t = Sums{p.x, p.y, p.z};
 #pragma unroll
     for (int d = 1; d < 64; d <<= 1)
         t = join(t, Sums{__shfl_xor(t.m, d), __shfl_xor(t.s, d), __shfl_xor(t.u, d)}, a.c);
@@ -495,24 +525,23 @@ __global__ __launch_bounds__(kThreads) void k_logprobs_join(LogprobArgs a)
     finish(a, row, t, target, valid, &logsum, &broken);
     if (a.top == 0) return;
     // the k-th largest of the slices' first few keys, twice as many as k, bounds what can be among the row's k largest
-    const Key* const keys = a.keys + row * a.slices * a.top;
     const int few = min(a.top, 2 * ((a.top + a.slices - 1) / a.slices)), heads = a.slices * few;
-    for (int i = tid; i < heads; i += kThreads) s_keys[i] = keys[i / few * a.top + i % few];
     if (tid == 0) {
         s_count = 0;
         s_least = 1;
     }
     __syncthreads();
+    for (int i = tid; i < heads; i += kThreads) s_keys[i] = s_all[i / few * a.top + i % few];
+    pad(s_keys, heads);
+    __syncthreads();
     for (int i = tid; i < heads; i += kThreads) {
         const Key head = s_keys[i];
-        int place = 0;
-        for (int j = 0; j < heads; ++j) place += s_keys[j] > head;
-        if (place == a.top - 1 && head) s_least = head;
+        if (head && larger(s_keys, heads, head) == a.top - 1) s_least = head;
     }
     __syncthreads();
     const Key least = s_least;
     for (int i = tid; i < a.slices * a.top; i += kThreads)
-        if (keys[i] >= least) s_keys[atomicAdd(&s_count, 1)] = keys[i];
+        if (s_all[i] >= least) s_keys[atomicAdd(&s_count, 1)] = s_all[i];
     __syncthreads();
     largest(s_keys, s_count, a.top, s_best);
     if (tid < a.top) write_top(a, row, tid, s_best[tid], t.m, logsum, broken);
