@@ -88,6 +88,7 @@ enum cpes_scale_mode { CPES_SCALE_ALPHA_OVER_N_SIGMA = 0, CPES_SCALE_ALPHA_OVER_
 #define CPES_MAX_STEP_SUBSPACES 32   /* subspaces per cpes_update_step call */
 #define CPES_STATIC_MAX_CHUNKS (1 << 20) /* chunks per cpes_partition_chunks_static call */
 #define CPES_MAX_HEAD_DIM 256        /* head dimension of a cpes_cache */
+#define CPES_MAX_HEADS 65536         /* key-value heads of a cpes_cache, query heads of cpes_attend */
 #define CPES_MAX_ALTERNATIVES 64     /* most likely tokens cpes_logprobs lists per row */
 #define CPES_MAX_SEQUENCES (1 << 20) /* sequences listed per cpes_pages_* call, rows per cpes_attend call */
 

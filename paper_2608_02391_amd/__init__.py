@@ -23,7 +23,7 @@ NORM_Z, NORM_RANK = 0, 1
 SCALE_ALPHA_OVER_N_SIGMA, SCALE_ALPHA_OVER_N = 0, 1
 SUB_ASCENDING = 1
 MAX_MEMBERS, MAX_REWARDS, MAX_GROUPS, MAX_PERMUTATION_K, MAX_STEP_SUBSPACES = 256, 4096, 1024, 256, 32
-MAX_HEAD_DIM, MAX_ALTERNATIVES, MAX_SEQUENCES = 256, 64, 1 << 20
+MAX_HEAD_DIM, MAX_HEADS, MAX_ALTERNATIVES, MAX_SEQUENCES = 256, 65536, 64, 1 << 20
 PAGES_OK, PAGES_SHORT, PAGES_BAD_SEQUENCE = 0, 1, 2
 
 EXPORTED = (

@@ -17,6 +17,9 @@ using cpes::aligned16;
 using cpes::fail;
 using cpes::hip_status;
 
+// No buffer has more; what is below adds up to byte offsets of 64 bits.
+constexpr double kMaxElements = 1152921504606846976.0 / 16;     // 2^60 / 16
+
 int check_cache(const cpes_cache* c, const char* fn)
 {
     if (!c) return fail(CPES_ERR_INVALID_ARGUMENT, "%s: cache is null", fn);
@@ -29,8 +32,14 @@ int check_cache(const cpes_cache* c, const char* fn)
     if (c->head_dim < 8 || c->head_dim > CPES_MAX_HEAD_DIM || c->head_dim % 8 != 0)
         return fail(CPES_ERR_INVALID_ARGUMENT, "%s: head_dim %d is not a multiple of 8 in [8, %d]", fn, c->head_dim,
                     CPES_MAX_HEAD_DIM);
-    if (c->layer_stride < 0 || c->page_stride < 0 || c->head_stride < 0 || c->token_stride < 0)
-        return fail(CPES_ERR_INVALID_ARGUMENT, "%s: negative cache stride", fn);
+    const struct {
+        int64_t stride;
+        int32_t count;
+    } dims[] = {{c->layer_stride, c->layers}, {c->page_stride, c->pages}, {c->head_stride, c->heads}, {c->token_stride, c->page_size}};
+    for (const auto& d : dims)
+        if (d.stride < 0 || (double)d.stride * d.count > kMaxElements)
+            return fail(CPES_ERR_INVALID_ARGUMENT, "%s: cache stride %lld negative or beyond any memory", fn, (long long)d.stride);
+    if (c->heads > CPES_MAX_HEADS) return fail(CPES_ERR_UNSUPPORTED, "%s: %d heads above CPES_MAX_HEADS", fn, c->heads);
     return CPES_OK;
 }
 
@@ -109,6 +118,8 @@ char* at_layer(const cpes_cache* c, void* base, int32_t layer)
 int page_args(const cpes_cache* c, cpes::PageArgs* a, const char* fn)
 {
     const int64_t e = elem_size(c->dtype), H = c->heads, P = c->page_size, D = c->head_dim;
+    if (2.0 * c->layers * H * P * D * e / 16 >= 2147483648.0)
+        return fail(CPES_ERR_UNSUPPORTED, "%s: a page of more than 32 GB", fn);
     int64_t run = D, outers = H, outer = c->head_stride, inners = P, inner = c->token_stride;
     if (P == 1 || inner == D) {
         run = P * D;
@@ -128,7 +139,6 @@ int page_args(const cpes_cache* c, cpes::PageArgs* a, const char* fn)
         }
     }
     const int64_t units = 2 * c->layers * outers * inners * (run * e / 16);
-    if (units >= ((int64_t)1 << 31)) return fail(CPES_ERR_UNSUPPORTED, "%s: a page of more than 32 GB", fn);
     a->k = static_cast<char*>(c->k_dev);
     a->v = static_cast<char*>(c->v_dev);
     a->page_bytes = c->page_stride * e;
@@ -312,8 +322,7 @@ int cpes_cache_append(const cpes_cache* cache, int32_t layer, const cpes_pool* p
     a.new_head_bytes = new_head_stride * e;
     a.n = n;
     a.heads = cache->heads;
-    const int64_t run = cache->head_dim * e / 16, token = run * cache->heads;
-    if (token >= ((int64_t)1 << 24)) return fail(CPES_ERR_UNSUPPORTED, "%s: a token of more than 256 MB", fn);
+    const int64_t run = cache->head_dim * e / 16, token = run * cache->heads;      // below 2^22
     a.run = cpes::Divisor((uint32_t)run);
     a.token = cpes::Divisor((uint32_t)token);
     return hip_status(cpes::launch_append(a, (hipStream_t)stream), fn);
@@ -321,7 +330,8 @@ int cpes_cache_append(const cpes_cache* cache, int32_t layer, const cpes_pool* p
 
 size_t cpes_attend_workspace_bytes(int32_t rows, int32_t q_heads, int32_t kv_heads, int32_t head_dim)
 {
-    if (rows < 0 || rows > CPES_MAX_SEQUENCES || kv_heads < 1 || q_heads < 1 || q_heads % kv_heads != 0 || head_dim < 8 ||
+    if (rows < 0 || rows > CPES_MAX_SEQUENCES || kv_heads < 1 || q_heads < 1 || q_heads > CPES_MAX_HEADS ||
+        q_heads % kv_heads != 0 || head_dim < 8 ||
         head_dim > CPES_MAX_HEAD_DIM || head_dim % 8 != 0)
         return 0;
     return attend_bytes(rows, q_heads, kv_heads, head_dim);
@@ -341,6 +351,7 @@ int cpes_attend(const cpes_cache* cache, int32_t layer, const cpes_pool* pool, i
     if (!rc) rc = check_list(rows, q_dev && out_dev, fn);
     if (!rc && (q_heads < 1 || q_heads % cache->heads != 0))
         rc = fail(CPES_ERR_INVALID_ARGUMENT, "%s: %d query heads for %d key-value heads", fn, q_heads, cache->heads);
+    if (!rc && q_heads > CPES_MAX_HEADS) rc = fail(CPES_ERR_UNSUPPORTED, "%s: %d query heads above CPES_MAX_HEADS", fn, q_heads);
     if (!rc && !std::isfinite(scale)) rc = fail(CPES_ERR_INVALID_ARGUMENT, "%s: scale %g is not finite", fn, (double)scale);
     if (!rc && (window < 0 || sinks < 0))
         rc = fail(CPES_ERR_INVALID_ARGUMENT, "%s: window %d or sinks %d negative", fn, window, sinks);

@@ -243,3 +243,18 @@ class FakeGpu:
 
     def __getattr__(self, name):
         return getattr(self.t, name)
+
+
+def test_sizes_beyond_any_memory(lib):
+    """Strides and counts whose products would overflow 64 bits, and more heads than the kernels count."""
+    for huge in (dict(layer_stride=1 << 62), dict(page_stride=1 << 60), dict(head_stride=1 << 61), dict(token_stride=1 << 62),
+                 dict(layer_stride=1 << 40, layers=1 << 30)):
+        for call in (fork, compact, append, attend):
+            refused(lib, BAD, call(lib, c=cache(**huge)), "stride")
+    for call in (fork, compact, append, attend):
+        refused(lib, UNSUPPORTED, call(lib, c=cache(heads=65537)), "heads")
+    refused(lib, UNSUPPORTED, attend(lib, heads=2 * 65536), "heads")
+    assert cp.cpes_attend_workspace_bytes(1, 2 * 65536, 2, 64) == 0
+    most = dict(layers=2 ** 31 - 1, heads=65536, page_size=2 ** 31 - 1, head_dim=256, layer_stride=0, page_stride=0, head_stride=0,
+                token_stride=0)
+    refused(lib, UNSUPPORTED, lib.cpes_pages_copy(REF(cache(**most)), 1, FAKE, FAKE, None), "32 GB")
