@@ -83,18 +83,20 @@ __device__ __forceinline__ float key_value(Key k)
 }
 __device__ __forceinline__ uint32_t key_token(Key k) { return ~(uint32_t)k; }
 
-// Sums of a piece of a row.
+// Sums of a piece of a row, its largest logit's own term of 1 left out of s: a
+// near-certain token's log probability is -ln (1 + s), and s may be far below the
+// roundings of 1.  A piece of nothing but -inf has no such term, and s = u = 0.
 struct Sums {
-    float m, s, u;       // largest logit, sum 2^t, sum t 2^t with t = c (x - m)
+    float m, s, u;       // largest logit, sum 2^t of the others, sum t 2^t, with t = c (x - m)
 };
 
 __device__ __forceinline__ Sums join(Sums a, Sums b, float c)
 {
-    const float m = fmaxf(a.m, b.m);
-    // a piece of nothing but -inf has s = u = 0 and moves nothing
-    const float da = a.m == m ? 0.f : fmaxf(c * (a.m - m), kFar), db = b.m == m ? 0.f : fmaxf(c * (b.m - m), kFar);
-    const float fa = exp2_hw(da), fb = exp2_hw(db);
-    return Sums{m, fa * a.s + fb * b.s, fa * (a.u + da * a.s) + fb * (b.u + db * b.s)};
+    const bool first = a.m >= b.m;
+    const Sums hi = first ? a : b, lo = first ? b : a;
+    const float d = lo.m == hi.m ? 0.f : fmaxf(c * (lo.m - hi.m), kFar), f = exp2_hw(d);
+    const float all = lo.m == -__builtin_inff() ? lo.s : lo.s + 1.f;
+    return Sums{hi.m, hi.s + f * all, hi.u + f * (lo.u + d * all)};
 }
 
 // The logit of a row's target, if it has one.
@@ -112,13 +114,13 @@ __device__ __forceinline__ void finish(const LogprobArgs& a, int64_t row, Sums t
                                        bool* broken)
 {
     const float nan = __builtin_nanf("");
-    const bool empty = t.s == 0.f;        // nothing but -inf
+    const bool empty = t.m == -__builtin_inff();
     *broken = !(t.s >= 0.f) || t.m == __builtin_inff();
     t.s -= a.excess * t.u;
-    *logsum = *broken ? nan : empty ? 0.f : logf(t.s);
+    *logsum = *broken ? nan : empty ? 0.f : log1pf(t.s);
     if (threadIdx.x != 0) return;
     if (a.logp) a.logp[row] = !valid ? 0.f : empty ? -__builtin_inff() : a.scale * (target - t.m) - *logsum;
-    if (a.entropy) a.entropy[row] = empty ? 0.f : *logsum - t.u / t.s * kLn2;
+    if (a.entropy) a.entropy[row] = *broken ? nan : empty ? 0.f : *logsum - t.u / (1.f + t.s) * kLn2;
     if (a.lse) a.lse[row] = *broken ? nan : a.scale * t.m + *logsum;
     if (a.stats) {
         a.stats[2 * row] = t.m;
@@ -182,6 +184,7 @@ constexpr int kRound = 64;                // threads that look at a vector each 
 constexpr int kCandidates = 768;          // a key's room; kRound threads can add 8 each to 256
 constexpr int kManyOwners = 3 * kMaxTop / 2;
 constexpr float kHuge = 1e30f;
+constexpr float kDominated = 1.f / 16;    // sum of the other logits' terms below which the largest one's thread is looked at again
 
 // A thread's sums while it reads.  Exponents are one fused multiply-add, c x - b
 // with b = c m rounded; what b lost is put right when the thread is done.  Where
@@ -238,8 +241,9 @@ struct Running {
 
     __device__ __forceinline__ Sums done(float c) const
     {
-        const float lost = far() ? 0.f : fmaf(m, c, -b), f = exp2_hw(-lost);
-        return Sums{m, f * s, f * (u - lost * s)};
+        if (m == -__builtin_inff()) return Sums{m, s, 0.f};
+        const float lost = far() ? 0.f : fmaf(m, c, -b), f = exp2_hw(-lost), rest = f * s - 1.f;
+        return Sums{m, rest < 0.f ? 0.f : rest, f * (u - lost * s)};
     }
 };
 
@@ -376,16 +380,65 @@ __global__ __launch_bounds__(kThreads, 5) void k_logprobs(LogprobArgs a)
             if (a.top > 0 && whole < kNoted) s_most[whole][tid] = bf16_above(all);
         }
         // the threads' sums join, in a fixed order
-        Sums t = run.done(a.c);
+        Sums mine = run.done(a.c);
+        auto joined = [&]() {
+            Sums t = mine;
 #pragma unroll
-        for (int d = 1; d < 64; d <<= 1)
-            t = join(t, Sums{__shfl_xor(t.m, d), __shfl_xor(t.s, d), __shfl_xor(t.u, d)}, a.c);
-        if ((tid & 63) == 0) s_sums[tid >> 6] = t;
-        if (tid == 0) s_count = s_items = 0;
-        __syncthreads();
-        t = s_sums[0];
+            for (int d = 1; d < 64; d <<= 1)
+                t = join(t, Sums{__shfl_xor(t.m, d), __shfl_xor(t.s, d), __shfl_xor(t.u, d)}, a.c);
+            if ((tid & 63) == 0) s_sums[tid >> 6] = t;
+            __syncthreads();
+            t = s_sums[0];
 #pragma unroll
-        for (int v = 1; v < kThreads / 64; ++v) t = join(t, s_sums[v], a.c);
+            for (int v = 1; v < kThreads / 64; ++v) t = join(t, s_sums[v], a.c);
+            return t;
+        };
+        if (tid == 0) {
+            s_count = s_items = 0;
+            s_owner[0] = kThreads;
+        }
+        Sums t = joined();
+        if (t.s < kDominated && t.m > -__builtin_inff()) {
+            // One logit dominates, and its thread's other terms have been rounded beside its 1: that thread's
+            // logits again, all threads together, without it.
+            if (run.m == t.m) atomicMin(&s_owner[0], tid);
+            __syncthreads();
+            const int32_t owner = s_owner[0];
+            if (tid == owner) mine.s = mine.u = 0.f;
+            Sums own = {t.m, 0.f, 0.f};
+            for (int32_t i = tid * kThreads + owner; i < vecs; i += kThreads * kThreads) {
+                float x[N];
+                floats_at(i, x);
+#pragma unroll
+                for (int j = 0; j < N; ++j) {
+                    const float d = fmaxf(a.c * (x[j] - t.m), kFar), e = x[j] == t.m ? 0.f : exp2_hw(d);
+                    own.s += e;
+                    own.u += d * e;
+                }
+            }
+            // the 1 of the largest stands in `mine`; these have none
+            if (mine.m == t.m) {
+                mine.s += own.s;
+                mine.u += own.u;
+            } else {
+                const float d = fmaxf(a.c * (mine.m - t.m), kFar), f = exp2_hw(d), all = mine.m == -__builtin_inff() ? 0.f : mine.s + 1.f;
+                mine = Sums{t.m, f * all + own.s, f * (mine.u + d * all) + own.u};
+            }
+            // now every thread's piece is relative to the largest, and they add up
+#pragma unroll
+            for (int d = 1; d < 64; d <<= 1) {
+                mine.s += __shfl_xor(mine.s, d);
+                mine.u += __shfl_xor(mine.u, d);
+            }
+            if ((tid & 63) == 0) s_sums[tid >> 6] = mine;
+            __syncthreads();
+            t.s = t.u = 0.f;
+#pragma unroll
+            for (int v = 0; v < kThreads / 64; ++v) {
+                t.s += s_sums[v].s;
+                t.u += s_sums[v].u;
+            }
+        }
         float logsum = 0.f;
         bool broken = false;
         if (a.slices == 1)
@@ -596,7 +649,8 @@ __global__ __launch_bounds__(kThreads) void k_logprobs_backward(LogprobGradArgs 
             const float logp = a.scale * (x - m) - logsum, p = exp2_hw(logp * kLog2e);
             // p = 0: no gradient, whatever ln p is
             float d = p == 0.f || empty ? 0.f : -p * (gp + h * (logp + entropy));
-            if (v == target) d += empty ? 0.f : gp;
+            // g (1 - p) without the difference, which a near-certain target would lose
+            if (v == target && !empty) d = (p == 0.f ? 0.f : -p * h * (logp + entropy)) - gp * expm1f(logp);
             return d;
         };
         V4u w[kGradUnroll];

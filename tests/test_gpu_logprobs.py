@@ -294,3 +294,29 @@ def test_captured_and_on_another_stream():
         eager = score(dx, t, top=9)
         assert all(torch.equal(o[k], eager[k]) for k in o)
         check(dx, t, o, top=9)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32], ids=["bf16", "fp32"])
+@pytest.mark.parametrize("rows,V", [(3, 151936), (900, 30011), (2, 700)])
+@pytest.mark.parametrize("lead", [16.0, 30.0, 60.0])
+def test_near_certain_tokens(dtype, rows, V, lead):
+    """One logit far above the others: its log probability -ln (1 + s), the entropy and its gradient
+    g (1 - p) are of the size of s, and keep their digits.  Each term of s is off by its exponential's 2^-21 and by
+    the roundings of an exponent of the size of the lead, relative."""
+    print(f"near certain V={V} lead={lead} {dtype}", flush=True)
+    x, t = logits(rows, V, dtype, 11, std=1.0)
+    x[torch.arange(rows), t] = lead
+    xd = x.cuda()
+    o = score(xd, t, top=2)
+    dx, one = torch.empty(rows, V, device="cuda", dtype=dtype), torch.ones(rows, device="cuda")
+    cp.cpes_logprobs_backward(xd, t.cuda(), o["stats"], None, one, None, dx)
+    rel = sum_bound(V) + 8 * H.EPS * (lead + 6)
+    for r in range(0, rows, max(1, rows // 3)):
+        d = x[r].double().numpy() - lead
+        s = np.exp(np.delete(d, int(t[r]))).sum()
+        logp, entropy = -math.log1p(s), math.log1p(s) - float((np.delete(d, int(t[r])) * np.exp(np.delete(d, int(t[r])))).sum()) / (1 + s)
+        assert int(o["top_ids"][r, 0]) == int(t[r])
+        for got, want in ((o["logp"][r], logp), (o["top_logp"][r, 0], logp), (o["entropy"][r], entropy)):
+            assert abs(float(got) - want) <= rel * abs(want) + 1e-38, (r, float(got), want)
+        want = s / (1 + s)
+        assert abs(float(dx[r, t[r]]) - want) <= (rel + H.rounding(dtype)) * want + 1e-38, (r, float(dx[r, t[r]]), want)
