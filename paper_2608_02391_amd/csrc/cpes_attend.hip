@@ -113,16 +113,34 @@ template <typename T> __device__ __forceinline__ float weight(float x);
 template <> __device__ __forceinline__ float weight<uint16_t>(float x) { return __builtin_amdgcn_exp2f(x * kLog2e); }
 template <> __device__ __forceinline__ float weight<float>(float x) { return expf(x); }
 
-// The larger of the four lanes that hold one query head's scores.
+// x of the lanes that hold one query head's scores: rows of 16 lanes swapped
+// pairwise, then halves, each pair holding both rows' values afterwards.
+__device__ __forceinline__ void swap_rows(float x, float* y, float* z)
+{
+    const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    *y = __uint_as_float(r[0]);
+    *z = __uint_as_float(r[1]);
+}
+__device__ __forceinline__ void swap_halves(float x, float* y, float* z)
+{
+    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    *y = __uint_as_float(r[0]);
+    *z = __uint_as_float(r[1]);
+}
+
 __device__ __forceinline__ float max_over_lanes(float x)
 {
-    x = fmaxf(x, __shfl_xor(x, 16));
-    return fmaxf(x, __shfl_xor(x, 32));
+    float y, z;
+    swap_rows(x, &y, &z);
+    swap_halves(fmaxf(y, z), &y, &z);
+    return fmaxf(y, z);
 }
 __device__ __forceinline__ float sum_over_lanes(float x)
 {
-    x += __shfl_xor(x, 16);
-    return x + __shfl_xor(x, 32);
+    float y, z;
+    swap_rows(x, &y, &z);
+    swap_halves(y + z, &y, &z);
+    return y + z;
 }
 
 // Where the positions of one tile lie: element offsets of their rows from the
@@ -518,14 +536,22 @@ __global__ __launch_bounds__(kThreads, DP == 256 ? 1 : 2) void k_attend(AttendAr
     }
     const int64_t units = tiles * a.heads * a.blocks;
     const int32_t waves = (int32_t)max((int64_t)1, min((int64_t)a.groups * kWaves, units / kShareTiles));
-    const int32_t w0 = blockIdx.x * kWaves, me = w0 + wave;
-    if (w0 >= waves) return;
+    // Consecutive shares to the waves of a workgroup -- or, where there are no more than
+    // workgroups, one to each, on as many CUs (one row of 2,000: 13.1 -> 12.3 us).  Token-major
+    // pages take the second order too: a workgroup's waves are then a head or two apart at the
+    // same positions, whose heads lie side by side in memory (64 rows: 104 -> 98 us; long
+    // rows of head-major pages are 2 % faster in the first).
+    const bool apart = waves <= (int32_t)gridDim.x || a.head_stride < a.token_stride;
+    const int32_t share0 = apart ? blockIdx.x : blockIdx.x * kWaves, step = apart ? gridDim.x : 1;
+    const int32_t me = share0 + wave * step;
+    if (share0 >= waves) return;
     const Shares shares(units, waves);
     if (!few) {
 #pragma unroll 1
         for (int w = 0; w < kWaves; ++w) {
-            if (w0 + w >= waves) break;
-            const int64_t at = shares.begin(w0 + w), t = at - quotient(at, tiles) * tiles;
+            const int32_t share = share0 + w * step;
+            if (share >= waves) break;
+            const int64_t at = shares.begin(share), t = at - quotient(at, tiles) * tiles;
             if (t >= upto - mine && t < upto) {
                 int64_t before = upto - mine;
                 int32_t r = r0;
