@@ -1,10 +1,11 @@
 // cpes_pages.hip -- gfx950 kernels of the key-value cache's pages: handing out,
 // forking, freeing, copying and compacting them, and the entry of new tokens.
 //
-// The bookkeeping (which pages are free, who gets which) is one workgroup of
-// 1,024 threads that walks the reference counts in ascending order, 16 pages a
-// thread and step, so the result is the same on every run: the lowest free
-// pages, in list order.  A sequence it works on is claimed by a mark in its
+// The bookkeeping (which pages are free, who gets which) is one workgroup of 1,024
+// threads, or 256, that walks the reference counts in ascending order, 16 pages
+// a thread and step, so the result is the same on every run: the lowest free
+// pages, in list order.  It is a chain of trips to memory and of barriers, and that
+// is its time: about 5 us for a few sequences, 3 of them any launch's.  A sequence it works on is claimed by a mark in its
 // length, which finds sequences listed twice and is taken back when the call
 // fails.  Data moves in a second launch over the whole GPU; without any, the
 // call is one launch.
@@ -63,9 +64,9 @@ __device__ __forceinline__ int32_t held_tokens(const PoolArgs& p, int32_t length
 }
 
 // Exclusive sum of x over the workgroup; *total receives the sum.  All threads.
-__device__ int32_t block_scan(int32_t x, int32_t* total)
+template <int BLOCK> __device__ int32_t block_scan(int32_t x, int32_t* total)
 {
-    __shared__ int32_t wave_sum[kPlanBlock / 64];
+    __shared__ int32_t wave_sum[BLOCK / 64];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     int32_t inc = x;
 #pragma unroll
@@ -78,7 +79,7 @@ __device__ int32_t block_scan(int32_t x, int32_t* total)
     __syncthreads();
     int32_t before = 0, all = 0;
 #pragma unroll
-    for (int w = 0; w < kPlanBlock / 64; ++w) {
+    for (int w = 0; w < BLOCK / 64; ++w) {
         const int32_t y = wave_sum[w];
         if (w < wave) before += y;
         all += y;
@@ -106,16 +107,16 @@ __device__ __forceinline__ void load_refs(const PoolArgs& p, int64_t first, int3
 // The lowest `want` free pages, ascending, into list (fewer if there are not
 // that many); their number is returned.  r holds the counts of the first step's
 // pages, 16 a thread.  All threads.
-__device__ int32_t lowest_free(const PoolArgs& p, int32_t r[16], int32_t want, int32_t* list)
+template <int BLOCK> __device__ int32_t lowest_free(const PoolArgs& p, int32_t r[16], int32_t want, int32_t* list)
 {
     int32_t found = 0;
-    for (int64_t base = 0; base < p.pages && found < want; base += 16 * kPlanBlock) {
+    for (int64_t base = 0; base < p.pages && found < want; base += 16 * BLOCK) {
         const int64_t first = base + 16 * (int64_t)threadIdx.x;
         int32_t mine = 0, total;
         if (base > 0) load_refs(p, first, 1, r);
 #pragma unroll
         for (int e = 0; e < 16; ++e) mine += r[e] <= 0;
-        int32_t at = found + block_scan(mine, &total);
+        int32_t at = found + block_scan<BLOCK>(mine, &total);
 #pragma unroll
         for (int e = 0; e < 16; ++e)
             if (r[e] <= 0) {
@@ -130,21 +131,21 @@ __device__ int32_t lowest_free(const PoolArgs& p, int32_t r[16], int32_t want, i
 
 // ---------------------------------------------------------------- reserve --
 // Claims every listed sequence, sums what they lack, takes that many of the
-// lowest free pages and hands them out, one wave per sequence at a time.  The
-// first 1,024 entries of the list stay in registers, and the first reference
-// counts are on their way while the sequences are claimed: the kernel is a chain
-// of trips to memory, and these are two of them.
-__global__ __launch_bounds__(kPlanBlock) void k_pages_reserve(PoolArgs p, int32_t n, const int32_t* seqs,
+// lowest free pages and hands them out, one wave per sequence at a time.  A
+// thread's first entry of the list stays in registers, and the first reference
+// counts are on their way while the sequences are claimed.
+template <int BLOCK>
+__global__ __launch_bounds__(BLOCK) void k_pages_reserve(PoolArgs p, int32_t n, const int32_t* seqs,
                                                               const int32_t* new_lengths, int32_t* ws, int32_t* status)
 {
-    __shared__ int32_t s_seq[kPlanBlock], s_from[kPlanBlock], s_need[kPlanBlock], s_at[kPlanBlock];
+    __shared__ int32_t s_seq[BLOCK], s_from[BLOCK], s_need[BLOCK], s_at[BLOCK];
     int32_t* const list = ws + kPagesHeader;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     int32_t r[16];
     load_refs(p, 16 * (int64_t)tid, 1, r);
     bool bad = false;
     int32_t seq0 = 0, len0 = 0, old0 = 0;               // of entry tid
-    for (int32_t i = tid; i < n; i += kPlanBlock) {
+    for (int32_t i = tid; i < n; i += BLOCK) {
         const int32_t s = seqs[i], len = new_lengths[i];
         if (!known(p, s) || len < 0 || (int64_t)len > capacity(p)) {
             bad = true;
@@ -177,40 +178,40 @@ __global__ __launch_bounds__(kPlanBlock) void k_pages_reserve(PoolArgs p, int32_
     const bool wide = p.width >= 1 << 20;
     int64_t want = 0;
     int32_t need0 = 0, at0 = 0;
-    for (int32_t base = 0; base < n && !bad; base += kPlanBlock) {
+    for (int32_t base = 0; base < n && !bad; base += BLOCK) {
         int32_t need = 0, lo, hi = 0, s, len, old;
         if (base + tid < n) need = entry(base + tid, &s, &len, &old);
-        const int32_t at = block_scan(wide ? need & 0xFFFF : need, &lo);
-        if (wide) block_scan(need >> 16, &hi);
+        const int32_t at = block_scan<BLOCK>(wide ? need & 0xFFFF : need, &lo);
+        if (wide) block_scan<BLOCK>(need >> 16, &hi);
         want += ((int64_t)hi << 16) + lo;
         if (base == 0) {
             need0 = need;
             at0 = at;
         }
     }
-    const bool once = n <= kPlanBlock && !wide;          // then these are all there is to know
-    const bool enough = !bad && want <= p.pages && lowest_free(p, r, (int32_t)want, list) == (int32_t)want;
+    const bool once = n <= BLOCK && !wide;          // then these are all there is to know
+    const bool enough = !bad && want <= p.pages && lowest_free<BLOCK>(p, r, (int32_t)want, list) == (int32_t)want;
     if (!enough) {
-        for (int32_t i = tid; i < n; i += kPlanBlock)
+        for (int32_t i = tid; i < n; i += BLOCK)
             if (known(p, seqs[i])) atomicAnd(&p.lengths[seqs[i]], ~kClaim);
         if (tid == 0 && status) *status = bad ? kBadSequence : kShort;
         return;
     }
     int32_t given = 0;
-    for (int32_t base = 0; base < n; base += kPlanBlock) {
+    for (int32_t base = 0; base < n; base += BLOCK) {
         int32_t need = need0, at = at0, total = 0, s = seq0, len = len0, old = old0;
         if (!once) {
             need = 0;
             if (base + tid < n) need = entry(base + tid, &s, &len, &old);
-            at = given + block_scan(need, &total);
+            at = given + block_scan<BLOCK>(need, &total);
         }
         if (base + tid < n) p.lengths[s] = max(old, len);
         s_seq[tid] = s;
         s_need[tid] = need;
         s_at[tid] = at;
         __syncthreads();
-        const int32_t here = min(n - base, kPlanBlock);
-        for (int32_t i = wave; i < here; i += kPlanBlock / 64) {
+        const int32_t here = min(n - base, BLOCK);
+        for (int32_t i = wave; i < here; i += BLOCK / 64) {
             int32_t* const row = row_of(p, s_seq[i]) + s_from[i];
             for (int32_t j = lane; j < s_need[i]; j += 64) {
                 const int32_t page = list[s_at[i] + j];
@@ -291,9 +292,10 @@ __global__ __launch_bounds__(kCopyBlock) void k_pages_copy(PageArgs c, int32_t p
 // ------------------------------------------------------------------- fork --
 // The plan claims the children (an empty one's length becomes the mark), takes
 // the lowest free page for each partly filled last page, writes it into the
-// child's table and sets the child's length; ws[0] says whether it went well.  As
-// in k_pages_reserve, the first entries and reference counts are in registers.
-__global__ __launch_bounds__(kPlanBlock) void k_pages_fork_plan(PoolArgs p, int32_t n, const int32_t* parents,
+// child's table and sets the child's length; ws[0] says whether it went well.  A
+// thread's first entry and the first reference counts are in registers, as there.
+template <int BLOCK>
+__global__ __launch_bounds__(BLOCK) void k_pages_fork_plan(PoolArgs p, int32_t n, const int32_t* parents,
                                                                 const int32_t* children, int32_t* ws, int32_t* status)
 {
     int32_t* const list = ws + kPagesHeader;
@@ -302,7 +304,7 @@ __global__ __launch_bounds__(kPlanBlock) void k_pages_fork_plan(PoolArgs p, int3
     load_refs(p, 16 * (int64_t)tid, 1, r);
     bool bad = false;
     int32_t child0 = 0, len0 = 0;         // of entry tid
-    for (int32_t i = tid; i < n; i += kPlanBlock) {
+    for (int32_t i = tid; i < n; i += BLOCK) {
         const int32_t a = parents[i], c = children[i];
         if (!known(p, a) || !known(p, c)) {
             bad = true;
@@ -319,16 +321,16 @@ __global__ __launch_bounds__(kPlanBlock) void k_pages_fork_plan(PoolArgs p, int3
     bad = __syncthreads_or(bad);
     auto length = [&](int32_t i) { return i == tid ? len0 : held_tokens(p, p.lengths[parents[i]]); };
     int32_t want = 0, at0 = 0;
-    for (int32_t base = 0; base < n && !bad; base += kPlanBlock) {
+    for (int32_t base = 0; base < n && !bad; base += BLOCK) {
         int32_t total;
-        const int32_t at = block_scan(base + tid < n && length(base + tid) % p.page_size != 0, &total);
+        const int32_t at = block_scan<BLOCK>(base + tid < n && length(base + tid) % p.page_size != 0, &total);
         if (base == 0) at0 = at;
         want += total;
     }
-    const bool enough = !bad && lowest_free(p, r, want, list) == want;
+    const bool enough = !bad && lowest_free<BLOCK>(p, r, want, list) == want;
     if (!enough) {
         // only a child that was empty and claimed here carries the mark alone
-        for (int32_t i = tid; i < n; i += kPlanBlock)
+        for (int32_t i = tid; i < n; i += BLOCK)
             if (known(p, children[i])) atomicCAS(&p.lengths[children[i]], kClaim, 0);
         if (tid == 0) {
             ws[0] = 0;
@@ -337,7 +339,7 @@ __global__ __launch_bounds__(kPlanBlock) void k_pages_fork_plan(PoolArgs p, int3
         return;
     }
     int32_t given = 0;
-    for (int32_t base = 0; base < n; base += kPlanBlock) {
+    for (int32_t base = 0; base < n; base += BLOCK) {
         int32_t total = 0, len = 0, c = child0;
         const bool mine = base + tid < n;
         if (mine) {
@@ -346,18 +348,18 @@ __global__ __launch_bounds__(kPlanBlock) void k_pages_fork_plan(PoolArgs p, int3
         }
         const int32_t last = len / p.page_size;
         const bool tail = len - last * p.page_size != 0;
-        const int32_t at = n <= kPlanBlock ? at0 : given + block_scan(tail, &total);
+        const int32_t at = n <= BLOCK ? at0 : given + block_scan<BLOCK>(tail, &total);
         if (tail) {
             row_of(p, c)[last] = list[at];
             p.refs[list[at]] = 1;
         }
         // the mark stays on while entries behind may read this length as a parent's
-        if (mine) p.lengths[c] = n > kPlanBlock ? len | kClaim : len;
+        if (mine) p.lengths[c] = n > BLOCK ? len | kClaim : len;
         given += total;
     }
-    if (n > kPlanBlock) {
+    if (n > BLOCK) {
         __syncthreads();                  // every parent's length has been read
-        for (int32_t i = tid; i < n; i += kPlanBlock) p.lengths[children[i]] &= ~kClaim;
+        for (int32_t i = tid; i < n; i += BLOCK) p.lengths[children[i]] &= ~kClaim;
     }
     if (tid == 0) {
         ws[0] = 1;
@@ -432,28 +434,29 @@ __device__ __host__ __forceinline__ CompactLists compact_lists(int32_t* ws, int3
     return l;
 }
 
-__global__ __launch_bounds__(kPlanBlock) void k_pages_compact_plan(PoolArgs p, int32_t* ws, int32_t* moved)
+template <int BLOCK>
+__global__ __launch_bounds__(BLOCK) void k_pages_compact_plan(PoolArgs p, int32_t* ws, int32_t* moved)
 {
     const CompactLists l = compact_lists(ws, p.pages);
-    const bool once = p.pages <= 16 * kPlanBlock;        // the counts of the one step stay in registers
+    const bool once = p.pages <= 16 * BLOCK;        // the counts of the one step stay in registers
     int32_t live = 0, r[16];
-    for (int64_t base = 0; base < p.pages; base += 16 * kPlanBlock) {
+    for (int64_t base = 0; base < p.pages; base += 16 * BLOCK) {
         int32_t mine = 0, total;
         load_refs(p, base + 16 * (int64_t)threadIdx.x, 0, r);
 #pragma unroll
         for (int e = 0; e < 16; ++e) mine += r[e] > 0;
-        block_scan(mine, &total);
+        block_scan<BLOCK>(mine, &total);
         live += total;
     }
     int32_t holes = 0, movers = 0;
-    for (int64_t base = 0; base < p.pages; base += 16 * kPlanBlock) {
+    for (int64_t base = 0; base < p.pages; base += 16 * BLOCK) {
         const int64_t first = base + 16 * (int64_t)threadIdx.x;
         int32_t mine = 0, total;
         if (!once) load_refs(p, first, 0, r);
         // both counts of a step fit 16 bits: one sum
 #pragma unroll
         for (int e = 0; e < 16; ++e) mine += first + e < live ? r[e] <= 0 : r[e] > 0 ? 1 << 16 : 0;
-        const int32_t before = block_scan(mine, &total);
+        const int32_t before = block_scan<BLOCK>(mine, &total);
         int32_t hole = holes + (before & 0xFFFF), mover = movers + (before >> 16);
 #pragma unroll
         for (int e = 0; e < 16; ++e) {
@@ -555,19 +558,33 @@ constexpr int kCopyGrid = 4096;
 constexpr int kAppendGrid = 1 << 20;
 constexpr double kCacheBytes = 256 << 20; // the last-level cache
 
+// Where 256 threads see all pages and sequences in one step, their plan is done
+// sooner: free, reserve and fork of four rollouts 19.6 us with 1,024, 17.5 so.
+constexpr int kSmallPlan = 256;
+bool small_plan(const PoolArgs& p, int32_t n)
+{
+    return n <= kSmallPlan && p.pages <= 16 * kSmallPlan;
+}
+
 }  // namespace
 
 hipError_t launch_pages_reserve(const PoolArgs& p, int32_t n, const int32_t* seqs, const int32_t* new_lengths,
                                 int32_t* ws, int32_t* status, hipStream_t s)
 {
-    hipLaunchKernelGGL(k_pages_reserve, dim3(1), dim3(kPlanBlock), 0, s, p, n, seqs, new_lengths, ws, status);
+    if (small_plan(p, n))
+        hipLaunchKernelGGL(k_pages_reserve<kSmallPlan>, dim3(1), dim3(kSmallPlan), 0, s, p, n, seqs, new_lengths, ws, status);
+    else
+        hipLaunchKernelGGL(k_pages_reserve<kPlanBlock>, dim3(1), dim3(kPlanBlock), 0, s, p, n, seqs, new_lengths, ws, status);
     return hipGetLastError();
 }
 
 hipError_t launch_pages_fork(const PageArgs& c, const PoolArgs& p, int32_t n, const int32_t* parents,
                              const int32_t* children, int32_t* ws, int32_t* status, hipStream_t s)
 {
-    hipLaunchKernelGGL(k_pages_fork_plan, dim3(1), dim3(kPlanBlock), 0, s, p, n, parents, children, ws, status);
+    if (small_plan(p, n))
+        hipLaunchKernelGGL(k_pages_fork_plan<kSmallPlan>, dim3(1), dim3(kSmallPlan), 0, s, p, n, parents, children, ws, status);
+    else
+        hipLaunchKernelGGL(k_pages_fork_plan<kPlanBlock>, dim3(1), dim3(kPlanBlock), 0, s, p, n, parents, children, ws, status);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess || n == 0) return e;
     const int32_t most = std::max<int32_t>((int32_t)pieces_of(c), p.width / kCopyBlock);
@@ -595,7 +612,10 @@ hipError_t launch_pages_copy(const PageArgs& c, int32_t pages, int32_t n, const 
 hipError_t launch_pages_compact(const PageArgs& c, const PoolArgs& p, const PoolArgs& packed, int32_t* ws,
                                 int32_t* moved, hipStream_t s)
 {
-    hipLaunchKernelGGL(k_pages_compact_plan, dim3(1), dim3(kPlanBlock), 0, s, p, ws, moved);
+    if (small_plan(p, 0))
+        hipLaunchKernelGGL(k_pages_compact_plan<kSmallPlan>, dim3(1), dim3(kSmallPlan), 0, s, p, ws, moved);
+    else
+        hipLaunchKernelGGL(k_pages_compact_plan<kPlanBlock>, dim3(1), dim3(kPlanBlock), 0, s, p, ws, moved);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
     // half of the pages move at most

@@ -222,3 +222,22 @@ def test_captured_cycle():
         for x, y in copies:
             r.k0[:, y], r.v0[:, y] = r.k0[:, x], r.v0[:, x]
         r.same(code)
+
+
+def test_random_life_of_a_larger_pool():
+    """More pages than the smaller plan takes, in a few steps of each kind."""
+    rng = np.random.default_rng(9)
+    r = Rig(300, 60, 5000, 3, layers=1, heads=1, dim=8)
+    for step in range(24):
+        empty = [s for s in range(300) if r.m.lengths[s] == 0]
+        full = [s for s in range(300) if r.m.lengths[s] > 0]
+        if step % 4 == 0:
+            seqs = [int(s) for s in rng.permutation(300)[:int(rng.integers(1, 290))]]
+            r.reserve(seqs, [int(rng.integers(0, 100)) for _ in seqs])
+        elif step % 4 == 1 and empty and full:
+            kids = [int(s) for s in rng.permutation(empty)[:int(rng.integers(1, 200))]]
+            r.fork([int(rng.choice(full)) for _ in kids], kids)
+        elif step % 4 == 2:
+            r.free([int(s) for s in rng.permutation(300)[:int(rng.integers(0, 150))]])
+        else:
+            r.compact()
