@@ -10,7 +10,11 @@
 // What bounds it: every key and value is read once, 2 D elements for 4 D
 // operations per query head, far below what the matrix instructions do; the
 // kernel is a stream from HBM, so the work is arranged for many wide loads in
-// flight and none of it waits on another wave.
+// flight and none of it waits on another wave.  8 rows of 65 to 131 thousand positions,
+// 32 heads on 8 of 128 in bf16 (2.95 GB): 446 us, 6.6 TB/s, as fast as a large copy;
+// 40 rows of up to 8,191 (306 MB): 51 us and 5.6 for the join, 6.0 TB/s while it
+// streams; the matrix units are busy 5 to 7 % of the time.  In fp32, 24 rows through a
+// window of 4,096 (591 MB): 96 us, 6.1 TB/s.
 //
 // Tiles.  A wave takes 32 positions (16 in fp32), about 16 KiB at D = 128.
 // Scores come out of the matrix instructions transposed, S^T = K Q^T with the

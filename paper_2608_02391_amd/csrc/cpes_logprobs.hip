@@ -3,31 +3,40 @@
 // gradient of the first two.
 //
 // Mathematics.  With z = scale x, M = max z, c = scale log2 e and t_v = c (x_v - max x) <= 0:
-//   s = sum 2^(t_v),  u = sum t_v 2^(t_v),
-//   lse = M + ln s,  ln p_v = z_v - M - ln s,  entropy = ln s - ln 2 u / s
-// (both terms of the entropy are positive: nothing cancels).  Pieces (max, s, u) of
-// a row join by 2^(t of the smaller maximum), u moving by s times that exponent as
-// well.  c rounded to fp32 is c (1 + r): to first order that adds r ln 2 u to s, which
-// is taken back at the end.
+//   s = sum 2^(t_v) over all but the largest,  u = sum t_v 2^(t_v),
+//   lse = M + ln (1 + s),  ln p_v = z_v - M - ln (1 + s),  entropy = ln (1 + s) - ln 2 u / (1 + s)
+// (both terms of the entropy are positive: nothing cancels, and a near-certain
+// token's numbers, of the size of s, keep their digits).  Pieces (max, s, u) of a row
+// join by 2^(t of the smaller maximum), u moving by the terms times that exponent
+// as well.  c rounded to fp32 is c (1 + r): to first order that adds r ln 2 u to s,
+// which is taken back at the end.
 //   dx_v = scale (g ([v = t] - p_v) - h p_v (ln p_v + entropy)).
 //
 // What bounds it: a logit is read once (and its gradient written once) for about
-// ten operations, close to what the vector units do in the time its bytes take,
-// so the loop holds no more than it must: one subtraction, product, exponential
-// and three sums a logit, the maximum by threes, and the alternatives cost nothing
-// until the row's end (below).
+// six instructions, close to what the vector units do in the time its bytes take,
+// so the loop holds no more than it must: one fused multiply-add for the exponent,
+// the exponential, two sums, the maximum and the minimum by threes; the next step's
+// loads are on their way meanwhile, and the alternatives cost a note of the step's
+// maximum.  4,096 rows of 151,936 in bf16 with 5 alternatives: 201 us, 6.2 TB/s, with
+// the vector units issuing in 79 % of cycles; the loop without its arithmetic takes
+// 182.  The gradient of 2,000 rows of 50,257: 60 us, 6.7 TB/s read and written.
 //
-// Split.  A row is one workgroup's where there are rows for the GPU; few rows are cut
-// into slices, joined by a second launch in slice order.
+// Split.  A row is one workgroup's where there are rows for the GPU (five a CU);
+// few rows are cut into slices, joined by a second launch in slice order: one row
+// of 151,936 with 20 alternatives in 16 us, 10 and 6, latencies of a dozen
+// trips to memory and barriers.
 //
 // Alternatives.  Order: value descending, then token ascending, as one 64-bit key,
 // so no two are equal and the result does not depend on who writes first.  A
 // thread keeps, with its running maximum, the step it first met it in, so the
-// maximum's key lies between those of the step's last and first token.  The k-th
-// largest of the 256 threads' lower ends bounds the row's k-th largest key from
-// below, and only threads whose upper end reaches that bound can hold a key from
-// there on: k of them, and a few that tie, whose logits, about k / 256 of the row,
-// are looked at again (from the caches).
+// maximum's key lies between those of the step's last and first token.  Each wave
+// ranks its lanes' lower ends; the least of the waves' k/4-th bounds the row's k-th
+// largest key from below, and only threads whose upper end reaches that bound can
+// hold a key from there on: k and a few.  Every thread notes each step's maximum in
+// LDS, so of those threads only the steps that reach the bound are read again, about
+// k x 64 bytes; reading all their logits again made 64 alternatives cost 180 us
+// on 4,096 rows, now 10.  Rows of ties go through exact keys, and where even these
+// overflow the buffer, through rounds that raise the bound.
 #include <algorithm>
 #include <type_traits>
 

@@ -5,10 +5,10 @@
 // threads, or 256, that walks the reference counts in ascending order, 16 pages
 // a thread and step, so the result is the same on every run: the lowest free
 // pages, in list order.  It is a chain of trips to memory and of barriers, and that
-// is its time: about 5 us for a few sequences, 3 of them any launch's.  A sequence it works on is claimed by a mark in its
-// length, which finds sequences listed twice and is taken back when the call
-// fails.  Data moves in a second launch over the whole GPU; without any, the
-// call is one launch.
+// is its time: about 4.6 us for a few sequences, 2.6 of them any launch's.  A
+// sequence it works on is claimed by a mark in its length, which finds sequences
+// listed twice and is taken back when the call fails.  Data moves in a second
+// launch over the whole GPU; without any, the call is one launch.
 #include <algorithm>
 
 #include "cpes_eval.hpp"
@@ -244,8 +244,12 @@ __device__ __forceinline__ int64_t unit_offset(const PageArgs& c, uint32_t u, bo
 constexpr int kCopyBlock = 256;
 constexpr int kCopyUnits = 4;             // 16-byte units a thread has in flight
 
-// Units [piece * kCopyBlock * kCopyUnits, ...) of page src to page dst.  NT: past
-// the caches, for copies that exceed them.
+// Units [piece * kCopyBlock * kCopyUnits, ...) of page src to page dst: a copy, bound
+// by HBM, 16 bytes a lane and four of them under way.  259 MB of a pool's pages, runs
+// of 8 KiB, move in 94 us, 5.5 TB/s read and written, against 6.7 of one large copy; the
+// tails of 256 rollouts, 47 MB from a few pages, in 13.5 us.  Eight under way
+// are half as fast, two or one-piece workgroups no faster.  NT: past the caches, for
+// copies that exceed them.
 template <bool NT>
 __device__ __forceinline__ void copy_piece(const PageArgs& c, int32_t src, int32_t dst, uint32_t piece)
 {
@@ -519,7 +523,9 @@ __global__ __launch_bounds__(kCopyBlock) void k_pages_compact(PageArgs c, PoolAr
 
 // ----------------------------------------------------------------- append --
 // `per` tokens a workgroup; where each goes is found once and kept in LDS, then
-// the threads move the tokens' 16-byte units, key and value together.
+// the threads move the tokens' 16-byte units, key and value together.  Bound by HBM, or
+// by the launch: 6,700 tokens of 4 KiB in 9.9 us (5.6 TB/s read and written), one token
+// of 48 rollouts in 2.9 us.
 constexpr int kAppendTokens = 64;         // most tokens of a workgroup
 constexpr int kAppendUnits = 4;           // units of keys (and of values) a thread should get
 
@@ -559,11 +565,14 @@ constexpr int kAppendGrid = 1 << 20;
 constexpr double kCacheBytes = 256 << 20; // the last-level cache
 
 // Where 256 threads see all pages and sequences in one step, their plan is done
-// sooner: free, reserve and fork of four rollouts 19.6 us with 1,024, 17.5 so.
+// sooner: free, reserve and fork of four rollouts 19.6 us with 1,024, 17.5 so.  A
+// reservation's pages are written by a wave a sequence, so more than a few
+// sequences want all waves (32 of up to 125 pages: 8.0 us with 256, 6.7 with 1,024).
 constexpr int kSmallPlan = 256;
-bool small_plan(const PoolArgs& p, int32_t n)
+constexpr int kSmallReserve = 16;
+bool small_plan(const PoolArgs& p, int32_t n, int32_t most)
 {
-    return n <= kSmallPlan && p.pages <= 16 * kSmallPlan;
+    return n <= most && p.pages <= 16 * kSmallPlan;
 }
 
 }  // namespace
@@ -571,7 +580,7 @@ bool small_plan(const PoolArgs& p, int32_t n)
 hipError_t launch_pages_reserve(const PoolArgs& p, int32_t n, const int32_t* seqs, const int32_t* new_lengths,
                                 int32_t* ws, int32_t* status, hipStream_t s)
 {
-    if (small_plan(p, n))
+    if (small_plan(p, n, kSmallReserve))
         hipLaunchKernelGGL(k_pages_reserve<kSmallPlan>, dim3(1), dim3(kSmallPlan), 0, s, p, n, seqs, new_lengths, ws, status);
     else
         hipLaunchKernelGGL(k_pages_reserve<kPlanBlock>, dim3(1), dim3(kPlanBlock), 0, s, p, n, seqs, new_lengths, ws, status);
@@ -581,7 +590,7 @@ hipError_t launch_pages_reserve(const PoolArgs& p, int32_t n, const int32_t* seq
 hipError_t launch_pages_fork(const PageArgs& c, const PoolArgs& p, int32_t n, const int32_t* parents,
                              const int32_t* children, int32_t* ws, int32_t* status, hipStream_t s)
 {
-    if (small_plan(p, n))
+    if (small_plan(p, n, kSmallPlan))
         hipLaunchKernelGGL(k_pages_fork_plan<kSmallPlan>, dim3(1), dim3(kSmallPlan), 0, s, p, n, parents, children, ws, status);
     else
         hipLaunchKernelGGL(k_pages_fork_plan<kPlanBlock>, dim3(1), dim3(kPlanBlock), 0, s, p, n, parents, children, ws, status);
@@ -612,7 +621,7 @@ hipError_t launch_pages_copy(const PageArgs& c, int32_t pages, int32_t n, const 
 hipError_t launch_pages_compact(const PageArgs& c, const PoolArgs& p, const PoolArgs& packed, int32_t* ws,
                                 int32_t* moved, hipStream_t s)
 {
-    if (small_plan(p, 0))
+    if (small_plan(p, 0, kSmallPlan))
         hipLaunchKernelGGL(k_pages_compact_plan<kSmallPlan>, dim3(1), dim3(kSmallPlan), 0, s, p, ws, moved);
     else
         hipLaunchKernelGGL(k_pages_compact_plan<kPlanBlock>, dim3(1), dim3(kPlanBlock), 0, s, p, ws, moved);
