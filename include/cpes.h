@@ -410,6 +410,8 @@ CPES_API int cpes_update_step32(void* w_dev, int64_t numel, int dtype, int32_t K
  *     replayed as sequences grow.  Nothing on the device is trusted to address
  *     memory: page ids outside [0, pages), sequence ids outside [0, sequences)
  *     and lengths beyond the table are caught there, as each call says.
+ *   - calls that change one pool or cache, or read what another changes, must not
+ *     overlap in time (one stream, or events between streams).
  *   - tensors start at any element; only cpes_cache has a rule for its rows. */
 
 /*

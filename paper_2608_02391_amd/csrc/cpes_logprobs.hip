@@ -187,8 +187,8 @@ __device__ void largest(Key* keys, int n, int k, Key* best)
 
 constexpr int kUnroll = 4;                // 16-byte loads of a thread and step
 constexpr int kMaxTop = 64;
-constexpr int kNoted = 32;                // steps whose maxima are kept
-constexpr int kItems = 512;               // of them looked at again
+constexpr int kNoted = 32;                // maxima a thread notes: of a step each, or of 2, 4, .. steps of longer rows
+constexpr int kItems = 512;               // of them whose steps are looked at again
 constexpr int kRound = 64;                // threads that look at a vector each while candidates may have to be thinned out
 constexpr int kCandidates = 768;          // a key's room; kRound threads can add 8 each to 256
 constexpr int kManyOwners = 3 * kMaxTop / 2;
@@ -349,7 +349,13 @@ __global__ __launch_bounds__(kThreads, 5) void k_logprobs(LogprobArgs a)
         if (a.slices == 1 && tid == 0) target = target_logit<T>(a, row, &valid);
         Running run = {-__builtin_inff(), -__builtin_inff(), 0.f, 0.f};
         int32_t met = 0;                  // the step the maximum was first met in
-        float most;
+        int32_t shift = 0;                // steps of a note
+        while ((steps - 1) >> shift >= kNoted) ++shift;
+        float most, noted = -__builtin_inff();
+        auto note = [&](int32_t step, float x) {
+            noted = step & ((1 << shift) - 1) ? fmaxf(noted, x) : x;
+            s_most[step >> shift][tid] = bf16_above(noted);
+        };
         V4u w[kUnroll];                   // the next step's, on their way while one is added
         auto load = [&](int32_t step) {
 #pragma unroll
@@ -366,7 +372,7 @@ __global__ __launch_bounds__(kThreads, 5) void k_logprobs(LogprobArgs a)
             for (int u = 0; u < kUnroll; ++u) unpack<T>(w[u], x + u * N);
             if (step + 1 < whole) load(step + 1);
             if (run.take<kUnroll * N>(x, a.c, &most)) met = step;
-            if (a.top > 0 && step < kNoted) s_most[step][tid] = bf16_above(most);
+            if (a.top > 0) note(step, most);
         }
         if (whole < steps) {
             float all = -__builtin_inff();
@@ -386,7 +392,7 @@ __global__ __launch_bounds__(kThreads, 5) void k_logprobs(LogprobArgs a)
 #pragma unroll
                 for (int v = 1; v < kUnroll; ++v) w[v - 1] = w[v];
             }
-            if (a.top > 0 && whole < kNoted) s_most[whole][tid] = bf16_above(all);
+            if (a.top > 0) note(whole, all);
         }
         // the threads' sums join, in a fixed order
         Sums mine = run.done(a.c);
@@ -490,31 +496,28 @@ __global__ __launch_bounds__(kThreads, 5) void k_logprobs(LogprobArgs a)
                     }
                 }
             };
-            bool whole_owners = steps > kNoted;
-            if (!whole_owners) {
-                // only the steps of theirs that reach the bound
-                if (high >= least)
-                    for (int32_t step = 0; step < steps; ++step)
-                        if (value_of(s_most[step][tid]) >= key_value(least) || least == 1) {
-                            const int at = atomicAdd(&s_items, 1);
-                            if (at < kItems) s_item[at] = (uint16_t)(step * kThreads + tid);
-                        }
-                __syncthreads();
-                const int items = s_items;
-                whole_owners = items > kItems;
-                if (!whole_owners) {
-                    for (int at = tid; at < items * kUnroll; at += kThreads) {
-                        const int32_t x = s_item[at / kUnroll];
-                        const int32_t i = (x / kThreads * kUnroll + at % kUnroll) * kThreads + x % kThreads;
-                        if (i < vecs) {
-                            float v[N];
-                            floats_at(i, v);
-                            collect(v, i);
-                        }
+            // only the steps of theirs whose notes reach the bound
+            if (high >= least)
+                for (int32_t at = 0; at <= (steps - 1) >> shift; ++at)
+                    if (value_of(s_most[at][tid]) >= key_value(least) || least == 1) {
+                        const int item = atomicAdd(&s_items, 1);
+                        if (item < kItems) s_item[item] = (uint16_t)(at * kThreads + tid);
                     }
-                    __syncthreads();
-                    whole_owners = s_count > kCandidates;
+            __syncthreads();
+            const int noted_items = s_items, vectors = kUnroll << shift;
+            bool whole_owners = noted_items > kItems;
+            if (!whole_owners) {
+                for (int at = tid; at < noted_items * vectors; at += kThreads) {
+                    const int32_t item = at / vectors, x = s_item[item];
+                    const int32_t i = (x / kThreads * vectors + at - item * vectors) * kThreads + x % kThreads;
+                    if (i < vecs) {
+                        float v[N];
+                        floats_at(i, v);
+                        collect(v, i);
+                    }
                 }
+                __syncthreads();
+                whole_owners = s_count > kCandidates;
             }
             int n = s_count;
             if (whole_owners) {

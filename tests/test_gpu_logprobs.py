@@ -320,3 +320,19 @@ def test_near_certain_tokens(dtype, rows, V, lead):
             assert abs(float(got) - want) <= rel * abs(want) + 1e-38, (r, float(got), want)
         want = s / (1 + s)
         assert abs(float(dx[r, t[r]]) - want) <= (rel + H.rounding(dtype)) * want + 1e-38, (r, float(dx[r, t[r]]), want)
+
+
+@pytest.mark.parametrize("rows,V,dtype", [(770, 151936, F32), (770, 300007, BF16), (2, 5000011, BF16)])
+@pytest.mark.parametrize("top", [1, 20, 64])
+def test_alternatives_of_long_rows(rows, V, dtype, top):
+    """Rows of more steps than a thread keeps notes of: notes of several steps each."""
+    print(f"long rows={rows} V={V} top={top} {dtype}", flush=True)
+    g = torch.Generator(device="cuda").manual_seed(top)
+    x = torch.randn(rows, V, generator=g, device="cuda").to(dtype)
+    t = torch.randint(0, V, (rows,))
+    o = score(x, t, top=top)
+    for r in range(0, rows, 97):
+        # ties by the lowest token: a stable sort
+        order = torch.sort(x[r].double(), descending=True, stable=True).indices[:top]
+        assert torch.equal(o["top_ids"][r], order), r
+    check(x[:2], t[:2], {k: y[:2] for k, y in o.items()}, top=top)
