@@ -21,10 +21,9 @@
 // the vector units issuing in 79 % of cycles; the loop without its arithmetic takes
 // 182.  The gradient of 2,000 rows of 50,257: 60 us, 6.7 TB/s read and written.
 //
-// Split.  A row is one workgroup's where there are rows for the GPU (five a CU);
-// few rows are cut into slices, joined by a second launch in slice order: one row
-// of 151,936 with 20 alternatives in 16 us, 10 and 6, latencies of a dozen
-// trips to memory and barriers.
+// Split.  A row is one workgroup's, five to a CU; where there are few long ones, they are
+// cut into slices, joined by a second launch in slice order: one row of 151,936
+// with 20 alternatives in 15 us, latencies of a dozen trips to memory and barriers.
 //
 // Alternatives.  Order: value descending, then token ascending, as one 64-bit key,
 // so no two are equal and the result does not depend on who writes first.  A
@@ -615,6 +614,7 @@ __global__ __launch_bounds__(kThreads) void k_logprobs_join(LogprobArgs a)
 // --------------------------------------------------------------- gradient --
 constexpr int64_t kMaxGrid = 1 << 20;     // workgroups per launch; larger jobs loop
 constexpr double kCacheBytes = 256 << 20; // the last-level cache
+constexpr int64_t kSliceBytes = kUnroll * kThreads * 16;      // one step of all threads
 
 template <typename T> __device__ __forceinline__ V4u pack(const float* x);
 template <> __device__ __forceinline__ V4u pack<float>(const float* x)
@@ -736,14 +736,17 @@ hipError_t backward_t(const LogprobGradArgs& a, hipStream_t s)
 
 }  // namespace
 
-// Slices of a row: none where the rows alone fill the GPU, otherwise enough for
-// six workgroups a CU, of at least a thread's vector each.
+// Slices of a row.  A second launch and its join cost 4 to 6 us, so only long rows
+// that leave CUs idle are cut, into two workgroups a CU at most and not below a
+// step of all threads: 100 rows of 151,936 12 us (17 whole, 17 in six workgroups a CU),
+// one row 8 (20 whole); 200 rows of 50,257 9.5 whole and 12.5 in two, 48 of 32,768 6.3 and 9.
 int logprob_slices(int32_t rows, int32_t vocab, int dtype, int32_t* per_slice)
 {
     const int n = dtype == 0 ? Vec<uint16_t>::n : Vec<float>::n;
+    const int64_t bytes = (int64_t)vocab * 16 / n;
     int64_t slices = 1;
-    if (rows > 0 && rows < 768)
-        slices = std::min<int64_t>(std::min<int64_t>(kMaxSlices, (1536 + rows - 1) / rows), std::max(1, vocab / (kThreads * n)));
+    if (rows > 0 && rows <= 256 && bytes >= 8 * kSliceBytes)
+        slices = std::min<int64_t>(std::min<int64_t>(kMaxSlices, 512 / rows), bytes / kSliceBytes);
     const int64_t per = ((vocab + slices - 1) / slices + n - 1) / n * n;
     *per_slice = (int32_t)std::min<int64_t>(per, INT32_MAX / n * n);
     return (int)((vocab + per - 1) / per);

@@ -336,3 +336,49 @@ def test_alternatives_of_long_rows(rows, V, dtype, top):
         order = torch.sort(x[r].double(), descending=True, stable=True).indices[:top]
         assert torch.equal(o["top_ids"][r], order), r
     check(x[:2], t[:2], {k: y[:2] for k, y in o.items()}, top=top)
+
+
+@pytest.mark.parametrize("rows", [1, 3, 40, 200, 256, 257])
+@pytest.mark.parametrize("V,dtype", [(65535, BF16), (65536, BF16), (140001, BF16), (32767, F32), (32768, F32), (70001, F32)])
+def test_sliced_rows(rows, V, dtype):
+    """Row counts and lengths on either side of the rule that cuts rows into slices."""
+    print(f"sliced rows={rows} V={V} {dtype}", flush=True)
+    x, t = logits(rows, V, dtype, rows + V)
+    x = x.cuda()
+    for top in (0, 7, 64):
+        o = score(x, t, top=top, scale=0.9)
+        pick = sorted({0, rows // 2, rows - 1})
+        check(x[pick], t[pick], {k: v[pick] for k, v in o.items()}, scale=0.9, top=top)
+
+
+@pytest.mark.parametrize("kind", ["equal", "descending", "one_slice", "few_values", "masked_but_few", "masked", "lowest", "nan", "inf"])
+def test_awkward_sliced_rows(kind):
+    """Ties across slices, slices of nothing but -inf, one slice that holds every large logit, broken ones."""
+    V, top, rows = 140003, 33, 3
+    print(f"awkward slices {kind}", flush=True)
+    v = torch.arange(V)
+    x = (v * 7919 % 101) / 16.0
+    if kind == "equal":
+        x = torch.full((V,), -2.5)
+    elif kind == "descending":
+        x = -v / 1000.0
+    elif kind == "one_slice":
+        x = torch.where((v > 100000) & (v < 100400), 20 + (v % 7) / 8.0, x)
+    elif kind == "few_values":
+        x = (v * 7919 % 2).float()
+    elif kind == "masked_but_few":
+        x = torch.where(v % 14000 == 9, x, torch.tensor(-math.inf))
+    elif kind == "masked":
+        x = torch.full((V,), -math.inf)
+    elif kind == "lowest":
+        x = torch.full((V,), torch.finfo(BF16).min)
+        x[77777] = 1.0
+    elif kind in ("nan", "inf"):
+        x[V - 2] = float(kind)
+    x = x.to(BF16)[None].repeat(rows, 1).contiguous().cuda()
+    t = torch.tensor([77777, 0, V - 1])
+    o = score(x, t, top=top)
+    if kind in ("nan", "inf"):
+        assert all(bool(torch.isnan(o[n]).all()) for n in ("logp", "entropy", "lse", "top_logp")) and bool((o["top_ids"] == -1).all())
+        return
+    check(x, t, o, top=top)
