@@ -21,8 +21,8 @@
 // the vector units issuing in 79 % of cycles; the loop without its arithmetic takes
 // 182.  The gradient of 2,000 rows of 50,257: 60 us, 6.7 TB/s read and written.
 //
-// Split.  A row is one workgroup's, five to a CU; where there are few long ones, they are
-// cut into slices, joined by a second launch in slice order: one row of 151,936
+// Split.  A row is one workgroup's, of 64 to 256 threads by its length, twenty waves to a
+// CU; where there are few long ones, they are cut into slices, joined by a second launch in slice order: one row of 151,936
 // with 20 alternatives in 15 us, latencies of a dozen trips to memory and barriers.
 //
 // Alternatives.  Order: value descending, then token ascending, as one 64-bit key,
@@ -171,12 +171,12 @@ __device__ __forceinline__ void pad(Key* keys, int n)
 // The k largest of the n keys in LDS, descending, into best (0 where there are
 // fewer): each key's place is the number of larger ones.  All threads; the keys
 // are distinct.
-__device__ void largest(Key* keys, int n, int k, Key* best)
+template <int K> __device__ void largest(Key* keys, int n, int k, Key* best)
 {
-    for (int i = threadIdx.x; i < k; i += kThreads) best[i] = 0;
+    for (int i = threadIdx.x; i < k; i += K) best[i] = 0;
     pad(keys, n);
     __syncthreads();
-    for (int i = threadIdx.x; i < n; i += kThreads) {
+    for (int i = threadIdx.x; i < n; i += K) {
         const Key x = keys[i];
         const int place = larger(keys, n, x);
         if (place < k) best[place] = x;
@@ -267,9 +267,9 @@ __device__ __forceinline__ uint16_t bf16_above(float x)
 // the key of this thread's maximum (0: no logits).  Each wave ranks its own lanes;
 // the least of the waves' (top / waves)-th keys is reached by `top` of them.  All
 // threads.
-__device__ int bound_by_waves(Key low, Key high, int top, Key* s_wave, int32_t* s_owner, int32_t* s_owners, Key* least)
+template <int K> __device__ int bound_by_waves(Key low, Key high, int top, Key* s_wave, int32_t* s_owner, int32_t* s_owners, Key* least)
 {
-    constexpr int kWaves = kThreads / 64;
+    constexpr int kWaves = K / 64;
     const int each = (top + kWaves - 1) / kWaves;
     int place = 0;
 #pragma unroll 8
@@ -293,12 +293,12 @@ __device__ int bound_by_waves(Key low, Key high, int top, Key* s_wave, int32_t* 
 }
 
 // The same exactly, from the exact keys of all threads' maxima: `top` owners, or all.
-__device__ int bound_exactly(Key key, int top, Key* s_keys, int32_t* s_owner, int32_t* s_owners, Key* least)
+template <int K> __device__ int bound_exactly(Key key, int top, Key* s_keys, int32_t* s_owner, int32_t* s_owners, Key* least)
 {
     s_keys[threadIdx.x] = key;
     if (threadIdx.x == 0) *s_owners = 0;
     __syncthreads();
-    const int place = larger(s_keys, kThreads, key);
+    const int place = larger(s_keys, K, key);
     const bool mine = key && place < top;
     if (mine) s_owner[place] = threadIdx.x;
     if (mine) atomicAdd(s_owners, 1);
@@ -311,14 +311,14 @@ __device__ int bound_exactly(Key key, int top, Key* s_keys, int32_t* s_owner, in
 
 // One slice of one row.  NT: the logits exceed the last-level cache, and are read
 // past the caches (622 million of bf16: 233 -> 206 us with 5 alternatives).
-template <typename T, bool NT>
-__global__ __launch_bounds__(kThreads, 5) void k_logprobs(LogprobArgs a)
+template <typename T, bool NT, int K>
+__global__ __launch_bounds__(K, K == 64 ? 3 : 5) void k_logprobs(LogprobArgs a)
 {
     constexpr int N = Vec<T>::n;
-    __shared__ Sums s_sums[kThreads / 64];
-    __shared__ Key s_keys[kCandidates], s_best[kMaxTop], s_wave[kThreads / 64];
-    __shared__ int32_t s_owner[kThreads], s_count, s_owners, s_items;
-    __shared__ uint16_t s_most[kNoted][kThreads], s_item[kItems];
+    __shared__ Sums s_sums[K / 64];
+    __shared__ Key s_keys[kCandidates], s_best[kMaxTop], s_wave[K / 64];
+    __shared__ int32_t s_owner[K], s_count, s_owners, s_items;
+    __shared__ uint16_t s_most[kNoted][K], s_item[kItems];
     const int tid = threadIdx.x;
     for (int64_t job = blockIdx.x; job < (int64_t)a.rows * a.slices; job += gridDim.x) {
         const int64_t row = job / a.slices;
@@ -326,9 +326,9 @@ __global__ __launch_bounds__(kThreads, 5) void k_logprobs(LogprobArgs a)
         const int64_t begin = (int64_t)slice * a.per_slice;
         const int32_t len = (int32_t)min((int64_t)a.per_slice, a.vocab - begin);
         const T* const x0 = static_cast<const T*>(a.x) + row * a.stride + begin;
-        const int32_t full = len / N, vecs = (len + N - 1) / N, steps = (vecs + kUnroll * kThreads - 1) / (kUnroll * kThreads);
+        const int32_t full = len / N, vecs = (len + N - 1) / N, steps = (vecs + kUnroll * K - 1) / (kUnroll * K);
 
-        const int32_t whole = full / (kUnroll * kThreads);
+        const int32_t whole = full / (kUnroll * K);
 
         // Vector i as floats; -inf behind the slice's end.
         auto floats_at = [&](int32_t i, float* x) {
@@ -360,7 +360,7 @@ __global__ __launch_bounds__(kThreads, 5) void k_logprobs(LogprobArgs a)
 #pragma unroll
             for (int u = 0; u < kUnroll; ++u) {
                 const V4uAnywhere* const q =
-                    reinterpret_cast<const V4uAnywhere*>(x0 + (int64_t)((step * kUnroll + u) * kThreads + tid) * N);
+                    reinterpret_cast<const V4uAnywhere*>(x0 + (int64_t)((step * kUnroll + u) * K + tid) * N);
                 w[u] = NT ? __builtin_nontemporal_load(q) : *q;
             }
         };
@@ -375,12 +375,12 @@ __global__ __launch_bounds__(kThreads, 5) void k_logprobs(LogprobArgs a)
         }
         if (whole < steps) {
             float all = -__builtin_inff();
-            int32_t i = whole * kUnroll * kThreads + tid;
+            int32_t i = whole * kUnroll * K + tid;
 #pragma unroll
             for (int u = 0; u < kUnroll; ++u)
-                if (i + u * kThreads < full) w[u] = *reinterpret_cast<const V4uAnywhere*>(x0 + (int64_t)(i + u * kThreads) * N);
+                if (i + u * K < full) w[u] = *reinterpret_cast<const V4uAnywhere*>(x0 + (int64_t)(i + u * K) * N);
 #pragma unroll 1
-            for (int u = 0; u < kUnroll; ++u, i += kThreads) {
+            for (int u = 0; u < kUnroll; ++u, i += K) {
                 float x[N];
                 if (i < full)
                     unpack<T>(w[0], x);
@@ -404,12 +404,12 @@ __global__ __launch_bounds__(kThreads, 5) void k_logprobs(LogprobArgs a)
             __syncthreads();
             t = s_sums[0];
 #pragma unroll
-            for (int v = 1; v < kThreads / 64; ++v) t = join(t, s_sums[v], a.c);
+            for (int v = 1; v < K / 64; ++v) t = join(t, s_sums[v], a.c);
             return t;
         };
         if (tid == 0) {
             s_count = s_items = 0;
-            s_owner[0] = kThreads;
+            s_owner[0] = K;
         }
         Sums t = joined();
         if (t.s < kDominated && t.m > -__builtin_inff()) {
@@ -420,7 +420,7 @@ __global__ __launch_bounds__(kThreads, 5) void k_logprobs(LogprobArgs a)
             const int32_t owner = s_owner[0];
             if (tid == owner) mine.s = mine.u = 0.f;
             Sums own = {t.m, 0.f, 0.f};
-            for (int32_t i = tid * kThreads + owner; i < vecs; i += kThreads * kThreads) {
+            for (int32_t i = tid * K + owner; i < vecs; i += K * K) {
                 float x[N];
                 floats_at(i, x);
 #pragma unroll
@@ -448,7 +448,7 @@ __global__ __launch_bounds__(kThreads, 5) void k_logprobs(LogprobArgs a)
             __syncthreads();
             t.s = t.u = 0.f;
 #pragma unroll
-            for (int v = 0; v < kThreads / 64; ++v) {
+            for (int v = 0; v < K / 64; ++v) {
                 t.s += s_sums[v].s;
                 t.u += s_sums[v].u;
             }
@@ -461,28 +461,28 @@ __global__ __launch_bounds__(kThreads, 5) void k_logprobs(LogprobArgs a)
             a.parts[job] = float4{t.m, t.s, t.u, 0.f};
 
         if (a.top > 0) {
-            const int32_t first = met * kUnroll * kThreads + tid;             // vectors of the step
+            const int32_t first = met * kUnroll * K + tid;             // vectors of the step
             auto token = [&](int32_t i, int j) { return (uint32_t)(begin + (int64_t)i * N + j); };
             Key low = 0, high = 0, least;
             if (tid < vecs) {
-                low = key_of(run.m, token(first + (kUnroll - 1) * kThreads, N - 1));
+                low = key_of(run.m, token(first + (kUnroll - 1) * K, N - 1));
                 high = key_of(run.m, token(first, 0));
             }
-            int owners = bound_by_waves(low, high, a.top, s_wave, s_owner, &s_owners, &least);
+            int owners = bound_by_waves<K>(low, high, a.top, s_wave, s_owner, &s_owners, &least);
             if (owners > kManyOwners) {
                 // many maxima tie: find where each was met
                 Key exact = 0;
                 if (tid < vecs)
                     for (int u = kUnroll - 1; u >= 0; --u) {
                         float x[N];
-                        floats_at(first + u * kThreads, x);
+                        floats_at(first + u * K, x);
 #pragma unroll
                         for (int j = N - 1; j >= 0; --j)
-                            if (x[j] == run.m && (first + u * kThreads) * N + j < len)
-                                exact = key_of(run.m, token(first + u * kThreads, j));
+                            if (x[j] == run.m && (first + u * K) * N + j < len)
+                                exact = key_of(run.m, token(first + u * K, j));
                     }
                 __syncthreads();
-                owners = bound_exactly(exact, a.top, s_keys, s_owner, &s_owners, &least);
+                owners = bound_exactly<K>(exact, a.top, s_keys, s_owner, &s_owners, &least);
             }
             // the owners' logits from the bound on
             auto collect = [&](const float* x, int32_t i) {
@@ -500,15 +500,15 @@ __global__ __launch_bounds__(kThreads, 5) void k_logprobs(LogprobArgs a)
                 for (int32_t at = 0; at <= (steps - 1) >> shift; ++at)
                     if (value_of(s_most[at][tid]) >= key_value(least) || least == 1) {
                         const int item = atomicAdd(&s_items, 1);
-                        if (item < kItems) s_item[item] = (uint16_t)(at * kThreads + tid);
+                        if (item < kItems) s_item[item] = (uint16_t)(at * K + tid);
                     }
             __syncthreads();
             const int noted_items = s_items, vectors = kUnroll << shift;
             bool whole_owners = noted_items > kItems;
             if (!whole_owners) {
-                for (int at = tid; at < noted_items * vectors; at += kThreads) {
+                for (int at = tid; at < noted_items * vectors; at += K) {
                     const int32_t item = at / vectors, x = s_item[item];
-                    const int32_t i = (x / kThreads * vectors + at - item * vectors) * kThreads + x % kThreads;
+                    const int32_t i = (x / K * vectors + at - item * vectors) * K + x % K;
                     if (i < vecs) {
                         float v[N];
                         floats_at(i, v);
@@ -529,7 +529,7 @@ __global__ __launch_bounds__(kThreads, 5) void k_logprobs(LogprobArgs a)
                     const int had = s_count;
                     __syncthreads();      // read by all before any candidate is added
                     if (had > kCandidates - 8 * kRound) {
-                        largest(s_keys, had, a.top, s_best);
+                        largest<K>(s_keys, had, a.top, s_best);
                         if (tid < a.top) s_keys[tid] = s_best[tid];
                         if (tid == 0) s_count = a.top;
                         least = s_best[a.top - 1];
@@ -537,7 +537,7 @@ __global__ __launch_bounds__(kThreads, 5) void k_logprobs(LogprobArgs a)
                     }
                     const int32_t item = item0 + tid, o = item / per;
                     if (tid < kRound && item < items) {
-                        const int32_t i = (item - o * per) * kThreads + s_owner[o];
+                        const int32_t i = (item - o * per) * K + s_owner[o];
                         if (i < vecs) {
                             float x[N];
                             floats_at(i, x);
@@ -548,7 +548,7 @@ __global__ __launch_bounds__(kThreads, 5) void k_logprobs(LogprobArgs a)
                 }
                 n = s_count;
             }
-            largest(s_keys, n, a.top, s_best);
+            largest<K>(s_keys, n, a.top, s_best);
             if (tid < a.top) {
                 if (a.slices == 1)
                     write_top(a, row, tid, s_best[tid], t.m, logsum, broken);
@@ -607,7 +607,7 @@ __global__ __launch_bounds__(kThreads) void k_logprobs_join(LogprobArgs a)
     for (int i = tid; i < a.slices * a.top; i += kThreads)
         if (s_all[i] >= least) s_keys[atomicAdd(&s_count, 1)] = s_all[i];
     __syncthreads();
-    largest(s_keys, s_count, a.top, s_best);
+    largest<kThreads>(s_keys, s_count, a.top, s_best);
     if (tid < a.top) write_top(a, row, tid, s_best[tid], t.m, logsum, broken);
 }
 
@@ -698,15 +698,33 @@ __global__ __launch_bounds__(kThreads) void k_logprobs_backward(LogprobGradArgs 
     }
 }
 
+template <typename T, int K>
+void logprobs_as(const LogprobArgs& a, hipStream_t s)
+{
+    const dim3 grid((unsigned)std::min((int64_t)a.rows * a.slices, kMaxGrid)), block(K);
+    if ((double)a.rows * a.vocab * sizeof(T) > kCacheBytes)
+        hipLaunchKernelGGL((k_logprobs<T, true, K>), grid, block, 0, s, a);
+    else
+        hipLaunchKernelGGL((k_logprobs<T, false, K>), grid, block, 0, s, a);
+}
+
+// Threads of a row (or slice): enough for a few vectors each, fewer where many short
+// rows can share a CU (8,192 rows of 1,000 with 20 alternatives: 113 us by 256
+// threads, 45 by 128, 34 by 64; of 16,000: 93, 71, 71; 4,096 of 32,768: 61, 61, 68).
+int logprob_threads(int64_t jobs, int64_t bytes)
+{
+    const int64_t short_row = jobs > 512 ? 16 << 10 : 4 << 10, middle = 3 * short_row;
+    return bytes <= short_row ? 64 : bytes <= middle ? 128 : 256;
+}
+
 template <typename T>
 hipError_t logprobs_t(const LogprobArgs& a, hipStream_t s)
 {
-    const int64_t jobs = (int64_t)a.rows * a.slices;
-    const dim3 grid((unsigned)std::min(jobs, kMaxGrid)), block(kThreads);
-    if ((double)a.rows * a.vocab * sizeof(T) > kCacheBytes)
-        hipLaunchKernelGGL((k_logprobs<T, true>), grid, block, 0, s, a);
-    else
-        hipLaunchKernelGGL((k_logprobs<T, false>), grid, block, 0, s, a);
+    switch (logprob_threads((int64_t)a.rows * a.slices, (int64_t)a.per_slice * sizeof(T))) {
+    case 64: logprobs_as<T, 64>(a, s); break;
+    case 128: logprobs_as<T, 128>(a, s); break;
+    default: logprobs_as<T, 256>(a, s); break;
+    }
     hipError_t e = hipGetLastError();
     if (e != hipSuccess || a.slices == 1) return e;
     hipLaunchKernelGGL(k_logprobs_join<T>, dim3((unsigned)a.rows), dim3(kThreads), 0, s, a);

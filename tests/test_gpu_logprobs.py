@@ -382,3 +382,21 @@ def test_awkward_sliced_rows(kind):
         assert all(bool(torch.isnan(o[n]).all()) for n in ("logp", "entropy", "lse", "top_logp")) and bool((o["top_ids"] == -1).all())
         return
     check(x, t, o, top=top)
+
+
+@pytest.mark.parametrize("rows", [5, 512, 513, 1100])
+@pytest.mark.parametrize("V,dtype", [(60, BF16), (300, BF16), (2048, BF16), (2049, BF16), (6144, BF16), (6145, BF16), (8192, BF16),
+                                     (8193, BF16), (24577, BF16), (1024, F32), (4097, F32), (12289, F32)])
+def test_short_rows(rows, V, dtype):
+    """Row lengths and counts on either side of the rule that picks a row's threads, ties among them."""
+    print(f"short rows={rows} V={V} {dtype}", flush=True)
+    x, t = logits(rows, V, dtype, rows + V)
+    x[1] = (x[1].float() * 2).round().to(dtype) / 2          # few values
+    x[2, 7:] = -math.inf
+    t[2] = 3
+    x[3] = 0.5
+    x = x.cuda()
+    for top in (0, 9, 64):
+        o = score(x, t, top=top)
+        pick = [0, 1, 2, 3, rows - 1]
+        check(x[pick], t[pick], {k: v[pick] for k, v in o.items()}, top=top)
