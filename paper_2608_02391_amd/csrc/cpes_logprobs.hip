@@ -21,9 +21,10 @@
 // the vector units issuing in 79 % of cycles; the loop without its arithmetic takes
 // 182.  The gradient of 2,000 rows of 50,257: 60 us, 6.7 TB/s read and written.
 //
-// Split.  A row is one workgroup's, of 64 to 256 threads by its length, twenty waves to a
-// CU; where there are few long ones, they are cut into slices, joined by a second launch in slice order: one row of 151,936
-// with 20 alternatives in 15 us, latencies of a dozen trips to memory and barriers.
+// Split.  A row is one workgroup's, of 64 to 256 threads by length and number of rows;
+// where there are few long ones, they are cut into slices, joined by a second launch
+// in slice order: one row of 151,936 with 20 alternatives in 15 us, latencies of a
+// dozen trips to memory and barriers.
 //
 // Alternatives.  Order: value descending, then token ascending, as one 64-bit key,
 // so no two are equal and the result does not depend on who writes first.  A
@@ -188,8 +189,11 @@ constexpr int kUnroll = 4;                // 16-byte loads of a thread and step
 constexpr int kMaxTop = 64;
 constexpr int kNoted = 32;                // maxima a thread notes: of a step each, or of 2, 4, .. steps of longer rows
 constexpr int kItems = 512;               // of them whose steps are looked at again
-constexpr int kRound = 64;                // threads that look at a vector each while candidates may have to be thinned out
-constexpr int kCandidates = 768;          // a key's room; kRound threads can add 8 each to 256
+// Threads that look at a vector each while candidates may have to be thinned out, and
+// candidates' room: they can add 8 each to 256.  64 threads have less, so that sixteen
+// such workgroups fit a CU.
+template <int K> constexpr int kRound = K == 64 ? 32 : 64;
+template <int K> constexpr int kCandidates = 256 + 8 * kRound<K>;
 constexpr int kManyOwners = 3 * kMaxTop / 2;
 constexpr float kHuge = 1e30f;
 constexpr float kDominated = 1.f / 16;    // sum of the other logits' terms below which the largest one's thread is looked at again
@@ -316,7 +320,7 @@ __global__ __launch_bounds__(K, K == 64 ? 3 : 5) void k_logprobs(LogprobArgs a)
 {
     constexpr int N = Vec<T>::n;
     __shared__ Sums s_sums[K / 64];
-    __shared__ Key s_keys[kCandidates], s_best[kMaxTop], s_wave[K / 64];
+    __shared__ Key s_keys[kCandidates<K>], s_best[kMaxTop], s_wave[K / 64];
     __shared__ int32_t s_owner[K], s_count, s_owners, s_items;
     __shared__ uint16_t s_most[kNoted][K], s_item[kItems];
     const int tid = threadIdx.x;
@@ -491,7 +495,7 @@ __global__ __launch_bounds__(K, K == 64 ? 3 : 5) void k_logprobs(LogprobArgs a)
                     const Key k = key_of(x[j], token(i, j));
                     if (k >= least && i * N + j < len) {
                         const int at = atomicAdd(&s_count, 1);
-                        if (at < kCandidates) s_keys[at] = k;
+                        if (at < kCandidates<K>) s_keys[at] = k;
                     }
                 }
             };
@@ -516,7 +520,7 @@ __global__ __launch_bounds__(K, K == 64 ? 3 : 5) void k_logprobs(LogprobArgs a)
                     }
                 }
                 __syncthreads();
-                whole_owners = s_count > kCandidates;
+                whole_owners = s_count > kCandidates<K>;
             }
             int n = s_count;
             if (whole_owners) {
@@ -525,10 +529,10 @@ __global__ __launch_bounds__(K, K == 64 ? 3 : 5) void k_logprobs(LogprobArgs a)
                 if (tid == 0) s_count = 0;
                 __syncthreads();
                 const int32_t per = steps * kUnroll, items = owners * per;
-                for (int32_t item0 = 0; item0 < items; item0 += kRound) {
+                for (int32_t item0 = 0; item0 < items; item0 += kRound<K>) {
                     const int had = s_count;
                     __syncthreads();      // read by all before any candidate is added
-                    if (had > kCandidates - 8 * kRound) {
+                    if (had > kCandidates<K> - 8 * kRound<K>) {
                         largest<K>(s_keys, had, a.top, s_best);
                         if (tid < a.top) s_keys[tid] = s_best[tid];
                         if (tid == 0) s_count = a.top;
@@ -536,7 +540,7 @@ __global__ __launch_bounds__(K, K == 64 ? 3 : 5) void k_logprobs(LogprobArgs a)
                         __syncthreads();
                     }
                     const int32_t item = item0 + tid, o = item / per;
-                    if (tid < kRound && item < items) {
+                    if (tid < kRound<K> && item < items) {
                         const int32_t i = (item - o * per) * K + s_owner[o];
                         if (i < vecs) {
                             float x[N];
@@ -708,19 +712,37 @@ void logprobs_as(const LogprobArgs& a, hipStream_t s)
         hipLaunchKernelGGL((k_logprobs<T, false, K>), grid, block, 0, s, a);
 }
 
-// Threads of a row (or slice): enough for a few vectors each, fewer where many short
-// rows can share a CU (8,192 rows of 1,000 with 20 alternatives: 113 us by 256
-// threads, 45 by 128, 34 by 64; of 16,000: 93, 71, 71; 4,096 of 32,768: 61, 61, 68).
-int logprob_threads(int64_t jobs, int64_t bytes)
+// Threads of a row (or slice).  Few rows: as many as have a few vectors each.  Many: so
+// few that all rows run at once, sixteen to a CU by 64 threads, while a row is not so
+// long that a CU needs more waves on its way.  us by 64, 128, 256 threads, 20 alternatives:
+//   8,192 rows of 1,000       28    46   114      2,000 rows of 50,257     45    50    53
+//   8,192 rows of 32,768     106   117   124      4,000 rows of 100,000   143   161   153
+//   1,000 rows of 50,257      31    29    33      1,300 rows of 151,936    97    89    83
+//     300 rows of 12,000      14    13    14      5,000 rows of 100,000   195   192   184
+// For many alternatives 64 maxima bound too little (64 of 2,000 rows of 12,000: 112, 29, 38).
+int logprob_threads(int64_t jobs, int64_t bytes, int top)
 {
-    const int64_t short_row = jobs > 512 ? 16 << 10 : 4 << 10, middle = 3 * short_row;
-    return bytes <= short_row ? 64 : bytes <= middle ? 128 : 256;
+    constexpr int64_t kCUs = 256;
+    int64_t by64 = 64 << 10, by128 = by64;               // the longest
+    if (jobs <= 2 * kCUs)
+        by64 = 4 << 10, by128 = 12 << 10;
+    else if (jobs <= 3 * kCUs)
+        by64 = 16 << 10, by128 = 48 << 10;
+    else if (jobs < 6 * kCUs)
+        by64 = 16 << 10, by128 = 200 << 10;
+    else if (jobs <= 16 * kCUs)
+        by64 = by128 = 200 << 10;
+    if (top > 40) {
+        by64 = 1 << 10;
+        by128 = std::min<int64_t>(by128, 64 << 10);
+    }
+    return bytes <= by64 ? 64 : bytes <= by128 ? 128 : 256;
 }
 
 template <typename T>
 hipError_t logprobs_t(const LogprobArgs& a, hipStream_t s)
 {
-    switch (logprob_threads((int64_t)a.rows * a.slices, (int64_t)a.per_slice * sizeof(T))) {
+    switch (logprob_threads((int64_t)a.rows * a.slices, (int64_t)a.per_slice * sizeof(T), a.top)) {
     case 64: logprobs_as<T, 64>(a, s); break;
     case 128: logprobs_as<T, 128>(a, s); break;
     default: logprobs_as<T, 256>(a, s); break;

@@ -400,3 +400,23 @@ def test_short_rows(rows, V, dtype):
         o = score(x, t, top=top)
         pick = [0, 1, 2, 3, rows - 1]
         check(x[pick], t[pick], {k: v[pick] for k, v in o.items()}, top=top)
+
+
+@pytest.mark.parametrize("rows,V,dtype", [(768, 24576, BF16), (769, 24577, BF16), (769, 102400, BF16), (1535, 102401, BF16),
+                                          (1535, 8193, BF16), (1536, 8193, BF16), (1536, 102400, BF16), (4096, 102401, BF16),
+                                          (4096, 32769, BF16), (4097, 32769, BF16), (4097, 32768, BF16), (1700, 51200, F32)])
+def test_many_rows(rows, V, dtype):
+    """Row counts and lengths on either side of the rule that picks a row's threads, and numbers of alternatives
+    on either side of its limit."""
+    print(f"many rows={rows} V={V} {dtype}", flush=True)
+    gen = torch.Generator(device="cuda").manual_seed(rows + V)
+    x = torch.empty(rows, V, dtype=dtype, device="cuda").normal_(0.0, 2.5, generator=gen)
+    t = torch.randint(0, V, (rows,), generator=torch.Generator().manual_seed(rows))
+    x[1] = x[1].mul(2).round() / 2                           # few values
+    x[2, 7:] = -math.inf
+    t[2] = 3
+    x[3] = 0.5
+    pick = [0, 1, 2, 3, rows // 2, rows - 1]
+    for top in (0, 40, 41, 64):
+        o = score(x, t, top=top)
+        check(x[pick], t[pick], {k: v[pick] for k, v in o.items()}, top=top)
