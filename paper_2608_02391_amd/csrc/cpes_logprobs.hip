@@ -712,30 +712,28 @@ void logprobs_as(const LogprobArgs& a, hipStream_t s)
         hipLaunchKernelGGL((k_logprobs<T, false, K>), grid, block, 0, s, a);
 }
 
-// Threads of a row (or slice).  Few rows: as many as have a few vectors each.  Many: so
-// few that all rows run at once, sixteen to a CU by 64 threads, while a row is not so
-// long that a CU needs more waves on its way.  us by 64, 128, 256 threads, 20 alternatives:
-//   8,192 rows of 1,000       28    46   114      2,000 rows of 50,257     45    50    53
-//   8,192 rows of 32,768     106   117   124      4,000 rows of 100,000   143   161   153
-//   1,000 rows of 50,257      31    29    33      1,300 rows of 151,936    97    89    83
-//     300 rows of 12,000      14    13    14      5,000 rows of 100,000   195   192   184
-// For many alternatives 64 maxima bound too little (64 of 2,000 rows of 12,000: 112, 29, 38).
+// Threads of a row (or slice).  Few rows: as many as have a few vectors each.  More: so
+// few that they all run at once, sixteen to a CU by 64 threads, while their starts
+// and ends count; longer ones only where the logits exceed the last-level cache.  us by
+// 64, 128, 256 threads, 20 alternatives:
+//   8,192 rows of 1,000       28    46   114      8,192 rows of 32,768    106   117   124
+//   2,000 rows of 24,000      27    28    35      4,096 rows of 100,000   144   161   153
+//   1,000 rows of 12,000      17    16    18      5,000 rows of 100,000   195   192   184
+//     300 rows of 12,000      14    13    14      1,300 rows of 151,936    97    89    83
+// (2,000 rows of 50,257, score and gradient in turn: 109, 109, 104.)  For many
+// alternatives 64 maxima bound too little (64 of 2,000 rows of 12,000: 112, 29, 38).
 int logprob_threads(int64_t jobs, int64_t bytes, int top)
 {
     constexpr int64_t kCUs = 256;
-    int64_t by64 = 64 << 10, by128 = by64;               // the longest
+    const bool far = (double)jobs * bytes > kCacheBytes;
+    int64_t by64 = 48 << 10, by128 = 48 << 10;           // the longest
     if (jobs <= 2 * kCUs)
         by64 = 4 << 10, by128 = 12 << 10;
-    else if (jobs <= 3 * kCUs)
-        by64 = 16 << 10, by128 = 48 << 10;
-    else if (jobs < 6 * kCUs)
-        by64 = 16 << 10, by128 = 200 << 10;
-    else if (jobs <= 16 * kCUs)
-        by64 = by128 = 200 << 10;
-    if (top > 40) {
-        by64 = 1 << 10;
-        by128 = std::min<int64_t>(by128, 64 << 10);
-    }
+    else if (jobs <= 4 * kCUs)
+        by64 = 16 << 10;
+    else if (far && jobs >= 6 * kCUs)
+        by64 = jobs <= 16 * kCUs ? 200 << 10 : 64 << 10;
+    if (top > 40) by64 = 1 << 10;
     return bytes <= by64 ? 64 : bytes <= by128 ? 128 : 256;
 }
 

@@ -420,3 +420,23 @@ def test_many_rows(rows, V, dtype):
     for top in (0, 40, 41, 64):
         o = score(x, t, top=top)
         check(x[pick], t[pick], {k: v[pick] for k, v in o.items()}, top=top)
+
+
+@pytest.mark.parametrize("rows,V,dtype", [(1024, 8193, BF16), (1025, 8193, BF16), (1024, 24576, BF16), (1025, 24577, BF16),
+                                          (2621, 51200, BF16), (2622, 51200, BF16), (1400, 100000, BF16), (1025, 300, F32)])
+def test_rows_and_cache(rows, V, dtype):
+    """Row counts on either side of the rule that picks a row's threads where the logits fit the last-level cache, and
+    do not."""
+    print(f"cache rows={rows} V={V} {dtype}", flush=True)
+    gen = torch.Generator(device="cuda").manual_seed(rows + V)
+    x = torch.empty(rows, V, dtype=dtype, device="cuda").normal_(0.0, 2.5, generator=gen)
+    t = torch.randint(0, V, (rows,), generator=torch.Generator().manual_seed(rows))
+    x[1] = x[1].mul(2).round() / 2
+    x[2, 7:] = -math.inf
+    t[2] = 3
+    x[3, 5] = 60.0                                           # a near-certain token
+    t[3] = 5
+    pick = [0, 1, 2, 3, rows // 2, rows - 1]
+    for top in (0, 17, 64):
+        o = score(x, t, top=top)
+        check(x[pick], t[pick], {k: v[pick] for k, v in o.items()}, top=top)
