@@ -143,7 +143,16 @@ __global__ __launch_bounds__(BLOCK) void k_pages_reserve(PoolArgs p, int32_t n, 
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     int32_t r[16];
     load_refs(p, 16 * (int64_t)tid, 1, r);
-    bool bad = false;
+    bool bad = false, claimed = false;
+    // A length that was negative before looks like a claim.  Up to a list entry a
+    // thread each knows what it claimed; of longer lists none is claimed then.
+    if (n > BLOCK) {
+        for (int32_t i = tid; i < n; i += BLOCK) bad |= known(p, seqs[i]) && p.lengths[seqs[i]] < 0;
+        if (__syncthreads_or(bad)) {
+            if (tid == 0 && status) *status = kBadSequence;
+            return;
+        }
+    }
     int32_t seq0 = 0, len0 = 0, old0 = 0;               // of entry tid
     for (int32_t i = tid; i < n; i += BLOCK) {
         const int32_t s = seqs[i], len = new_lengths[i];
@@ -157,6 +166,7 @@ __global__ __launch_bounds__(BLOCK) void k_pages_reserve(PoolArgs p, int32_t n, 
             seq0 = s;
             len0 = len;
             old0 = old & ~kClaim;
+            claimed = old >= 0;
         }
     }
     bad = __syncthreads_or(bad);
@@ -193,7 +203,7 @@ __global__ __launch_bounds__(BLOCK) void k_pages_reserve(PoolArgs p, int32_t n, 
     const bool enough = !bad && want <= p.pages && lowest_free<BLOCK>(p, r, (int32_t)want, list) == (int32_t)want;
     if (!enough) {
         for (int32_t i = tid; i < n; i += BLOCK)
-            if (known(p, seqs[i])) atomicAnd(&p.lengths[seqs[i]], ~kClaim);
+            if (n > BLOCK ? known(p, seqs[i]) : claimed) atomicAnd(&p.lengths[seqs[i]], ~kClaim);
         if (tid == 0 && status) *status = bad ? kBadSequence : kShort;
         return;
     }
@@ -306,7 +316,17 @@ __global__ __launch_bounds__(BLOCK) void k_pages_fork_plan(PoolArgs p, int32_t n
     const int tid = threadIdx.x;
     int32_t r[16];
     load_refs(p, 16 * (int64_t)tid, 1, r);
-    bool bad = false;
+    bool bad = false, claimed = false;
+    if (n > BLOCK) {                      // a length that is the mark already, as there
+        for (int32_t i = tid; i < n; i += BLOCK) bad |= known(p, children[i]) && p.lengths[children[i]] != 0;
+        if (__syncthreads_or(bad)) {
+            if (tid == 0) {
+                ws[0] = 0;
+                if (status) *status = kBadSequence;
+            }
+            return;
+        }
+    }
     int32_t child0 = 0, len0 = 0;         // of entry tid
     for (int32_t i = tid; i < n; i += BLOCK) {
         const int32_t a = parents[i], c = children[i];
@@ -316,10 +336,12 @@ __global__ __launch_bounds__(BLOCK) void k_pages_fork_plan(PoolArgs p, int32_t n
         }
         // a parent that is itself a child of this call is empty, or carries the mark: it counts as empty
         const int32_t len = held_tokens(p, p.lengths[a]);
-        bad |= atomicCAS(&p.lengths[c], 0, kClaim) != 0;
+        const bool mine = atomicCAS(&p.lengths[c], 0, kClaim) == 0;
+        bad |= !mine;
         if (i == tid) {
             child0 = c;
             len0 = len;
+            claimed = mine;
         }
     }
     bad = __syncthreads_or(bad);
@@ -335,7 +357,7 @@ __global__ __launch_bounds__(BLOCK) void k_pages_fork_plan(PoolArgs p, int32_t n
     if (!enough) {
         // only a child that was empty and claimed here carries the mark alone
         for (int32_t i = tid; i < n; i += BLOCK)
-            if (known(p, children[i])) atomicCAS(&p.lengths[children[i]], kClaim, 0);
+            if (n > BLOCK ? known(p, children[i]) : claimed) atomicCAS(&p.lengths[children[i]], kClaim, 0);
         if (tid == 0) {
             ws[0] = 0;
             if (status) *status = bad ? kBadSequence : kShort;

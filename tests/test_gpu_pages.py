@@ -241,3 +241,22 @@ def test_random_life_of_a_larger_pool():
             r.free([int(s) for s in rng.permutation(300)[:int(rng.integers(0, 150))]])
         else:
             r.compact()
+
+
+@pytest.mark.parametrize("n", [1, 5, 300, 1500])
+@pytest.mark.parametrize("length", [-1, -5, -2 ** 31])
+def test_negative_lengths_are_left_alone(n, length):
+    """A sequence whose length is negative is refused, and the call changes nothing."""
+    print(f"negative lengths n={n} {length}", flush=True)
+    r = Rig(2 * n, 4, 64, 16)
+    r.lengths[n // 2] = length
+    before = [x.clone() for x in (r.lengths, r.refs, r.table)]
+    for call in ("reserve", "fork"):
+        r.status.fill_(9)
+        if call == "reserve":
+            cp.cpes_pages_reserve(r.pool, ints(range(n)), ints([1] * n), r.ws, status=r.status)
+        else:
+            cp.cpes_pages_fork(r.cache, r.pool, ints(range(n, 2 * n)), ints(range(n)), r.ws, status=r.status)
+        assert int(r.status) == 2
+        for a, b in zip((r.lengths, r.refs, r.table), before):
+            assert torch.equal(a, b), call
