@@ -57,12 +57,6 @@ typedef V2u V2uAnywhere __attribute__((aligned(2)));
 constexpr int kWaves = kAttendWaves;
 constexpr int kThreads = 64 * kWaves;
 constexpr int kShareTiles = 2;            // tiles of a wave's share at least
-// A workgroup of four waves takes a row where none has more than this many tiles,
-// or four times as many and rows and heads alone fill the GPU (64 rows of 700
-// positions, 8 heads: 42 us in shares, 31 so); of eight waves where none has more
-// than twice as many (one row of 600: 15.4 us in shares, 9.4 so; of 2,000: 15 and 22).
-constexpr int kShortTiles = 16;
-constexpr int64_t kManyJobs = 256;
 constexpr int64_t kMaxGrid = 1 << 20;     // workgroups of the short and the join launch
 constexpr float kLog2e = 1.44269504088896340736f;
 
@@ -544,8 +538,9 @@ __global__ __launch_bounds__(kThreads, DP == 256 ? 1 : 2) void k_attend(AttendAr
     // workgroups, one to each, on as many CUs (one row of 2,000: 13.1 -> 12.3 us).  Token-major
     // pages take the second order too: a workgroup's waves are then a head or two apart at the
     // same positions, whose heads lie side by side in memory (64 rows: 104 -> 98 us; long
-    // rows of head-major pages are 2 % faster in the first).
-    const bool apart = waves <= (int32_t)gridDim.x || a.head_stride < a.token_stride;
+    // rows of head-major pages are 2 % faster in the first), and so do more query heads of a
+    // key-value head than a wave takes, which read the same pages (32 on 1: 38.4 -> 37.3).
+    const bool apart = waves <= (int32_t)gridDim.x || a.head_stride < a.token_stride || a.blocks > 1;
     const int32_t share0 = apart ? blockIdx.x : blockIdx.x * kWaves, step = apart ? gridDim.x : 1;
     const int32_t me = share0 + wave * step;
     if (share0 >= waves) return;
@@ -842,22 +837,44 @@ hipError_t attend_shares(const AttendArgs& a, int64_t jobs, hipStream_t s)
     return hipGetLastError();
 }
 
+// Tiles of the longest row up to which a workgroup takes a row (and head), with few rows
+// and heads, and with so many that they nearly fill the GPU: shares balance any lengths,
+// but cost a search and a second launch, 6 to 8 us.  us by shares and so, 32 heads on 8, rows
+// as long as the table, and where two numbers follow, of 1/30 to all of it:
+//   head_dim  64, bf16:   1 row of 1,200  10.9, 10.4    1 of 1,600  11.4, 12.2    32 of 1,700  24, 21 (17, 15)
+//   head_dim 128, bf16:   1 row of 800    12.3, 12.0    1 of 1,000  11.8, 14.9    32 of 1,200  31, 28 (21, 19)
+//   head_dim 128, fp32:   1 row of 250    12.2, 11.0    1 of 500    13.2, 19.5    32 of 500    35, 27 (23, 21)
+//   head_dim 256, bf16:   1 row of 200    14.8, 12.4    1 of 300    13.3, 15.6    32 of 500    32, 27 (23, 21)
+struct RowTiles {
+    int32_t few, many;
+};
+template <typename T, int DP>
+constexpr RowTiles kRowTiles = DP == 256                          ? RowTiles{8, 16}
+                               : std::is_same<T, uint16_t>::value ? (DP == 64 ? RowTiles{40, 64} : RowTiles{26, 40})
+                                                                  : (DP == 64 ? RowTiles{32, 64} : RowTiles{20, 32});
+constexpr int64_t kManyJobs = 160;
+// Tiles from which on eight waves share a row, where one such workgroup a CU is enough:
+// 1 row of 500 of head_dim 64 6.4 us by four and 6.0 by eight, 32 rows of 800 13.6 and
+// 12.0, but 64 rows of 400 of head_dim 128 20.7 and 23.8.  The widest fp32 pieces take
+// longer to join than they save (250 positions of head_dim 128: 11.0 and 11.8).
+template <typename T, int DP> constexpr int kEightWaves = std::is_same<T, float>::value && DP == 128 ? 16 : 4;
+constexpr int64_t kEightJobs = 256;
+
 template <typename T, int DP, bool kWhole>
 hipError_t attend_as(const AttendArgs& a, hipStream_t s)
 {
     const int64_t jobs = (int64_t)a.rows * a.heads * a.blocks;
     const int64_t most = ((int64_t)a.width * a.page_size + Tile<T>::n - 1) / Tile<T>::n;      // tiles of a row
-    if (jobs <= kMaxGrid && (most <= kShortTiles || (most <= 4 * kShortTiles && jobs >= kManyJobs))) {
-        hipLaunchKernelGGL((k_attend_short<T, DP, kWhole, 4>), dim3((unsigned)jobs), dim3(256), 0, s, a);
-        return hipGetLastError();
-    }
+    if (jobs > kMaxGrid || most > (jobs >= kManyJobs ? kRowTiles<T, DP>.many : kRowTiles<T, DP>.few))
+        return attend_shares<T, DP, kWhole>(a, jobs, s);
     if constexpr (DP <= 128) {            // eight waves of the widest heads would not fit the registers
-        if (jobs <= kMaxGrid && most <= 2 * kShortTiles) {
+        if (most > kEightWaves<T, DP> && jobs <= kEightJobs) {
             hipLaunchKernelGGL((k_attend_short<T, DP, kWhole, 8>), dim3((unsigned)jobs), dim3(512), 0, s, a);
             return hipGetLastError();
         }
     }
-    return attend_shares<T, DP, kWhole>(a, jobs, s);
+    hipLaunchKernelGGL((k_attend_short<T, DP, kWhole, 4>), dim3((unsigned)jobs), dim3(256), 0, s, a);
+    return hipGetLastError();
 }
 
 template <typename T, int DP>

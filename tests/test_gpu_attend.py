@@ -384,3 +384,27 @@ def test_every_launch_of_a_size(rows, longest):
     c = Case(lens, 2, 64, 16, BF16, layers=1, layer=0, width=-(-longest // 16), seed=rows)
     q = c.queries(4)
     c.check(q, *c.run(q))
+
+
+@pytest.mark.parametrize("rows", [3, 79, 80, 128, 129])
+@pytest.mark.parametrize("dim,dtype,few,many", [(64, BF16, 40, 64), (128, BF16, 26, 40), (256, BF16, 8, 16), (64, F32, 32, 64),
+                                                (128, F32, 20, 32), (256, F32, 8, 16)])
+def test_every_launch_of_a_type(dim, dtype, few, many, rows):
+    """Table widths on either side of the rules that give a row to one workgroup, and to four or eight waves of it, for
+    each type and head size, with few, many and more than enough rows."""
+    page, tile = 16, 32 if dtype == BF16 else 16
+    for most in (1, 4, 5, 16, 17, few, few + 1, many, many + 1):
+        longest = most * tile
+        print(f"launch dim={dim} {dtype} rows={rows} longest={longest}", flush=True)
+        lens = [longest if r == rows // 2 else longest - 1 if r == 0 else (13 * r) % min(41, longest) for r in range(rows)]
+        c = Case(lens, 2, dim, page, dtype, layers=1, layer=0, width=longest // page, seed=rows + most)
+        q = c.queries(6)
+        c.check(q, *c.run(q))
+
+
+def test_heads_of_several_waves():
+    """More query heads of a key-value head than a wave takes, over rows in many shares."""
+    print("heads of several waves", flush=True)
+    c = Case([3000, 1, 0, 1777, 900], 1, 64, 16, BF16, layers=1, layer=0, seed=4, width=400)
+    q = c.queries(40)
+    c.check(q, *c.run(q))
