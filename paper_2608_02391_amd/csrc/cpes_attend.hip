@@ -860,11 +860,24 @@ constexpr int64_t kManyJobs = 160;
 template <typename T, int DP> constexpr int kEightWaves = std::is_same<T, float>::value && DP == 128 ? 16 : 4;
 constexpr int64_t kEightJobs = 256;
 
+// Tiles a row has at most: its table's, or its window's and sinks'.  A window begins
+// inside a tile and may end inside another.  us by the table's alone (shares) and so,
+// rows of 4,000 in bf16, 32 heads on 8 of 128, 4 sinks: 1 row, window of 193  11.5, 5.8;
+// 32 rows, 449  19.8, 12.1;  96 rows, 449  45.4, 32.2, and 1,217  87.6, 72.8.
+template <int TILE>
+int64_t most_tiles(const AttendArgs& a)
+{
+    const int64_t table = ((int64_t)a.width * a.page_size + TILE - 1) / TILE;
+    if (a.window == 0) return table;
+    const int64_t window = ((int64_t)a.window + 2 * TILE - 2) / TILE, sinks = ((int64_t)a.sinks + TILE - 1) / TILE;
+    return std::min(table, window + sinks);
+}
+
 template <typename T, int DP, bool kWhole>
 hipError_t attend_as(const AttendArgs& a, hipStream_t s)
 {
     const int64_t jobs = (int64_t)a.rows * a.heads * a.blocks;
-    const int64_t most = ((int64_t)a.width * a.page_size + Tile<T>::n - 1) / Tile<T>::n;      // tiles of a row
+    const int64_t most = most_tiles<Tile<T>::n>(a);
     if (jobs > kMaxGrid || most > (jobs >= kManyJobs ? kRowTiles<T, DP>.many : kRowTiles<T, DP>.few))
         return attend_shares<T, DP, kWhole>(a, jobs, s);
     if constexpr (DP <= 128) {            // eight waves of the widest heads would not fit the registers

@@ -408,3 +408,31 @@ def test_heads_of_several_waves():
     c = Case([3000, 1, 0, 1777, 900], 1, 64, 16, BF16, layers=1, layer=0, seed=4, width=400)
     q = c.queries(40)
     c.check(q, *c.run(q))
+
+
+@pytest.mark.parametrize("dtype,dim,few,many", [(BF16, 64, 40, 64), (BF16, 128, 26, 40), (BF16, 256, 8, 16), (F32, 128, 20, 32)])
+@pytest.mark.parametrize("rows", [8, 81])
+@pytest.mark.parametrize("sinks", [0, 37])
+def test_windows_decide_the_launch_of_wide_tables(dtype, dim, few, many, rows, sinks):
+    """A window's tiles bound a row's, however wide its table: windows on either side of each rule, over rows that are
+    shorter, as long, and begin it anywhere inside a tile."""
+    tile, page = 32 if dtype == BF16 else 16, 16
+    for tiles in (1, 2, 5, few - 1, few, few + 1, many - 1, many, many + 1):
+        window = tiles * tile - tile + 1 + 7 * tiles % tile
+        print(f"window launch dim={dim} {dtype} rows={rows} sinks={sinks} window={window}", flush=True)
+        near = [0, 1, window - 1, window, window + 1, window + sinks, window + tile - 1, window + tile + sinks + 3]
+        lens = [near[r] if r < len(near) else window + 977 if r == 40 else (13 * r) % 61 for r in range(rows)][::-1]
+        c = Case(lens, 2, dim, page, dtype, layers=1, layer=0, width=4000, window=window, sinks=sinks, seed=rows + tiles)
+        q = c.queries(4)
+        c.check(q, *c.run(q))
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32], ids=["bf16", "fp32"])
+@pytest.mark.parametrize("dim,page,window,sinks", [(64, 16, 3000, 37), (128, 5, 1700, 4), (256, 32, 1000, 0), (40, 24, 30, 3000)])
+def test_long_windows_of_wide_tables(dtype, dim, page, window, sinks):
+    """Windows and sinks of more tiles than one workgroup takes: shares that end and begin anywhere."""
+    print(f"long window dim={dim} page={page} window={window} sinks={sinks} {dtype}", flush=True)
+    c = Case([0, 1, 17, 2500, 36, 0, 3040, 777, 33, 5000, 138, 5], 2, dim, page, dtype, width=70000 // page, window=window,
+             sinks=sinks, seed=dim)
+    q = c.queries(6)
+    c.check(q, *c.run(q))
