@@ -603,8 +603,8 @@ CPES_API size_t cpes_logprobs_workspace_bytes(int32_t rows, int32_t vocab, int32
  *   = 0); entries behind the vocabulary's end are -inf and -1.
  * Each logit is read once.  Sums are fp32 within a thread and a workgroup.
  * Logits of -inf have probability 0; a row of nothing but -inf has lse = -inf,
- * entropy 0 and log probabilities -inf.  A NaN or +inf makes the row's numbers
- * NaN and its alternatives -1.
+ * entropy 0 and log probabilities -inf.  A NaN or +inf, whatever stands beside it,
+ * makes the row's numbers NaN and its alternatives -1.
  * Errors: x NULL, rows < 0, vocab < 1, stride < vocab with more than one row,
  *   scale not positive or above FLT_MAX / 2, logp without targets, top outside [0,
  *   CPES_MAX_ALTERNATIVES] or without both outputs -> CPES_ERR_INVALID_ARGUMENT;

@@ -118,7 +118,9 @@ template <typename T> __device__ __forceinline__ float target_logit(const Logpro
     return *valid ? value_of(static_cast<const T*>(a.x)[row * a.stride + v]) : 0.f;
 }
 
-// Writes a finished row's numbers; every thread gets what the alternatives need.
+// Writes a finished row's numbers; every thread gets what the alternatives need.  A
+// row without a finite logit is empty, or broken if a NaN is among its logits: the
+// maximum passes NaNs over, the sum does not.
 __device__ __forceinline__ void finish(const LogprobArgs& a, int64_t row, Sums t, float target, bool valid, float* logsum,
                                        bool* broken)
 {
@@ -128,7 +130,7 @@ __device__ __forceinline__ void finish(const LogprobArgs& a, int64_t row, Sums t
     t.s -= a.excess * t.u;
     *logsum = *broken ? nan : empty ? 0.f : log1pf(t.s);
     if (threadIdx.x != 0) return;
-    if (a.logp) a.logp[row] = !valid ? 0.f : empty ? -__builtin_inff() : a.scale * (target - t.m) - *logsum;
+    if (a.logp) a.logp[row] = !valid ? 0.f : *broken ? nan : empty ? -__builtin_inff() : a.scale * (target - t.m) - *logsum;
     if (a.entropy) a.entropy[row] = *broken ? nan : empty ? 0.f : *logsum - t.u / (1.f + t.s) * kLn2;
     if (a.lse) a.lse[row] = *broken ? nan : a.scale * t.m + *logsum;
     if (a.stats) {
