@@ -648,7 +648,7 @@ __global__ __launch_bounds__(kThreads) void k_logprobs_backward(LogprobGradArgs 
 {
     constexpr int kGradUnroll = kFarLoad ? 4 : 2;
     constexpr int N = Vec<T>::n;
-    const int32_t vecs = (a.vocab + N - 1) / N, full = a.vocab / N;
+    const int32_t full = a.vocab / N, vecs = full + (a.vocab % N != 0);      // any vocabulary the argument holds
     const int64_t chunks = (vecs + kGradUnroll * kThreads - 1) / (kGradUnroll * kThreads);
     for (int64_t job = blockIdx.x; job < (int64_t)a.rows * chunks; job += gridDim.x) {
         const int64_t row = job / chunks;
