@@ -95,8 +95,8 @@ class Rollouts:
         self.page_ws = torch.empty(cp.cpes_pages_workspace_bytes(pages), dtype=torch.uint8, device="cuda")
         self.attend_ws = torch.empty(cp.cpes_attend_workspace_bytes(rows, model.q_heads, model.kv_heads, model.head_dim),
                                      dtype=torch.uint8, device="cuda")
-        self.score_ws = torch.empty(max(cp.cpes_logprobs_workspace_bytes(r, model.vocab, alternatives) for r in range(1, rows + 1)),
-                                    dtype=torch.uint8, device="cuda")
+        self.score_ws = torch.empty(cp.cpes_logprobs_workspace_bytes(rows, model.vocab, alternatives), dtype=torch.uint8,
+                                    device="cuda")
         self.status = torch.zeros(1, dtype=INT32, device="cuda")
         self.moved = torch.zeros(1, dtype=INT32, device="cuda")
         self.prompt_ids = torch.arange(prompts, dtype=INT32, device="cuda")

@@ -549,7 +549,7 @@ CPES_API int cpes_cache_append(const cpes_cache* cache, int32_t layer, const cpe
                                const int32_t* seqs_dev, const int32_t* positions_dev, const void* k_new_dev,
                                const void* v_new_dev, int64_t new_stride, int64_t new_head_stride, void* stream);
 
-/* Workspace bytes of cpes_attend for `rows` rows (0 for invalid arguments). */
+/* Workspace bytes of cpes_attend on up to `rows` rows (0 for invalid arguments). */
 CPES_API size_t cpes_attend_workspace_bytes(int32_t rows, int32_t q_heads, int32_t kv_heads, int32_t head_dim);
 
 /*
@@ -584,7 +584,9 @@ CPES_API int cpes_attend(const cpes_cache* cache, int32_t layer, const cpes_pool
                          int64_t out_stride, int64_t out_head_stride, float* lse_dev, void* workspace_dev,
                          size_t workspace_bytes, void* stream);
 
-/* Workspace bytes of cpes_logprobs (0 for invalid arguments). */
+/* Workspace bytes of cpes_logprobs on up to `rows` rows with up to `top`
+ * alternatives, in either type: one sized for the largest batch serves it as its
+ * rows end (0 for invalid arguments, or where none is needed). */
 CPES_API size_t cpes_logprobs_workspace_bytes(int32_t rows, int32_t vocab, int32_t top);
 
 /*

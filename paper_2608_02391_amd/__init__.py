@@ -613,6 +613,7 @@ def _logits(x, what: str = "logits"):
 
 
 def cpes_logprobs_workspace_bytes(rows: int, vocab: int, top: int = 0) -> int:
+    """Enough for any number of rows up to ``rows``: a batch keeps its workspace as its rows end."""
     return int(load().cpes_logprobs_workspace_bytes(rows, vocab, top))
 
 

@@ -94,6 +94,7 @@ inline __host__ __device__ int64_t attend_part_floats(int dim)
 }
 
 constexpr int kMaxSlices = 64;           // workgroups of one row of logits at most
+constexpr int kMaxSlicedRows = 256;      // more rows are not cut into slices
 
 struct LogprobArgs {
     const void* x;

@@ -400,10 +400,14 @@ int cpes_attend(const cpes_cache* cache, int32_t layer, const cpes_pool* pool, i
 size_t cpes_logprobs_workspace_bytes(int32_t rows, int32_t vocab, int32_t top)
 {
     if (rows < 0 || vocab < 1 || top < 0 || top > CPES_MAX_ALTERNATIVES) return 0;
-    int32_t per;
-    const int slices = std::max(cpes::logprob_slices(rows, vocab, CPES_BF16, &per),
-                                cpes::logprob_slices(rows, vocab, CPES_F32, &per));
-    return logprob_bytes(rows, slices, top);
+    // the most that any number of rows up to this takes: fewer rows are cut into more slices
+    size_t most = 0;
+    for (int32_t r = 1; r <= std::min<int32_t>(rows, cpes::kMaxSlicedRows); ++r)
+        for (int dtype : {CPES_BF16, CPES_F32}) {
+            int32_t per;
+            most = std::max(most, logprob_bytes(r, cpes::logprob_slices(r, vocab, dtype, &per), top));
+        }
+    return most;
 }
 
 int cpes_logprobs(const void* x_dev, int dtype, int32_t rows, int32_t vocab, int64_t stride, float scale,

@@ -785,7 +785,7 @@ int logprob_slices(int32_t rows, int32_t vocab, int dtype, int32_t* per_slice)
     const int n = dtype == 0 ? Vec<uint16_t>::n : Vec<float>::n;
     const int64_t bytes = (int64_t)vocab * 16 / n;
     int64_t slices = 1;
-    if (rows > 0 && rows <= 256 && bytes >= 8 * kSliceBytes)
+    if (rows > 0 && rows <= kMaxSlicedRows && bytes >= 8 * kSliceBytes)
         slices = std::min<int64_t>(std::min<int64_t>(kMaxSlices, 512 / rows), bytes / kSliceBytes);
     const int64_t per = ((vocab + slices - 1) / slices + n - 1) / n * n;
     *per_slice = (int32_t)std::min<int64_t>(per, INT32_MAX / n * n);

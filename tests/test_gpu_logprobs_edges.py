@@ -74,3 +74,19 @@ def test_largest_vocabularies(V, dtype):
         part = dx[0, s:s + (1 << 28)]
         here = sum(1 for v in special if s <= v < s + part.numel())
         assert int(((part < low) | (part > high)).sum()) <= here, s
+
+
+@pytest.mark.parametrize("vocab", [151936, 70001])
+def test_one_workspace_as_rows_end(vocab):
+    """The workspace of the first batch scores what is left of it, whichever number that is."""
+    top, most = 20, 300
+    x, t = logits(most, vocab, BF16, 3)
+    x, dt = x.cuda(), t.cuda()
+    ws = torch.empty(cp.cpes_logprobs_workspace_bytes(most, vocab, top), dtype=torch.uint8, device="cuda")
+    f = lambda *shape: torch.empty(*shape, device="cuda")
+    for rows in (300, 257, 256, 200, 100, 65, 48, 33, 32, 8, 7, 2, 1):
+        o = dict(logp=f(rows), entropy=f(rows), lse=f(rows), top_logp=f(rows, top),
+                 top_ids=torch.empty(rows, top, dtype=torch.int64, device="cuda"))
+        cp.cpes_logprobs(x[:rows], dt[:rows], workspace=ws, **o)
+        pick = sorted({0, rows // 2, rows - 1})
+        check(x[pick], t[pick], {k: v[pick] for k, v in o.items()}, top=top)
