@@ -160,13 +160,13 @@ def _torch():
     return _torch_module
 
 
-def _dtype_code(t) -> int:
+def _dtype_code(t, what: str = "weights") -> int:
     code = _dtype_codes.get(t.dtype)
     if code is None:
         _torch()                        # the table is empty before the first call
         code = _dtype_codes.get(t.dtype)
     if code is None:
-        raise TypeError(f"weights must be bfloat16 or float32, not {t.dtype}")
+        raise TypeError(f"{what} must be bfloat16 or float32, not {t.dtype}")
     return code
 
 
@@ -457,7 +457,7 @@ def paged_cache(k, v) -> Cache:
     if k.stride(4) != 1 and k.shape[4] > 1:
         raise ValueError("the head dimension must be contiguous")
     st = k.stride()
-    cache = Cache(k.data_ptr(), v.data_ptr(), st[0], st[1], st[2], st[3], *k.shape, _dtype_code(k))
+    cache = Cache(k.data_ptr(), v.data_ptr(), st[0], st[1], st[2], st[3], *k.shape, _dtype_code(k, "keys and values"))
     cache._tensors = (k, v)     # the descriptor holds raw pointers: keep the storage alive with it
     cache._dtype = k.dtype
     return cache
@@ -631,7 +631,7 @@ def cpes_logprobs(logits, targets, logp, entropy=None, lse=None, stats=None, top
             raise ValueError("top_logp and top_ids must both be [rows, k]")
         top = top_ids.shape[1]
     ws, size = _workspace(workspace)
-    _check((_lib or load()).cpes_logprobs(x, _dtype_code(logits), rows, vocab, stride, scale,
+    _check((_lib or load()).cpes_logprobs(x, _dtype_code(logits, "logits"), rows, vocab, stride, scale,
                                           _buffer(targets, "targets", rows, int64), _floats(logp, "logp", rows),
                                           _floats(entropy, "entropy", rows), _floats(lse, "lse", rows),
                                           _floats(stats, "stats", 2 * rows), top, _floats(top_logp, "top_logp", rows * top),
@@ -646,7 +646,7 @@ def cpes_logprobs_backward(logits, targets, stats, entropy, d_logp, d_entropy, d
     dx, d_rows, d_vocab, d_stride = _logits(d_logits, "d_logits")
     if (d_rows, d_vocab) != (rows, vocab) or d_logits.dtype != logits.dtype:
         raise ValueError("d_logits must have the shape and dtype of the logits")
-    _check((_lib or load()).cpes_logprobs_backward(x, _dtype_code(logits), rows, vocab, stride, scale,
+    _check((_lib or load()).cpes_logprobs_backward(x, _dtype_code(logits, "logits"), rows, vocab, stride, scale,
                                                    _buffer(targets, "targets", rows, _torch().int64), _floats(stats, "stats", 2 * rows),
                                                    _floats(entropy, "entropy", rows), _floats(d_logp, "d_logp", rows),
                                                    _floats(d_entropy, "d_entropy", rows), dx, d_stride, _stream(stream)))
