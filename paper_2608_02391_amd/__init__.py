@@ -446,11 +446,16 @@ def cpes_update_step(w, offsets: Sequence[int], seeds: Sequence[int], signs: Seq
 
 # ------------------------------------------------------ evaluating a member --
 
+def _same_strides(a, b, shape) -> bool:
+    """Whether two tensors of a shape lie alike: the stride of a dimension of one entry addresses nothing."""
+    return a == b or all(x == y or n <= 1 for x, y, n in zip(a, b, shape))
+
+
 def paged_cache(k, v) -> Cache:
     """A key-value cache in pages: k and v of shape [layers, pages, heads,
     page_size, head_dim], bfloat16 or float32, with the same strides and the
     last dimension contiguous (token-major pages are a transposed view)."""
-    if k.dim() != 5 or k.shape != v.shape or k.dtype != v.dtype or k.stride() != v.stride():
+    if k.dim() != 5 or k.shape != v.shape or k.dtype != v.dtype or not _same_strides(k.stride(), v.stride(), k.shape):
         raise ValueError("keys and values must be [layers, pages, heads, page_size, head_dim] of one shape, dtype and strides")
     if not (k.is_cuda and v.is_cuda):
         raise ValueError("keys and values must be GPU tensors")
@@ -571,7 +576,7 @@ def cpes_cache_append(cache: Cache, layer: int, pool: Pool, k_new, v_new, positi
     shape = (k_new.shape[0], cache.heads, cache.head_dim)
     k, row, head = _rows(k_new, "k_new", shape, cache._dtype)
     v, v_row, v_head = _rows(v_new, "v_new", shape, cache._dtype)
-    if (v_row, v_head) != (row, head):
+    if not _same_strides((row, head), (v_row, v_head), shape):
         raise ValueError("k_new and v_new must have the same strides")
     _check((_lib or load()).cpes_cache_append(ctypes.byref(cache), layer, ctypes.byref(pool), shape[0],
                                               _int32_list(seqs, "seqs", shape[0]),
