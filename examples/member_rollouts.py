@@ -97,21 +97,28 @@ class Rollouts:
                                      dtype=torch.uint8, device="cuda")
         self.score_ws = torch.empty(cp.cpes_logprobs_workspace_bytes(rows, model.vocab, alternatives), dtype=torch.uint8,
                                     device="cuda")
-        self.status = torch.zeros(1, dtype=INT32, device="cuda")
+        self.status, self.worst = (torch.zeros(1, dtype=INT32, device="cuda") for _ in range(2))
         self.moved = torch.zeros(1, dtype=INT32, device="cuda")
         self.prompt_ids = torch.arange(prompts, dtype=INT32, device="cuda")
         self.child_ids = torch.arange(prompts, S, dtype=INT32, device="cuda")
         self.parents = self.prompt_ids.repeat_interleave(each)
 
+    def note(self):
+        """A page call writes its own status over the last one's: the worst since the last check is kept beside it."""
+        torch.maximum(self.worst, self.status, out=self.worst)
+
     def check(self):
-        """The status of the last page call (a synchronisation: where a program may wait)."""
-        if int(self.status) != cp.PAGES_OK:
-            raise RuntimeError(f"page call failed with status {int(self.status)}")
+        """Whether a page call has failed since the last check (a synchronisation: where a program may wait)."""
+        worst = int(self.worst)
+        if worst != cp.PAGES_OK:
+            self.worst.zero_()
+            raise RuntimeError(f"page call failed with status {worst}")
 
     def step(self, seqs, tokens, pos):
         """One new token for each listed sequence, at positions `pos`: logits [rows, vocabulary]."""
         m, rows = self.model, len(seqs)
         cp.cpes_pages_reserve(self.pool, seqs, pos + 1, self.page_ws, status=self.status)
+        self.note()
         x = m.embed(tokens, pos)
         heads = torch.empty(rows, m.q_heads, m.head_dim, dtype=BF16, device="cuda")
         for layer in range(m.layers):
@@ -149,6 +156,7 @@ class Rollouts:
         pick among the alternatives."""
         logits = self.prefill(prompts).repeat_interleave(self.each, 0)
         cp.cpes_pages_fork(self.cache, self.pool, self.parents, self.child_ids, self.page_ws, status=self.status)
+        self.note()
         self.check()
         pos = torch.tensor([len(p) for p in prompts], dtype=INT32, device="cuda").repeat_interleave(self.each)
         tokens, logps, entropies = [], [], []
@@ -167,10 +175,12 @@ class Rollouts:
     def drop(self, seqs):
         """Sequences end; the pages that stay move to the front of the cache."""
         cp.cpes_pages_free(self.pool, seqs, status=self.status)
+        self.note()
         cp.cpes_pages_compact(self.cache, self.pool, self.pool, self.page_ws, moved=self.moved)
 
     def clear(self):
         cp.cpes_pages_free(self.pool, torch.arange(len(self.lengths), dtype=INT32, device="cuda"), status=self.status)
+        self.note()
 
 
 def reward(tokens, logps, goal):

@@ -457,7 +457,9 @@ typedef struct cpes_pool {
     int32_t page_size;
 } cpes_pool;
 
-/* What the page calls report in status_dev (NULL, or a device int32). */
+/* What the page calls report in status_dev (NULL, or a device int32).  A call
+ * overwrites it: where several run before it is looked at, each has its own, or
+ * the largest is kept. */
 enum cpes_pages_status {
     CPES_PAGES_OK = 0,
     CPES_PAGES_SHORT = 1,       /* not enough free pages: nothing was changed */
