@@ -60,6 +60,9 @@
 extern "C" {
 #endif
 
+/* Raised when a call or a struct that was there changes; calls can be added without
+ * (the ones that evaluate a member were): a program that may meet a library without
+ * them looks the symbol up. */
 #define CPES_ABI_VERSION 8
 
 /* Exported symbols (the library is built with hidden default visibility). */
@@ -542,8 +545,10 @@ CPES_API int cpes_pages_compact(const cpes_cache* cache, const cpes_pool* pool, 
  * one layer: token i belongs to sequence seqs[i] (device int32[n]; NULL: i) and
  * position positions[i] (device int32[n]); element d of head h of token i is
  * k_new[i * new_stride + h * new_head_stride + d], and the same of v_new.  Bit
- * copies.  Tokens whose sequence or position is out of range, or whose table
- * entry names no page, are skipped.  Two tokens at one place leave either.
+ * copies.  Tokens whose sequence or position is outside the table, or whose table
+ * entry names no page, are skipped.  The table alone decides, not the length: a
+ * table that was filled with -1 has no page for a token whose reservation failed.
+ * Two tokens at one place leave parts of either.
  * Errors: null pointers, n < 0, a layer out of range, negative strides, a bad
  *   cache or a pool that does not fit it -> CPES_ERR_INVALID_ARGUMENT.
  */
@@ -568,10 +573,11 @@ CPES_API size_t cpes_attend_workspace_bytes(int32_t rows, int32_t q_heads, int32
  * sums and the output are held in fp32, and the weights of bf16 values carry 16
  * bits of mantissa into the matrix instructions.  out has the cache's dtype:
  * element d of head i of row r at out[r * out_stride + i * out_head_stride + d].
- * A row that sees nothing (an empty sequence, an id out of range) gets out = 0
- * and lse = -inf, as does one whose scores are all -inf; positions whose table
- * entry names no page are not seen.  The result does not depend on the
- * contents of unseen positions, nor on the run.
+ * Of a sequence the first 2^31 - 65 positions count.  A row that sees nothing (an
+ * empty sequence, an id out of range) gets out = 0 and lse = -inf, as does one
+ * whose scores are all -inf; positions whose table entry names no page are not
+ * seen.  The result does not depend on the contents of unseen positions, nor on
+ * the run.
  * workspace: as cpes_attend_workspace_bytes, 16-byte aligned; needs no
  * particular contents, and calls that overlap in time need their own.
  * Errors: null pointers, rows < 0, q_heads not a positive multiple of the
@@ -599,7 +605,7 @@ CPES_API size_t cpes_logprobs_workspace_bytes(int32_t rows, int32_t vocab, int32
  *   p_v = e^(z_v - lse);
  *   alternatives: the `top` tokens of largest x in descending order, ties by the
  *   lowest token, and their log probabilities.
- * targets_dev: device int64[rows]; a target outside [0, vocab) scores 0.
+ * targets_dev: device int64[rows]; a target outside [0, vocab) scores 0, in any row.
  * logp_dev, entropy_dev, lse_dev: NULL, or device float32[rows].
  * stats_dev: NULL, or device float32[2 * rows]: max x and ln sum_v e^(z_v - scale
  *   max x), what cpes_logprobs_backward needs.

@@ -106,7 +106,8 @@ __device__ __forceinline__ Row row_at(const AttendArgs& a, int32_t r)
 
 // e^x for x <= 0: the hardware's 2^x.  Scores and maxima stay in natural units,
 // so that lse loses nothing on a way through base 2.  The product's rounding
-// is |x| 2^-24 of the weight, which an fp32 cache's outputs would show.
+// is |x| 2^-24 of the weight, which an fp32 cache's outputs would show; the lse of a
+// bf16 cache carries it, as the mean of |x| 2^-24 under the weights.
 template <typename T> __device__ __forceinline__ float weight(float x);
 template <> __device__ __forceinline__ float weight<uint16_t>(float x) { return __builtin_amdgcn_exp2f(x * kLog2e); }
 template <> __device__ __forceinline__ float weight<float>(float x) { return expf(x); }

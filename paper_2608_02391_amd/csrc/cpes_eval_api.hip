@@ -157,8 +157,8 @@ constexpr size_t round16(size_t x)
     return (x + 15) / 16 * 16;
 }
 
-// Workgroups of an attention launch: two per CU of four waves, one where a
-// head's tiles fill the registers of a whole SIMD.
+// Workgroups of an attention launch on the 256 CUs of an MI355X: two per CU of four
+// waves, one where a head's tiles fill the registers of a whole SIMD.
 int attend_groups(int32_t head_dim)
 {
     return head_dim > 128 ? 256 : 512;

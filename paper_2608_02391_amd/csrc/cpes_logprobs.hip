@@ -722,7 +722,14 @@ void logprobs_as(const LogprobArgs& a, hipStream_t s)
 //   2,000 rows of 24,000      27    28    35      4,096 rows of 100,000   144   161   153
 //   1,000 rows of 12,000      17    16    18      5,000 rows of 100,000   195   192   184
 //     300 rows of 12,000      14    13    14      1,300 rows of 151,936    97    89    83
-// (2,000 rows of 50,257, score and gradient in turn: 109, 109, 104.)  For many
+// The range between, where the logits fit the cache, by the same three, of logits that
+// are there and of others:
+//   rows of 50,257             2,000                          1,000
+//   20 alternatives       44  49  52    56  57  59       30  28  33    33  31  34
+//   none                  35  41  40    47  48  49       21  21  25    25  24  27
+//   and the gradient     102 105 100   114 119 112       62  57  57    68  69  68
+// 256 threads, which the rule takes there, are 1 % faster where a gradient follows and
+// 5 to 20 % slower for scores alone; it does not tell the two apart.  For many
 // alternatives 64 maxima bound too little (64 of 2,000 rows of 12,000: 112, 29, 38).
 int logprob_threads(int64_t jobs, int64_t bytes, int top)
 {
