@@ -94,6 +94,7 @@ enum cpes_scale_mode { CPES_SCALE_ALPHA_OVER_N_SIGMA = 0, CPES_SCALE_ALPHA_OVER_
 #define CPES_MAX_HEADS 65536         /* key-value heads of a cpes_cache, query heads of cpes_attend */
 #define CPES_MAX_ALTERNATIVES 64     /* most likely tokens cpes_logprobs lists per row */
 #define CPES_MAX_SEQUENCES (1 << 20) /* sequences listed per cpes_pages_* call, rows per cpes_attend call */
+#define CPES_MAX_TREE 256            /* drafted tokens of one sequence in a tree (chains of cpes_attend_tree: any) */
 
 typedef struct cpes_subspace {
     int64_t offset;          /* first parameter (no map) or first map entry */
@@ -540,6 +541,35 @@ CPES_API int cpes_pages_copy(const cpes_cache* cache, int32_t n, const int32_t* 
 CPES_API int cpes_pages_compact(const cpes_cache* cache, const cpes_pool* pool, const cpes_pool* packed,
                                 void* workspace_dev, size_t workspace_bytes, int32_t* moved_dev, void* stream);
 
+/* Workspace bytes of cpes_pages_keep on up to `n` sequences with up to `longest`
+ * drafted tokens each; 0 for n < 0 or a `longest` outside [1, CPES_MAX_TREE]. */
+CPES_API size_t cpes_pages_keep_workspace_bytes(int32_t n, int32_t longest);
+
+/*
+ * cpes_pages_keep -- drafted tokens that were not confirmed leave the cache.  The
+ * newest T = starts[i + 1] - starts[i] tokens of sequence seqs[i] (device int32[n];
+ * NULL: i) are drafted ones, in the order in which they entered the cache; the
+ * first kept[i] entries of path[i * longest ..] (device int32[n * longest], as
+ * cpes_tree_accept leaves them) are the ones that stay, ascending in [0, T).  Their
+ * keys and values move together, in every layer, behind the tokens in front of the
+ * drafted ones; the sequence's length falls by T - kept[i], and the pages it then
+ * no longer needs are given back (table entries -1, reference counts one lower).
+ * All or nothing: a sequence id out of range or listed twice, starts (device
+ * int32[n + 1]) that fall or lie more than `longest` apart, a sequence shorter than
+ * its drafted tokens or of a length that is negative or beyond its table, kept outside
+ * [0, T] or a path that does not ascend in [0, T) give CPES_PAGES_BAD_SEQUENCE, and then
+ * nothing has changed.  A token whose table entry names no page moves nowhere.
+ * Pages with drafted tokens belong to one sequence: a fork in between shares them,
+ * and leaves either's contents undefined.
+ * Errors: as cpes_pages_fork; null pointers, longest < 1 -> CPES_ERR_INVALID_ARGUMENT;
+ *   longest above CPES_MAX_TREE -> CPES_ERR_UNSUPPORTED; workspace, as
+ *   cpes_pages_keep_workspace_bytes, too small or not 16-byte aligned -> CPES_ERR_WORKSPACE.
+ */
+CPES_API int cpes_pages_keep(const cpes_cache* cache, const cpes_pool* pool, int32_t n, const int32_t* seqs_dev,
+                             const int32_t* starts_dev, int32_t longest, const int32_t* kept_dev,
+                             const int32_t* path_dev, void* workspace_dev, size_t workspace_bytes, int32_t* status_dev,
+                             void* stream);
+
 /*
  * cpes_cache_append -- the keys and values of n new tokens enter their pages in
  * one layer: token i belongs to sequence seqs[i] (device int32[n]; NULL: i) and
@@ -592,6 +622,67 @@ CPES_API int cpes_attend(const cpes_cache* cache, int32_t layer, const cpes_pool
                          int64_t out_stride, int64_t out_head_stride, float* lse_dev, void* workspace_dev,
                          size_t workspace_bytes, void* stream);
 
+/* Workspace bytes of cpes_attend_tree on up to `rows` sequences with up to `tokens` new
+ * tokens in all and `longest` each (0 for invalid arguments). */
+CPES_API size_t cpes_attend_tree_workspace_bytes(int32_t rows, int32_t tokens, int32_t longest, int32_t q_heads,
+                                                 int32_t kv_heads, int32_t head_dim);
+
+/*
+ * cpes_attend_tree -- attention of several new tokens per sequence over the paged
+ * cache of one layer: a tree of drafted tokens, or a chain of them (a prompt, or a
+ * piece of one).  Row r asks for sequence s = seqs[r] (device int32[rows]; NULL: r);
+ * its new tokens are rows starts[r] .. starts[r + 1] - 1 of q and out (starts: device
+ * int32[rows + 1]), T of them, and the newest T of the n = lengths[s] tokens in the
+ * cache, in the same order (their keys and values are there).  Token i of a row
+ * hangs from token parents[starts[r] + i] of it, one before it, or with -1 from the
+ * b = n - T tokens in front of them (device int32[tokens]; any other number counts as
+ * -1; NULL: from token i - 1).  With depth_i its number of ancestors in the tree, it
+ * stands at position b + depth_i of its text and sees the b tokens in front, its
+ * ancestors and itself; with window > 0 only those at positions p of that text with
+ *   p > b + depth_i - window  or  p < sinks.
+ * Scores, sums and outputs are those of cpes_attend (out, and lse: NULL, or device
+ * float32[tokens * q_heads]), to which it gives the same results for trees of one
+ * token up to roundings.  Of a sequence the first 2^31 - 65 positions count.  The
+ * tokens of a sequence that has fewer than T, or of an id out of range, get out = 0
+ * and lse = -inf; positions whose table entry names no page are not seen.  A row
+ * whose starts fall, lie outside [0, tokens] or more than `longest` apart is left out,
+ * and rows behind one whose starts fall may be; what no row covers is left as it was.  The result of a token does not
+ * depend on the contents of positions it does not see (other branches, too), nor on the
+ * run.
+ * workspace: as cpes_attend_tree_workspace_bytes, 16-byte aligned; needs no
+ * particular contents, and calls that overlap in time need their own.
+ * Errors: as cpes_attend; tokens < 0, longest outside [1, tokens] with tokens > 0 ->
+ *   CPES_ERR_INVALID_ARGUMENT; rows above CPES_MAX_SEQUENCES, longest above
+ *   CPES_MAX_TREE with parents -> CPES_ERR_UNSUPPORTED.
+ */
+CPES_API int cpes_attend_tree(const cpes_cache* cache, int32_t layer, const cpes_pool* pool, int32_t rows,
+                              const int32_t* seqs_dev, const int32_t* starts_dev, int32_t tokens, int32_t longest,
+                              const int32_t* parents_dev, const void* q_dev, int64_t q_stride, int64_t q_head_stride,
+                              int32_t q_heads, float scale, int32_t window, int32_t sinks, void* out_dev,
+                              int64_t out_stride, int64_t out_head_stride, float* lse_dev, void* workspace_dev,
+                              size_t workspace_bytes, void* stream);
+
+/*
+ * cpes_tree_accept -- which drafted tokens the model confirms.  Row r's tree is
+ * tokens starts[r] .. starts[r + 1] - 1 of drafted and sampled (device int64[tokens]),
+ * with parents as in cpes_attend_tree.  Token 0 of a row is no guess (the last step
+ * sampled it) and always stays; from a token that stays the walk goes on to the lowest
+ * one that hangs from it and is the token sampled behind it, drafted[j] == sampled[i],
+ * and ends where there is none.
+ *   kept_dev (device int32[rows]): tokens that stay; path_dev (device int32[rows *
+ *   longest]): which, ascending, then -1; next_dev (device int64[rows]): the token
+ *   sampled behind the last of them, the next step's token 0.
+ * Where each sampled token comes from the model's own distribution behind its branch
+ * (cpes_sample), the text is distributed as if nothing had been drafted.  Rows without
+ * tokens, and rows whose starts fall, lie outside [0, tokens] or more than `longest`
+ * apart, get kept = 0 and next = -1.
+ * Errors: null pointers, rows < 0, tokens < 0, longest < 1 -> CPES_ERR_INVALID_ARGUMENT;
+ *   rows above CPES_MAX_SEQUENCES, longest above CPES_MAX_TREE -> CPES_ERR_UNSUPPORTED.
+ */
+CPES_API int cpes_tree_accept(int32_t rows, const int32_t* starts_dev, int32_t tokens, int32_t longest,
+                              const int32_t* parents_dev, const int64_t* drafted_dev, const int64_t* sampled_dev,
+                              int32_t* kept_dev, int32_t* path_dev, int64_t* next_dev, void* stream);
+
 /* Workspace bytes of cpes_logprobs on up to `rows` rows with up to `top`
  * alternatives, in either type: one sized for the largest batch serves it as its
  * rows end (0 for invalid arguments, or where none is needed). */
@@ -641,6 +732,37 @@ CPES_API int cpes_logprobs_backward(const void* x_dev, int dtype, int32_t rows, 
                                     float scale, const int64_t* targets_dev, const float* stats_dev,
                                     const float* entropy_dev, const float* d_logp_dev, const float* d_entropy_dev,
                                     void* dx_dev, int64_t dx_stride, void* stream);
+
+/* Workspace bytes of cpes_sample on up to `rows` rows in either type (0 for invalid
+ * arguments, or where none is needed). */
+CPES_API size_t cpes_sample_workspace_bytes(int32_t rows, int32_t vocab);
+
+/*
+ * cpes_sample -- a token for each row of logits x (`dtype`, row r at x + r * stride,
+ * `vocab` entries) from a given number u = uniforms[r] (device float32[rows], in [0,
+ * 1)).  With z = scale * x (scale = 1 / temperature) and w_v = e^(z_v - max z), in
+ * the order of descending x, ties by the lowest token:
+ *   top_k > 0:  only the first top_k tokens stay;
+ *   top_p < 1:  of these only the ones in front of which less than top_p of their
+ *               weight lies (the fewest that reach it, one at least);
+ *   min_p > 0:  of these only the ones with ln w_v >= ln min_p.
+ * token = the lowest v of those that stay with sum_{v' <= v} w_v' > u sum w, and
+ * logp = ln(w_token / sum w), both sums over those that stay.  Weights and sums are in
+ * 64 bits: a token is off its place only where u is within their roundings of a
+ * border.  top_k = 1 takes the most likely token.  A u below 0 or NaN counts as 0, one
+ * of 1 or more takes the last token that has a weight.
+ * tokens_dev: device int64[rows]; logp_dev: NULL, or device float32[rows].
+ * Logits of -inf are never chosen; a row of nothing but -inf has token -1 and logp
+ * -inf, one with a NaN or +inf token -1 and logp NaN.
+ * workspace: 16-byte aligned; needs no particular contents, and calls that overlap in
+ * time need their own.
+ * Errors: x, uniforms or tokens NULL, rows < 0, vocab < 1, stride < vocab with more than
+ *   one row, scale not positive or above FLT_MAX / 2, top_k < 0, top_p outside (0, 1],
+ *   min_p outside [0, 1] -> CPES_ERR_INVALID_ARGUMENT; workspace -> CPES_ERR_WORKSPACE.
+ */
+CPES_API int cpes_sample(const void* x_dev, int dtype, int32_t rows, int32_t vocab, int64_t stride, float scale,
+                         int32_t top_k, float top_p, float min_p, const float* uniforms_dev, int64_t* tokens_dev,
+                         float* logp_dev, void* workspace_dev, size_t workspace_bytes, void* stream);
 
 /* ---------------- test hooks and measurement utilities ------------------ */
 

@@ -23,7 +23,7 @@ NORM_Z, NORM_RANK = 0, 1
 SCALE_ALPHA_OVER_N_SIGMA, SCALE_ALPHA_OVER_N = 0, 1
 SUB_ASCENDING = 1
 MAX_MEMBERS, MAX_REWARDS, MAX_GROUPS, MAX_PERMUTATION_K, MAX_STEP_SUBSPACES = 256, 4096, 1024, 256, 32
-MAX_HEAD_DIM, MAX_HEADS, MAX_ALTERNATIVES, MAX_SEQUENCES = 256, 65536, 64, 1 << 20
+MAX_HEAD_DIM, MAX_HEADS, MAX_ALTERNATIVES, MAX_SEQUENCES, MAX_TREE = 256, 65536, 64, 1 << 20, 256
 PAGES_OK, PAGES_SHORT, PAGES_BAD_SEQUENCE = 0, 1, 2
 
 EXPORTED = (
@@ -33,7 +33,8 @@ EXPORTED = (
     "cpes_update", "cpes_update_step", "cpes_update_step32", "cpes_pages_workspace_bytes", "cpes_pages_reserve",
     "cpes_pages_fork", "cpes_pages_free", "cpes_pages_copy", "cpes_pages_compact", "cpes_cache_append",
     "cpes_attend_workspace_bytes", "cpes_attend", "cpes_logprobs_workspace_bytes", "cpes_logprobs",
-    "cpes_logprobs_backward", "cpes_debug_philox", "cpes_debug_normals", "cpes_debug_bm_grid",
+    "cpes_logprobs_backward", "cpes_pages_keep_workspace_bytes", "cpes_pages_keep", "cpes_attend_tree_workspace_bytes",
+    "cpes_attend_tree", "cpes_tree_accept", "cpes_sample_workspace_bytes", "cpes_sample", "cpes_debug_philox", "cpes_debug_normals", "cpes_debug_bm_grid",
     "cpes_debug_prp", "cpes_rng_probe", "cpes_probe_map_copy", "cpes_probe_copy", "cpes_fill_normal",
     "cpes_last_error", "cpes_abi_version",
 )
@@ -107,6 +108,14 @@ def load(path: str = LIB_PATH) -> ctypes.CDLL:
         "cpes_logprobs_workspace_bytes": [i32, i32, i32],
         "cpes_logprobs": [vp, i32, i32, i32, i64, f32, vp, vp, vp, vp, vp, i32, vp, vp, vp, size, vp],
         "cpes_logprobs_backward": [vp, i32, i32, i32, i64, f32, vp, vp, vp, vp, vp, vp, i64, vp],
+        "cpes_pages_keep_workspace_bytes": [i32, i32],
+        "cpes_pages_keep": [kc, pp, i32, vp, vp, i32, vp, vp, vp, size, vp, vp],
+        "cpes_attend_tree_workspace_bytes": [i32, i32, i32, i32, i32, i32],
+        "cpes_attend_tree": [kc, i32, pp, i32, vp, vp, i32, i32, vp, vp, i64, i64, i32, f32, i32, i32, vp, i64, i64, vp, vp,
+                             size, vp],
+        "cpes_tree_accept": [i32, vp, i32, i32, vp, vp, vp, vp, vp, vp, vp],
+        "cpes_sample_workspace_bytes": [i32, i32],
+        "cpes_sample": [vp, i32, i32, i32, i64, f32, i32, f32, f32, vp, vp, vp, vp, size, vp],
         "cpes_debug_philox": [u64, u32, u64, i64, vp, vp],
         "cpes_debug_normals": [u64, i64, i64, vp, vp],
         "cpes_debug_bm_grid": [u32, i64, vp, vp, vp, vp],
@@ -570,6 +579,31 @@ def cpes_pages_compact(cache: Cache, pool: Pool, packed: Pool, workspace, moved=
                                                _int32_list(moved, "moved", 1), _stream(stream)))
 
 
+def cpes_pages_keep_workspace_bytes(n: int, longest: int) -> int:
+    return int(load().cpes_pages_keep_workspace_bytes(n, longest))
+
+
+def _starts(t) -> int:
+    """Rows of an int32 [rows + 1] list of where each row's tokens begin."""
+    if t.numel() < 1:
+        raise ValueError("starts must hold rows + 1 entries")
+    return t.numel() - 1
+
+
+def cpes_pages_keep(cache: Cache, pool: Pool, starts, kept, path, workspace, seqs=None, status=None, stream=None) -> None:
+    """Of the drafted tokens starts[i] .. starts[i + 1] - 1 of sequences seqs[i] (None: i), the newest in the cache,
+    the first kept[i] of path[i] ([n, longest], as cpes_tree_accept leaves them) stay and move together; the
+    sequences' other pages are given back."""
+    n = _starts(starts)
+    if path.dim() != 2 or path.shape[0] != n:
+        raise ValueError(f"path must be [{n}, longest]")
+    ws, size = _workspace(workspace)
+    _check((_lib or load()).cpes_pages_keep(ctypes.byref(cache), ctypes.byref(pool), n, _int32_list(seqs, "seqs", n),
+                                            _int32_list(starts, "starts"), path.shape[1], _int32_list(kept, "kept", n),
+                                            _int32_list(path, "path"), ws, size, _int32_list(status, "status", 1),
+                                            _stream(stream)))
+
+
 def cpes_cache_append(cache: Cache, layer: int, pool: Pool, k_new, v_new, positions, seqs=None, stream=None) -> None:
     """Keys and values of new tokens ([tokens, heads, head_dim], rows may be apart)
     enter the pages of sequences seqs[i] (None: i) at positions[i]."""
@@ -604,6 +638,45 @@ def cpes_attend(cache: Cache, layer: int, pool: Pool, q, out, lse=None, seqs=Non
                                         _int32_list(seqs, "seqs", rows), qp, q_row, q_head, heads,
                                         dim ** -0.5 if scale is None else scale, window, sinks, op, o_row,
                                         o_head, _floats(lse, "lse", rows * heads), ws, size, _stream(stream)))
+
+
+def cpes_attend_tree_workspace_bytes(rows: int, tokens: int, longest: int, q_heads: int, kv_heads: int, head_dim: int) -> int:
+    return int(load().cpes_attend_tree_workspace_bytes(rows, tokens, longest, q_heads, kv_heads, head_dim))
+
+
+def cpes_attend_tree(cache: Cache, layer: int, pool: Pool, q, out, starts, longest: int, parents=None, lse=None, seqs=None,
+                     scale: Optional[float] = None, window: int = 0, sinks: int = 0, workspace=None, stream=None) -> None:
+    """Attention of the newest tokens of sequences seqs[r] (None: r) over the cache: tokens starts[r] .. starts[r + 1]
+    - 1 (at most ``longest``) of q and out [tokens, q_heads, head_dim] (rows and heads may be apart) are a tree with
+    ``parents`` (int32 [tokens], within the row; None: a chain).  lse is float32 [tokens, q_heads]; scale defaults to
+    head_dim ** -0.5."""
+    shape, dtype = q.shape, cache._dtype
+    if len(shape) != 3 or shape[2] != cache.head_dim:
+        raise ValueError(f"q must be [tokens, q_heads, {cache.head_dim}], not {tuple(shape)}")
+    tokens, heads, dim = shape
+    rows = _starts(starts)
+    qp, q_row, q_head = _rows(q, "q", shape, dtype)
+    op, o_row, o_head = _rows(out, "out", shape, dtype)
+    ws, size = _workspace(workspace)
+    _check((_lib or load()).cpes_attend_tree(ctypes.byref(cache), layer, ctypes.byref(pool), rows,
+                                             _int32_list(seqs, "seqs", rows), _int32_list(starts, "starts"), tokens, longest,
+                                             _int32_list(parents, "parents", tokens), qp, q_row, q_head, heads,
+                                             dim ** -0.5 if scale is None else scale, window, sinks, op, o_row, o_head,
+                                             _floats(lse, "lse", tokens * heads), ws, size, _stream(stream)))
+
+
+def cpes_tree_accept(starts, drafted, sampled, kept, path, next_tokens, parents=None, stream=None) -> None:
+    """The walk down each row's tree along the sampled tokens: ``drafted`` and ``sampled`` int64 [tokens]; ``kept`` int32
+    [rows], ``path`` int32 [rows, longest] and ``next_tokens`` int64 [rows] receive how many tokens stay, which, and
+    the token behind them."""
+    rows, tokens, int64 = _starts(starts), drafted.numel(), _torch().int64
+    if path.dim() != 2 or path.shape[0] != rows:
+        raise ValueError(f"path must be [{rows}, longest]")
+    _check((_lib or load()).cpes_tree_accept(rows, _int32_list(starts, "starts"), tokens, path.shape[1],
+                                             _int32_list(parents, "parents", tokens), _buffer(drafted, "drafted", 0, int64),
+                                             _buffer(sampled, "sampled", tokens, int64), _int32_list(kept, "kept", rows),
+                                             _int32_list(path, "path"), _buffer(next_tokens, "next_tokens", rows, int64),
+                                             _stream(stream)))
 
 
 def _logits(x, what: str = "logits"):
@@ -655,6 +728,23 @@ def cpes_logprobs_backward(logits, targets, stats, entropy, d_logp, d_entropy, d
                                                    _buffer(targets, "targets", rows, _torch().int64), _floats(stats, "stats", 2 * rows),
                                                    _floats(entropy, "entropy", rows), _floats(d_logp, "d_logp", rows),
                                                    _floats(d_entropy, "d_entropy", rows), dx, d_stride, _stream(stream)))
+
+
+def cpes_sample_workspace_bytes(rows: int, vocab: int) -> int:
+    """Enough for any number of rows up to ``rows``."""
+    return int(load().cpes_sample_workspace_bytes(rows, vocab))
+
+
+def cpes_sample(logits, uniforms, tokens, logp=None, scale: float = 1.0, top_k: int = 0, top_p: float = 1.0,
+                min_p: float = 0.0, workspace=None, stream=None) -> None:
+    """tokens[r] (int64) drawn from logits [rows, vocabulary] times ``scale`` by uniforms[r] (float32, in [0, 1)), among
+    the ``top_k`` most likely (0: all), the fewest of them that hold ``top_p`` of their probability, and those with
+    at least ``min_p`` of the largest one; logp float32 [rows], among these."""
+    x, rows, vocab, stride = _logits(logits)
+    ws, size = _workspace(workspace)
+    _check((_lib or load()).cpes_sample(x, _dtype_code(logits, "logits"), rows, vocab, stride, scale, top_k, top_p, min_p,
+                                        _floats(uniforms, "uniforms", rows), _buffer(tokens, "tokens", rows, _torch().int64),
+                                        _floats(logp, "logp", rows), ws, size, _stream(stream)))
 
 
 def cpes_debug_philox(seed: int, domain: int, q0: int, nblocks: int, out, stream=None) -> None:

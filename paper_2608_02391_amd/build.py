@@ -11,7 +11,7 @@ CSRC = os.path.join(PKG, "csrc")
 INCLUDE = os.path.join(ROOT, "include")
 LIB = os.path.join(PKG, "libcpes.so")
 SOURCES = ["cpes_api.hip", "cpes_kernels.hip", "cpes_eval_api.hip", "cpes_pages.hip", "cpes_attend.hip",
-           "cpes_logprobs.hip"]
+           "cpes_tree.hip", "cpes_logprobs.hip", "cpes_sample.hip"]
 ARCH = "gfx950"
 
 HIPCC_FLAGS = [

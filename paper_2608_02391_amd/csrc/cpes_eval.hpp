@@ -64,6 +64,41 @@ struct AppendArgs {
     Divisor run, token;          // 16-byte units of one head, and of all heads, of one token
 };
 
+constexpr int kMaxTree = 256;            // CPES_MAX_TREE
+
+// The end of a step with drafted tokens: what stays of them moves together.
+struct KeepArgs {
+    PoolArgs pool;
+    char* k;
+    char* v;
+    const int32_t* seqs;
+    const int32_t* starts;
+    const int32_t* kept;
+    const int32_t* path;
+    int32_t* ws;                 // whether the call goes on; per row where its drafted tokens begin and how many stay; their pages
+    int64_t page_bytes, layer_bytes, head_bytes, token_bytes;   // strides
+    int32_t n, longest;
+    int32_t span;                // pages that `longest` tokens may touch
+    Divisor run, heads;          // 16-byte units of one head of a token; heads
+    uint32_t units;              // of a token: 2 * layers * heads * run
+};
+
+inline __host__ __device__ int64_t keep_words(int64_t n, int64_t span)
+{
+    return kPagesHeader + n * (2 + span);
+}
+
+struct AcceptArgs {
+    const int32_t* starts;
+    const int32_t* parents;
+    const int64_t* drafted;
+    const int64_t* sampled;
+    int32_t* kept;
+    int32_t* path;
+    int64_t* next;
+    int32_t rows, tokens, longest;
+};
+
 constexpr int kAttendHeads = 16;         // query heads of a workgroup: the columns of a matrix instruction
 constexpr int kAttendWaves = 4;          // of a workgroup, each with a share of the tiles
 
@@ -93,6 +128,61 @@ inline __host__ __device__ int64_t attend_part_floats(int dim)
     return 2 * kAttendHeads + (int64_t)kAttendHeads * dim;
 }
 
+struct TreeArgs {
+    const void* k;               // of the layer
+    const void* v;
+    const void* q;
+    void* out;
+    float* lse;
+    const int32_t* seqs;
+    const int32_t* starts;
+    const int32_t* parents;
+    const int32_t* table;
+    const int32_t* lengths;
+    float* parts;                // partial results, two per share
+    int2* joins;                 // per job: the shares it begins and ends in
+    int64_t page_stride, head_stride, token_stride, table_stride;
+    int64_t q_stride, q_head_stride, out_stride, out_head_stride;
+    int32_t rows, tokens, longest;
+    int32_t heads, group;        // q_heads = heads * group
+    int32_t columns;             // queries of a job: 16 * sets * beside
+    int32_t sets;                // of 16 queries, of a wave
+    int32_t beside;              // waves of a job on the same positions
+    int32_t job_heads, blocks;   // a group's query heads in `blocks` blocks of job_heads
+    int32_t job_tokens, pieces;  // a row's tokens in pieces of job_tokens, `pieces` at most
+    int32_t dim, page_size, page_shift, pages, width, sequences;   // page_shift < 0: no power of two
+    int32_t window, sinks;
+    int32_t groups;              // workgroups launched for shares
+    float scale;
+};
+
+// How jobs are cut, from what the host knows.
+struct TreeShape {
+    int32_t sets, beside, columns, job_heads, blocks, job_tokens, pieces;
+};
+
+inline TreeShape tree_shape(int32_t longest, int32_t group, int32_t dim)
+{
+    TreeShape t;
+    const int64_t queries = (int64_t)longest * group;
+    const int32_t most = dim > 128 ? 2 : 4;             // sets that fit a wave's registers
+    t.sets = queries <= 16 ? 1 : queries <= 32 ? 2 : most;
+    t.beside = 1;
+    while (t.beside < 4 && 16 * t.sets * t.beside < queries) t.beside *= 2;
+    t.columns = 16 * t.sets * t.beside;
+    t.job_heads = group < t.columns ? group : t.columns;
+    t.blocks = (group + t.job_heads - 1) / t.job_heads;
+    t.job_tokens = t.columns / t.job_heads;
+    t.pieces = (longest + t.job_tokens - 1) / t.job_tokens;
+    return t;
+}
+
+// One partial result of a wave: 16 * sets maxima, as many sums, then the output rows.
+inline __host__ __device__ int64_t tree_part_floats(int sets, int dim)
+{
+    return 16 * (int64_t)sets * (2 + dim);
+}
+
 constexpr int kMaxSlices = 64;           // workgroups of one row of logits at most
 constexpr int kMaxSlicedRows = 256;      // more rows are not cut into slices
 
@@ -113,6 +203,29 @@ struct LogprobArgs {
     float scale;
     float c;                     // scale log2 e
     float excess;                // (c / (scale log2 e) - 1) ln 2
+};
+
+constexpr int kSampleLanes = 64;
+constexpr int kSampleBlocks = 256;       // blocks of a row at most, a sum each, and 64 maxima
+
+struct SampleArgs {
+    const void* x;
+    const float* uniforms;
+    int64_t* tokens;
+    float* logp;
+    uint16_t* notes;             // [rows][blocks][64]: maxima of 64 parts of each block
+    double* sums;                // [rows][blocks]
+    float* refs;                 // [rows][blocks]: what the sums' exponents are relative to
+    float* most;                 // [rows][strips]: maxima, NaN where there is one
+    int64_t stride;
+    int32_t rows, vocab;
+    int32_t slices;              // workgroups of a row, kSampleWaves strips each
+    int32_t strip_steps;         // steps of a strip
+    int32_t shift;               // 2^shift steps a block
+    int32_t top_k;               // 0: all
+    double top_p;
+    double least;                // ln min_p, or -inf
+    double scale, c;             // c = scale log2 e
 };
 
 struct LogprobGradArgs {
@@ -137,9 +250,14 @@ hipError_t launch_pages_copy(const PageArgs& c, int32_t pages, int32_t n, const 
                              hipStream_t s);
 hipError_t launch_pages_compact(const PageArgs& c, const PoolArgs& p, const PoolArgs& packed, int32_t* ws,
                                 int32_t* moved, hipStream_t s);
+hipError_t launch_pages_keep(const KeepArgs& a, int32_t* status, hipStream_t s);
+hipError_t launch_tree_accept(const AcceptArgs& a, hipStream_t s);
 hipError_t launch_append(const AppendArgs& a, hipStream_t s);
 hipError_t launch_attend(int dtype, const AttendArgs& a, hipStream_t s);
 int logprob_slices(int32_t rows, int32_t vocab, int dtype, int32_t* per_slice);
+hipError_t launch_attend_tree(int dtype, const TreeArgs& a, hipStream_t s);
+void sample_split(int32_t rows, int32_t vocab, int dtype, int32_t* slices, int32_t* strip_steps, int32_t* shift);
+hipError_t launch_sample(int dtype, const SampleArgs& a, hipStream_t s);
 hipError_t launch_logprobs(int dtype, const LogprobArgs& a, hipStream_t s);
 hipError_t launch_logprobs_backward(int dtype, const LogprobGradArgs& a, hipStream_t s);
 

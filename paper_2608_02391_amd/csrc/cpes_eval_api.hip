@@ -89,6 +89,14 @@ int check_layer(const cpes_cache* c, int32_t layer, const char* fn)
     return CPES_OK;
 }
 
+int check_longest(int32_t longest, const char* fn)
+{
+    if (longest < 1) return fail(CPES_ERR_INVALID_ARGUMENT, "%s: longest %d is not positive", fn, longest);
+    if (longest > CPES_MAX_TREE)
+        return fail(CPES_ERR_UNSUPPORTED, "%s: longest %d above CPES_MAX_TREE", fn, longest);
+    return CPES_OK;
+}
+
 cpes::PoolArgs pool_args(const cpes_pool* p)
 {
     cpes::PoolArgs a;
@@ -169,6 +177,57 @@ int32_t head_blocks(int32_t group)
     return (group + cpes::kAttendHeads - 1) / cpes::kAttendHeads;
 }
 
+// log2 of a page's tokens, -1 if that is no whole number.
+int32_t page_shift(int32_t page_size)
+{
+    for (int b = 0; b < 31; ++b)
+        if (page_size == (int32_t)1 << b) return b;
+    return -1;
+}
+
+bool check_heads(int32_t q_heads, int32_t kv_heads, int32_t head_dim)
+{
+    return kv_heads >= 1 && q_heads >= 1 && q_heads <= CPES_MAX_HEADS && q_heads % kv_heads == 0 && head_dim >= 8 &&
+           head_dim <= CPES_MAX_HEAD_DIM && head_dim % 8 == 0;
+}
+
+// What attention over one layer of the cache needs, whatever its rows are.
+int check_attend(const cpes_cache* cache, int32_t layer, const cpes_pool* pool, int32_t q_heads, float scale, int32_t window,
+                 int32_t sinks, int64_t q_stride, int64_t q_head_stride, int64_t out_stride, int64_t out_head_stride,
+                 const char* fn)
+{
+    int rc = check_cache(cache, fn);
+    if (!rc) rc = check_pool(pool, false, fn);
+    if (!rc) rc = check_fit(cache, pool, fn);
+    if (!rc) rc = check_layer(cache, layer, fn);
+    if (!rc && (q_heads < 1 || q_heads % cache->heads != 0))
+        rc = fail(CPES_ERR_INVALID_ARGUMENT, "%s: %d query heads for %d key-value heads", fn, q_heads, cache->heads);
+    if (!rc && q_heads > CPES_MAX_HEADS) rc = fail(CPES_ERR_UNSUPPORTED, "%s: %d query heads above CPES_MAX_HEADS", fn, q_heads);
+    if (!rc && !std::isfinite(scale)) rc = fail(CPES_ERR_INVALID_ARGUMENT, "%s: scale %g is not finite", fn, (double)scale);
+    if (!rc && (window < 0 || sinks < 0))
+        rc = fail(CPES_ERR_INVALID_ARGUMENT, "%s: window %d or sinks %d negative", fn, window, sinks);
+    if (!rc && (q_stride < 0 || q_head_stride < 0 || out_stride < 0 || out_head_stride < 0))
+        rc = fail(CPES_ERR_INVALID_ARGUMENT, "%s: negative stride", fn);
+    return rc;
+}
+
+// Workgroups of the shares of trees: two per CU, one where a wave's state fills its SIMD's registers.
+int tree_groups(const cpes::TreeShape& t, int32_t head_dim)
+{
+    return head_dim > 128 || t.sets > 2 ? 256 : 512;
+}
+
+size_t tree_parts_bytes(const cpes::TreeShape& t, int32_t head_dim)
+{
+    return 2 * (size_t)tree_groups(t, head_dim) * cpes::kAttendWaves * cpes::tree_part_floats(t.sets, head_dim) * sizeof(float);
+}
+
+// Two partial results a wave, then the shares of every job.
+size_t tree_bytes(int32_t rows, const cpes::TreeShape& t, int32_t kv_heads, int32_t head_dim)
+{
+    return round16(tree_parts_bytes(t, head_dim) + (size_t)rows * t.pieces * kv_heads * t.blocks * sizeof(int2));
+}
+
 // Two partial results a share, then the shares of every row and head block.
 size_t attend_parts_bytes(int32_t head_dim)
 {
@@ -178,6 +237,17 @@ size_t attend_parts_bytes(int32_t head_dim)
 size_t attend_bytes(int32_t rows, int32_t q_heads, int32_t kv_heads, int32_t head_dim)
 {
     return round16(attend_parts_bytes(head_dim) + (size_t)rows * kv_heads * head_blocks(q_heads / kv_heads) * sizeof(int2));
+}
+
+constexpr int kSampleWaves = 4;          // strips of a slice
+
+size_t sample_bytes(int32_t rows, int32_t vocab, int dtype)
+{
+    int32_t slices, steps, shift;
+    cpes::sample_split(rows, vocab, dtype, &slices, &steps, &shift);
+    if (slices == 1) return 0;
+    const size_t strips = (size_t)slices * kSampleWaves, blocks = strips * (((steps - 1) >> shift) + 1);
+    return rows * round16(blocks * (cpes::kSampleLanes * sizeof(uint16_t) + sizeof(double) + sizeof(float)) + strips * sizeof(float));
 }
 
 size_t logprob_bytes(int32_t rows, int32_t slices, int32_t top)
@@ -330,10 +400,7 @@ int cpes_cache_append(const cpes_cache* cache, int32_t layer, const cpes_pool* p
 
 size_t cpes_attend_workspace_bytes(int32_t rows, int32_t q_heads, int32_t kv_heads, int32_t head_dim)
 {
-    if (rows < 0 || rows > CPES_MAX_SEQUENCES || kv_heads < 1 || q_heads < 1 || q_heads > CPES_MAX_HEADS ||
-        q_heads % kv_heads != 0 || head_dim < 8 ||
-        head_dim > CPES_MAX_HEAD_DIM || head_dim % 8 != 0)
-        return 0;
+    if (rows < 0 || rows > CPES_MAX_SEQUENCES || !check_heads(q_heads, kv_heads, head_dim)) return 0;
     return attend_bytes(rows, q_heads, kv_heads, head_dim);
 }
 
@@ -344,19 +411,9 @@ int cpes_attend(const cpes_cache* cache, int32_t layer, const cpes_pool* pool, i
 {
     cpes::clear_error();
     const char* fn = "cpes_attend";
-    int rc = check_cache(cache, fn);
-    if (!rc) rc = check_pool(pool, false, fn);
-    if (!rc) rc = check_fit(cache, pool, fn);
-    if (!rc) rc = check_layer(cache, layer, fn);
+    int rc = check_attend(cache, layer, pool, q_heads, scale, window, sinks, q_stride, q_head_stride, out_stride,
+                          out_head_stride, fn);
     if (!rc) rc = check_list(rows, q_dev && out_dev, fn);
-    if (!rc && (q_heads < 1 || q_heads % cache->heads != 0))
-        rc = fail(CPES_ERR_INVALID_ARGUMENT, "%s: %d query heads for %d key-value heads", fn, q_heads, cache->heads);
-    if (!rc && q_heads > CPES_MAX_HEADS) rc = fail(CPES_ERR_UNSUPPORTED, "%s: %d query heads above CPES_MAX_HEADS", fn, q_heads);
-    if (!rc && !std::isfinite(scale)) rc = fail(CPES_ERR_INVALID_ARGUMENT, "%s: scale %g is not finite", fn, (double)scale);
-    if (!rc && (window < 0 || sinks < 0))
-        rc = fail(CPES_ERR_INVALID_ARGUMENT, "%s: window %d or sinks %d negative", fn, window, sinks);
-    if (!rc && (q_stride < 0 || q_head_stride < 0 || out_stride < 0 || out_head_stride < 0))
-        rc = fail(CPES_ERR_INVALID_ARGUMENT, "%s: negative stride", fn);
     if (!rc) rc = check_workspace(workspace_dev, workspace_bytes, attend_bytes(rows, q_heads, cache->heads, cache->head_dim), fn);
     if (rc || rows == 0) return rc;
     cpes::AttendArgs a;
@@ -385,9 +442,7 @@ int cpes_attend(const cpes_cache* cache, int32_t layer, const cpes_pool* pool, i
     a.blocks = head_blocks(a.group);
     a.dim = cache->head_dim;
     a.page_size = cache->page_size;
-    a.page_shift = -1;
-    for (int b = 0; b < 31; ++b)
-        if (cache->page_size == (int32_t)1 << b) a.page_shift = b;
+    a.page_shift = page_shift(cache->page_size);
     a.pages = cache->pages;
     a.width = pool->width;
     a.sequences = pool->sequences;
@@ -481,6 +536,204 @@ int cpes_logprobs_backward(const void* x_dev, int dtype, int32_t rows, int32_t v
     a.vocab = vocab;
     a.scale = scale;
     return hip_status(cpes::launch_logprobs_backward(dtype, a, (hipStream_t)stream), fn);
+}
+
+size_t cpes_pages_keep_workspace_bytes(int32_t n, int32_t longest)
+{
+    if (n < 0 || longest < 1 || longest > CPES_MAX_TREE) return 0;
+    return round16((size_t)cpes::keep_words(n, longest + 1) * sizeof(int32_t));
+}
+
+int cpes_pages_keep(const cpes_cache* cache, const cpes_pool* pool, int32_t n, const int32_t* seqs_dev,
+                    const int32_t* starts_dev, int32_t longest, const int32_t* kept_dev, const int32_t* path_dev,
+                    void* workspace_dev, size_t workspace_bytes, int32_t* status_dev, void* stream)
+{
+    cpes::clear_error();
+    const char* fn = "cpes_pages_keep";
+    cpes::PageArgs page;                  // checked for its size
+    int rc = check_cache(cache, fn);
+    if (!rc) rc = check_pool(pool, true, fn);
+    if (!rc) rc = check_fit(cache, pool, fn);
+    if (!rc) rc = check_list(n, starts_dev && kept_dev && path_dev, fn);
+    if (!rc && n > pool->sequences)
+        rc = fail(CPES_ERR_INVALID_ARGUMENT, "%s: %d of %d sequences listed", fn, n, pool->sequences);
+    if (!rc) rc = check_longest(longest, fn);
+    if (!rc) rc = check_workspace(workspace_dev, workspace_bytes, cpes_pages_keep_workspace_bytes(n, longest), fn);
+    if (!rc) rc = page_args(cache, &page, fn);
+    if (rc) return rc;
+    const int64_t e = elem_size(cache->dtype), run = cache->head_dim * e / 16;
+    cpes::KeepArgs a;
+    a.pool = pool_args(pool);
+    a.k = page.k;
+    a.v = page.v;
+    a.seqs = seqs_dev;
+    a.starts = starts_dev;
+    a.kept = kept_dev;
+    a.path = path_dev;
+    a.ws = static_cast<int32_t*>(workspace_dev);
+    a.page_bytes = page.page_bytes;
+    a.layer_bytes = page.layer_bytes;
+    a.head_bytes = cache->head_stride * e;
+    a.token_bytes = cache->token_stride * e;
+    a.n = n;
+    a.longest = longest;
+    // `longest` tokens that begin at the end of a page, and end at the beginning of one
+    a.span = (int32_t)std::min<int64_t>(longest + 1, ((int64_t)longest - 1 + pool->page_size - 1) / pool->page_size + 1);
+    a.run = cpes::Divisor((uint32_t)run);
+    a.heads = cpes::Divisor((uint32_t)cache->heads);
+    a.units = (uint32_t)(2 * (int64_t)cache->layers * cache->heads * run);      // below a page's
+    return hip_status(cpes::launch_pages_keep(a, status_dev, (hipStream_t)stream), fn);
+}
+
+size_t cpes_attend_tree_workspace_bytes(int32_t rows, int32_t tokens, int32_t longest, int32_t q_heads, int32_t kv_heads,
+                                        int32_t head_dim)
+{
+    if (rows < 0 || rows > CPES_MAX_SEQUENCES || tokens < 0 || (tokens > 0 && (longest < 1 || longest > tokens)) ||
+        !check_heads(q_heads, kv_heads, head_dim))
+        return 0;
+    return tree_bytes(rows, cpes::tree_shape(std::max(1, longest), q_heads / kv_heads, head_dim), kv_heads, head_dim);
+}
+
+int cpes_attend_tree(const cpes_cache* cache, int32_t layer, const cpes_pool* pool, int32_t rows, const int32_t* seqs_dev,
+                     const int32_t* starts_dev, int32_t tokens, int32_t longest, const int32_t* parents_dev,
+                     const void* q_dev, int64_t q_stride, int64_t q_head_stride, int32_t q_heads, float scale,
+                     int32_t window, int32_t sinks, void* out_dev, int64_t out_stride, int64_t out_head_stride,
+                     float* lse_dev, void* workspace_dev, size_t workspace_bytes, void* stream)
+{
+    cpes::clear_error();
+    const char* fn = "cpes_attend_tree";
+    int rc = check_attend(cache, layer, pool, q_heads, scale, window, sinks, q_stride, q_head_stride, out_stride,
+                          out_head_stride, fn);
+    if (!rc) rc = check_list(rows, starts_dev, fn);
+    if (!rc && tokens < 0) rc = fail(CPES_ERR_INVALID_ARGUMENT, "%s: %d tokens", fn, tokens);
+    if (!rc && tokens > 0 && (!q_dev || !out_dev)) rc = fail(CPES_ERR_INVALID_ARGUMENT, "%s: q or out are null", fn);
+    if (!rc && tokens > 0 && (longest < 1 || longest > tokens))
+        rc = fail(CPES_ERR_INVALID_ARGUMENT, "%s: longest %d outside [1, %d]", fn, longest, tokens);
+    if (!rc && tokens > 0 && parents_dev && longest > CPES_MAX_TREE)
+        rc = fail(CPES_ERR_UNSUPPORTED, "%s: longest %d above CPES_MAX_TREE", fn, longest);
+    if (rc) return rc;
+    const cpes::TreeShape shape = cpes::tree_shape(std::max(1, longest), q_heads / cache->heads, cache->head_dim);
+    rc = check_workspace(workspace_dev, workspace_bytes, tree_bytes(rows, shape, cache->heads, cache->head_dim), fn);
+    if (rc || rows == 0 || tokens == 0) return rc;
+    cpes::TreeArgs a;
+    a.k = at_layer(cache, cache->k_dev, layer);
+    a.v = at_layer(cache, cache->v_dev, layer);
+    a.q = q_dev;
+    a.out = out_dev;
+    a.lse = lse_dev;
+    a.seqs = seqs_dev;
+    a.starts = starts_dev;
+    a.parents = parents_dev;
+    a.table = pool->table_dev;
+    a.lengths = pool->lengths_dev;
+    a.groups = tree_groups(shape, cache->head_dim);
+    a.parts = static_cast<float*>(workspace_dev);
+    a.joins = reinterpret_cast<int2*>(static_cast<char*>(workspace_dev) + tree_parts_bytes(shape, cache->head_dim));
+    a.page_stride = cache->page_stride;
+    a.head_stride = cache->head_stride;
+    a.token_stride = cache->token_stride;
+    a.table_stride = pool->table_stride;
+    a.q_stride = q_stride;
+    a.q_head_stride = q_head_stride;
+    a.out_stride = out_stride;
+    a.out_head_stride = out_head_stride;
+    a.rows = rows;
+    a.tokens = tokens;
+    a.longest = longest;
+    a.heads = cache->heads;
+    a.group = q_heads / cache->heads;
+    a.columns = shape.columns;
+    a.sets = shape.sets;
+    a.beside = shape.beside;
+    a.job_heads = shape.job_heads;
+    a.blocks = shape.blocks;
+    a.job_tokens = shape.job_tokens;
+    a.pieces = shape.pieces;
+    a.dim = cache->head_dim;
+    a.page_size = cache->page_size;
+    a.page_shift = page_shift(cache->page_size);
+    a.pages = cache->pages;
+    a.width = pool->width;
+    a.sequences = pool->sequences;
+    a.window = window;
+    a.sinks = sinks;
+    a.scale = scale;
+    return hip_status(cpes::launch_attend_tree(cache->dtype, a, (hipStream_t)stream), fn);
+}
+
+int cpes_tree_accept(int32_t rows, const int32_t* starts_dev, int32_t tokens, int32_t longest, const int32_t* parents_dev,
+                     const int64_t* drafted_dev, const int64_t* sampled_dev, int32_t* kept_dev, int32_t* path_dev,
+                     int64_t* next_dev, void* stream)
+{
+    cpes::clear_error();
+    const char* fn = "cpes_tree_accept";
+    int rc = check_list(rows, starts_dev && kept_dev && path_dev && next_dev, fn);
+    if (!rc && tokens < 0) rc = fail(CPES_ERR_INVALID_ARGUMENT, "%s: %d tokens", fn, tokens);
+    if (!rc && tokens > 0 && (!drafted_dev || !sampled_dev))
+        rc = fail(CPES_ERR_INVALID_ARGUMENT, "%s: drafted or sampled tokens are null", fn);
+    if (!rc) rc = check_longest(longest, fn);
+    if (rc || rows == 0) return rc;
+    cpes::AcceptArgs a;
+    a.starts = starts_dev;
+    a.parents = parents_dev;
+    a.drafted = drafted_dev;
+    a.sampled = sampled_dev;
+    a.kept = kept_dev;
+    a.path = path_dev;
+    a.next = next_dev;
+    a.rows = rows;
+    a.tokens = tokens;
+    a.longest = longest;
+    return hip_status(cpes::launch_tree_accept(a, (hipStream_t)stream), fn);
+}
+
+size_t cpes_sample_workspace_bytes(int32_t rows, int32_t vocab)
+{
+    if (rows < 0 || vocab < 1) return 0;
+    // the most that any number of rows up to this takes: fewer rows are cut into more slices
+    size_t most = 0;
+    for (int32_t r = 1; r <= std::min<int32_t>(rows, cpes::kMaxSlicedRows); ++r)
+        for (int dtype : {CPES_BF16, CPES_F32}) most = std::max(most, sample_bytes(r, vocab, dtype));
+    return most;
+}
+
+int cpes_sample(const void* x_dev, int dtype, int32_t rows, int32_t vocab, int64_t stride, float scale, int32_t top_k,
+                float top_p, float min_p, const float* uniforms_dev, int64_t* tokens_dev, float* logp_dev,
+                void* workspace_dev, size_t workspace_bytes, void* stream)
+{
+    cpes::clear_error();
+    const char* fn = "cpes_sample";
+    int rc = check_logits(x_dev, dtype, rows, vocab, stride, scale, fn);
+    if (!rc && rows > 0 && (!uniforms_dev || !tokens_dev))
+        rc = fail(CPES_ERR_INVALID_ARGUMENT, "%s: uniforms or tokens are null", fn);
+    if (!rc && top_k < 0) rc = fail(CPES_ERR_INVALID_ARGUMENT, "%s: top_k %d is negative", fn, top_k);
+    if (!rc && !(top_p > 0.f && top_p <= 1.f))
+        rc = fail(CPES_ERR_INVALID_ARGUMENT, "%s: top_p %g outside (0, 1]", fn, (double)top_p);
+    if (!rc && !(min_p >= 0.f && min_p <= 1.f))
+        rc = fail(CPES_ERR_INVALID_ARGUMENT, "%s: min_p %g outside [0, 1]", fn, (double)min_p);
+    if (rc) return rc;
+    rc = check_workspace(workspace_dev, workspace_bytes, sample_bytes(rows, vocab, dtype), fn);
+    if (rc || rows == 0) return rc;
+    cpes::SampleArgs a;
+    a.x = x_dev;
+    a.uniforms = uniforms_dev;
+    a.tokens = tokens_dev;
+    a.logp = logp_dev;
+    cpes::sample_split(rows, vocab, dtype, &a.slices, &a.strip_steps, &a.shift);
+    const size_t strips = (size_t)a.slices * kSampleWaves, blocks = strips * (((a.strip_steps - 1) >> a.shift) + 1);
+    a.sums = static_cast<double*>(workspace_dev);
+    a.notes = reinterpret_cast<uint16_t*>(a.sums + rows * blocks);
+    a.refs = reinterpret_cast<float*>(a.notes + rows * blocks * cpes::kSampleLanes);
+    a.most = a.refs + rows * blocks;
+    a.stride = stride;
+    a.rows = rows;
+    a.vocab = vocab;
+    a.top_k = top_k >= vocab ? 0 : top_k;
+    a.top_p = top_p;
+    a.least = min_p > 0.f ? std::log((double)min_p) : -INFINITY;
+    a.scale = scale;
+    a.c = (double)scale * M_LOG2E;
+    return hip_status(cpes::launch_sample(dtype, a, (hipStream_t)stream), fn);
 }
 
 }  // extern "C"

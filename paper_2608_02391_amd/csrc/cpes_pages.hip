@@ -1,5 +1,6 @@
 // cpes_pages.hip -- gfx950 kernels of the key-value cache's pages: handing out,
-// forking, freeing, copying and compacting them, and the entry of new tokens.
+// forking, freeing, copying and compacting them, the entry of new tokens, and of
+// drafted ones the walk that finds which stay and their way together.
 //
 // The bookkeeping (which pages are free, who gets which) is one workgroup of 1,024
 // threads, or 256, that walks the reference counts in ascending order, 16 pages
@@ -543,6 +544,195 @@ __global__ __launch_bounds__(kCopyBlock) void k_pages_compact(PageArgs c, PoolAr
     }
 }
 
+// ------------------------------------------------------------------- keep --
+// The plan claims the sequences as a reservation does, checks them and their paths,
+// and then, a thread to a page of a row's drafted tokens, notes the page for the
+// second launch and gives it back where the kept ones end before it.  In ws: whether it
+// went well; per row where its drafted tokens begin and how many stay; their pages.
+template <int BLOCK> __global__ __launch_bounds__(BLOCK) void k_pages_keep_plan(KeepArgs a, int32_t* status)
+{
+    const PoolArgs& p = a.pool;
+    int32_t* const rows = a.ws + kPagesHeader;
+    int32_t* const pages = rows + 2 * (int64_t)a.n;
+    const int tid = threadIdx.x;
+    auto seq_of = [&](int32_t i) { return a.seqs ? a.seqs[i] : i; };
+    bool bad = false, claimed = false;
+    if (a.n > BLOCK) {                    // a length that is negative before, as in a reservation
+        for (int32_t i = tid; i < a.n; i += BLOCK) bad |= known(p, seq_of(i)) && p.lengths[seq_of(i)] < 0;
+        if (__syncthreads_or(bad)) {
+            if (tid == 0) {
+                a.ws[0] = 0;
+                if (status) *status = kBadSequence;
+            }
+            return;
+        }
+    }
+    for (int32_t i = tid; i < a.n; i += BLOCK) {
+        const int32_t s = seq_of(i), kept = a.kept[i];
+        const int64_t drafted = (int64_t)a.starts[i + 1] - a.starts[i];
+        if (!known(p, s) || drafted < 0 || drafted > a.longest || kept < 0 || kept > drafted) {
+            bad = true;
+            continue;
+        }
+        const int32_t old = atomicOr(&p.lengths[s], kClaim), length = old & ~kClaim;
+        if (i == tid) claimed = old >= 0;
+        bad |= old < 0 || length < drafted || (int64_t)length > capacity(p);
+        int32_t last = -1;
+        for (int32_t j = 0; j < kept; ++j) {
+            const int32_t node = a.path[(int64_t)i * a.longest + j];
+            bad |= node <= last || node >= drafted;
+            last = node;
+        }
+        rows[2 * (int64_t)i] = length - (int32_t)drafted;
+        rows[2 * (int64_t)i + 1] = kept;
+    }
+    bad = __syncthreads_or(bad);          // and the rows are written
+    if (bad) {
+        for (int32_t i = tid; i < a.n; i += BLOCK)
+            if (a.n > BLOCK ? known(p, seq_of(i)) : claimed) atomicAnd(&p.lengths[seq_of(i)], ~kClaim);
+    } else {
+        for (int64_t at = tid; at < (int64_t)a.n * a.span; at += BLOCK) {
+            const int32_t i = (int32_t)(at / a.span), j = (int32_t)(at - (int64_t)i * a.span), s = seq_of(i);
+            const int32_t base = rows[2 * (int64_t)i], length = base + rows[2 * (int64_t)i + 1];
+            const int32_t old = p.lengths[s] & ~kClaim, slot = base / p.page_size + j;
+            int32_t page = -1;
+            if (slot < pages_of(old, p.page_size)) {
+                int32_t* const entry = row_of(p, s) + slot;
+                page = *entry;
+                if (slot >= pages_of(length, p.page_size)) {
+                    *entry = -1;
+                    if (page >= 0 && page < p.pages) atomicSub(&p.refs[page], 1);
+                }
+            }
+            pages[at] = page;
+        }
+        __syncthreads();                  // every length has been read
+        for (int32_t i = tid; i < a.n; i += BLOCK) p.lengths[seq_of(i)] = rows[2 * (int64_t)i] + rows[2 * (int64_t)i + 1];
+    }
+    if (tid == 0) {
+        a.ws[0] = !bad;
+        if (status) *status = bad ? kBadSequence : kOk;
+    }
+}
+
+// The moves, `per` workgroups a row: a thread takes a 16-byte unit of all the row's
+// tokens that move, in ascending order.  None is written to that is still to be read: the
+// j-th of an ascending path lies at j or behind it, and its place is j.
+constexpr int kKeepMoves = 4;             // of a thread under way
+
+__global__ __launch_bounds__(kCopyBlock) void k_pages_keep(KeepArgs a, int32_t per)
+{
+    __shared__ int64_t s_from[kMaxTree], s_to[kMaxTree];
+    __shared__ int32_t s_moves;
+    if (a.ws[0] == 0) return;
+    const int32_t page_size = a.pool.page_size;
+    const int32_t* const rows = a.ws + kPagesHeader;
+    for (int64_t job = blockIdx.x; job < (int64_t)a.n * per; job += gridDim.x) {
+        const int32_t i = (int32_t)(job / per), part = (int32_t)(job - (int64_t)i * per);
+        const int32_t base = rows[2 * (int64_t)i], kept = rows[2 * (int64_t)i + 1], first = base / page_size;
+        const int32_t* const pages = rows + 2 * (int64_t)a.n + (int64_t)i * a.span;
+        const int32_t j = threadIdx.x;
+        int64_t from = -1, to = -1;
+        if (j < kept) {
+            const int32_t node = a.path[(int64_t)i * a.longest + j];
+            if (node != j) {
+                auto place = [&](int32_t pos) -> int64_t {
+                    const int32_t at = pos / page_size, page = pages[at - first];
+                    return page >= 0 && page < a.pool.pages ? page * a.page_bytes + (pos - at * page_size) * a.token_bytes : -1;
+                };
+                from = place(base + node);
+                to = place(base + j);
+            }
+        }
+        // the moves in order: each wave's behind the ones before
+        const bool moves = from >= 0 && to >= 0;
+        const uint64_t mine = __ballot(moves);
+        if (threadIdx.x == 0) s_moves = 0;
+        __syncthreads();
+#pragma unroll
+        for (int w = 0; w < kCopyBlock / 64; ++w) {
+            if ((threadIdx.x >> 6) == w) {
+                const int32_t at = s_moves + __popcll(mine & ((1ull << (threadIdx.x & 63)) - 1));
+                if (moves) {
+                    s_from[at] = from;
+                    s_to[at] = to;
+                }
+                if ((threadIdx.x & 63) == 0) s_moves += __popcll(mine);
+            }
+            __syncthreads();
+        }
+        const int32_t count = s_moves;
+        for (uint32_t u = part * kCopyBlock + threadIdx.x; count > 0 && u < a.units; u += per * kCopyBlock) {
+            const uint32_t run = a.run.of(u), rest = a.heads.of(run);
+            const int64_t at = (int64_t)(u - run * a.run.d) * 16 + (int64_t)(run - rest * a.heads.d) * a.head_bytes +
+                               (int64_t)(rest >> 1) * a.layer_bytes;
+            char* const q = (rest & 1 ? a.v : a.k) + at;
+            for (int32_t m0 = 0; m0 < count; m0 += kKeepMoves) {
+                V4u x[kKeepMoves];
+#pragma unroll
+                for (int m = 0; m < kKeepMoves; ++m)
+                    if (m0 + m < count) x[m] = load16(q + s_from[m0 + m]);
+#pragma unroll
+                for (int m = 0; m < kKeepMoves; ++m)
+                    if (m0 + m < count) store16(q + s_to[m0 + m], x[m]);
+            }
+        }
+        __syncthreads();                  // the moves have been read
+    }
+}
+
+// ------------------------------------------------------------------ accept --
+// A wave a row: a lane holds up to four nodes' parents and drafted tokens, and each step
+// of the walk is a comparison and a ballot per 64 nodes.  Bound by the launch and two
+// trips to memory.
+__global__ __launch_bounds__(64) void k_tree_accept(AcceptArgs a)
+{
+    __shared__ int64_t s_sampled[kMaxTree];
+    __shared__ int32_t s_path[kMaxTree];
+    const int32_t r = blockIdx.x, lane = threadIdx.x;
+    const int64_t begin = a.starts[r], nodes = a.starts[r + 1] - begin;
+    int32_t* const path = a.path + (int64_t)r * a.longest;
+    int32_t kept = 0;
+    int64_t next = -1;
+    if (begin >= 0 && nodes > 0 && nodes <= a.longest && begin + nodes <= a.tokens) {
+        int32_t parent[kMaxTree / 64];
+        int64_t drafted[kMaxTree / 64];
+#pragma unroll
+        for (int b = 0; b < kMaxTree / 64; ++b) {
+            const int32_t i = b * 64 + lane;
+            parent[b] = -1;
+            drafted[b] = 0;
+            if (i < nodes) {
+                parent[b] = a.parents ? a.parents[begin + i] : i - 1;
+                if (parent[b] >= i) parent[b] = -1;
+                drafted[b] = a.drafted[begin + i];
+                s_sampled[i] = a.sampled[begin + i];
+            }
+        }
+        __syncthreads();
+        int32_t at = 0;
+        while (at >= 0) {
+            next = s_sampled[at];
+            if (lane == 0) s_path[kept] = at;
+            ++kept;
+            int32_t below = -1;
+#pragma unroll
+            for (int b = 0; b < kMaxTree / 64; ++b) {
+                // a node hangs from one before it, so the walk ascends and ends
+                const uint64_t those = __ballot(parent[b] == at && drafted[b] == next);
+                if (below < 0 && those) below = b * 64 + __ffsll((unsigned long long)those) - 1;
+            }
+            at = below;
+        }
+        __syncthreads();
+    }
+    for (int32_t j = lane; j < a.longest; j += 64) path[j] = j < kept ? s_path[j] : -1;
+    if (lane == 0) {
+        a.kept[r] = kept;
+        a.next[r] = next;
+    }
+}
+
 // ----------------------------------------------------------------- append --
 // `per` tokens a workgroup; where each goes is found once and kept in LDS, then
 // the threads move the tokens' 16-byte units, key and value together.  Bound by HBM, or
@@ -656,6 +846,26 @@ hipError_t launch_pages_compact(const PageArgs& c, const PoolArgs& p, const Pool
         hipLaunchKernelGGL(k_pages_compact<true>, grid, block, 0, s, c, p, packed, ws);
     else
         hipLaunchKernelGGL(k_pages_compact<false>, grid, block, 0, s, c, p, packed, ws);
+    return hipGetLastError();
+}
+
+hipError_t launch_pages_keep(const KeepArgs& a, int32_t* status, hipStream_t s)
+{
+    if (small_plan(a.pool, a.n, kSmallPlan))
+        hipLaunchKernelGGL(k_pages_keep_plan<kSmallPlan>, dim3(1), dim3(kSmallPlan), 0, s, a, status);
+    else
+        hipLaunchKernelGGL(k_pages_keep_plan<kPlanBlock>, dim3(1), dim3(kPlanBlock), 0, s, a, status);
+    hipError_t e = hipGetLastError();
+    if (e != hipSuccess || a.n == 0) return e;
+    const int32_t per = std::max<int32_t>(1, std::min<int64_t>((a.units + kCopyBlock - 1) / kCopyBlock, 4 * kCopyGrid / a.n));
+    hipLaunchKernelGGL(k_pages_keep, dim3((unsigned)std::min<int64_t>((int64_t)a.n * per, 4 * kCopyGrid)), dim3(kCopyBlock), 0,
+                       s, a, per);
+    return hipGetLastError();
+}
+
+hipError_t launch_tree_accept(const AcceptArgs& a, hipStream_t s)
+{
+    hipLaunchKernelGGL(k_tree_accept, dim3((unsigned)a.rows), dim3(64), 0, s, a);
     return hipGetLastError();
 }
 

@@ -1,0 +1,264 @@
+"""Tokens drawn from rows of logits by given numbers, against a plain draw in 64 bits."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+import draft_helpers as D
+import paper_2608_02391_amd as cp
+
+pytestmark = pytest.mark.gpu
+BF16, F32 = torch.bfloat16, torch.float32
+
+# Weights are off by 2^-39 at most and sums by some roundings of 64 bits: a draw nearer than this to a
+# border (of the tokens, or of what top_p keeps), relative to the sum, may fall on either side.
+NEAR = 2.0 ** -38
+
+
+def run(x, u, top_k=0, top_p=1.0, min_p=0.0, scale=1.0, stream=None, logp=True):
+    rows, vocab = x.shape
+    ws = torch.full((cp.cpes_sample_workspace_bytes(rows, vocab),), 0xFF, dtype=torch.uint8, device="cuda")
+    token = torch.full((rows,), -7, dtype=torch.int64, device="cuda")
+    lp = torch.full((rows,), 77.0, device="cuda") if logp else None
+    cp.cpes_sample(x, u, token, logp=lp, scale=scale, top_k=top_k, top_p=top_p, min_p=min_p, workspace=ws, stream=stream)
+    return token, lp
+
+
+def check(x, u, rows=None, **kw):
+    """The draw of every row (or of some), but for those on a border; their number is returned."""
+    token, logp = run(x, u, **kw)
+    token, logp, host, hu, near = token.cpu(), logp.cpu(), x.double().cpu().numpy(), u.cpu().tolist(), 0
+    for r in range(len(host)) if rows is None else rows:
+        ref, ref_logp, margin = D.draw(host[r], hu[r], **kw)
+        if margin < NEAR and int(token[r]) != ref:
+            near += 1
+            continue
+        assert int(token[r]) == ref, (r, int(token[r]), ref, hu[r], margin, kw)
+        if math.isnan(ref_logp):
+            assert math.isnan(float(logp[r]))
+        elif ref < 0:
+            assert float(logp[r]) == ref_logp
+        elif margin >= NEAR:
+            # 64-bit sums as above, then one rounding to 32 bits
+            assert abs(float(logp[r]) - ref_logp) <= 2.0 ** -24 * abs(ref_logp) + 2.0 ** -37, (r, float(logp[r]), ref_logp, kw)
+    assert near <= 1
+    return token, logp
+
+
+def logits(rows, vocab, dtype, seed=0, std=2.5, likely=8):
+    g = torch.Generator().manual_seed(seed)
+    x = torch.randn(rows, vocab, generator=g) * std
+    for i in range(min(likely, vocab)):
+        x[torch.arange(rows), torch.randint(0, vocab, (rows,), generator=g)] = 14.0 - 1.5 * math.log(i + 1) + 0.1 * torch.randn(rows, generator=g)
+    return x.to(dtype).cuda(), torch.rand(rows, generator=g).cuda()
+
+
+FILTERS = [dict(), dict(top_k=1), dict(top_k=7), dict(top_p=0.9), dict(min_p=0.05), dict(top_k=20, top_p=0.8),
+           dict(top_p=0.95, min_p=0.02, scale=0.7), dict(top_k=50, top_p=0.6, min_p=0.3, scale=1.5), dict(top_k=9, min_p=0.2),
+           dict(scale=0.6), dict(top_p=0.3, scale=1.3), dict(min_p=1.0)]
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32], ids=["bf16", "fp32"])
+@pytest.mark.parametrize("vocab", [1, 2, 7, 8, 9, 300, 511, 2047, 2048, 2049, 8191, 8200, 32768, 50257])
+def test_vocabularies(vocab, dtype):
+    print(f"sample vocab={vocab} {dtype}", flush=True)
+    for i, f in enumerate(FILTERS):
+        x, u = logits(9, vocab, dtype, seed=vocab + i)
+        check(x, u, **f)
+
+
+@pytest.mark.parametrize("rows", [1, 2, 40, 256, 257, 600])
+@pytest.mark.parametrize("filters", FILTERS[:7], ids=lambda f: ",".join(f) or "none")
+def test_rows(rows, filters):
+    """Rows cut into slices, and whole ones."""
+    print(f"sample rows={rows} {filters}", flush=True)
+    x, u = logits(rows, 40000, BF16, seed=rows)
+    check(x, u, rows=range(0, rows, max(1, rows // 40)), **filters)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32], ids=["bf16", "fp32"])
+@pytest.mark.parametrize("rows", [3, 300])
+def test_large_vocabulary(dtype, rows):
+    x, u = logits(rows, 151936, dtype, seed=rows, likely=200)
+    for f in FILTERS:
+        check(x, u, rows=range(0, rows, max(1, rows // 12)), **f)
+
+
+@pytest.mark.parametrize("filters", [dict(top_p=0.95), dict(top_k=400), dict(top_k=3000), dict(top_k=1000, top_p=0.7), dict(min_p=0.001),
+                                     dict(top_p=0.999, min_p=1e-4), dict(top_p=0.5, scale=0.25), dict(top_k=20000, min_p=0.01)],
+                         ids=lambda f: ",".join(f"{k}={v}" for k, v in f.items()))
+@pytest.mark.parametrize("dtype,rows,vocab", [(BF16, 5, 30000), (F32, 5, 30000), (BF16, 300, 9000), (F32, 300, 9001), (BF16, 2, 151936)])
+def test_flat_rows(dtype, rows, vocab, filters):
+    """Thousands of tokens stay: the bounding key is found by its digits."""
+    print(f"sample flat {dtype} {rows}x{vocab} {filters}", flush=True)
+    x, u = logits(rows, vocab, dtype, seed=vocab, likely=0)
+    check(x, u, rows=range(0, rows, max(1, rows // 10)), **filters)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32], ids=["bf16", "fp32"])
+@pytest.mark.parametrize("vocab", [100, 5000, 40000])
+def test_ties(vocab, dtype):
+    """Equal logits stay by the lowest token: all alike, few values, signs of zero."""
+    g = torch.Generator().manual_seed(vocab)
+    u = torch.rand(6, generator=g).cuda()
+    same = torch.full((6, vocab), 1.25).to(dtype).cuda()
+    few = torch.randint(0, 3, (6, vocab), generator=g).to(dtype).cuda()
+    zeros = torch.where(torch.rand(6, vocab, generator=g) < 0.5, torch.tensor(0.0), torch.tensor(-0.0)).to(dtype).cuda()
+    for x in (same, few, zeros):
+        for f in [dict(), dict(top_k=1), dict(top_k=5), dict(top_k=vocab - 1), dict(top_p=0.25), dict(top_k=60, top_p=0.5), dict(min_p=1.0),
+                  dict(min_p=0.9, top_k=3), dict(top_k=700, top_p=0.33)]:
+            token, _ = check(x, u, **f)
+            if f == dict(top_k=1):
+                assert torch.equal(token, x.float().cpu().argmax(-1))
+
+
+def test_values_close_together():
+    """fp32 logits that one bf16 number stands for."""
+    g = torch.Generator().manual_seed(5)
+    for sign in (1, -1):
+        x = (sign * 5.0 + torch.rand(8, 20000, generator=g) * 2e-4).cuda()
+        u = torch.rand(8, generator=g).cuda()
+        for f in (dict(top_k=1), dict(top_k=3), dict(top_k=40), dict(top_k=300, top_p=0.5), dict(top_p=0.001), dict(top_p=0.5),
+                  dict(top_k=50, scale=3e4), dict(min_p=0.9999), dict(top_p=0.9, scale=1e5), dict(scale=1e5)):
+            check(x, u, **f)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32], ids=["bf16", "fp32"])
+@pytest.mark.parametrize("rows", [12, 300])
+def test_masks_and_broken_rows(dtype, rows):
+    """-inf is never chosen; rows of nothing else, with NaN or +inf; the type's lowest value is a number."""
+    x, u = logits(rows, 20000, dtype, seed=3)
+    inf, lowest = math.inf, torch.finfo(dtype).min
+    x[0] = -inf
+    x[1, 7:] = -inf
+    x[2, :19999] = -inf
+    x[3, 100] = math.nan
+    x[4, 19999] = inf
+    x[5] = -inf
+    x[5, 3] = math.nan
+    x[6] = lowest
+    x[6, ::3] = -inf
+    x[7] = -inf
+    x[7, 12345] = lowest
+    x[8, ::2] = -inf
+    x[9, 5000:] = lowest
+    x[10, :] = -3e38
+    x[10, 11] = 3e38
+    x[11] = -inf
+    x[11, 9000:9040] = 4.0
+    for f in FILTERS + [dict(top_p=0.99, scale=0.25), dict(top_k=3000)]:
+        token, logp = check(x, u, rows=range(12), **f)
+        assert int(token[0]) == -1 and float(logp[0]) == -inf and token[3:6].tolist() == [-1, -1, -1]
+        assert bool(torch.isnan(logp[3:6]).all()) and int(token[2]) == 19999 and int(token[7]) == 12345
+        assert float(logp[2]) == 0.0 and float(logp[7]) == 0.0
+
+
+@pytest.mark.parametrize("filters", [dict(), dict(top_k=4), dict(top_p=0.9), dict(top_p=0.95, scale=0.2), dict(min_p=0.1)],
+                         ids=lambda f: ",".join(f) or "none")
+def test_ends_of_the_uniform_numbers(filters):
+    """0 and below, NaN, the last number below 1, 1 and above."""
+    us = [0.0, -0.0, -3.0, math.nan, 1 - 2.0 ** -24, 1.0, 7.0, math.inf, -math.inf, 2.0 ** -149]
+    for dtype in (BF16, F32):
+        for rows in (10, 300):
+            x, _ = logits(rows, 9000, dtype, seed=6)
+            x[:, :2200] = -math.inf
+            x[:, 8000:] = -math.inf
+            u = torch.tensor((us * 30)[:rows]).cuda()
+            token, _ = check(x, u, rows=range(10), **filters)
+            assert int(token.min()) >= 2200 and int(token.max()) < 8000
+
+
+@pytest.mark.parametrize("scale", [1e-30, 1e-6, 0.01, 30.0, 1e4, 1e20, 1.7e38])
+@pytest.mark.parametrize("dtype", [BF16, F32], ids=["bf16", "fp32"])
+def test_scales(scale, dtype):
+    """From a uniform draw over what is not forbidden to the most likely token alone."""
+    x, u = logits(6, 9000, dtype, seed=7)
+    x[1, 4000:] = -math.inf
+    x[2] *= 1e30
+    x[3] *= 1e-30
+    for f in (dict(), dict(top_k=6), dict(top_p=0.7), dict(min_p=0.5), dict(top_k=5, top_p=0.5)):
+        check(x, u, scale=scale, **f)
+
+
+def test_strides_alignment_and_missing_outputs():
+    g = torch.Generator().manual_seed(8)
+    for dtype in (BF16, F32):
+        wide = torch.randn(7 * 3001 + 5, generator=g).to(dtype).cuda()
+        x = wide[5:].view(7, 3001)[:, :2999]
+        u = torch.rand(7, generator=g).cuda()
+        for f in FILTERS:
+            token, _ = check(x, u, **f)
+            alone, _ = run(x, u, logp=False, **f)
+            assert torch.equal(alone.cpu(), token)
+    one = torch.randn(4000, generator=g).cuda()
+    check(one[None], u[:1], top_k=30)
+    check(one[None].expand(1, -1), u[:1])
+    empty = torch.empty(0, 100, device="cuda")
+    run(empty, torch.empty(0, device="cuda"))
+
+
+def test_a_row_does_not_depend_on_the_others():
+    """A row's draw is the same among few rows (cut into slices) and among many, but on a border."""
+    x, u = logits(400, 30000, BF16, seed=9)
+    for f in FILTERS:
+        many, many_logp = run(x, u, **f)
+        few, few_logp = run(x[:3], u[:3], **f)
+        assert torch.equal(many[:3], few) and float((many_logp[:3] - few_logp).abs().max()) <= 2.0 ** -23 * float(few_logp.abs().max()) + 2.0 ** -36
+        again, again_logp = run(x, u, **f)
+        assert torch.equal(many, again) and torch.equal(many_logp, again_logp)
+
+
+def test_draws_follow_the_distribution():
+    """A grid of uniform numbers draws each token as often as its probability says, up to one."""
+    x = torch.tensor([1.0, -math.inf, 3.0, 2.5, 0.0, 2.0], dtype=F32)
+    n = 4096
+    u = ((torch.arange(n) + 0.5) / n).float().cuda()
+    token, logp = run(x.expand(n, -1).contiguous().cuda(), u, scale=0.8)
+    p = torch.softmax(x.double() * float(np.float32(0.8)), -1)
+    count = torch.bincount(token.cpu(), minlength=6)
+    assert float((count - n * p).abs().max()) <= 1.0 + 1e-6
+    assert bool((logp.cpu().double() - p.log()[token.cpu()]).abs().max() < 1e-6)
+
+
+def test_captured_draws():
+    """Replays read the logits and numbers of the moment; streams are respected."""
+    for rows in (2, 300):
+        x, u = logits(rows, 40000, BF16, seed=10)
+        ws = torch.empty(cp.cpes_sample_workspace_bytes(rows, 40000), dtype=torch.uint8, device="cuda")
+        for f in (dict(), dict(top_k=20, top_p=0.9), dict(top_p=0.9, scale=0.3)):
+            token, logp = torch.empty(rows, dtype=torch.int64, device="cuda"), torch.empty(rows, device="cuda")
+            cp.cpes_sample(x, u, token, logp=logp, workspace=ws, **f)
+            torch.cuda.synchronize()
+            graph = torch.cuda.CUDAGraph()
+            with torch.cuda.graph(graph):
+                cp.cpes_sample(x, u, token, logp=logp, workspace=ws, **f)
+            for turn in range(3):
+                fresh, fu = logits(rows, 40000, BF16, seed=20 + turn)
+                x.copy_(fresh)
+                u.copy_(fu)
+                token.fill_(-9)
+                graph.replay()
+                torch.cuda.synchronize()
+                eager, eager_logp = run(x, u, **f)
+                assert torch.equal(token, eager) and torch.equal(logp, eager_logp)
+
+
+def test_many_logits():
+    """A row of more than 2^27 tokens, and rows that begin beyond 2^32 bytes."""
+    n = (1 << 27) + 12345
+    x = torch.zeros(1, n, dtype=BF16, device="cuda")
+    x[0, n - 3] = 30.0
+    token, logp = run(x, torch.tensor([0.5], device="cuda"))
+    total = math.exp(-30.0) * (n - 1) + 1
+    assert int(token) == n - 3 and abs(float(logp) + math.log(total)) < 1e-6
+    token, _ = run(x, torch.tensor([0.5], device="cuda"), top_k=4, scale=1e-3)
+    assert int(token) in (0, 1, 2, n - 3)
+    token, _ = run(x[:, :1 << 27], torch.tensor([0.75], device="cuda"))
+    assert int(token) == 3 << 25
+    del x
+    rows, vocab = 9, 1 << 28
+    y = torch.zeros(rows, vocab, dtype=BF16, device="cuda")
+    y[8, 99] = 40.0
+    token, _ = run(y, torch.full((rows,), 0.5, device="cuda"))
+    assert int(token[8]) == 99 and bool((token[:8] == vocab // 2).all())
