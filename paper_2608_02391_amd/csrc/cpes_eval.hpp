@@ -206,7 +206,15 @@ struct LogprobArgs {
 };
 
 constexpr int kSampleLanes = 64;
-constexpr int kSampleBlocks = 256;       // blocks of a row at most, a sum each, and 64 maxima
+constexpr int kSampleWaves = 4;          // strips of a slice, where a row is cut into slices
+constexpr int kSampleBlocks = 256;       // blocks of such a row at most
+constexpr int kSampleRows = 1024;        // more rows are all cut alike
+
+// How a row of logits is cut: into slices of a workgroup (0: one wave does the row), strips
+// of a wave, blocks of 2^shift steps.
+struct SampleSplit {
+    int32_t slices, waves, strip_steps, shift, blocks;
+};
 
 struct SampleArgs {
     const void* x;
@@ -214,14 +222,13 @@ struct SampleArgs {
     int64_t* tokens;
     float* logp;
     uint16_t* notes;             // [rows][blocks][64]: maxima of 64 parts of each block
+    uint16_t* samples;           // [rows][blocks][64]: a logit of each of these parts
     double* sums;                // [rows][blocks]
     float* refs;                 // [rows][blocks]: what the sums' exponents are relative to
     float* most;                 // [rows][strips]: maxima, NaN where there is one
     int64_t stride;
     int32_t rows, vocab;
-    int32_t slices;              // workgroups of a row, kSampleWaves strips each
-    int32_t strip_steps;         // steps of a strip
-    int32_t shift;               // 2^shift steps a block
+    int32_t slices, waves, strip_steps, shift;
     int32_t top_k;               // 0: all
     double top_p;
     double least;                // ln min_p, or -inf
@@ -256,7 +263,7 @@ hipError_t launch_append(const AppendArgs& a, hipStream_t s);
 hipError_t launch_attend(int dtype, const AttendArgs& a, hipStream_t s);
 int logprob_slices(int32_t rows, int32_t vocab, int dtype, int32_t* per_slice);
 hipError_t launch_attend_tree(int dtype, const TreeArgs& a, hipStream_t s);
-void sample_split(int32_t rows, int32_t vocab, int dtype, int32_t* slices, int32_t* strip_steps, int32_t* shift);
+SampleSplit sample_split(int32_t rows, int32_t vocab, int dtype);
 hipError_t launch_sample(int dtype, const SampleArgs& a, hipStream_t s);
 hipError_t launch_logprobs(int dtype, const LogprobArgs& a, hipStream_t s);
 hipError_t launch_logprobs_backward(int dtype, const LogprobGradArgs& a, hipStream_t s);

@@ -239,15 +239,12 @@ size_t attend_bytes(int32_t rows, int32_t q_heads, int32_t kv_heads, int32_t hea
     return round16(attend_parts_bytes(head_dim) + (size_t)rows * kv_heads * head_blocks(q_heads / kv_heads) * sizeof(int2));
 }
 
-constexpr int kSampleWaves = 4;          // strips of a slice
-
 size_t sample_bytes(int32_t rows, int32_t vocab, int dtype)
 {
-    int32_t slices, steps, shift;
-    cpes::sample_split(rows, vocab, dtype, &slices, &steps, &shift);
-    if (slices == 1) return 0;
-    const size_t strips = (size_t)slices * kSampleWaves, blocks = strips * (((steps - 1) >> shift) + 1);
-    return rows * round16(blocks * (cpes::kSampleLanes * sizeof(uint16_t) + sizeof(double) + sizeof(float)) + strips * sizeof(float));
+    const cpes::SampleSplit x = cpes::sample_split(rows, vocab, dtype);
+    if (x.slices == 0) return 0;
+    return rows * round16((size_t)x.blocks * (2 * cpes::kSampleLanes * sizeof(uint16_t) + sizeof(double) + sizeof(float)) +
+                          (size_t)x.slices * x.waves * sizeof(float));
 }
 
 size_t logprob_bytes(int32_t rows, int32_t slices, int32_t top)
@@ -692,8 +689,10 @@ size_t cpes_sample_workspace_bytes(int32_t rows, int32_t vocab)
     if (rows < 0 || vocab < 1) return 0;
     // the most that any number of rows up to this takes: fewer rows are cut into more slices
     size_t most = 0;
-    for (int32_t r = 1; r <= std::min<int32_t>(rows, cpes::kMaxSlicedRows); ++r)
-        for (int dtype : {CPES_BF16, CPES_F32}) most = std::max(most, sample_bytes(r, vocab, dtype));
+    for (int dtype : {CPES_BF16, CPES_F32}) {
+        for (int32_t r = 1; r <= std::min<int32_t>(rows, cpes::kSampleRows); ++r) most = std::max(most, sample_bytes(r, vocab, dtype));
+        most = std::max(most, sample_bytes(rows, vocab, dtype));
+    }
     return most;
 }
 
@@ -719,12 +718,17 @@ int cpes_sample(const void* x_dev, int dtype, int32_t rows, int32_t vocab, int64
     a.uniforms = uniforms_dev;
     a.tokens = tokens_dev;
     a.logp = logp_dev;
-    cpes::sample_split(rows, vocab, dtype, &a.slices, &a.strip_steps, &a.shift);
-    const size_t strips = (size_t)a.slices * kSampleWaves, blocks = strips * (((a.strip_steps - 1) >> a.shift) + 1);
-    a.sums = static_cast<double*>(workspace_dev);
-    a.notes = reinterpret_cast<uint16_t*>(a.sums + rows * blocks);
-    a.refs = reinterpret_cast<float*>(a.notes + rows * blocks * cpes::kSampleLanes);
-    a.most = a.refs + rows * blocks;
+    const cpes::SampleSplit split = cpes::sample_split(rows, vocab, dtype);
+    a.slices = split.slices;
+    a.waves = split.waves;
+    a.strip_steps = split.strip_steps;
+    a.shift = split.shift;
+    const size_t blocks = (size_t)rows * split.blocks;
+    a.notes = static_cast<uint16_t*>(workspace_dev);            // 16 bytes at a time
+    a.samples = a.notes + blocks * cpes::kSampleLanes;
+    a.sums = reinterpret_cast<double*>(a.samples + blocks * cpes::kSampleLanes);
+    a.refs = reinterpret_cast<float*>(a.sums + blocks);
+    a.most = a.refs + blocks;
     a.stride = stride;
     a.rows = rows;
     a.vocab = vocab;

@@ -35,17 +35,22 @@ namespace cpes {
 namespace {
 
 typedef unsigned int V4u __attribute__((ext_vector_type(4)));
+typedef unsigned int V2u __attribute__((ext_vector_type(2)));
 typedef V4u V4uAnywhere __attribute__((aligned(2)));
 typedef unsigned long long Key;
 
-constexpr int kWaves = 4;                 // of a reading workgroup, a strip each
 constexpr int kUnroll = 4;                // vectors of a lane and step
 constexpr int kCandidates = 512;          // tokens that are ranked
-constexpr int kDigit = 11;                // bits of a key that one reading settles
-constexpr int kBins = 1 << kDigit;
+constexpr int kParts = 384;               // parts of blocks that are read again for them
+constexpr int kFirstParts = 48;           // and how many at first, where top_p decides
+constexpr int kCounted = 128;             // keys ranked by counting
+constexpr int kDepth = 8;                 // vectors of a thread under way where the row is read again
 constexpr int64_t kMaxGrid = 1 << 20;
+constexpr int kFewRows = 256;
+constexpr int kManyBlocks = 96;          // of a row among many
+constexpr int kReadGroups = 1024;        // workgroups that read few rows
 constexpr double kExact = 2048.0;         // c x up to which the rounding of c max x, 2^-42, is let through
-constexpr double kFar = -900.0;           // weights below 2^kFar of the largest count as 0
+constexpr double kFar = -100.0;           // weights below 2^kFar of the largest count as 0
 
 template <typename T> struct Vec { static constexpr int n = 16 / sizeof(T); };
 
@@ -122,6 +127,103 @@ __device__ __forceinline__ double power(double t, const double* table)
     return __longlong_as_double(__double_as_longlong(w) + ((long long)(int)(k & ~31u) << 47));
 }
 
+// The same for the pass over the logits, which does little else: 2^(k / 16) for all k there
+// are, so that no exponent has to be put together, and a series off by (ln 2 / 32)^5 / 120 =
+// 4e-11 at most, to either side.  Relative to some logit of the wave's, exponents go from
+// kLow, which stands for what is below and gives 0, to kRoom.
+constexpr int kLow = -112, kRoom = 15, kSteps = 16;
+constexpr int kPowers = (kRoom + 1 - kLow) * kSteps;
+
+template <int K> __device__ __forceinline__ void fill_powers(double* powers)
+{
+    for (int i = threadIdx.x; i < kPowers; i += K)
+        powers[i] = i == 0 ? 0.0 : ldexp(kTwoTo[2 * (i % kSteps)], i / kSteps + kLow);
+}
+
+__device__ __forceinline__ double quick_power(double t, const double* powers)
+{
+    constexpr double kRound = 0x1.8p+48 - kLow;         // 1.5 2^52 / 16, and the table's beginning: the low bits are its index
+    constexpr double a1 = 0.69314718055994530942, a2 = a1 * a1 / 2, a3 = a2 * a1 / 3, a4 = a3 * a1 / 4;
+    const double y = t + kRound, r = t - (y - kRound);
+    const double f = powers[(uint32_t)__double_as_longlong(y)];
+    const double p = r * fma(r, fma(r, fma(r, a4, a3), a2), a1);
+    return fma(f, p, f);
+}
+
+// The logits of a vector one after the other, so that a loop over them need not be unrolled: most
+// of what is behind the pass over the logits runs once a row, and what such code costs is its way
+// into the instruction cache (the whole of it unrolled: a row's rest in 27 us, so in 12).
+template <typename T> struct Logits {
+    V4u w;
+
+    __device__ __forceinline__ float next()
+    {
+        if constexpr (std::is_same<T, uint16_t>::value) {
+            const float x = __uint_as_float(w[0] << 16);
+            w[0] = __builtin_amdgcn_alignbit(w[1], w[0], 16);
+            w[1] = __builtin_amdgcn_alignbit(w[2], w[1], 16);
+            w[2] = __builtin_amdgcn_alignbit(w[3], w[2], 16);
+            w[3] >>= 16;
+            return x;
+        } else {
+            const float x = __uint_as_float(w[0]);
+            w[0] = w[1];
+            w[1] = w[2];
+            w[2] = w[3];
+            return x;
+        }
+    }
+};
+
+// Vector i of a row of `count` logits; -inf behind its end.
+template <typename T> __device__ __forceinline__ V4u vector_at(const T* x0, int64_t count, int64_t i)
+{
+    constexpr int N = Vec<T>::n;
+    if ((i + 1) * N <= count) return *reinterpret_cast<const V4uAnywhere*>(x0 + i * N);
+    constexpr uint32_t kNone = std::is_same<T, uint16_t>::value ? 0xFF80FF80u : 0xFF800000u;
+    V4u w = {kNone, kNone, kNone, kNone};
+#pragma unroll
+    for (int j = 0; j < N; ++j)
+        if (i * N + j < count) {
+            const T x = x0[i * N + j];
+            if constexpr (std::is_same<T, uint16_t>::value)
+                w[j >> 1] = j & 1 ? (w[j >> 1] & 0xFFFFu) | (uint32_t)x << 16 : (w[j >> 1] & 0xFFFF0000u) | x;
+            else
+                w[j] = __float_as_uint(x);
+        }
+    return w;
+}
+
+// x of the lane that the DPP control names, 0 where there is none.
+template <int CONTROL, int ROWS, typename X> __device__ __forceinline__ X from_lane(X x)
+{
+    if constexpr (sizeof(X) == 4) {
+        return __builtin_bit_cast(X, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, x), CONTROL, ROWS, 0xF, false));
+    } else {
+        const V2u v = __builtin_bit_cast(V2u, x);
+        V2u y;
+        y[0] = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v[0], CONTROL, ROWS, 0xF, false);
+        y[1] = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v[1], CONTROL, ROWS, 0xF, false);
+        return __builtin_bit_cast(X, y);
+    }
+}
+
+// Sum over the wave's lanes up to and including each: rows of 16 by shifts, then each row's last lane
+// to the next row, and the second row's to the upper half.
+template <typename X> __device__ __forceinline__ X wave_scan(X x)
+{
+    x += from_lane<0x111, 0xF>(x);
+    x += from_lane<0x112, 0xF>(x);
+    x += from_lane<0x114, 0xF>(x);
+    x += from_lane<0x118, 0xF>(x);
+    x += from_lane<0x142, 0xA>(x);
+    x += from_lane<0x143, 0xC>(x);
+    return x;
+}
+
+// The wave's sum, in lane 63.
+template <typename X> __device__ __forceinline__ X wave_sum(X x) { return wave_scan(x); }
+
 // What a strip's tokens are, as vectors: [first, last), with `behind` tokens short of whole ones.
 template <typename T> struct Strip {
     int64_t first;        // vector
@@ -137,35 +239,16 @@ template <typename T> struct Strip {
     }
 };
 
-// Vector i of a row as floats; -inf behind the row's end.
-template <typename T> __device__ __forceinline__ void floats_at(const T* x0, int32_t vocab, int64_t i, float* x)
-{
-    constexpr int N = Vec<T>::n;
-    if ((i + 1) * N <= vocab) {
-        unpack<T>(*reinterpret_cast<const V4uAnywhere*>(x0 + i * N), x);
-    } else {
-#pragma unroll
-        for (int j = 0; j < N; ++j) x[j] = i * N + j < vocab ? value_of(x0[i * N + j]) : -__builtin_inff();
-    }
-}
-
 __device__ __forceinline__ int32_t blocks_of_strip(const SampleArgs& a)
 {
     return ((a.strip_steps - 1) >> a.shift) + 1;
 }
 
-__device__ __forceinline__ double wave_sum(double x)
-{
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) x += __shfl_xor(x, d);
-    return x;
-}
-
-// One strip, by a wave: notes, sums and what they are relative to, of its blocks; the
-// strip's maximum is returned to all lanes.
-template <typename T, bool kSums>
-__device__ float read_strip(const SampleArgs& a, const T* x0, int32_t strip, const double* table, uint16_t* notes, double* sums,
-                            float* refs)
+// One strip, by a wave: notes, samples, sums and what they are relative to, of its blocks;
+// the strip's maximum is returned to all lanes.  NT: past the caches.
+template <typename T, bool kSums, bool NT, bool kQuick>
+__device__ float read_strip(const SampleArgs& a, const T* x0, int32_t strip, const double* powers, const double* table,
+                            uint16_t* notes, uint16_t* samples, double* sums, float* refs)
 {
     constexpr int N = Vec<T>::n, M = kUnroll * N;
     const int lane = threadIdx.x & 63;
@@ -174,14 +257,20 @@ __device__ float read_strip(const SampleArgs& a, const T* x0, int32_t strip, con
     const int32_t whole = (int32_t)max((int64_t)0, min((int64_t)s.steps, ((int64_t)a.vocab / N - s.first) / (kSampleLanes * kUnroll)));
     float most = -__builtin_inff(), ref = -__builtin_inff(), noted = -__builtin_inff();
     double sum = 0.0, base = 0.0;
-    // exponents up to 64 above what they are relative to are let through
-    const float room = (float)fmin(64.0 / a.c, 1e38);
+    const float room = (float)fmin(kRoom / a.c, 1e38);
     V4u w[kUnroll];
     auto load = [&](int32_t step) {
-        const T* const q = x0 + (s.first + (int64_t)step * (kSampleLanes * kUnroll) + lane) * N;
+        const int64_t i = s.first + (int64_t)step * (kSampleLanes * kUnroll) + lane;
 #pragma unroll
-        for (int u = 0; u < kUnroll; ++u) w[u] = *reinterpret_cast<const V4uAnywhere*>(q + u * kSampleLanes * N);
+        for (int u = 0; u < kUnroll; ++u) {
+            const V4uAnywhere* const at = reinterpret_cast<const V4uAnywhere*>(x0 + (i + u * kSampleLanes) * N);
+            if (step < whole)
+                w[u] = NT ? __builtin_nontemporal_load(at) : *at;
+            else
+                w[u] = vector_at(x0, a.vocab, i + u * kSampleLanes);
+        }
     };
+    auto term = [&](double t) { return kQuick ? quick_power(t, powers) : t > kLow ? power(t, table) : 0.0; };
     auto take = [&](const float* x) {
         float top = x[0];
 #pragma unroll
@@ -195,7 +284,8 @@ __device__ float read_strip(const SampleArgs& a, const T* x0, int32_t strip, con
 #pragma unroll
                 for (int d = 1; d < 64; d <<= 1) high = fmaxf(high, __shfl_xor(high, d));
                 if (high < __builtin_inff()) {
-                    if (ref > -__builtin_inff()) sum *= power(fmax(a.c * ((double)ref - (double)high), kFar), table);
+                    const double t = a.c * ((double)ref - (double)high);
+                    sum = t < 2 * kLow ? 0.0 : sum * power(t, table);
                     ref = high;
                     base = a.c * (double)ref;
                 }
@@ -203,46 +293,40 @@ __device__ float read_strip(const SampleArgs& a, const T* x0, int32_t strip, con
             if (fabs(base) <= kExact) {
                 if (ref > -__builtin_inff()) {
 #pragma unroll
-                    for (int j = 0; j < M; ++j) sum += power(fmax(fma((double)x[j], a.c, -base), kFar - 100.0), table);
+                    for (int j = 0; j < M; ++j) sum += term(fmax(fma((double)x[j], a.c, -base), (double)kLow));
                 }
             } else {
 #pragma unroll
-                for (int j = 0; j < M; ++j) sum += power(fmax(((double)x[j] - (double)ref) * a.c, kFar - 100.0), table);
+                for (int j = 0; j < M; ++j) sum += term(fmax(((double)x[j] - (double)ref) * a.c, (double)kLow));
             }
         }
     };
-    auto end_block = [&](int32_t step) {
+    auto end_block = [&](int32_t step, float sample) {
         const int32_t b = step >> a.shift;
         notes[b * 64 + lane] = note_of(noted);
+        samples[b * 64 + lane] = note_of(sample);
         noted = -__builtin_inff();
         if constexpr (kSums) {
             const double all = wave_sum(sum);
-            if (lane == 0) {
-                sums[b] = all < 0x1p-900 ? 0.0 : all;           // nothing but -inf, each of which has added 2^-1000
+            if (lane == 63) {
+                sums[b] = all;
                 refs[b] = ref;
             }
             sum = 0.0;
         }
     };
-    if (whole > 0) load(0);
-    for (int32_t step = 0; step < whole; ++step) {
+    if (s.steps > 0) load(0);
+    for (int32_t step = 0; step < s.steps; ++step) {
         float x[M];
 #pragma unroll
         for (int u = 0; u < kUnroll; ++u) unpack<T>(w[u], x + u * N);
-        if (step + 1 < whole) load(step + 1);
+        if (step + 1 < s.steps) load(step + 1);
         take(x);
-        if ((step & (per - 1)) == per - 1 || step + 1 == s.steps) end_block(step);
-    }
-    if (whole < s.steps) {
-        float x[M];
-#pragma unroll
-        for (int u = 0; u < kUnroll; ++u)
-            floats_at(x0, a.vocab, s.first + (int64_t)whole * (kSampleLanes * kUnroll) + u * kSampleLanes + lane, x + u * N);
-        take(x);
-        end_block(whole);
+        if ((step & (per - 1)) == per - 1 || step + 1 == s.steps) end_block(step, x[0]);
     }
     for (int32_t b = s.steps == 0 ? 0 : ((s.steps - 1) >> a.shift) + 1; b < blocks; ++b) {
         notes[b * 64 + lane] = kNoteNothing;
+        samples[b * 64 + lane] = kNoteNothing;
         if (kSums && lane == 0) {
             sums[b] = 0.0;
             refs[b] = -__builtin_inff();
@@ -253,12 +337,14 @@ __device__ float read_strip(const SampleArgs& a, const T* x0, int32_t strip, con
     return most;
 }
 
-// What the rest of a row's work keeps in LDS.
-template <int K, int BLOCKS> struct Shared {
-    uint16_t notes[BLOCKS * 64];
+// What a row's work keeps in LDS.
+template <int K, int BLOCKS, int BINS> struct Shared {
+    static constexpr int kBins = BINS;    // of a histogram
+    static constexpr int kBlocks = BLOCKS;
+    alignas(16) uint16_t notes[BLOCKS * 64];          // maxima of the parts of each block
     double sums[BLOCKS];
     float refs[BLOCKS];
-    float most[BLOCKS];                   // of strips
+    int32_t ties[BLOCKS];
     double table[32];
     double wave[K / 64];
     Key wave_mass[K / 64];
@@ -266,49 +352,56 @@ template <int K, int BLOCKS> struct Shared {
     union {
         struct {
             Key keys[kCandidates], ranked[kCandidates];
-            double weights[kCandidates];
         };
         struct {
-            Key mass[kBins];              // of a digit's tokens, in units of 2^-units
-            uint32_t count[kBins];
+            Key mass[BINS];               // of a bin's tokens, as whole numbers
+            uint32_t count[BINS];
         };
     };
-    uint32_t bins[256];
     int32_t number, place, token;
+    float value;
     uint32_t found;
-    double rest, total;
+    double total;
     Key bound;
 };
 
 // Sum over the workgroup's threads up to and including each; *total receives all.
-template <int K, typename X> __device__ X block_scan(X x, X* wave, X* total)
+template <int K, typename X> __device__ __forceinline__ X block_scan(X x, X* wave, X* total)
 {
     const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
-    X y = x;
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) {
-        const X z = __shfl_up(y, d);
-        if (lane >= d) y += z;
-    }
+    const X y = wave_scan(x);
     __syncthreads();
     if (lane == 63) wave[w] = y;
     __syncthreads();
     X before = 0, all = 0;
-#pragma unroll
+#pragma unroll 1
     for (int i = 0; i < K / 64; ++i) {
-        if (i < w) before += wave[i];
-        all += wave[i];
+        const X z = wave[i];
+        if (i < w) before += z;
+        all += z;
     }
     *total = all;
     return before + y;
 }
 
-template <typename T, int K, int BLOCKS> struct RowWork {
-    typedef Shared<K, BLOCKS> S;
-    static constexpr int N = Vec<T>::n;
+// What stays of a row: orders above `order`, and of those alike the first `ties`.
+struct Cut {
+    uint32_t order;
+    int32_t ties;
+
+    __device__ __forceinline__ Cut stricter(Cut o) const
+    {
+        return order != o.order ? (order > o.order ? *this : o) : Cut{order, min(ties, o.ties)};
+    }
+};
+constexpr Cut kEverything = {0, 0};       // order 0 is a NaN's
+
+template <typename T, typename S, int K> struct RowWork {
+    static constexpr int N = Vec<T>::n, kBins = S::kBins;
     const SampleArgs& a;
     S& s;
     const T* x0;
+    const uint16_t* samples;              // a logit of each part of the blocks
     float m;                              // the row's largest logit
     int32_t blocks;
     int32_t tid;
@@ -321,11 +414,6 @@ template <typename T, int K, int BLOCKS> struct RowWork {
     }
     // whether ln w >= ln min_p
     __device__ __forceinline__ bool likely(float x) const { return a.scale * ((double)x - (double)m) >= a.least; }
-    // whether a token is among those that stay, given the least key
-    __device__ __forceinline__ bool stays(float x, uint32_t token, Key least) const
-    {
-        return key_of(x, token) >= least && likely(x);
-    }
 
     // First token of a block; blocks follow each other in token order.
     __device__ __forceinline__ int64_t block_begin(int32_t b) const
@@ -336,43 +424,66 @@ template <typename T, int K, int BLOCKS> struct RowWork {
     }
 
     // Of the tokens [from, to) that stay the first up to which more than `rest` lies; where
-    // roundings leave none, the last that has a weight.  Into s.token, -1 if there is none.
-    __device__ void locate(int64_t from, int64_t to, double rest, Key least)
+    // roundings leave none, the last that has a weight.  Into s.token, -1 if there is none, and its logit
+    // into s.value.  `ties`: how many of the cut's ties before `from` stay.
+    __device__ void locate(int64_t from, int64_t to, double rest, Cut cut, int32_t ties)
     {
+        const float edge = cut.order ? value_at(cut.order) : -__builtin_inff();       // those above it stay
         if (tid == 0) s.token = -1;
+#pragma unroll 1
         for (int64_t at = from; at < to; at += K * N) {
             const int64_t i = at / N + tid;
-            float x[N];
-            floats_at(x0, (int32_t)min((int64_t)a.vocab, to), i, x);
-            double w[N], mine = 0.0, total;
-            int32_t last = -1;
-#pragma unroll
-            for (int j = 0; j < N; ++j) {
-                w[j] = stays(x[j], (uint32_t)(i * N + j), least) ? weight(x[j]) : 0.0;
-                mine += w[j];
-                if (w[j] > 0.0) last = j;
+            const V4u w = vector_at(x0, to, i);
+            uint32_t alike = 0, all_alike = 0;
+            if (cut.order != 0) {
+                Logits<T> x = {w};
+#pragma unroll 1
+                for (int j = 0; j < N; ++j) alike += x.next() == edge;
+                alike = block_scan<K>(alike, s.wave_count, &all_alike) - alike + ties;
             }
+            // the sum up to each token from `before` on: all of them, or up to the first above `limit`
+            auto sum_from = [&](double before, double limit, int32_t* which, float* value) {
+                Logits<T> x = {w};
+                uint32_t tie = alike;
+                double sum = before;
+                *which = -1;
+#pragma unroll 1
+                for (int j = 0; j < N; ++j) {
+                    const float y = x.next();
+                    bool stays = y > edge;
+                    if (cut.order != 0 && y == edge) stays = tie++ < (uint32_t)cut.ties;
+                    const double v = stays && likely(y) ? weight(y) : 0.0;
+                    if (v > 0.0) {
+                        *which = j;
+                        *value = y;
+                        sum += v;
+                        if (sum > limit) break;
+                    }
+                }
+                return sum;
+            };
+            int32_t last;
+            float value = 0.f;
+            double total;
+            const double mine = sum_from(0.0, __builtin_inf(), &last, &value);
+            ties += all_alike;
             if (tid == 0) s.place = K;
             const double upto = block_scan<K>(mine, s.wave, &total);
-            if (last >= 0) atomicMax(&s.token, (int32_t)(i * N + last));
-            if (upto > rest && last >= 0) atomicMin(&s.place, tid);
-            __syncthreads();
-            const bool found = s.place < K;
-            if (found && tid == s.place) {
-                double before = upto - mine;
-                int32_t j = last;
-#pragma unroll
-                for (int e = N - 1; e >= 0; --e) {
-                    // the sum up to e, as it was added
-                    double sum = before;
-#pragma unroll
-                    for (int f = 0; f <= e; ++f) sum += w[f];
-                    if (w[e] > 0.0 && sum > rest) j = e;
-                }
-                s.token = (int32_t)(i * N + j);
+            if (last >= 0) {
+                atomicMax(&s.token, (int32_t)(i * N + last));
+                if (upto > rest) atomicMin(&s.place, tid);
             }
             __syncthreads();
-            if (found) return;
+            const int32_t place = s.place;
+            if (place < K ? tid == place : last >= 0 && s.token == (int32_t)(i * N + last)) {
+                if (place < K) {
+                    sum_from(upto - mine, rest, &last, &value);
+                    s.token = (int32_t)(i * N + last);
+                }
+                s.value = value;
+            }
+            __syncthreads();
+            if (place < K) return;
             rest -= total;
         }
     }
@@ -392,8 +503,8 @@ template <typename T, int K, int BLOCKS> struct RowWork {
         return total;
     }
 
-    // From the blocks' sums up to each the token.
-    __device__ void pick(double total, Key least)
+    // From the blocks' sums up to each the token; s.ties holds the ties before each block where there is a cut.
+    __device__ void pick(double total, Cut cut)
     {
         const double target = uniform() * total;
         if (tid == 0) s.place = blocks;
@@ -412,112 +523,185 @@ template <typename T, int K, int BLOCKS> struct RowWork {
             __syncthreads();
         }
         const double before = b ? s.sums[b - 1] : 0.0;
-        locate(block_begin(b), b + 1 < blocks ? block_begin(b + 1) : (int64_t)a.vocab, target - before, least);
+        locate(block_begin(b), b + 1 < blocks ? block_begin(b + 1) : (int64_t)a.vocab, target - before, cut, cut.order ? s.ties[b] : 0);
         __syncthreads();
         // weights at the edge of what counts as 0 made that block: the first token that has one
         if (s.token < 0) {
             __syncthreads();
-            locate(0, a.vocab, 0.0, least);
+            locate(0, a.vocab, 0.0, cut, 0);
             __syncthreads();
         }
     }
 
-    float u;
+    float u;                              // the number given
     __device__ __forceinline__ double uniform() const
     {
         constexpr double kLast = 1.0 - 0x1p-53;
         return u > 0.f ? fmin((double)u, kLast) : 0.0;      // a NaN is not above 0
     }
 
-    // The order of the r-th largest note (0: fewer have any tokens), and how many notes reach it.
-    __device__ uint32_t note_of_rank(int32_t r)
+    // Calls f(x, token) for the logits of vectors [first, last) of a row that ends at `to`, THREADS
+    // threads a vector each, kDepth of them under way.
+    template <int THREADS, typename F> __device__ __forceinline__ void each_logit(int64_t first, int64_t last, int64_t to, int thread, F f)
     {
-        uint32_t prefix = 0;
-        int32_t left = r;
-        for (int level = 0; level < 2; ++level) {
-            for (int i = tid; i < 256; i += K) s.bins[i] = 0;
-            if (tid == 0) s.found = 0;
-            __syncthreads();
-            for (int i = tid; i < blocks * 64; i += K) {
-                const uint32_t n = s.notes[i];
-                if (n > kNoteNothing && (level == 0 || n >> 8 == prefix)) atomicAdd(&s.bins[level == 0 ? n >> 8 : n & 255], 1);
+        const int64_t full = to / N;
+#pragma unroll 1
+        for (int64_t i0 = first + thread; i0 < last; i0 += THREADS * kDepth) {
+            V4u w[kDepth];
+#pragma unroll
+            for (int d = 0; d < kDepth; ++d)
+                if (i0 + d * THREADS < min(last, full)) w[d] = *reinterpret_cast<const V4uAnywhere*>(x0 + (i0 + d * THREADS) * N);
+#pragma unroll 1
+            for (int64_t i = i0; i < min(last, i0 + THREADS * kDepth); i += THREADS) {
+                Logits<T> x = {w[0]};
+                if (i >= full) x.w = vector_at(x0, to, i);
+#pragma unroll 1
+                for (int j = 0; j < N; ++j) f(x.next(), (uint32_t)(i * N + j));
+#pragma unroll
+                for (int d = 1; d < kDepth; ++d) w[d - 1] = w[d];
             }
-            __syncthreads();
-            if (tid < 64) {
-                // four bins a lane, from the top
-                uint32_t c[4], mine = 0;
-#pragma unroll
-                for (int e = 0; e < 4; ++e) mine += c[e] = s.bins[255 - 4 * tid - e];
-                uint32_t upto = mine;
-#pragma unroll
-                for (int d = 1; d < 64; d <<= 1) {
-                    const uint32_t y = __shfl_up(upto, d);
-                    if (tid >= d) upto += y;
-                }
-                uint32_t before = upto - mine;
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    if ((int32_t)before < left && (int32_t)(before + c[e]) >= left) {
-                        s.found = 256 + 255 - 4 * tid - e;
-                        s.number = left - (int32_t)before;
-                    }
-                    before += c[e];
-                }
-            }
-            __syncthreads();
-            const uint32_t found = s.found;
-            if (found == 0) return 0;
-            prefix = (prefix << 8) | (found - 256);
-            left = s.number;
-            __syncthreads();
         }
-        return prefix;
     }
 
-    // All tokens from `bound` on into s.keys; their number, which may exceed what there is room for.
-    __device__ int32_t collect(float bound, uint32_t note)
+    // Bins of the notes, by how far they are below the largest logit.
+    static constexpr float kPerOctave = kBins / 64;
+    __device__ __forceinline__ int note_bin(uint32_t order) const
     {
-        if (tid == 0) s.number = 0;
+        // a note of fp32 logits may be rounded up beyond the largest
+        return (int)fminf(fmaxf(m - value_at(order << 16), 0.f) * (float)a.c * kPerOctave, kBins - 1.f);
+    }
+
+    // Counts the notes in their bins: s.number receives the first bin up to which there are `rank` of
+    // them and s.found how many there are; where these are more than `most`, the bin in front of the
+    // first up to which there are so many, and the number up to there.  kBins - 1, and all of
+    // them, if there are fewer than `rank`.
+    __device__ void count_notes(uint32_t rank, uint32_t most)
+    {
+        for (int i = tid; i < kBins; i += K) s.count[i] = 0;
         __syncthreads();
-        const int32_t per_strip = blocks_of_strip(a);
+#pragma unroll 1
         for (int i = tid; i < blocks * 64; i += K) {
-            if (s.notes[i] < note || s.notes[i] <= kNoteNothing) continue;
-            const int32_t b = i >> 6, lane = i & 63, strip = b / per_strip, in = (b - strip * per_strip) << a.shift;
-            const int32_t steps = min(1 << a.shift, a.strip_steps - in);
-            for (int32_t v = 0; v < steps * kUnroll; ++v) {
-                const int64_t at = ((int64_t)strip * a.strip_steps + in) * (kSampleLanes * kUnroll) + v * kSampleLanes + lane;
-                float x[N];
-                floats_at(x0, a.vocab, at, x);
-#pragma unroll
-                for (int j = 0; j < N; ++j)
-                    if (x[j] >= bound && x[j] > -__builtin_inff()) {
-                        const int32_t n = atomicAdd(&s.number, 1);
-                        if (n < kCandidates) s.keys[n] = key_of(x[j], (uint32_t)(at * N + j));
-                    }
+            const uint32_t order = s.notes[i];
+            if (order > kNoteNothing) atomicAdd(&s.count[note_bin(order)], 1u);
+        }
+        __syncthreads();
+        constexpr int PER = kBins / K;
+        uint32_t mine = 0, all;
+#pragma unroll 1
+        for (int e = 0; e < PER; ++e) mine += s.count[tid * PER + e];
+        uint32_t upto = block_scan<K>(mine, s.wave_count, &all) - mine;
+        if (tid == 0) {
+            s.number = kBins - 1;
+            s.found = all;
+        }
+        __syncthreads();
+#pragma unroll 1
+        for (int e = 0; e < PER; ++e) {
+            const uint32_t before = upto;
+            upto += s.count[tid * PER + e];
+            if (upto <= most ? before < rank && upto >= rank : before <= most && before < rank) {
+                s.number = tid * PER + e - (upto <= most ? 0 : 1);
+                s.found = upto <= most ? upto : before;
             }
         }
         __syncthreads();
-        const int32_t n = s.number;
+    }
+
+    // The least logit that the parts with notes in bins up to `bin` can have as their maximum.  All
+    // tokens from it on lie in such parts, and each such part has one.
+    __device__ __forceinline__ float least_of_bins(int bin) const
+    {
+        uint32_t o = note_of(m - (bin + 1) / ((float)a.c * kPerOctave));          // or near it
+        while (o < 0xFF7F && note_bin(o) > bin) ++o;
+        while (o > kNoteNothing + 1u && note_bin(o - 1) <= bin) --o;
+        // a note above 0 is rounded up, one below is the beginning of what it stands for
+        return value_at(o > 0x8000 ? ((o - 1) << 16) + 1 : o << 16);
+    }
+
+    // All tokens x >= bound of the parts whose notes lie in bins up to `bin` into s.keys; their number,
+    // which may exceed what there is room for.  The parts are listed, and then read together.
+    __device__ int32_t collect(int bin, float bound)
+    {
+        uint32_t* const parts = reinterpret_cast<uint32_t*>(s.ranked);
+        const uint32_t least = max((uint32_t)note_of(bound), kNoteNothing + 1u);
+        if (tid == 0) s.number = s.place = 0;
         __syncthreads();
-        return n;
+#pragma unroll 1
+        for (int i = tid; i < blocks * 64; i += K) {
+            const uint32_t order = s.notes[i];
+            if (order >= least && note_bin(order) <= bin) {
+                const int at = atomicAdd(&s.place, 1);
+                if (at < kParts) parts[at] = i;
+            }
+        }
+        __syncthreads();
+        const int32_t listed = s.place;
+        if (listed > kParts) return kCandidates + 1;
+        const int32_t per_strip = blocks_of_strip(a), vectors = kUnroll << a.shift;
+#pragma unroll 1
+        for (int64_t item = tid; item < (int64_t)listed * vectors; item += K) {
+            const int32_t part = (int32_t)(item >> (2 + a.shift)), v = (int32_t)(item & (vectors - 1)), i = parts[part];
+            const int32_t b = i >> 6, lane = i & 63, strip = b / per_strip, in = (b - strip * per_strip) << a.shift;
+            if (in + v / kUnroll >= a.strip_steps) continue;
+            const int64_t at = ((int64_t)strip * a.strip_steps + in) * (kSampleLanes * kUnroll) + v * kSampleLanes + lane;
+            Logits<T> x = {vector_at(x0, a.vocab, at)};
+#pragma unroll 1
+            for (int j = 0; j < N; ++j) {
+                const float y = x.next();
+                if (y >= bound && y > -__builtin_inff()) {
+                    const int32_t to = atomicAdd(&s.number, 1);
+                    if (to < kCandidates) s.keys[to] = key_of(y, (uint32_t)(at * N + j));
+                }
+            }
+        }
+        __syncthreads();
+        const int32_t found = s.number;
+        __syncthreads();
+        return found;
+    }
+
+    // The n keys in s.keys in descending order, in s.ranked.
+    __device__ void rank(int32_t n)
+    {
+        if (n <= kCounted) {
+            // each key's place is the number of larger ones
+            for (int i = tid; i < n; i += K) {
+                const Key mine = s.keys[i];
+                int32_t place = 0;
+#pragma unroll 4
+                for (int j = 0; j < n; ++j) place += s.keys[j] > mine;
+                s.ranked[place] = mine;
+            }
+            __syncthreads();
+            return;
+        }
+        int size = 2 * kCounted;
+        while (size < n) size *= 2;
+        for (int i = tid; i < size; i += K) s.ranked[i] = i < n ? s.keys[i] : 0;
+        __syncthreads();
+        for (int k = 2; k <= size; k *= 2)
+            for (int j = k / 2; j > 0; j /= 2) {
+                for (int t = tid; t < size / 2; t += K) {
+                    const int i = 2 * t - (t & (j - 1)), o = i + j;
+                    const Key x = s.ranked[i], y = s.ranked[o];
+                    if ((x < y) == ((i & k) == 0)) {
+                        s.ranked[i] = y;
+                        s.ranked[o] = x;
+                    }
+                }
+                __syncthreads();
+            }
     }
 
     // From the n tokens in s.keys, which are all from some key on: true, with the token in
-    // s.token and the weight of those that stay in s.total, if they hold all that stay.
-    // total: the row's weight, where top_p of it counts.
-    __device__ bool from_candidates(int32_t n, bool bounded, double total)
+    // s.token, its logit in s.value and the weight of those that stay in s.total, if they hold
+    // all that stay.  bounded: nothing behind them stays.  total: the row's weight, where top_p
+    // of it counts; *weighs receives that of the n.
+    __device__ bool from_candidates(int32_t n, bool bounded, double total, double* weighs)
     {
         constexpr int PER = (kCandidates + K - 1) / K;
-        // ranks: how many are larger
-#pragma unroll 1
-        for (int i = tid; i < n; i += K) {
-            const Key mine = s.keys[i];
-            int32_t place = 0;
-            for (int j = 0; j < n; ++j) place += s.keys[j] > mine;
-            s.ranked[place] = mine;
-        }
+        rank(n);
         if (tid == 0) s.place = n;
-        __syncthreads();
         const int32_t first = a.top_k > 0 ? min(a.top_k, n) : n;
         double w[PER], mine = 0.0, all;
 #pragma unroll
@@ -527,6 +711,7 @@ template <typename T, int K, int BLOCKS> struct RowWork {
             mine += w[e];
         }
         double upto = block_scan<K>(mine, s.wave, &all) - mine;
+        *weighs = all;
         const double enough = a.top_p * (a.top_k > 0 ? all : total);
         const bool part = a.top_p < 1.0;
 #pragma unroll
@@ -539,26 +724,20 @@ template <typename T, int K, int BLOCKS> struct RowWork {
         const int32_t kept = min(s.place, first);
         // nothing of them was cut off: more may stay
         if (kept == n && !bounded && !(part && !(all < enough)) && !(a.top_k > 0 && n >= a.top_k)) return false;
-        // in token order
-#pragma unroll 1
-        for (int i = tid; i < kept; i += K) {
-            const Key k = s.ranked[i];
-            const uint32_t token = key_token(k);
-            int32_t place = 0;
-            for (int j = 0; j < kept; ++j) place += key_token(s.ranked[j]) < token;
-            s.keys[place] = k;
-        }
+        // in token order: keys that begin with the token
+        for (int i = tid; i < kept; i += K) s.keys[i] = s.ranked[i] << 32 | s.ranked[i] >> 32;
         if (tid == 0) {
             s.token = -1;
-            s.place = K;
+            s.found = K;
         }
         __syncthreads();
+        rank(kept);
         int32_t last = -1;
         mine = 0.0;
 #pragma unroll
         for (int e = 0; e < PER; ++e) {
             const int32_t i = tid * PER + e;
-            w[e] = i < kept ? weight(key_value(s.keys[i])) : 0.0;
+            w[e] = i < kept ? weight(value_at((uint32_t)s.ranked[i])) : 0.0;
             mine += w[e];
             if (w[e] > 0.0) last = i;
         }
@@ -566,14 +745,15 @@ template <typename T, int K, int BLOCKS> struct RowWork {
         const double rest = uniform() * all;
         if (tid == 0) s.total = all;
         if (last >= 0) atomicMax(&s.token, last);
-        if (upto > rest && last >= 0) atomicMin(&s.place, tid);
+        if (upto > rest && last >= 0) atomicMin(&s.found, (uint32_t)tid);
         __syncthreads();
         const int32_t fallback = s.token;
+        const uint32_t owner = s.found;
         __syncthreads();
-        if (s.place == K ? tid == 0 : tid == s.place) {
+        if (owner == K ? tid == 0 : tid == (int)owner) {
             int32_t at = fallback;
             double before = upto - mine;
-            if (s.place < K) {
+            if (owner < K) {
                 at = last;
                 bool found = false;
 #pragma unroll
@@ -585,72 +765,90 @@ template <typename T, int K, int BLOCKS> struct RowWork {
                     }
                 }
             }
-            s.token = (int32_t)key_token(s.keys[at]);
+            s.token = (int32_t)~(uint32_t)(s.ranked[at] >> 32);
+            s.value = value_at((uint32_t)s.ranked[at]);
         }
         __syncthreads();
         return true;
     }
 
-    // The least key of those that stay, found digit by digit from histograms of the row:
-    // by number (the first `number` of the order) or by weight (as many as it takes to
-    // reach share of `total`).  *weight receives the weight from that key on.
-    __device__ Key search(int64_t number, double enough, bool by_weight, double* weight_from)
+    // The cut that leaves the first `number` of the order (by_weight: as many as it takes to
+    // reach `enough`), found by reading the row again: a histogram of what lies in [lo, hi] of
+    // the orders, and of the bin it ends in again, until that is one order.  Where it does
+    // not end in [lo, hi], everything is looked at.  *weight receives the weight that is left.
+    __device__ Cut search(uint32_t lo, uint32_t hi, int64_t number, double enough, bool by_weight, double* weight_left)
     {
+        constexpr uint32_t kFirst = 0x00800000, kLast = 0xFF7FFFFF;            // finite numbers
         // weights as whole numbers, so that their sums do not depend on the order: 2^units for the largest
         const int units = min(44, 62 - (32 - __clz((int)a.vocab)));
         const double unit = (double)((uint64_t)1 << units);
         const int64_t vecs = ((int64_t)a.vocab + N - 1) / N;
-        const double target = by_weight ? enough * unit : 0.0;
-        Key prefix = 0, above_mass = 0;
-        int64_t above = 0;
-        int shift = 64;
-        // digits of 11, 11 and 10 bits of the value, then of the token
-        while (shift > 0) {
-            const int bits = shift == 42 || shift == 10 ? 10 : kDigit, low = shift - bits;
+        bool above_known = false;
+        double above = 0.0;               // weight, and number, of what lies above hi
+        int64_t above_count = 0;
+        while (true) {
+            int sh = 0;
+            while (((hi - lo) >> sh) >= kBins) ++sh;
             for (int i = tid; i < kBins; i += K) {
                 s.mass[i] = 0;
                 s.count[i] = 0;
             }
-            if (tid == 0) s.found = 0;
             __syncthreads();
-            for (int64_t i = tid; i < vecs; i += K) {
-                float x[N];
-                floats_at(x0, a.vocab, i, x);
-#pragma unroll
-                for (int j = 0; j < N; ++j) {
-                    const Key k = key_of(x[j], (uint32_t)(i * N + j));
-                    if (k != 0 && (shift == 64 || k >> shift == prefix)) {
-                        const uint32_t bin = (uint32_t)(k >> low) & ((1u << bits) - 1);
-                        atomicAdd(&s.mass[bin], (Key)(weight(x[j]) * unit + 0.5));
-                        atomicAdd(&s.count[bin], 1u);
-                    }
+            double mine = 0.0;
+            uint32_t mine_count = 0;
+            const float least = value_at(lo), most = value_at(hi), known_from = above_known ? most : __builtin_inff();
+            each_logit<K>(0, vecs, a.vocab, tid, [&](float x, uint32_t) {
+                if (!(x >= least) || x > known_from) return;
+                const double w = weight(x);
+                if (x > most) {
+                    mine += w;
+                    ++mine_count;
+                } else {
+                    const uint32_t bin = (order_of(x) - lo) >> sh;
+                    atomicAdd(&s.mass[bin], (Key)(w * unit + 0.5));
+                    atomicAdd(&s.count[bin], 1u);
                 }
+            });
+            if (!above_known) {
+                uint32_t count;
+                block_scan<K>(mine, s.wave, &above);
+                block_scan<K>(mine_count, s.wave_count, &count);
+                above_count = count;
             }
             __syncthreads();
-            // from the top: the bin in which the number or the weight is reached; where roundings leave
-            // none, the lowest with anything in it
+            // from the top: the bin in which the number or the weight is reached
             constexpr int PER = kBins / K;
-            const int top = (1 << bits) - 1 - tid * PER;
+            const int top = kBins - 1 - tid * PER;
             Key mass = 0, all_mass;
             uint32_t count = 0, all_count;
-#pragma unroll
-            for (int e = 0; e < PER; ++e)
-                if (top - e >= 0) {
-                    mass += s.mass[top - e];
-                    count += s.count[top - e];
-                }
-            Key mass_upto = above_mass + block_scan<K>(mass, s.wave_mass, &all_mass) - mass;
-            int64_t count_upto = above + block_scan<K>(count, s.wave_count, &all_count) - count;
-            const auto reached = [&](Key x, int64_t n) { return by_weight ? !((double)x < target) : n >= number; };
-            const bool none = !reached(above_mass + all_mass, above + all_count);
-#pragma unroll
+#pragma unroll 1
+            for (int e = 0; e < PER; ++e) {
+                mass += s.mass[top - e];
+                count += s.count[top - e];
+            }
+            Key mass_upto = block_scan<K>(mass, s.wave_mass, &all_mass) - mass;
+            uint32_t count_upto = block_scan<K>(count, s.wave_count, &all_count) - count;
+            const auto reached = [&](Key x, uint32_t n) {
+                return by_weight ? !(above + (double)x / unit < enough) : above_count + n >= number;
+            };
+            const bool inside = !reached(0, 0) && reached(all_mass, all_count);
+            const bool everything = lo == kFirst && hi == kLast;
+            if (!inside && !above_known && !everything) {
+                lo = kFirst;
+                hi = kLast;
+                __syncthreads();
+                continue;
+            }
+            if (tid == 0) s.found = 0;
+            __syncthreads();
+            // where roundings leave none, the lowest with anything in it
+#pragma unroll 1
             for (int e = 0; e < PER; ++e) {
                 const int bin = top - e;
-                if (bin < 0 || s.count[bin] == 0) continue;
+                if (s.count[bin] == 0) continue;
                 const Key m1 = mass_upto + s.mass[bin];
-                const int64_t n1 = count_upto + s.count[bin];
-                const bool first = mass_upto == above_mass && count_upto == above;       // nothing above it in here
-                if (none ? n1 == above + all_count : reached(m1, n1) && (first || !reached(mass_upto, count_upto))) {
+                const uint32_t n1 = count_upto + s.count[bin];
+                if (inside ? reached(m1, n1) && !reached(mass_upto, count_upto) : n1 == all_count) {
                     s.found = bin + 1;
                     s.bound = mass_upto;
                     s.number = (int32_t)count_upto;
@@ -660,54 +858,141 @@ template <typename T, int K, int BLOCKS> struct RowWork {
             }
             __syncthreads();
             const uint32_t found = s.found;
-            if (found == 0) return 1;                        // no tokens at all
-            const uint32_t bin = found - 1;
-            above_mass = s.bound;
-            above = s.number;
-            prefix = (prefix << bits) | bin;
-            shift = low;
-            const bool single = s.count[bin] == 1 || (!by_weight && above + s.count[bin] == number);
-            const Key here = s.mass[bin];
-            __syncthreads();
-            if (single || shift == 0) {
-                *weight_from = (double)(above_mass + here) / unit;
-                return max(prefix << shift, (Key)1);
+            if (found == 0) {             // nothing that counts
+                *weight_left = above;
+                return kEverything;
             }
+            const uint32_t bin = found - 1, here = s.count[bin];
+            const double each = (double)s.mass[bin] / unit;
+            above += (double)s.bound / unit;
+            above_count += (uint32_t)s.number;
+            above_known = true;
+            __syncthreads();
+            hi = min(hi, lo + (bin << sh) + ((1u << sh) - 1));
+            lo += bin << sh;
+            if (sh > 0) continue;
+            // `here` logits alike: as many of them as it takes, by the lowest tokens
+            int64_t ties = here;
+            if (inside) {
+                if (by_weight) {
+                    const double w = weight(value_at(lo));
+                    ties = w > 0.0 ? (int64_t)ceil((enough - above) / w * (1 - 0x1p-50)) : here;
+                    ties = max((int64_t)1, min((int64_t)here, ties));
+                } else {
+                    ties = number - above_count;
+                }
+            }
+            *weight_left = above + each * ((double)ties / here);
+            return Cut{lo, (int32_t)ties};
         }
-        return 1;
     }
 
-    // The row's sums once more, of the tokens that stay.
-    __device__ double sums_of(Key least)
+    // Orders between which a share of the row's weight (or number) should end, from the
+    // samples below `from`, whose tokens are known: `enough` of `all` lies below it.  Each
+    // sample stands for its share of them; four standard deviations to either side.
+    __device__ void guess(uint32_t from, double enough, double all, bool by_weight, uint32_t* lo, uint32_t* hi)
+    {
+        // bins of 1/32 octaves of weight below `from` (1/8 where there are few)
+        constexpr double per = kBins / 64;
+        const float top = value_at(from);
+        for (int i = tid; i < kBins; i += K) {
+            s.mass[i] = 0;
+            s.count[i] = 0;
+        }
+        __syncthreads();
+        auto bin_of = [&](float x) { return (int)fmin(a.c * ((double)top - (double)x) * per, kBins - 1.0); };
+        for (int i = tid; i < blocks * 64; i += K) {
+            const uint32_t n = samples[i];
+            if (n <= kNoteNothing || (n << 16) >= from) continue;
+            const float x = value_at(n << 16);
+            const int bin = bin_of(x);
+            atomicAdd(&s.count[bin], 1u);
+        }
+        __syncthreads();
+        constexpr int PER = kBins / K;
+        double mass = 0.0, square = 0.0, all_mass, all_square;
+        auto bin_weight = [&](int bin) { return by_weight ? power(-(double)bin / per, s.table) : 1.0; };
+#pragma unroll 1
+        for (int e = 0; e < PER; ++e) {
+            const int bin = tid * PER + e;
+            const double w = bin_weight(bin), n = s.count[bin];
+            mass += n * w;
+            square += n * w * w;
+        }
+        double upto = block_scan<K>(mass, s.wave, &all_mass) - mass;
+        double upto_square = block_scan<K>(square, s.wave, &all_square) - square;
+        const double target = enough / all * all_mass;
+        if (tid == 0) {
+            s.found = kBins;
+            s.number = 0;
+            s.place = kBins;
+        }
+        __syncthreads();
+#pragma unroll 1
+        for (int e = 0; e < PER; ++e) {
+            const int bin = tid * PER + e;
+            const double w = bin_weight(bin), n = s.count[bin];
+            upto += n * w;
+            upto_square += n * w * w;
+            const double far = 4.0 * sqrt(upto_square) + 2.0 * w;
+            if (upto + far < target) atomicMax(&s.number, bin);               // it ends behind this bin
+            if (upto - far > target) atomicMin(&s.place, bin);                // it has ended
+        }
+        __syncthreads();
+        const int first = s.number, last = s.place;
+        __syncthreads();
+        auto value_of_bin = [&](double bin) { return (float)((double)top - bin / per / a.c); };
+        *hi = first == 0 ? from - 1 : order_of(value_of_bin(first));
+        const float low = last >= kBins - 1 ? -__builtin_inff() : value_of_bin(last + 1);
+        *lo = low > -3.4e38f ? order_of(low) : 0x00800000u;
+        *lo = min(*lo, *hi);
+    }
+
+    // The row's sums once more, of the tokens that stay; s.ties receives the cut's ties before each block.
+    __device__ double sums_of(Cut cut)
     {
         const int lane = tid & 63;
+        const float above = cut.order ? value_at(cut.order) : -__builtin_inff(), edge = cut.order ? above : __builtin_nanf("");
+        const bool least_matters = a.least > -__builtin_inf();
         __syncthreads();
         for (int32_t b = tid >> 6; b < blocks; b += K / 64) {
             const int64_t from = block_begin(b), to = b + 1 < blocks ? block_begin(b + 1) : (int64_t)a.vocab;
             double sum = 0.0;
+            int32_t ties = 0;
             // blocks begin at whole vectors, but for those behind the row's end
-            for (int64_t i = from / N + lane; from < to && i * N < to; i += 64) {
-                float x[N];
-                floats_at(x0, (int32_t)to, i, x);
-#pragma unroll
-                for (int j = 0; j < N; ++j)
-                    if (stays(x[j], (uint32_t)(i * N + j), least)) sum += weight(x[j]);
-            }
+            if (from < to)
+                each_logit<64>(from / N, (to + N - 1) / N, to, lane, [&](float x, uint32_t) {
+                    ties += x == edge;
+                    if (x > above && (!least_matters || likely(x))) sum += weight(x);
+                });
             sum = wave_sum(sum);
-            if (lane == 0) {
+            ties = wave_sum(ties);
+            if (lane == 63) {
                 s.sums[b] = sum;
                 s.refs[b] = m;
+                s.ties[b] = ties;
             }
         }
         __syncthreads();
+        if (cut.order != 0) {
+            uint32_t all;
+            const int32_t mine = tid < blocks ? s.ties[tid] : 0;
+            const int32_t before = (int32_t)block_scan<K>((uint32_t)mine, s.wave_count, &all) - mine;
+            if (tid < blocks) {
+                const float x = value_at(cut.order);
+                const int32_t stay = max(0, min(mine, cut.ties - before));
+                if (stay > 0 && likely(x)) s.sums[tid] += stay * weight(x);
+                s.ties[tid] = before;
+            }
+            __syncthreads();
+        }
         return total_of_blocks();
     }
 
     // Everything behind the pass over the logits.
-    __device__ void finish(int64_t row, float most, bool sums)
+    __device__ void finish(int64_t row, bool sums)
     {
         const float nan = __builtin_nanf("");
-        m = most;
         const bool broken = !(m < __builtin_inff()), empty = m == -__builtin_inff();
         if (broken || empty) {
             if (tid == 0) {
@@ -716,15 +1001,13 @@ template <typename T, int K, int BLOCKS> struct RowWork {
             }
             return;
         }
-        u = a.uniforms[row];
         double total = 0.0;
         if (sums) total = total_of_blocks();
         const bool filters = a.top_k > 0 || a.top_p < 1.0 || a.least > -__builtin_inf();
         if (!filters) {
-            pick(total, 1);
+            pick(total, kEverything);
         } else {
             bool done = false;
-            const bool many = a.top_k > 3 * kCandidates / 4;
             // with min_p a bound is known
             float bound = -__builtin_inff();
             const bool known = a.least > -__builtin_inf() && !(a.top_k > 0 && a.top_p < 1.0);      // all of the first top_k count there
@@ -732,32 +1015,48 @@ template <typename T, int K, int BLOCKS> struct RowWork {
                 const double x = (double)m + a.least / a.scale * (1 + 1e-9) - 1e-30;
                 if (x > -3.3e38) bound = nextafterf((float)x, -__builtin_inff());
             }
-            for (int attempt = 0; attempt < 2 && !done && !many; ++attempt) {
-                const int32_t rank = a.top_k > 0 ? a.top_k : attempt == 0 ? 96 : 3 * kCandidates / 4;
-                const uint32_t order = note_of_rank(rank);
-                // notes of fp32 logits are rounded up: the one below is exceeded
-                float from = -3.402823466e38f;
-                if (order > 0) from = value_at((std::is_same<T, float>::value ? order - 1 : order) << 16);
-                if (order > 0 && order - 1 <= kNoteNothing) from = -3.402823466e38f;
-                const bool all = order == 0;
-                const bool bounded = all || (known && bound >= from);
-                const float least = known ? fmaxf(bound, from) : from;
-                const int32_t n = collect(least, note_of(least));
-                if (n > kCandidates) break;
-                done = from_candidates(n, bounded, total);
-                if (a.top_k > 0) break;
+            uint32_t below = order_of(m) + 1;                   // orders from here on are known, and what they weigh
+            double weighs = 0.0;
+            if (a.top_k <= kParts) {
+                // Each part has a token that reaches its note.  top_p alone may need few or many of them.
+#pragma unroll 1
+                for (int attempt = 0; attempt < 2 && !done; ++attempt) {
+                    count_notes(a.top_k > 0 ? a.top_k : attempt == 0 ? kFirstParts : kParts, a.top_k > 0 && known ? 1u << 30 : kParts);
+                    const int bin = s.number;
+                    const uint32_t parts = s.found;
+                    if (bin < 0 || (a.top_k > 0 && bin < kBins - 1 && parts < (uint32_t)a.top_k)) break;
+                    // every note of these bins, and all tokens from the lowest value in them on
+                    const bool all = bin == kBins - 1;
+                    const float from = all ? -3.402823466e38f : least_of_bins(bin);
+                    const bool bounded = all || (known && bound >= from);
+                    const float least = known ? fmaxf(bound, from) : from;
+                    __syncthreads();
+                    const int32_t found = collect(bin, least);
+                    if (found > kCandidates) break;
+                    done = from_candidates(found, bounded, total, &weighs);
+                    below = order_of(least);
+                    if (a.top_k > 0 || all) break;
+                }
             }
             if (!done) {
-                Key least = 1;
-                double among = total;
-                if (a.top_k > 0) least = search(a.top_k, 0.0, false, &among);
-                if (a.top_p < 1.0) {
-                    double ignored;
-                    least = max(least, search(0, a.top_p * among, true, &ignored));
+                Cut cut = kEverything;
+                double among = total, ignored;
+                uint32_t lo, hi;
+                __syncthreads();
+                if (a.top_k > 0) {
+                    guess(order_of(m) + 1, a.top_k, a.vocab, false, &lo, &hi);
+                    cut = search(lo, hi, a.top_k, 0.0, false, &among);
                 }
-                const double kept = sums_of(least);
-                pick(kept, least);
-                total = kept;
+                if (a.top_p < 1.0) {
+                    const double enough = a.top_p * among;
+                    if (a.top_k > 0)
+                        lo = cut.order ? cut.order : 0x00800000u, hi = 0xFF7FFFFFu;
+                    else
+                        guess(below, enough - weighs, total - weighs, true, &lo, &hi);
+                    cut = cut.stricter(search(lo, hi, 0, enough, true, &ignored));
+                }
+                total = sums_of(cut);
+                pick(total, cut);
             } else {
                 total = s.total;
             }
@@ -765,83 +1064,110 @@ template <typename T, int K, int BLOCKS> struct RowWork {
         if (tid == 0) {
             const int32_t token = s.token;
             a.tokens[row] = token;
-            if (a.logp) a.logp[row] = token < 0 ? nan : (float)(a.scale * ((double)value_of(x0[token]) - (double)m) - log(total));
+            if (a.logp) a.logp[row] = token < 0 ? nan : (float)(a.scale * ((double)s.value - (double)m) - log(total));
         }
     }
 };
 
-template <typename T, bool kSums> __global__ __launch_bounds__(64 * kWaves) void k_sample(SampleArgs a)
+// A row of few steps, by one wave.
+constexpr int kRowSteps = 4;
+template <typename T, bool kSums> __global__ __launch_bounds__(64, 3) void k_sample(SampleArgs a)
 {
-    constexpr int K = 64 * kWaves, BLOCKS = kSampleBlocks / 2;
-    __shared__ Shared<K, BLOCKS> s;
-    const int tid = threadIdx.x, wave = tid >> 6;
+    typedef Shared<64, kRowSteps, 512> S;
+    __shared__ S s;
+    __shared__ uint16_t s_samples[kRowSteps * 64];
+    const int tid = threadIdx.x;
     if (tid < 32) s.table[tid] = kTwoTo[tid];
     __syncthreads();
     for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
         const T* const x0 = static_cast<const T*>(a.x) + row * a.stride;
-        const int32_t per = blocks_of_strip(a);
-        const float top = read_strip<T, kSums>(a, x0, wave, s.table, s.notes + wave * per * 64, s.sums + wave * per, s.refs + wave * per);
-        if ((tid & 63) == 0) s.most[wave] = top;
+        const float u = a.uniforms[row];
+        const float m = read_strip<T, kSums, false, false>(a, x0, 0, nullptr, s.table, s.notes, s_samples, s.sums, s.refs);
         __syncthreads();
-        float m = s.most[0];
-#pragma unroll
-        for (int w = 1; w < kWaves; ++w) m = most_of(m, s.most[w]);
-        RowWork<T, K, BLOCKS> work{a, s, x0, 0.f, per * kWaves, tid, 0.f};
-        work.finish(row, m, kSums);
+        RowWork<T, S, 64> work{a, s, x0, s_samples, m, blocks_of_strip(a), tid, u};
+        work.finish(row, kSums);
         __syncthreads();
     }
 }
 
-// A slice of a row.
-template <typename T, bool kSums> __global__ __launch_bounds__(64 * kWaves) void k_sample_read(SampleArgs a)
+// A slice of a row: what its waves find out about their strips goes to the workspace.
+constexpr int kReadThreads = 64 * kSampleWaves;
+template <typename T, bool kSums, bool NT> __global__ __launch_bounds__(kReadThreads, 4) void k_sample_read(SampleArgs a)
 {
-    __shared__ double s_table[32];
+    __shared__ double s_table[32], s_powers[kSums ? kPowers : 1];
     const int tid = threadIdx.x, wave = tid >> 6;
-    if (tid < 32) s_table[tid] = kTwoTo[tid];
+    if (kSums) {
+        if (tid < 32) s_table[tid] = kTwoTo[tid];
+        fill_powers<kReadThreads>(s_powers);
+    }
     __syncthreads();
-    const int64_t row = blockIdx.x / a.slices;
-    const int32_t strips = a.slices * kWaves, strip = (int32_t)(blockIdx.x - row * a.slices) * kWaves + wave;
-    const int32_t per = blocks_of_strip(a);
-    const int64_t at = (row * strips + strip) * per;
-    const float top = read_strip<T, kSums>(a, static_cast<const T*>(a.x) + row * a.stride, strip, s_table, a.notes + at * 64,
-                                           a.sums + at, a.refs + at);
-    if ((tid & 63) == 0) a.most[row * strips + strip] = top;
+    const int32_t strips = a.slices * kSampleWaves, per = blocks_of_strip(a);
+    for (int64_t job = blockIdx.x; job < (int64_t)a.rows * a.slices; job += gridDim.x) {
+        const int64_t row = job / a.slices;
+        const int32_t strip = (int32_t)(job - row * a.slices) * kSampleWaves + wave;
+        const int64_t at = (row * strips + strip) * per;
+        const float top = read_strip<T, kSums, NT, true>(a, static_cast<const T*>(a.x) + row * a.stride, strip, s_powers, s_table,
+                                                         a.notes + at * 64, a.samples + at * 64, a.sums + at, a.refs + at);
+        if ((tid & 63) == 0) a.most[row * strips + strip] = top;
+    }
 }
 
-// The rest of a row that several workgroups have read.
-constexpr int kJoinThreads = 1024;
-template <typename T, bool kSums> __global__ __launch_bounds__(kJoinThreads) void k_sample_join(SampleArgs a)
+// The rest of such a row.
+template <typename T, bool kSums, int K, int BLOCKS> __global__ __launch_bounds__(K, 4) void k_sample_join(SampleArgs a)
 {
-    __shared__ Shared<kJoinThreads, kSampleBlocks> s;
-    const int tid = threadIdx.x;
+    typedef Shared<K, BLOCKS, 2048> S;
+    __shared__ S s;
+    const int tid = threadIdx.x, lane = tid & 63;
     const int64_t row = blockIdx.x;
-    const int32_t strips = a.slices * kWaves, per = blocks_of_strip(a), blocks = strips * per;
+    const int32_t strips = a.slices * kSampleWaves, per = blocks_of_strip(a), blocks = strips * per;
+    const bool filters = a.top_k > 0 || a.top_p < 1.0 || a.least > -__builtin_inf();
+    // at most 128 strips: two a lane
+    const float* const most = a.most + row * strips;
+    float m = lane < strips ? most[lane] : -__builtin_inff(), m2 = 64 + lane < strips ? most[64 + lane] : -__builtin_inff();
+    const float u = a.uniforms[row];
     if (tid < 32) s.table[tid] = kTwoTo[tid];
-    if (tid < strips) s.most[tid] = a.most[row * strips + tid];
     if (kSums && tid < blocks) {
         s.sums[tid] = a.sums[row * blocks + tid];
         s.refs[tid] = a.refs[row * blocks + tid];
     }
-    const uint32_t* const notes = reinterpret_cast<const uint32_t*>(a.notes + row * blocks * 64);
-    for (int i = tid; i < blocks * 32; i += kJoinThreads) reinterpret_cast<uint32_t*>(s.notes)[i] = notes[i];
+    if (filters) {
+        // eight notes to a load
+        const V4u* const notes = reinterpret_cast<const V4u*>(a.notes + row * blocks * 64);
+        V4u n[BLOCKS * 8 / K];
+#pragma unroll
+        for (int v = 0; v < BLOCKS * 8 / K; ++v)
+            if (v * K + tid < blocks * 8) n[v] = notes[v * K + tid];
+#pragma unroll
+        for (int v = 0; v < BLOCKS * 8 / K; ++v)
+            if (v * K + tid < blocks * 8) reinterpret_cast<V4u*>(s.notes)[v * K + tid] = n[v];
+    }
+    m = most_of(m, m2);
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) m = most_of(m, __shfl_xor(m, d));
     __syncthreads();
-    float m = s.most[0];
-    for (int i = 1; i < strips; ++i) m = most_of(m, s.most[i]);
-    RowWork<T, kJoinThreads, kSampleBlocks> work{a, s, static_cast<const T*>(a.x) + row * a.stride, 0.f, blocks, tid, 0.f};
-    work.finish(row, m, kSums);
+    RowWork<T, S, K> work{a, s, static_cast<const T*>(a.x) + row * a.stride, a.samples + row * blocks * 64, m, blocks, tid, u};
+    work.finish(row, kSums);
 }
+
+constexpr double kCacheBytes = 256 << 20; // the last-level cache
 
 template <typename T, bool kSums> hipError_t sample_as(const SampleArgs& a, hipStream_t s)
 {
-    const dim3 block(64 * kWaves);
-    if (a.slices == 1) {
-        hipLaunchKernelGGL((k_sample<T, kSums>), dim3((unsigned)std::min<int64_t>(a.rows, kMaxGrid)), block, 0, s, a);
+    if (a.slices == 0) {
+        hipLaunchKernelGGL((k_sample<T, kSums>), dim3((unsigned)std::min<int64_t>(a.rows, kMaxGrid)), dim3(64), 0, s, a);
         return hipGetLastError();
     }
-    hipLaunchKernelGGL((k_sample_read<T, kSums>), dim3((unsigned)(a.rows * a.slices)), block, 0, s, a);
+    const dim3 grid((unsigned)std::min<int64_t>((int64_t)a.rows * a.slices, kMaxGrid));
+    if ((double)a.rows * a.vocab * sizeof(T) > kCacheBytes)
+        hipLaunchKernelGGL((k_sample_read<T, kSums, true>), grid, dim3(kReadThreads), 0, s, a);
+    else
+        hipLaunchKernelGGL((k_sample_read<T, kSums, false>), grid, dim3(kReadThreads), 0, s, a);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
-    hipLaunchKernelGGL((k_sample_join<T, kSums>), dim3((unsigned)a.rows), dim3(kJoinThreads), 0, s, a);
+    if (a.rows <= kFewRows)
+        hipLaunchKernelGGL((k_sample_join<T, kSums, 512, kSampleBlocks>), dim3((unsigned)a.rows), dim3(512), 0, s, a);
+    else
+        hipLaunchKernelGGL((k_sample_join<T, kSums, 256, kManyBlocks>), dim3((unsigned)a.rows), dim3(256), 0, s, a);
     return hipGetLastError();
 }
 
@@ -854,20 +1180,22 @@ template <typename T> hipError_t sample_t(const SampleArgs& a, hipStream_t s)
 
 }  // namespace
 
-// How a row is cut: workgroups, steps of a wave's strip, steps of a block.
-void sample_split(int32_t rows, int32_t vocab, int dtype, int32_t* slices, int32_t* strip_steps, int32_t* shift)
+// How a row is cut.
+SampleSplit sample_split(int32_t rows, int32_t vocab, int dtype)
 {
     const int64_t step = kSampleLanes * kUnroll * (dtype == 0 ? Vec<uint16_t>::n : Vec<float>::n);
     const int64_t steps = (vocab + step - 1) / step;
-    int64_t cut = 1;
-    if (rows > 0 && rows <= kMaxSlicedRows && steps >= 8 * kWaves / 4)
-        cut = std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(32, 512 / rows), steps / kWaves));
-    const int64_t per = (steps + cut * kWaves - 1) / (cut * kWaves);
-    *slices = (int32_t)((steps + per * kWaves - 1) / (per * kWaves));
-    *strip_steps = (int32_t)per;
-    const int64_t most = (*slices == 1 ? kSampleBlocks / 2 : kSampleBlocks) / (*slices * kWaves);
-    *shift = 0;
-    while (((per - 1) >> *shift) + 1 > most) ++*shift;
+    SampleSplit x = {0, 1, (int32_t)steps, 0, (int32_t)steps};
+    if (steps <= kRowSteps) return x;
+    x.waves = kSampleWaves;
+    const int64_t cut = std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(32, kReadGroups / std::max(1, rows)), steps / kSampleWaves));
+    const int64_t per = (steps + cut * x.waves - 1) / (cut * x.waves);
+    x.slices = (int32_t)((steps + per * x.waves - 1) / (per * x.waves));
+    x.strip_steps = (int32_t)per;
+    const int64_t most = (rows <= kFewRows ? kSampleBlocks : kManyBlocks) / (x.slices * x.waves);
+    while (((per - 1) >> x.shift) + 1 > most) ++x.shift;
+    x.blocks = x.slices * x.waves * (int32_t)(((per - 1) >> x.shift) + 1);
+    return x;
 }
 
 hipError_t launch_sample(int dtype, const SampleArgs& a, hipStream_t s)
