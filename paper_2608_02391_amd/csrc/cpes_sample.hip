@@ -50,7 +50,7 @@ constexpr int kFewRows = 256;
 constexpr int kManyBlocks = 96;          // of a row among many
 constexpr int kReadGroups = 1024;        // workgroups that read few rows
 constexpr double kExact = 2048.0;         // c x up to which the rounding of c max x, 2^-42, is let through
-constexpr double kFar = -100.0;           // weights below 2^kFar of the largest count as 0
+constexpr double kFar = -52.0;           // weights below 2^kFar of the largest count as 0
 
 template <typename T> struct Vec { static constexpr int n = 16 / sizeof(T); };
 
@@ -127,27 +127,28 @@ __device__ __forceinline__ double power(double t, const double* table)
     return __longlong_as_double(__double_as_longlong(w) + ((long long)(int)(k & ~31u) << 47));
 }
 
-// The same for the pass over the logits, which does little else: 2^(k / 16) for all k there
-// are, so that no exponent has to be put together, and a series off by (ln 2 / 32)^5 / 120 =
-// 4e-11 at most, to either side.  Relative to some logit of the wave's, exponents go from
-// kLow, which stands for what is below and gives 0, to kRoom.
-constexpr int kLow = -112, kRoom = 15, kSteps = 16;
-constexpr int kPowers = (kRoom + 1 - kLow) * kSteps;
+// The same for the pass over the logits, which does little else and is bound by it: t comes as cells of
+// 1/64 octave from kLow on, whose beginnings are in a table that leaves no exponent to be put
+// together; in a cell 2^(r / 64) = 1 + a1 r + a2 r^2 + a3 r^3, r < 1, off by 2^-37.5 at most (a minimax
+// fit that is exact at 0).  The conversion takes what is below the table, -inf too, to its first entry,
+// which is 0, and the fraction's clamp takes -inf's NaN to 0.
+constexpr int kLow = -56, kRoom = 7, kCells = 64;
+constexpr int kPowers = (kRoom + 1 - kLow) * kCells;
 
 template <int K> __device__ __forceinline__ void fill_powers(double* powers)
 {
     for (int i = threadIdx.x; i < kPowers; i += K)
-        powers[i] = i == 0 ? 0.0 : ldexp(kTwoTo[2 * (i % kSteps)], i / kSteps + kLow);
+        powers[i] = i == 0 ? 0.0 : ldexp(kTwoTo[i % kCells / 2] * (i & 1 ? 0x1.02c9a3e778061p+0 : 1.0), i / kCells + kLow);
 }
 
-__device__ __forceinline__ double quick_power(double t, const double* powers)
+// sum + 2^t for t of `cells` / 64 + kLow.
+__device__ __forceinline__ double add_power(double sum, double cells, const double* powers)
 {
-    constexpr double kRound = 0x1.8p+48 - kLow;         // 1.5 2^52 / 16, and the table's beginning: the low bits are its index
-    constexpr double a1 = 0.69314718055994530942, a2 = a1 * a1 / 2, a3 = a2 * a1 / 3, a4 = a3 * a1 / 4;
-    const double y = t + kRound, r = t - (y - kRound);
-    const double f = powers[(uint32_t)__double_as_longlong(y)];
-    const double p = r * fma(r, fma(r, fma(r, a4, a3), a2), a1);
-    return fma(f, p, f);
+    uint32_t cell;
+    double r;
+    asm("v_cvt_u32_f64_e32 %0, %1" : "=v"(cell) : "v"(cells));
+    asm("v_fract_f64_e64 %0, %1 clamp" : "=v"(r) : "v"(cells));
+    return fma(powers[cell], fma(r, fma(r, fma(r, 0x1.c90fc991be8ebp-23, 0x1.ebfa7f9763063p-15), 0x1.62e43029bdff8p-7), 1.0), sum);
 }
 
 // The logits of a vector one after the other, so that a loop over them need not be unrolled: most
@@ -270,7 +271,13 @@ __device__ float read_strip(const SampleArgs& a, const T* x0, int32_t strip, con
                 w[u] = vector_at(x0, a.vocab, i + u * kSampleLanes);
         }
     };
-    auto term = [&](double t) { return kQuick ? quick_power(t, powers) : t > kLow ? power(t, table) : 0.0; };
+    const double cells = a.c * kCells;
+    auto add = [&](double t) {
+        if constexpr (kQuick)
+            sum = add_power(sum, t, powers);
+        else if (t > 0.0)
+            sum += power(t / kCells + kLow, table);
+    };
     auto take = [&](const float* x) {
         float top = x[0];
 #pragma unroll
@@ -287,17 +294,17 @@ __device__ float read_strip(const SampleArgs& a, const T* x0, int32_t strip, con
                     const double t = a.c * ((double)ref - (double)high);
                     sum = t < 2 * kLow ? 0.0 : sum * power(t, table);
                     ref = high;
-                    base = a.c * (double)ref;
+                    base = cells * (double)ref + kLow * kCells;
                 }
             }
-            if (fabs(base) <= kExact) {
+            if (fabs(base) <= kExact * kCells) {
                 if (ref > -__builtin_inff()) {
 #pragma unroll
-                    for (int j = 0; j < M; ++j) sum += term(fmax(fma((double)x[j], a.c, -base), (double)kLow));
+                    for (int j = 0; j < M; ++j) add(fma((double)x[j], cells, -base));
                 }
             } else {
 #pragma unroll
-                for (int j = 0; j < M; ++j) sum += term(fmax(((double)x[j] - (double)ref) * a.c, (double)kLow));
+                for (int j = 0; j < M; ++j) add(((double)x[j] - (double)ref) * cells - kLow * kCells);
             }
         }
     };
@@ -347,7 +354,6 @@ template <int K, int BLOCKS, int BINS> struct Shared {
     int32_t ties[BLOCKS];
     double table[32];
     double wave[K / 64];
-    Key wave_mass[K / 64];
     uint32_t wave_count[K / 64];
     union {
         struct {
@@ -362,7 +368,6 @@ template <int K, int BLOCKS, int BINS> struct Shared {
     float value;
     uint32_t found;
     double total;
-    Key bound;
 };
 
 // Sum over the workgroup's threads up to and including each; *total receives all.
@@ -555,7 +560,7 @@ template <typename T, typename S, int K> struct RowWork {
             for (int64_t i = i0; i < min(last, i0 + THREADS * kDepth); i += THREADS) {
                 Logits<T> x = {w[0]};
                 if (i >= full) x.w = vector_at(x0, to, i);
-#pragma unroll 1
+#pragma unroll 2
                 for (int j = 0; j < N; ++j) f(x.next(), (uint32_t)(i * N + j));
 #pragma unroll
                 for (int d = 1; d < kDepth; ++d) w[d - 1] = w[d];
@@ -779,16 +784,29 @@ template <typename T, typename S, int K> struct RowWork {
     __device__ Cut search(uint32_t lo, uint32_t hi, int64_t number, double enough, bool by_weight, double* weight_left)
     {
         constexpr uint32_t kFirst = 0x00800000, kLast = 0xFF7FFFFF;            // finite numbers
-        // weights as whole numbers, so that their sums do not depend on the order: 2^units for the largest
-        const int units = min(44, 62 - (32 - __clz((int)a.vocab)));
-        const double unit = (double)((uint64_t)1 << units);
+        // bf16 logits have 16 bits of order, and a bin may be one of them, whose weight is its number of times one weight
+        constexpr int kLeast = std::is_same<T, uint16_t>::value ? 16 : 0;
+        const auto logit = [](uint32_t o) { return value_at(kLeast > 0 && o < 0x80000000u ? o | 0xFFFFu : o); };
         const int64_t vecs = ((int64_t)a.vocab + N - 1) / N;
+        double* const masses = reinterpret_cast<double*>(s.mass);
         bool above_known = false;
         double above = 0.0;               // weight, and number, of what lies above hi
         int64_t above_count = 0;
+#pragma unroll 1
         while (true) {
-            int sh = 0;
+            if (kLeast > 0) {
+                lo &= 0xFFFF0000u;
+                hi |= 0x0000FFFFu;
+                // nothing lies above hi where the bins reach that far
+                if (!above_known && (order_of(m) - lo) >> kLeast < kBins) hi = order_of(m) | 0xFFFFu;
+            }
+            int sh = kLeast;
             while (((hi - lo) >> sh) >= kBins) ++sh;
+            const bool alike = kLeast > 0 && sh == kLeast;
+            const float least = value_at(lo), most = value_at(hi), known_from = above_known ? most : __builtin_inff();
+            // weights as whole numbers, so that their sums do not depend on the order: 2^units for the largest of them
+            const int units = 62 - (32 - __clz((int)a.vocab));
+            const double unit = (double)((uint64_t)1 << units) / fmax(weight(fminf(most, m)), 0x1p-100);
             for (int i = tid; i < kBins; i += K) {
                 s.mass[i] = 0;
                 s.count[i] = 0;
@@ -796,16 +814,14 @@ template <typename T, typename S, int K> struct RowWork {
             __syncthreads();
             double mine = 0.0;
             uint32_t mine_count = 0;
-            const float least = value_at(lo), most = value_at(hi), known_from = above_known ? most : __builtin_inff();
             each_logit<K>(0, vecs, a.vocab, tid, [&](float x, uint32_t) {
-                if (!(x >= least) || x > known_from) return;
-                const double w = weight(x);
+                if (!(x >= least) || x > known_from || x == -__builtin_inff()) return;
                 if (x > most) {
-                    mine += w;
+                    mine += weight(x);
                     ++mine_count;
                 } else {
                     const uint32_t bin = (order_of(x) - lo) >> sh;
-                    atomicAdd(&s.mass[bin], (Key)(w * unit + 0.5));
+                    if (!alike) atomicAdd(&s.mass[bin], (Key)(weight(x) * unit + 0.5));
                     atomicAdd(&s.count[bin], 1u);
                 }
             });
@@ -819,71 +835,83 @@ template <typename T, typename S, int K> struct RowWork {
             // from the top: the bin in which the number or the weight is reached
             constexpr int PER = kBins / K;
             const int top = kBins - 1 - tid * PER;
-            Key mass = 0, all_mass;
+            double mass = 0.0, all_mass;
             uint32_t count = 0, all_count;
 #pragma unroll 1
             for (int e = 0; e < PER; ++e) {
-                mass += s.mass[top - e];
-                count += s.count[top - e];
+                const int bin = top - e;
+                const uint32_t n = s.count[bin];
+                double w = 0.0;
+                if (n) w = alike ? n * weight(logit(lo + ((uint32_t)bin << sh))) : (double)s.mass[bin] / unit;
+                masses[bin] = w;
+                mass += w;
+                count += n;
             }
-            Key mass_upto = block_scan<K>(mass, s.wave_mass, &all_mass) - mass;
+            double mass_upto = block_scan<K>(mass, s.wave, &all_mass) - mass;
             uint32_t count_upto = block_scan<K>(count, s.wave_count, &all_count) - count;
-            const auto reached = [&](Key x, uint32_t n) {
-                return by_weight ? !(above + (double)x / unit < enough) : above_count + n >= number;
-            };
-            const bool inside = !reached(0, 0) && reached(all_mass, all_count);
-            const bool everything = lo == kFirst && hi == kLast;
-            if (!inside && !above_known && !everything) {
+            const auto reached = [&](double x, uint32_t n) { return by_weight ? !(above + x < enough) : above_count + n >= number; };
+            const bool inside = !reached(0.0, 0) && reached(all_mass, all_count);
+            if (!inside && !above_known && !(lo <= kFirst && hi >= order_of(m))) {
                 lo = kFirst;
                 hi = kLast;
                 __syncthreads();
                 continue;
             }
-            if (tid == 0) s.found = 0;
+            if (tid == 0) {
+                s.found = 0;
+                s.place = 0;
+            }
             __syncthreads();
-            // where roundings leave none, the lowest with anything in it
+            // the first bin with anything in it that reaches it; where roundings leave none, the lowest one
 #pragma unroll 1
             for (int e = 0; e < PER; ++e) {
                 const int bin = top - e;
-                if (s.count[bin] == 0) continue;
-                const Key m1 = mass_upto + s.mass[bin];
-                const uint32_t n1 = count_upto + s.count[bin];
-                if (inside ? reached(m1, n1) && !reached(mass_upto, count_upto) : n1 == all_count) {
-                    s.found = bin + 1;
-                    s.bound = mass_upto;
-                    s.number = (int32_t)count_upto;
-                }
-                mass_upto = m1;
-                count_upto = n1;
+                const uint32_t n = s.count[bin];
+                mass_upto += masses[bin];
+                count_upto += n;
+                if (n && reached(mass_upto, count_upto)) atomicMax(&s.found, (uint32_t)bin + 1);
+                if (n && count_upto == all_count) s.place = bin + 1;
             }
             __syncthreads();
-            const uint32_t found = s.found;
+            const uint32_t found = inside && s.found ? s.found : s.place;
             if (found == 0) {             // nothing that counts
                 *weight_left = above;
                 return kEverything;
             }
             const uint32_t bin = found - 1, here = s.count[bin];
-            const double each = (double)s.mass[bin] / unit;
-            above += (double)s.bound / unit;
-            above_count += (uint32_t)s.number;
+            const double weighs = masses[bin];
+            __syncthreads();
+            // what lies above that bin
+            mass = 0.0;
+            count = 0;
+#pragma unroll 1
+            for (int e = 0; e < PER; ++e)
+                if ((uint32_t)(top - e) > bin) {
+                    mass += masses[top - e];
+                    count += s.count[top - e];
+                }
+            block_scan<K>(mass, s.wave, &all_mass);
+            block_scan<K>(count, s.wave_count, &all_count);
+            above += all_mass;
+            above_count += all_count;
             above_known = true;
             __syncthreads();
             hi = min(hi, lo + (bin << sh) + ((1u << sh) - 1));
             lo += bin << sh;
-            if (sh > 0) continue;
+            if (sh > kLeast) continue;
             // `here` logits alike: as many of them as it takes, by the lowest tokens
             int64_t ties = here;
             if (inside) {
                 if (by_weight) {
-                    const double w = weight(value_at(lo));
-                    ties = w > 0.0 ? (int64_t)ceil((enough - above) / w * (1 - 0x1p-50)) : here;
-                    ties = max((int64_t)1, min((int64_t)here, ties));
+                    const double w = weighs / here;
+                    if (w > 0.0) ties = (int64_t)fmin(ceil((enough - above) / w * (1 - 0x1p-50)), (double)here);
+                    ties = max(ties, (int64_t)1);
                 } else {
-                    ties = number - above_count;
+                    ties = max((int64_t)1, min((int64_t)here, number - above_count));
                 }
             }
-            *weight_left = above + each * ((double)ties / here);
-            return Cut{lo, (int32_t)ties};
+            *weight_left = above + weighs * ((double)ties / here);
+            return Cut{order_of(logit(lo)), (int32_t)ties};
         }
     }
 

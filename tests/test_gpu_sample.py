@@ -11,9 +11,10 @@ import paper_2608_02391_amd as cp
 pytestmark = pytest.mark.gpu
 BF16, F32 = torch.bfloat16, torch.float32
 
-# Weights are off by 2^-39 at most and sums by some roundings of 64 bits: a draw nearer than this to a
-# border (of the tokens, or of what top_p keeps), relative to the sum, may fall on either side.
-NEAR = 2.0 ** -38
+# Weights are off by 2^-37.5 at most, those of a whole row's sum by as much again, and sums by some roundings of
+# 64 bits: a draw nearer than this to a border (of the tokens, or of what top_p keeps), relative to the sum, may fall
+# on either side.
+NEAR = 2.0 ** -36
 
 
 def run(x, u, top_k=0, top_p=1.0, min_p=0.0, scale=1.0, stream=None, logp=True):
@@ -41,7 +42,7 @@ def check(x, u, rows=None, **kw):
             assert float(logp[r]) == ref_logp
         elif margin >= NEAR:
             # 64-bit sums as above, then one rounding to 32 bits
-            assert abs(float(logp[r]) - ref_logp) <= 2.0 ** -24 * abs(ref_logp) + 2.0 ** -37, (r, float(logp[r]), ref_logp, kw)
+            assert abs(float(logp[r]) - ref_logp) <= 2.0 ** -24 * abs(ref_logp) + 2.0 ** -36, (r, float(logp[r]), ref_logp, kw)
     assert near <= 1
     return token, logp
 
