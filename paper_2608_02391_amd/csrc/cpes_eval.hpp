@@ -210,10 +210,13 @@ constexpr int kSampleWaves = 4;          // strips of a slice, where a row is cu
 constexpr int kSampleBlocks = 256;       // blocks of such a row at most
 constexpr int kSampleRows = 1024;        // more rows are all cut alike
 
-// How a row of logits is cut: into slices of a workgroup (0: one wave does the row), strips
-// of a wave, blocks of 2^shift steps.
+// How a row of logits is cut: into slices of a workgroup (0: one wave does the row) and strips
+// of a wave; a strip into blocks of 2^shift steps, of which there are `slots`, and parts of
+// 2^note_shift, room for note_slots of which, stored 2^group together.
 struct SampleSplit {
-    int32_t slices, waves, strip_steps, shift, blocks;
+    int32_t slices, waves, strip_steps, shift, slots, note_shift, note_slots, group;
+
+    int32_t strips() const { return (slices > 0 ? slices : 1) * waves; }
 };
 
 struct SampleArgs {
@@ -221,14 +224,15 @@ struct SampleArgs {
     const float* uniforms;
     int64_t* tokens;
     float* logp;
-    uint16_t* notes;             // [rows][blocks][64]: maxima of 64 parts of each block
-    uint16_t* samples;           // [rows][blocks][64]: a logit of each of these parts
-    double* sums;                // [rows][blocks]
-    float* refs;                 // [rows][blocks]: what the sums' exponents are relative to
+    uint16_t* notes;             // [rows][strips][note_slots / 2^group][64][2^group]: maxima of the lanes' parts
+    uint16_t* samples;           // a logit of each of these parts
+    double* sums;                // [rows][strips][slots]
+    float* refs;                 // [rows][strips][slots]: what the sums' exponents are relative to
     float* most;                 // [rows][strips]: maxima, NaN where there is one
     int64_t stride;
     int32_t rows, vocab;
-    int32_t slices, waves, strip_steps, shift;
+    int32_t slices, waves, strip_steps, shift, slots, note_shift, note_slots, group;
+    bool notes_kept, samples_kept;
     int32_t top_k;               // 0: all
     double top_p;
     double least;                // ln min_p, or -inf

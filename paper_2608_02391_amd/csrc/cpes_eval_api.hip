@@ -243,8 +243,8 @@ size_t sample_bytes(int32_t rows, int32_t vocab, int dtype)
 {
     const cpes::SampleSplit x = cpes::sample_split(rows, vocab, dtype);
     if (x.slices == 0) return 0;
-    return rows * round16((size_t)x.blocks * (2 * cpes::kSampleLanes * sizeof(uint16_t) + sizeof(double) + sizeof(float)) +
-                          (size_t)x.slices * x.waves * sizeof(float));
+    return rows * round16((size_t)x.strips() * (x.note_slots * 2 * cpes::kSampleLanes * sizeof(uint16_t) +
+                                                x.slots * (sizeof(double) + sizeof(float)) + sizeof(float)));
 }
 
 size_t logprob_bytes(int32_t rows, int32_t slices, int32_t top)
@@ -723,12 +723,16 @@ int cpes_sample(const void* x_dev, int dtype, int32_t rows, int32_t vocab, int64
     a.waves = split.waves;
     a.strip_steps = split.strip_steps;
     a.shift = split.shift;
-    const size_t blocks = (size_t)rows * split.blocks;
+    a.slots = split.slots;
+    a.note_shift = split.note_shift;
+    a.note_slots = split.note_slots;
+    a.group = split.group;
+    const size_t strips = (size_t)rows * split.strips(), notes = strips * split.note_slots * cpes::kSampleLanes;
     a.notes = static_cast<uint16_t*>(workspace_dev);            // 16 bytes at a time
-    a.samples = a.notes + blocks * cpes::kSampleLanes;
-    a.sums = reinterpret_cast<double*>(a.samples + blocks * cpes::kSampleLanes);
-    a.refs = reinterpret_cast<float*>(a.sums + blocks);
-    a.most = a.refs + blocks;
+    a.samples = a.notes + notes;
+    a.sums = reinterpret_cast<double*>(a.samples + notes);
+    a.refs = reinterpret_cast<float*>(a.sums + strips * split.slots);
+    a.most = a.refs + strips * split.slots;
     a.stride = stride;
     a.rows = rows;
     a.vocab = vocab;

@@ -40,7 +40,6 @@ typedef V4u V4uAnywhere __attribute__((aligned(2)));
 typedef unsigned long long Key;
 
 constexpr int kUnroll = 4;                // vectors of a lane and step
-constexpr int kCandidates = 512;          // tokens that are ranked
 constexpr int kParts = 384;               // parts of blocks that are read again for them
 constexpr int kFirstParts = 48;           // and how many at first, where top_p decides
 constexpr int kCounted = 128;             // keys ranked by counting
@@ -48,6 +47,7 @@ constexpr int kDepth = 8;                 // vectors of a thread under way where
 constexpr int64_t kMaxGrid = 1 << 20;
 constexpr int kFewRows = 256;
 constexpr int kManyBlocks = 96;          // of a row among many
+constexpr int kManyParts = 32;           // and parts, of 64 lanes
 constexpr int kReadGroups = 1024;        // workgroups that read few rows
 constexpr double kExact = 2048.0;         // c x up to which the rounding of c max x, 2^-42, is let through
 constexpr double kFar = -52.0;           // weights below 2^kFar of the largest count as 0
@@ -141,14 +141,36 @@ template <int K> __device__ __forceinline__ void fill_powers(double* powers)
         powers[i] = i == 0 ? 0.0 : ldexp(kTwoTo[i % kCells / 2] * (i & 1 ? 0x1.02c9a3e778061p+0 : 1.0), i / kCells + kLow);
 }
 
-// sum + 2^t for t of `cells` / 64 + kLow.
-__device__ __forceinline__ double add_power(double sum, double cells, const double* powers)
+// sum + 2^t for N exponents t = cells(j) / 64 + kLow.  The table's entries of the next four are asked for
+// before the last four are used: a wave waits for none of them (4,096 rows of 151,936: 385 us each on its
+// own, 345 so).
+template <int N, typename F> __device__ __forceinline__ double add_powers(double sum, const double* powers, F cells)
 {
-    uint32_t cell;
-    double r;
-    asm("v_cvt_u32_f64_e32 %0, %1" : "=v"(cell) : "v"(cells));
-    asm("v_fract_f64_e64 %0, %1 clamp" : "=v"(r) : "v"(cells));
-    return fma(powers[cell], fma(r, fma(r, fma(r, 0x1.c90fc991be8ebp-23, 0x1.ebfa7f9763063p-15), 0x1.62e43029bdff8p-7), 1.0), sum);
+    constexpr int G = 4;
+    double f[2][G], r[2][G];
+    auto ask = [&](int j) {
+#pragma unroll
+        for (int e = 0; e < G; ++e) {
+            const double t = cells(j + e);
+            uint32_t cell;
+            asm("v_cvt_u32_f64_e32 %0, %1" : "=v"(cell) : "v"(t));
+            asm("v_fract_f64_e64 %0, %1 clamp" : "=v"(r[j / G & 1][e]) : "v"(t));
+            f[j / G & 1][e] = powers[cell];
+        }
+    };
+    ask(0);
+#pragma unroll
+    for (int j = 0; j < N; j += G) {
+        __builtin_amdgcn_sched_barrier(0);
+        if (j + G < N) ask(j + G);
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int e = 0; e < G; ++e) {
+            const double x = r[j / G & 1][e];
+            sum = fma(f[j / G & 1][e], fma(x, fma(x, fma(x, 0x1.c90fc991be8ebp-23, 0x1.ebfa7f9763063p-15), 0x1.62e43029bdff8p-7), 1.0), sum);
+        }
+    }
+    return sum;
 }
 
 // The logits of a vector one after the other, so that a loop over them need not be unrolled: most
@@ -240,10 +262,32 @@ template <typename T> struct Strip {
     }
 };
 
-__device__ __forceinline__ int32_t blocks_of_strip(const SampleArgs& a)
-{
-    return ((a.strip_steps - 1) >> a.shift) + 1;
-}
+// 16 bits a part of each lane, stored for up to 8 parts together.  They cost more than their bytes: 39 MB of
+// them, however stored, make the pass over 4,096 rows of 151,936 without sums 230 us long, 184 without
+// any; so where rows are many a part is of 4 steps and more.
+struct Notes {
+    V4u w;
+
+    __device__ __forceinline__ void push(uint16_t x)
+    {
+        w[0] = __builtin_amdgcn_alignbit(w[1], w[0], 16);
+        w[1] = __builtin_amdgcn_alignbit(w[2], w[1], 16);
+        w[2] = __builtin_amdgcn_alignbit(w[3], w[2], 16);
+        w[3] = w[3] >> 16 | (uint32_t)x << 16;
+    }
+    // The last 2^group of them, a lane's beside each other.
+    __device__ __forceinline__ void store(uint16_t* to, int32_t group, int lane) const
+    {
+        if (group == 3)
+            reinterpret_cast<V4u*>(to)[lane] = w;
+        else if (group == 2)
+            reinterpret_cast<V2u*>(to)[lane] = V2u{w[2], w[3]};
+        else if (group == 1)
+            reinterpret_cast<uint32_t*>(to)[lane] = w[3];
+        else
+            to[lane] = (uint16_t)(w[3] >> 16);
+    }
+};
 
 // One strip, by a wave: notes, samples, sums and what they are relative to, of its blocks;
 // the strip's maximum is returned to all lanes.  NT: past the caches.
@@ -251,38 +295,27 @@ template <typename T, bool kSums, bool NT, bool kQuick>
 __device__ float read_strip(const SampleArgs& a, const T* x0, int32_t strip, const double* powers, const double* table,
                             uint16_t* notes, uint16_t* samples, double* sums, float* refs)
 {
-    constexpr int N = Vec<T>::n, M = kUnroll * N;
+    constexpr int N = Vec<T>::n;
     const int lane = threadIdx.x & 63;
     const Strip<T> s(a, strip);
-    const int32_t blocks = blocks_of_strip(a), per = 1 << a.shift;
+    const int32_t per = 1 << a.shift, per_part = 1 << a.note_shift;
+    Notes note = {}, sample = {};
     const int32_t whole = (int32_t)max((int64_t)0, min((int64_t)s.steps, ((int64_t)a.vocab / N - s.first) / (kSampleLanes * kUnroll)));
     float most = -__builtin_inff(), ref = -__builtin_inff(), noted = -__builtin_inff();
     double sum = 0.0, base = 0.0;
     const float room = (float)fmin(kRoom / a.c, 1e38);
-    V4u w[kUnroll];
-    auto load = [&](int32_t step) {
-        const int64_t i = s.first + (int64_t)step * (kSampleLanes * kUnroll) + lane;
-#pragma unroll
-        for (int u = 0; u < kUnroll; ++u) {
-            const V4uAnywhere* const at = reinterpret_cast<const V4uAnywhere*>(x0 + (i + u * kSampleLanes) * N);
-            if (step < whole)
-                w[u] = NT ? __builtin_nontemporal_load(at) : *at;
-            else
-                w[u] = vector_at(x0, a.vocab, i + u * kSampleLanes);
-        }
-    };
     const double cells = a.c * kCells;
-    auto add = [&](double t) {
-        if constexpr (kQuick)
-            sum = add_power(sum, t, powers);
-        else if (t > 0.0)
-            sum += power(t / kCells + kLow, table);
+    V4u w[kUnroll];
+    auto load = [&](int32_t step, int u) {
+        const V4uAnywhere* const at =
+            reinterpret_cast<const V4uAnywhere*>(x0 + (s.first + (int64_t)step * (kSampleLanes * kUnroll) + u * kSampleLanes + lane) * N);
+        w[u] = NT ? __builtin_nontemporal_load(at) : *at;
     };
+    // the N logits of a vector
     auto take = [&](const float* x) {
         float top = x[0];
 #pragma unroll
-        for (int j = 1; j < M; ++j) top = most_of(top, x[j]);
-        most = most_of(most, top);
+        for (int j = 1; j < N; ++j) top = most_of(top, x[j]);
         noted = most_of(noted, top);
         if constexpr (kSums) {
             if (__any(top > ref + room)) {
@@ -297,22 +330,34 @@ __device__ float read_strip(const SampleArgs& a, const T* x0, int32_t strip, con
                     base = cells * (double)ref + kLow * kCells;
                 }
             }
-            if (fabs(base) <= kExact * kCells) {
-                if (ref > -__builtin_inff()) {
+            auto add = [&](auto t) {
+                if constexpr (kQuick) {
+                    sum = add_powers<N>(sum, powers, t);
+                } else {
 #pragma unroll
-                    for (int j = 0; j < M; ++j) add(fma((double)x[j], cells, -base));
+                    for (int j = 0; j < N; ++j)
+                        if (t(j) > 0.0) sum += power(t(j) / kCells + kLow, table);
                 }
+            };
+            if (fabs(base) <= kExact * kCells) {
+                if (ref > -__builtin_inff()) add([&](int j) { return fma((double)x[j], cells, -base); });
             } else {
-#pragma unroll
-                for (int j = 0; j < M; ++j) add(((double)x[j] - (double)ref) * cells - kLow * kCells);
+                add([&](int j) { return ((double)x[j] - (double)ref) * cells - kLow * kCells; });
             }
         }
     };
-    auto end_block = [&](int32_t step, float sample) {
-        const int32_t b = step >> a.shift;
-        notes[b * 64 + lane] = note_of(noted);
-        samples[b * 64 + lane] = note_of(sample);
-        noted = -__builtin_inff();
+    const int32_t together = (1 << a.group) - 1;
+    auto end_part = [&](int32_t p, uint16_t most_here, uint16_t one) {
+        if (a.notes_kept) {
+            note.push(most_here);
+            if ((p & together) == together) note.store(notes + (p & ~together) * 64, a.group, lane);
+        }
+        if (a.samples_kept) {
+            sample.push(one);
+            if ((p & together) == together) sample.store(samples + (p & ~together) * 64, a.group, lane);
+        }
+    };
+    auto end_block = [&](int32_t b) {
         if constexpr (kSums) {
             const double all = wave_sum(sum);
             if (lane == 63) {
@@ -322,33 +367,65 @@ __device__ float read_strip(const SampleArgs& a, const T* x0, int32_t strip, con
             sum = 0.0;
         }
     };
-    if (s.steps > 0) load(0);
-    for (int32_t step = 0; step < s.steps; ++step) {
-        float x[M];
+    if (whole > 0) {
 #pragma unroll
-        for (int u = 0; u < kUnroll; ++u) unpack<T>(w[u], x + u * N);
-        if (step + 1 < s.steps) load(step + 1);
-        take(x);
-        if ((step & (per - 1)) == per - 1 || step + 1 == s.steps) end_block(step, x[0]);
+        for (int u = 0; u < kUnroll; ++u) load(0, u);
     }
-    for (int32_t b = s.steps == 0 ? 0 : ((s.steps - 1) >> a.shift) + 1; b < blocks; ++b) {
-        notes[b * 64 + lane] = kNoteNothing;
-        samples[b * 64 + lane] = kNoteNothing;
-        if (kSums && lane == 0) {
-            sums[b] = 0.0;
-            refs[b] = -__builtin_inff();
+    for (int32_t step = 0; step < s.steps; ++step) {
+        if (step >= whole) {
+            // the row's last step
+#pragma unroll 1
+            for (int u = 0; u < kUnroll; ++u) {
+                const V4u last = vector_at(x0, a.vocab, s.first + (int64_t)step * (kSampleLanes * kUnroll) + u * kSampleLanes + lane);
+                w[0] = w[1];
+                w[1] = w[2];
+                w[2] = w[3];
+                w[3] = last;
+            }
+        }
+        float one = 0.f;
+        if constexpr (kSums) {
+            // a vector at a time: the registers are for the powers
+#pragma unroll
+            for (int u = 0; u < kUnroll; ++u) {
+                float x[N];
+                unpack<T>(w[u], x);
+                if (step + 1 < whole) load(step + 1, u);
+                if (u == 0) one = x[0];
+                take(x);
+            }
+        } else {
+            float x[kUnroll][N];
+#pragma unroll
+            for (int u = 0; u < kUnroll; ++u) unpack<T>(w[u], x[u]);
+            if (step + 1 < whole) {
+#pragma unroll
+                for (int u = 0; u < kUnroll; ++u) load(step + 1, u);
+            }
+            one = x[0][0];
+#pragma unroll
+            for (int u = 0; u < kUnroll; ++u) take(x[u]);
+        }
+        if ((step & (per - 1)) == per - 1 || step + 1 == s.steps) end_block(step >> a.shift);
+        if ((step & (per_part - 1)) == per_part - 1 || step + 1 == s.steps) {
+            most = most_of(most, noted);
+            end_part(step >> a.note_shift, note_of(noted), note_of(one));
+            noted = -__builtin_inff();
         }
     }
+    static_assert(kUnroll == 4, "the last step fills w from behind");
+    for (int32_t b = s.steps == 0 ? 0 : ((s.steps - 1) >> a.shift) + 1; b < a.slots; ++b) end_block(b);
+    for (int32_t p = s.steps == 0 ? 0 : ((s.steps - 1) >> a.note_shift) + 1; p < a.note_slots; ++p) end_part(p, kNoteNothing, kNoteNothing);
 #pragma unroll
     for (int d = 1; d < 64; d <<= 1) most = most_of(most, __shfl_xor(most, d));
     return most;
 }
 
 // What a row's work keeps in LDS.
-template <int K, int BLOCKS, int BINS> struct Shared {
+template <int K, int BLOCKS, int PARTS, int BINS> struct Shared {
+    static constexpr int kCandidates = BINS > 1024 ? BINS / 2 : 512;      // tokens that are ranked
     static constexpr int kBins = BINS;    // of a histogram
-    static constexpr int kBlocks = BLOCKS;
-    alignas(16) uint16_t notes[BLOCKS * 64];          // maxima of the parts of each block
+    alignas(16) uint16_t notes[PARTS * 64];           // maxima of parts
     double sums[BLOCKS];
     float refs[BLOCKS];
     int32_t ties[BLOCKS];
@@ -402,13 +479,13 @@ struct Cut {
 constexpr Cut kEverything = {0, 0};       // order 0 is a NaN's
 
 template <typename T, typename S, int K> struct RowWork {
-    static constexpr int N = Vec<T>::n, kBins = S::kBins;
+    static constexpr int N = Vec<T>::n, kBins = S::kBins, kCandidates = S::kCandidates;
     const SampleArgs& a;
     S& s;
     const T* x0;
-    const uint16_t* samples;              // a logit of each part of the blocks
+    const uint16_t* samples;              // a logit of each part
     float m;                              // the row's largest logit
-    int32_t blocks;
+    int32_t blocks, parts;                // parts of 64 lanes
     int32_t tid;
 
     __device__ __forceinline__ double weight(float x) const
@@ -423,7 +500,7 @@ template <typename T, typename S, int K> struct RowWork {
     // First token of a block; blocks follow each other in token order.
     __device__ __forceinline__ int64_t block_begin(int32_t b) const
     {
-        const int32_t per_strip = blocks_of_strip(a), strip = b / per_strip, i = b - strip * per_strip;
+        const int32_t strip = b / a.slots, i = b - strip * a.slots;
         return min((int64_t)a.vocab, ((int64_t)strip * a.strip_steps + min((int64_t)a.strip_steps, (int64_t)i << a.shift)) *
                                          (kSampleLanes * kUnroll * N));
     }
@@ -539,6 +616,7 @@ template <typename T, typename S, int K> struct RowWork {
     }
 
     float u;                              // the number given
+    uint32_t weights_from = 0;            // where not 0, s.mass holds the weights of bf16 logits of orders from here on
     __device__ __forceinline__ double uniform() const
     {
         constexpr double kLast = 1.0 - 0x1p-53;
@@ -585,7 +663,7 @@ template <typename T, typename S, int K> struct RowWork {
         for (int i = tid; i < kBins; i += K) s.count[i] = 0;
         __syncthreads();
 #pragma unroll 1
-        for (int i = tid; i < blocks * 64; i += K) {
+        for (int i = tid; i < parts * 64; i += K) {
             const uint32_t order = s.notes[i];
             if (order > kNoteNothing) atomicAdd(&s.count[note_bin(order)], 1u);
         }
@@ -627,26 +705,28 @@ template <typename T, typename S, int K> struct RowWork {
     // which may exceed what there is room for.  The parts are listed, and then read together.
     __device__ int32_t collect(int bin, float bound)
     {
-        uint32_t* const parts = reinterpret_cast<uint32_t*>(s.ranked);
+        uint32_t* const list = reinterpret_cast<uint32_t*>(s.ranked);
         const uint32_t least = max((uint32_t)note_of(bound), kNoteNothing + 1u);
         if (tid == 0) s.number = s.place = 0;
         __syncthreads();
 #pragma unroll 1
-        for (int i = tid; i < blocks * 64; i += K) {
+        for (int i = tid; i < parts * 64; i += K) {
             const uint32_t order = s.notes[i];
             if (order >= least && note_bin(order) <= bin) {
                 const int at = atomicAdd(&s.place, 1);
-                if (at < kParts) parts[at] = i;
+                if (at < kParts) list[at] = i;
             }
         }
         __syncthreads();
         const int32_t listed = s.place;
         if (listed > kParts) return kCandidates + 1;
-        const int32_t per_strip = blocks_of_strip(a), vectors = kUnroll << a.shift;
+        const int32_t vectors = kUnroll << a.note_shift;
 #pragma unroll 1
         for (int64_t item = tid; item < (int64_t)listed * vectors; item += K) {
-            const int32_t part = (int32_t)(item >> (2 + a.shift)), v = (int32_t)(item & (vectors - 1)), i = parts[part];
-            const int32_t b = i >> 6, lane = i & 63, strip = b / per_strip, in = (b - strip * per_strip) << a.shift;
+            const int32_t part = (int32_t)(item >> (2 + a.note_shift)), v = (int32_t)(item & (vectors - 1)), i = list[part];
+            // a strip's notes are groups of parts, of each group the lanes', of each lane the parts'
+            const int32_t strip = i / (a.note_slots * 64), rest = i - strip * a.note_slots * 64, lane = rest >> a.group & 63;
+            const int32_t in = ((rest >> (6 + a.group) << a.group) + (rest & ((1 << a.group) - 1))) << a.note_shift;
             if (in + v / kUnroll >= a.strip_steps) continue;
             const int64_t at = ((int64_t)strip * a.strip_steps + in) * (kSampleLanes * kUnroll) + v * kSampleLanes + lane;
             Logits<T> x = {vector_at(x0, a.vocab, at)};
@@ -802,7 +882,7 @@ template <typename T, typename S, int K> struct RowWork {
             }
             int sh = kLeast;
             while (((hi - lo) >> sh) >= kBins) ++sh;
-            const bool alike = kLeast > 0 && sh == kLeast;
+            const bool alike = kLeast > 0 && sh == kLeast, above_before = above_known || hi < order_of(m);
             const float least = value_at(lo), most = value_at(hi), known_from = above_known ? most : __builtin_inff();
             // weights as whole numbers, so that their sums do not depend on the order: 2^units for the largest of them
             const int units = 62 - (32 - __clz((int)a.vocab));
@@ -896,6 +976,7 @@ template <typename T, typename S, int K> struct RowWork {
             above_count += all_count;
             above_known = true;
             __syncthreads();
+            const uint32_t from = lo;
             hi = min(hi, lo + (bin << sh) + ((1u << sh) - 1));
             lo += bin << sh;
             if (sh > kLeast) continue;
@@ -911,6 +992,14 @@ template <typename T, typename S, int K> struct RowWork {
                 }
             }
             *weight_left = above + weighs * ((double)ties / here);
+            if (alike && !above_before) {
+                // every token that stays lies in a bin: one weight each, for the sums that follow
+                weights_from = from;
+#pragma unroll 1
+                for (int i = tid; i < kBins; i += K)
+                    if (s.count[i]) masses[i] = weight(logit(from + ((uint32_t)i << kLeast)));
+                __syncthreads();
+            }
             return Cut{order_of(logit(lo)), (int32_t)ties};
         }
     }
@@ -920,6 +1009,11 @@ template <typename T, typename S, int K> struct RowWork {
     // sample stands for its share of them; four standard deviations to either side.
     __device__ void guess(uint32_t from, double enough, double all, bool by_weight, uint32_t* lo, uint32_t* hi)
     {
+        if (!a.samples_kept) {
+            *lo = 0x00800000u;
+            *hi = 0xFF7FFFFFu;
+            return;
+        }
         // bins of 1/32 octaves of weight below `from` (1/8 where there are few)
         constexpr double per = kBins / 64;
         const float top = value_at(from);
@@ -929,7 +1023,7 @@ template <typename T, typename S, int K> struct RowWork {
         }
         __syncthreads();
         auto bin_of = [&](float x) { return (int)fmin(a.c * ((double)top - (double)x) * per, kBins - 1.0); };
-        for (int i = tid; i < blocks * 64; i += K) {
+        for (int i = tid; i < parts * 64; i += K) {
             const uint32_t n = samples[i];
             if (n <= kNoteNothing || (n << 16) >= from) continue;
             const float x = value_at(n << 16);
@@ -982,6 +1076,7 @@ template <typename T, typename S, int K> struct RowWork {
         const int lane = tid & 63;
         const float above = cut.order ? value_at(cut.order) : -__builtin_inff(), edge = cut.order ? above : __builtin_nanf("");
         const bool least_matters = a.least > -__builtin_inf();
+        const double* const weights = reinterpret_cast<const double*>(s.mass);
         __syncthreads();
         for (int32_t b = tid >> 6; b < blocks; b += K / 64) {
             const int64_t from = block_begin(b), to = b + 1 < blocks ? block_begin(b + 1) : (int64_t)a.vocab;
@@ -991,7 +1086,8 @@ template <typename T, typename S, int K> struct RowWork {
             if (from < to)
                 each_logit<64>(from / N, (to + N - 1) / N, to, lane, [&](float x, uint32_t) {
                     ties += x == edge;
-                    if (x > above && (!least_matters || likely(x))) sum += weight(x);
+                    if (x > above && (!least_matters || likely(x)))
+                        sum += weights_from ? weights[(order_of(x) - weights_from) >> 16] : weight(x);
                 });
             sum = wave_sum(sum);
             ties = wave_sum(ties);
@@ -1051,8 +1147,8 @@ template <typename T, typename S, int K> struct RowWork {
                 for (int attempt = 0; attempt < 2 && !done; ++attempt) {
                     count_notes(a.top_k > 0 ? a.top_k : attempt == 0 ? kFirstParts : kParts, a.top_k > 0 && known ? 1u << 30 : kParts);
                     const int bin = s.number;
-                    const uint32_t parts = s.found;
-                    if (bin < 0 || (a.top_k > 0 && bin < kBins - 1 && parts < (uint32_t)a.top_k)) break;
+                    const uint32_t listed = s.found;
+                    if (bin < 0 || (a.top_k > 0 && bin < kBins - 1 && listed < (uint32_t)a.top_k)) break;
                     // every note of these bins, and all tokens from the lowest value in them on
                     const bool all = bin == kBins - 1;
                     const float from = all ? -3.402823466e38f : least_of_bins(bin);
@@ -1081,6 +1177,7 @@ template <typename T, typename S, int K> struct RowWork {
                         lo = cut.order ? cut.order : 0x00800000u, hi = 0xFF7FFFFFu;
                     else
                         guess(below, enough - weighs, total - weighs, true, &lo, &hi);
+                    weights_from = 0;
                     cut = cut.stricter(search(lo, hi, 0, enough, true, &ignored));
                 }
                 total = sums_of(cut);
@@ -1101,9 +1198,9 @@ template <typename T, typename S, int K> struct RowWork {
 constexpr int kRowSteps = 4;
 template <typename T, bool kSums> __global__ __launch_bounds__(64, 3) void k_sample(SampleArgs a)
 {
-    typedef Shared<64, kRowSteps, 512> S;
+    typedef Shared<64, kRowSteps, kRowSteps, 512> S;
     __shared__ S s;
-    __shared__ uint16_t s_samples[kRowSteps * 64];
+    __shared__ alignas(16) uint16_t s_samples[kRowSteps * 64];
     const int tid = threadIdx.x;
     if (tid < 32) s.table[tid] = kTwoTo[tid];
     __syncthreads();
@@ -1112,7 +1209,7 @@ template <typename T, bool kSums> __global__ __launch_bounds__(64, 3) void k_sam
         const float u = a.uniforms[row];
         const float m = read_strip<T, kSums, false, false>(a, x0, 0, nullptr, s.table, s.notes, s_samples, s.sums, s.refs);
         __syncthreads();
-        RowWork<T, S, 64> work{a, s, x0, s_samples, m, blocks_of_strip(a), tid, u};
+        RowWork<T, S, 64> work{a, s, x0, s_samples, m, a.slots, a.note_slots, tid, u};
         work.finish(row, kSums);
         __syncthreads();
     }
@@ -1129,26 +1226,25 @@ template <typename T, bool kSums, bool NT> __global__ __launch_bounds__(kReadThr
         fill_powers<kReadThreads>(s_powers);
     }
     __syncthreads();
-    const int32_t strips = a.slices * kSampleWaves, per = blocks_of_strip(a);
+    const int32_t strips = a.slices * kSampleWaves;
     for (int64_t job = blockIdx.x; job < (int64_t)a.rows * a.slices; job += gridDim.x) {
         const int64_t row = job / a.slices;
         const int32_t strip = (int32_t)(job - row * a.slices) * kSampleWaves + wave;
-        const int64_t at = (row * strips + strip) * per;
+        const int64_t at = (row * strips + strip) * a.slots, note = (row * strips + strip) * a.note_slots * 64;
         const float top = read_strip<T, kSums, NT, true>(a, static_cast<const T*>(a.x) + row * a.stride, strip, s_powers, s_table,
-                                                         a.notes + at * 64, a.samples + at * 64, a.sums + at, a.refs + at);
+                                                         a.notes + note, a.samples + note, a.sums + at, a.refs + at);
         if ((tid & 63) == 0) a.most[row * strips + strip] = top;
     }
 }
 
 // The rest of such a row.
-template <typename T, bool kSums, int K, int BLOCKS> __global__ __launch_bounds__(K, 4) void k_sample_join(SampleArgs a)
+template <typename T, bool kSums, int K, int BLOCKS, int PARTS> __global__ __launch_bounds__(K, 4) void k_sample_join(SampleArgs a)
 {
-    typedef Shared<K, BLOCKS, 2048> S;
+    typedef Shared<K, BLOCKS, PARTS, 2048> S;
     __shared__ S s;
     const int tid = threadIdx.x, lane = tid & 63;
     const int64_t row = blockIdx.x;
-    const int32_t strips = a.slices * kSampleWaves, per = blocks_of_strip(a), blocks = strips * per;
-    const bool filters = a.top_k > 0 || a.top_p < 1.0 || a.least > -__builtin_inf();
+    const int32_t strips = a.slices * kSampleWaves, blocks = strips * a.slots, parts = strips * a.note_slots;
     // at most 128 strips: two a lane
     const float* const most = a.most + row * strips;
     float m = lane < strips ? most[lane] : -__builtin_inff(), m2 = 64 + lane < strips ? most[64 + lane] : -__builtin_inff();
@@ -1158,22 +1254,22 @@ template <typename T, bool kSums, int K, int BLOCKS> __global__ __launch_bounds_
         s.sums[tid] = a.sums[row * blocks + tid];
         s.refs[tid] = a.refs[row * blocks + tid];
     }
-    if (filters) {
+    if (a.notes_kept) {
         // eight notes to a load
-        const V4u* const notes = reinterpret_cast<const V4u*>(a.notes + row * blocks * 64);
-        V4u n[BLOCKS * 8 / K];
+        const V4u* const notes = reinterpret_cast<const V4u*>(a.notes + row * parts * 64);
+        V4u n[PARTS * 8 / K];
 #pragma unroll
-        for (int v = 0; v < BLOCKS * 8 / K; ++v)
-            if (v * K + tid < blocks * 8) n[v] = notes[v * K + tid];
+        for (int v = 0; v < PARTS * 8 / K; ++v)
+            if (v * K + tid < parts * 8) n[v] = notes[v * K + tid];
 #pragma unroll
-        for (int v = 0; v < BLOCKS * 8 / K; ++v)
-            if (v * K + tid < blocks * 8) reinterpret_cast<V4u*>(s.notes)[v * K + tid] = n[v];
+        for (int v = 0; v < PARTS * 8 / K; ++v)
+            if (v * K + tid < parts * 8) reinterpret_cast<V4u*>(s.notes)[v * K + tid] = n[v];
     }
     m = most_of(m, m2);
 #pragma unroll
     for (int d = 1; d < 64; d <<= 1) m = most_of(m, __shfl_xor(m, d));
     __syncthreads();
-    RowWork<T, S, K> work{a, s, static_cast<const T*>(a.x) + row * a.stride, a.samples + row * blocks * 64, m, blocks, tid, u};
+    RowWork<T, S, K> work{a, s, static_cast<const T*>(a.x) + row * a.stride, a.samples + row * parts * 64, m, blocks, parts, tid, u};
     work.finish(row, kSums);
 }
 
@@ -1193,16 +1289,19 @@ template <typename T, bool kSums> hipError_t sample_as(const SampleArgs& a, hipS
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
     if (a.rows <= kFewRows)
-        hipLaunchKernelGGL((k_sample_join<T, kSums, 512, kSampleBlocks>), dim3((unsigned)a.rows), dim3(512), 0, s, a);
+        hipLaunchKernelGGL((k_sample_join<T, kSums, 512, kSampleBlocks, kSampleBlocks>), dim3((unsigned)a.rows), dim3(512), 0, s, a);
     else
-        hipLaunchKernelGGL((k_sample_join<T, kSums, 256, kManyBlocks>), dim3((unsigned)a.rows), dim3(256), 0, s, a);
+        hipLaunchKernelGGL((k_sample_join<T, kSums, 256, kManyBlocks, kManyParts>), dim3((unsigned)a.rows), dim3(256), 0, s, a);
     return hipGetLastError();
 }
 
-template <typename T> hipError_t sample_t(const SampleArgs& a, hipStream_t s)
+template <typename T> hipError_t sample_t(SampleArgs a, hipStream_t s)
 {
-    // the row's whole weight counts where nothing bounds it, or top_p of all of it does
+    // the row's whole weight counts where nothing bounds it, or top_p of all of it does; its samples
+    // help where many tokens may stay
     const bool filters = a.top_k > 0 || a.top_p < 1.0 || a.least > -__builtin_inf();
+    a.notes_kept = filters;
+    a.samples_kept = a.top_k > kParts || (a.top_p < 1.0 && a.top_k == 0);
     return !filters || (a.top_p < 1.0 && a.top_k == 0) ? sample_as<T, true>(a, s) : sample_as<T, false>(a, s);
 }
 
@@ -1213,17 +1312,24 @@ SampleSplit sample_split(int32_t rows, int32_t vocab, int dtype)
 {
     const int64_t step = kSampleLanes * kUnroll * (dtype == 0 ? Vec<uint16_t>::n : Vec<float>::n);
     const int64_t steps = (vocab + step - 1) / step;
-    SampleSplit x = {0, 1, (int32_t)steps, 0, (int32_t)steps};
-    if (steps <= kRowSteps) return x;
-    x.waves = kSampleWaves;
-    const int64_t cut = std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(32, kReadGroups / std::max(1, rows)), steps / kSampleWaves));
-    const int64_t per = (steps + cut * x.waves - 1) / (cut * x.waves);
-    x.slices = (int32_t)((steps + per * x.waves - 1) / (per * x.waves));
-    x.strip_steps = (int32_t)per;
-    const int64_t most = (rows <= kFewRows ? kSampleBlocks : kManyBlocks) / (x.slices * x.waves);
-    while (((per - 1) >> x.shift) + 1 > most) ++x.shift;
-    x.blocks = x.slices * x.waves * (int32_t)(((per - 1) >> x.shift) + 1);
-    return x;
+    SampleSplit x = {0, 1, (int32_t)steps, 0, 0, 0, 0, 0};
+    int64_t blocks = kRowSteps, parts = kRowSteps;
+    if (steps > kRowSteps) {
+        x.waves = kSampleWaves;
+        const int64_t cut = std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(32, kReadGroups / std::max(1, rows)), steps / kSampleWaves));
+        x.strip_steps = (int32_t)((steps + cut * x.waves - 1) / (cut * x.waves));
+        x.slices = (int32_t)((steps + (int64_t)x.strip_steps * x.waves - 1) / ((int64_t)x.strip_steps * x.waves));
+        blocks = (rows <= kFewRows ? kSampleBlocks : kManyBlocks) / (x.slices * x.waves);
+        parts = (rows <= kFewRows ? kSampleBlocks : kManyParts) / (x.slices * x.waves);
+    }
+    while ((x.slots = ((x.strip_steps - 1) >> x.shift) + 1) > blocks) ++x.shift;
+    // as many parts as there is room for, rounded up to what is stored together
+    for (x.note_shift = x.shift;; ++x.note_shift) {
+        const int32_t n = ((x.strip_steps - 1) >> x.note_shift) + 1;
+        for (x.group = 0; x.group < 3 && 1 << x.group < n; ++x.group) {}
+        x.note_slots = (((n - 1) >> x.group) + 1) << x.group;
+        if (x.note_slots <= parts) return x;
+    }
 }
 
 hipError_t launch_sample(int dtype, const SampleArgs& a, hipStream_t s)
