@@ -43,7 +43,7 @@ constexpr int kUnroll = 4;                // vectors of a lane and step
 constexpr int kParts = 384;               // parts of blocks that are read again for them
 constexpr int kFirstParts = 48;           // and how many at first, where top_p decides
 constexpr int kCounted = 128;             // keys ranked by counting
-constexpr int kDepth = 8;                 // vectors of a thread under way where the row is read again
+constexpr int kDepth = 4;                 // vectors of a thread under way where the row is read again
 constexpr int64_t kMaxGrid = 1 << 20;
 constexpr int kFewRows = 256;
 constexpr int kManyBlocks = 96;          // of a row among many
@@ -1289,7 +1289,7 @@ template <typename T, bool kSums> hipError_t sample_as(const SampleArgs& a, hipS
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
     if (a.rows <= kFewRows)
-        hipLaunchKernelGGL((k_sample_join<T, kSums, 512, kSampleBlocks, kSampleBlocks>), dim3((unsigned)a.rows), dim3(512), 0, s, a);
+        hipLaunchKernelGGL((k_sample_join<T, kSums, 1024, kSampleBlocks, kSampleBlocks>), dim3((unsigned)a.rows), dim3(1024), 0, s, a);
     else
         hipLaunchKernelGGL((k_sample_join<T, kSums, 256, kManyBlocks, kManyParts>), dim3((unsigned)a.rows), dim3(256), 0, s, a);
     return hipGetLastError();
