@@ -146,6 +146,7 @@ struct TreeArgs {
     int32_t rows, tokens, longest;
     int32_t heads, group;        // q_heads = heads * group
     int32_t columns;             // queries of a job: 16 * sets * beside
+    bool wide;
     int32_t sets;                // of 16 queries, of a wave
     int32_t beside;              // waves of a job on the same positions
     int32_t job_heads, blocks;   // a group's query heads in `blocks` blocks of job_heads
@@ -158,15 +159,16 @@ struct TreeArgs {
 
 // How jobs are cut, from what the host knows.
 struct TreeShape {
+    bool wide;                   // bf16 of up to 128 dims, more than 32 queries: through shared memory
     int32_t sets, beside, columns, job_heads, blocks, job_tokens, pieces;
 };
 
-inline TreeShape tree_shape(int32_t longest, int32_t group, int32_t dim)
+inline TreeShape tree_shape(bool bf16, int32_t longest, int32_t group, int32_t dim)
 {
     TreeShape t;
     const int64_t queries = (int64_t)longest * group;
-    const int32_t most = dim > 128 ? 2 : 4;             // sets that fit a wave's registers
-    t.sets = queries <= 16 ? 1 : queries <= 32 ? 2 : most;
+    t.wide = bf16 && dim <= 128 && queries > 32;
+    t.sets = queries <= 16 ? 1 : 2;                     // what fits a wave's registers
     t.beside = 1;
     while (t.beside < 4 && 16 * t.sets * t.beside < queries) t.beside *= 2;
     t.columns = 16 * t.sets * t.beside;

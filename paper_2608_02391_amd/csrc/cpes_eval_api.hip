@@ -214,7 +214,7 @@ int check_attend(const cpes_cache* cache, int32_t layer, const cpes_pool* pool, 
 // Workgroups of the shares of trees: two per CU, one where a wave's state fills its SIMD's registers.
 int tree_groups(const cpes::TreeShape& t, int32_t head_dim)
 {
-    return head_dim > 128 || t.sets > 2 ? 256 : 512;
+    return t.wide || (head_dim <= 128 && t.sets == 1) ? 512 : 256;
 }
 
 size_t tree_parts_bytes(const cpes::TreeShape& t, int32_t head_dim)
@@ -588,7 +588,10 @@ size_t cpes_attend_tree_workspace_bytes(int32_t rows, int32_t tokens, int32_t lo
     if (rows < 0 || rows > CPES_MAX_SEQUENCES || tokens < 0 || (tokens > 0 && (longest < 1 || longest > tokens)) ||
         !check_heads(q_heads, kv_heads, head_dim))
         return 0;
-    return tree_bytes(rows, cpes::tree_shape(std::max(1, longest), q_heads / kv_heads, head_dim), kv_heads, head_dim);
+    size_t most = 0;             // either type's
+    for (bool bf16 : {false, true})
+        most = std::max(most, tree_bytes(rows, cpes::tree_shape(bf16, std::max(1, longest), q_heads / kv_heads, head_dim), kv_heads, head_dim));
+    return most;
 }
 
 int cpes_attend_tree(const cpes_cache* cache, int32_t layer, const cpes_pool* pool, int32_t rows, const int32_t* seqs_dev,
@@ -609,7 +612,7 @@ int cpes_attend_tree(const cpes_cache* cache, int32_t layer, const cpes_pool* po
     if (!rc && tokens > 0 && parents_dev && longest > CPES_MAX_TREE)
         rc = fail(CPES_ERR_UNSUPPORTED, "%s: longest %d above CPES_MAX_TREE", fn, longest);
     if (rc) return rc;
-    const cpes::TreeShape shape = cpes::tree_shape(std::max(1, longest), q_heads / cache->heads, cache->head_dim);
+    const cpes::TreeShape shape = cpes::tree_shape(cache->dtype == CPES_BF16, std::max(1, longest), q_heads / cache->heads, cache->head_dim);
     rc = check_workspace(workspace_dev, workspace_bytes, tree_bytes(rows, shape, cache->heads, cache->head_dim), fn);
     if (rc || rows == 0 || tokens == 0) return rc;
     cpes::TreeArgs a;
@@ -640,6 +643,7 @@ int cpes_attend_tree(const cpes_cache* cache, int32_t layer, const cpes_pool* po
     a.heads = cache->heads;
     a.group = q_heads / cache->heads;
     a.columns = shape.columns;
+    a.wide = shape.wide;
     a.sets = shape.sets;
     a.beside = shape.beside;
     a.job_heads = shape.job_heads;

@@ -543,7 +543,7 @@ __device__ __forceinline__ int64_t job_index(const TreeArgs& a, int32_t r, int32
 
 // All jobs' tiles form one line, cut into equal shares, one for `beside` waves.
 template <typename T, int DP, bool kWhole, int NQ>
-__global__ __launch_bounds__(kThreads, DP == 256 || NQ == 4 ? 1 : 2) void k_tree(TreeArgs a)
+__global__ __launch_bounds__(kThreads, DP == 256 || NQ > 1 ? 1 : 2) void k_tree(TreeArgs a)
 {
     typedef Work<T, DP, kWhole, NQ> W;
     constexpr int TILE = Tile<T>::n;
@@ -695,7 +695,7 @@ __device__ __forceinline__ bool find_job(const TreeArgs& a, int64_t j, int32_t* 
 // A workgroup to a job: `beside` waves on the same positions, kWaves / beside of them
 // taking turns at the tiles, whose pieces join in shared memory.
 template <typename T, int DP, bool kWhole, int NQ>
-__global__ __launch_bounds__(kThreads, DP == 256 || NQ == 4 ? 1 : 2) void k_tree_jobs(TreeArgs a)
+__global__ __launch_bounds__(kThreads, DP == 256 || NQ > 1 ? 1 : 2) void k_tree_jobs(TreeArgs a)
 {
     typedef Work<T, DP, kWhole, NQ> W;
     constexpr int TILE = Tile<T>::n;
@@ -776,6 +776,516 @@ __global__ __launch_bounds__(kThreads, DP == 256 || NQ == 4 ? 1 : 2) void k_tree
         __syncthreads();
     }
     if (team == 0) work.write_out();
+}
+
+// ------------------------------------------------------------ many queries --
+// bf16, more than 32 queries a job: the workgroup's waves share a tile of 64 positions in
+// shared memory, 32 queries a wave, on the 32 x 32 matrix instruction.  With 64 queries two
+// waves take half of the tile each for the same queries and join at the end; with 128 every
+// wave takes all of it.  A key and a value are read from memory once for up to 128
+// queries, the next tile's are on their way in registers while one is worked on, and two
+// workgroups a CU let one's softmax run beside the other's products.
+typedef float V16f __attribute__((ext_vector_type(16)));
+
+constexpr int kWideTile = 64;
+constexpr int kWideShare = 4;             // tiles of a workgroup's share at least
+constexpr int kWideColumns = 32;          // of a wave
+
+template <int DP> struct WideShared {
+    // A column of 16-byte pieces of the keys is read at once: their rows lie 16 bytes further apart than they are long.
+    static constexpr int kRow = DP + 8;
+    uint16_t keys[2][kWideTile * kRow];
+    uint16_t values[2][kWideTile * DP];
+    uint32_t odd[2][2];                   // positions with values that are not finite, where not all queries see all of a tile
+    Family<2> family[kWaves];
+};
+
+template <int DP> struct Wide {
+    static constexpr int PIECES = DP / 8, ROWS = kThreads / PIECES, LOADS = kWideTile / ROWS, BLOCKS = DP / 32;
+
+    const TreeArgs& a;
+    WideShared<DP>& s;
+    const int tid, lane, wave, sub, team, teams;
+
+    Row row;
+    Span span;
+    int32_t kv, block;
+    bool valid;                           // the lane's query: column sub * 32 + lane % 32
+    int32_t low, high, every_low, every_high;
+    V4u q[DP / 16];
+    float unit;                           // of the scores, as powers of 2
+    float m, l;                           // l is this lane's share
+    V16f o[BLOCKS];                       // o[b][i]: dim BLOCKS * (8 (i / 4) + 4 (lane / 32) + i % 4) + b
+
+    __device__ __forceinline__ Wide(const TreeArgs& args, WideShared<DP>& shared)
+        : a(args), s(shared), tid(threadIdx.x), lane(threadIdx.x & 63), wave(__builtin_amdgcn_readfirstlane(threadIdx.x >> 6)),
+          sub(wave % args.beside), team(wave / args.beside), teams(kWaves / args.beside)
+    {
+    }
+
+    __device__ __forceinline__ const uint16_t* keys_at() const { return static_cast<const uint16_t*>(a.k) + kv * a.head_stride; }
+    __device__ __forceinline__ const uint16_t* values_at() const { return static_cast<const uint16_t*>(a.v) + kv * a.head_stride; }
+
+    __device__ __forceinline__ void begin(const Row& r, const Span& x, int32_t hh)
+    {
+        row = r;
+        span = x;
+        kv = hh / a.blocks;
+        block = hh - kv * a.blocks;
+        const bool tree = a.parents != nullptr;
+        Family<2>& family = s.family[wave];
+        const int32_t column = sub * kWideColumns + (lane & 31), token = column / a.job_heads;
+        const int32_t head = block * a.job_heads + column - token * a.job_heads;
+        const int32_t i = span.from + min(token, span.count - 1);
+        valid = token < span.count && head < a.group;
+        int32_t depth = i;
+        if (tree) {
+            wave_sync();                  // the last job's are no longer read
+            const int32_t last = span.from + span.count;
+            for (int32_t j = lane; j < last; j += 64) {
+                const int32_t parent = a.parents[row.first + j];
+                family.parent[j] = (int16_t)(parent >= 0 && parent < j ? parent : -1);
+            }
+            wave_sync();
+            depth = 0;
+            for (int32_t j = family.parent[i]; j >= 0; j = family.parent[j]) ++depth;
+            if (lane < kWideColumns) {
+#pragma unroll
+                for (int w = 0; w <= kWords; ++w) family.above[lane][w] = 0;
+                int32_t at = depth;
+                for (int32_t j = i; j >= 0; j = family.parent[j], --at)
+                    if (a.window == 0 || depth - at < a.window || (int64_t)row.base + at < a.sinks)
+                        family.above[lane][j >> 5] |= 1u << (j & 31);
+            }
+            wave_sync();
+        }
+        high = row.base < 0 ? 0 : tree ? row.base : row.base + i + 1;
+        low = a.window > 0 && row.base >= 0 ? (int32_t)max((int64_t)row.base + depth + 1 - a.window, (int64_t)0) : 0;
+        const uint16_t* const p = static_cast<const uint16_t*>(a.q) + (int64_t)(row.first + i) * a.q_stride +
+                                  (int64_t)(kv * a.group + min(head, a.group - 1)) * a.q_head_stride;
+#pragma unroll
+        for (int e = 0; e < DP / 16; ++e) {
+            const int d = 8 * (lane >> 5) + 16 * e;
+            q[e] = *reinterpret_cast<const V4uAnywhere*>(p + (d < a.dim ? d : 0));
+            if (d >= a.dim || !valid) q[e] = V4u{0, 0, 0, 0};
+            if (a.scale < 0.f) q[e] ^= 0x80008000u;       // of -q with -scale
+        }
+        unit = fmaxf(fabsf(a.scale) * kLog2e, 1e-37f);    // -inf stays below all scores
+        every_high = row.base < 0 ? 0 : tree ? row.base : row.base + span.from + 1;
+        every_low = 0;
+        if (a.window > 0 && row.base >= 0)
+            every_low = (int32_t)max((int64_t)row.base + (tree ? span.from + span.count : span.from + span.count - 1) + 1 - a.window, (int64_t)0);
+        m = -__builtin_inff();
+        l = 0.f;
+#pragma unroll
+        for (int b = 0; b < BLOCKS; ++b)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) o[b][e] = 0.f;
+    }
+
+    // Whether all queries of the job see all of a tile's positions that have a page.
+    __device__ __forceinline__ bool whole(int32_t pos0) const
+    {
+        return pos0 + kWideTile <= every_high && (pos0 >= every_low || pos0 + kWideTile <= a.sinks);
+    }
+
+    // Positions pos0 .. + 31 that the lane's query sees.
+    __device__ __forceinline__ uint32_t seen_from(int32_t pos0) const
+    {
+        uint32_t seen = bits_below(high - pos0) & ~(bits_below(low - pos0) & ~bits_below(a.sinks - pos0));
+        if (a.parents && row.base >= 0) {
+            const int32_t off = pos0 - row.base;
+            if (off > -32 && off < kMaxTree) {
+                const int32_t w = off >> 5, shift = off & 31;
+                const uint32_t* const above = s.family[wave].above[lane & 31];
+                const uint32_t lo = w >= 0 ? above[w] : 0u, hi = above[w + 1];
+                seen |= shift ? lo >> shift | hi << (32 - shift) : lo;
+            }
+        }
+        return valid ? seen : 0u;
+    }
+
+    // The lane's position of a tile: its row's offset in the cache, -1 without a page.
+    __device__ __forceinline__ int32_t ask(int32_t pos0) const
+    {
+        const int32_t pos = pos0 + lane, at = a.page_shift >= 0 ? pos >> a.page_shift : pos / a.page_size;
+        int32_t id = -1;
+        if (pos < span.end) id = (a.table + (int64_t)row.seq * a.table_stride)[at];
+        return id;
+    }
+    __device__ __forceinline__ int64_t place(int32_t id, int32_t pos0) const
+    {
+        const int32_t pos = pos0 + lane, at = a.page_shift >= 0 ? pos >> a.page_shift : pos / a.page_size;
+        return id >= 0 && id < a.pages ? id * a.page_stride + (pos - at * a.page_size) * a.token_stride : -1;
+    }
+
+    // A thread's pieces of a tile's rows; rows without a page are zeros.
+    V4u key[LOADS], val[LOADS];
+    __device__ __forceinline__ void load(int64_t at)
+    {
+        const int piece = tid % PIECES;
+#pragma unroll
+        for (int k = 0; k < LOADS; ++k) {
+            const int r = tid / PIECES + k * ROWS;
+            const uint32_t lo = __shfl((uint32_t)(uint64_t)at, r), hi = __shfl((uint32_t)((uint64_t)at >> 32), r);
+            const int64_t from = (int64_t)(((uint64_t)hi << 32) | lo);
+            key[k] = val[k] = V4u{0, 0, 0, 0};
+            if (from >= 0 && 8 * piece < a.dim) {
+                key[k] = *reinterpret_cast<const V4uAnywhere*>(keys_at() + from + 8 * piece);
+                val[k] = *reinterpret_cast<const V4uAnywhere*>(values_at() + from + 8 * piece);
+            }
+        }
+    }
+    __device__ __forceinline__ void store(int buffer, bool edge)
+    {
+        const int piece = tid % PIECES;
+#pragma unroll
+        for (int k = 0; k < LOADS; ++k) {
+            const int r = tid / PIECES + k * ROWS;
+            *reinterpret_cast<V4u*>(&s.keys[buffer][r * s.kRow + piece * 8]) = key[k];
+            *reinterpret_cast<V4u*>(&s.values[buffer][r * DP + piece * 8]) = val[k];
+        }
+        if (edge) {
+#pragma unroll
+            for (int k = 0; k < LOADS; ++k) {
+                bool odd = false;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) odd |= (val[k][e] & 0x7F80u) == 0x7F80u || (val[k][e] & 0x7F800000u) == 0x7F800000u;
+                const int r = tid / PIECES + k * ROWS;
+                if (odd) atomicOr(&s.odd[buffer][r >> 5], 1u << (r & 31));
+            }
+        }
+    }
+
+    // Folds half `part` of the tile in a buffer into the state.
+    __device__ __forceinline__ void fold(int buffer, int part, int32_t pos0, bool edge, uint32_t there)
+    {
+        const int h = lane >> 5, r0 = 32 * part;
+        V16f x;
+#pragma unroll
+        for (int e = 0; e < 16; ++e) x[e] = 0.f;
+        const uint16_t* const krow = &s.keys[buffer][(r0 + (lane & 31)) * s.kRow + 8 * h];
+#pragma unroll
+        for (int i = 0; i < DP / 16; ++i)
+            x = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(V8bf, *reinterpret_cast<const V4u*>(krow + 16 * i)),
+                                                        __builtin_bit_cast(V8bf, q[i]), x, 0, 0, 0);
+        uint32_t seen = ~0u;
+        if (edge) {
+            seen = seen_from(pos0 + r0) & there;
+#pragma unroll
+            for (int e = 0; e < 16; ++e)
+                if (!(seen >> (8 * (e >> 2) + 4 * h + (e & 3)) & 1)) x[e] = -__builtin_inff();
+        }
+        float top = x[0];
+#pragma unroll
+        for (int e = 1; e < 16; ++e) top = fmaxf(top, x[e]);
+        float y, z;
+        swap_halves(top, &y, &z);
+        const float most = fmaxf(m, fmaxf(y, z));
+        // nothing seen yet: any finite base gives weights of 0
+        const float shift = most == -__builtin_inff() ? 0.f : -most * unit;
+        const float keep = __builtin_amdgcn_exp2f(fmaf(m, unit, shift));
+        m = most;
+        float sum = 0.f;
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+            x[e] = __builtin_amdgcn_exp2f(fmaf(x[e], unit, shift));
+            sum += x[e];
+        }
+        l = l * keep + sum;
+        if (__any(keep != 1.f)) {
+#pragma unroll
+            for (int b = 0; b < BLOCKS; ++b) o[b] *= keep;
+        }
+        if (edge && __builtin_amdgcn_readfirstlane(s.odd[buffer][0] | s.odd[buffer][1])) {
+            // values that are not finite: for the queries that see them only, and then no longer there
+#pragma unroll 1
+            for (uint32_t left = __builtin_amdgcn_readfirstlane(s.odd[buffer][part]); left; left &= left - 1) {
+                const int r = __builtin_ctz(left);
+                float w = x[0];
+#pragma unroll
+                for (int e = 1; e < 16; ++e)
+                    if (e == 4 * (r >> 3) + (r & 3)) w = x[e];
+                w = __shfl(w, (lane & 31) + 32 * (r >> 2 & 1));
+                const uint16_t* const p = &s.values[buffer][(r0 + r) * DP + 4 * BLOCKS * h];
+                if (seen >> r & 1) {
+#pragma unroll
+                    for (int b = 0; b < BLOCKS; ++b)
+#pragma unroll
+                        for (int e = 0; e < 16; ++e)
+                            o[b][e] = fmaf(w, __uint_as_float((uint32_t)p[BLOCKS * (8 * (e >> 2) + (e & 3)) + b] << 16), o[b][e]);
+                }
+            }
+            __syncthreads();
+#pragma unroll 1
+            for (int i = tid; i < kWideTile * DP / 2; i += kThreads) {
+                const int r = 2 * i / DP, its = teams == 1 ? part : r >> 5;
+                if (r >> 5 == its && (s.odd[buffer][its] >> (r & 31) & 1)) reinterpret_cast<uint32_t*>(s.values[buffer])[i] = 0;
+            }
+            __syncthreads();
+        }
+        V8bf hi[2], lo[2];
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+            hi[e >> 3][e & 7] = (__bf16)x[e];
+            lo[e >> 3][e & 7] = (__bf16)(x[e] - (float)hi[e >> 3][e & 7]);
+        }
+        // positions 16 t + {0 .. 3, 8 .. 11} + 4 h of the half, dims BLOCKS (lane % 32) .. of each
+        const uint16_t* const vrow = &s.values[buffer][(r0 + 4 * h) * DP + BLOCKS * (lane & 31)];
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+            uint32_t v[8][BLOCKS / 2];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const uint16_t* const p = vrow + (16 * t + 8 * (j >> 2) + (j & 3)) * DP;
+                if constexpr (BLOCKS == 4) {
+                    const V2u w = *reinterpret_cast<const V2u*>(p);
+                    v[j][0] = w[0];
+                    v[j][1] = w[1];
+                } else {
+                    v[j][0] = *reinterpret_cast<const uint32_t*>(p);
+                }
+            }
+#pragma unroll
+            for (int b = 0; b < BLOCKS; ++b) {
+                V4u w;
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    w[i] = __builtin_amdgcn_perm(v[2 * i + 1][b >> 1], v[2 * i][b >> 1], b & 1 ? 0x07060302u : 0x05040100u);
+                const V8bf v8 = __builtin_bit_cast(V8bf, w);
+                o[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v8, hi[t], o[b], 0, 0, 0);
+                o[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v8, lo[t], o[b], 0, 0, 0);
+            }
+        }
+    }
+
+    // Tiles [first, last) of the job.
+    __device__ __forceinline__ void run(int32_t first, int32_t last)
+    {
+        __syncthreads();                  // the buffers are no longer read
+        if (tid < 4) s.odd[tid >> 1][tid & 1] = 0;
+        int32_t pos0 = span.at(first, kWideTile);
+        int64_t at = place(ask(pos0), pos0);
+        load(at);
+        int32_t id = -1;
+        if (first + 1 < last) id = ask(span.at(first + 1, kWideTile));
+        __syncthreads();
+        store(0, !whole(pos0));
+        uint64_t there = __ballot(at >= 0);
+#pragma unroll 1
+        for (int32_t i = first; i < last; ++i) {
+            const int buffer = (i - first) & 1;
+            const bool more = i + 1 < last;
+            const int32_t next = more ? span.at(i + 1, kWideTile) : 0;
+            __syncthreads();              // the tile is there, and the other buffer free
+            if (more) {
+                at = place(id, next);
+                load(at);
+                if (i + 2 < last) id = ask(span.at(i + 2, kWideTile));
+                if (tid < 2) s.odd[buffer ^ 1][tid] = 0;
+            }
+            const bool edge = there != ~0ull || !whole(pos0);
+#pragma unroll 1
+            for (int part = team; part < 2; part += teams) fold(buffer, part, pos0, edge, (uint32_t)(there >> (32 * part)));
+            if (more) {
+                there = __ballot(at >= 0);
+                pos0 = next;
+                const bool odd_counts = there != ~0ull || !whole(pos0);
+                if (odd_counts) __syncthreads();          // the marks have been cleared
+                store(buffer ^ 1, odd_counts);
+            }
+        }
+        // two waves with the same queries: the second hands its piece to the first
+        if (teams == 2) {
+            __syncthreads();
+            float* const to = reinterpret_cast<float*>(&s) + sub * 64 * (16 * BLOCKS + 2);
+            if (team == 1) {
+                to[lane] = m;
+                to[64 + lane] = l;
+#pragma unroll
+                for (int b = 0; b < BLOCKS; ++b)
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) to[(2 + 16 * b + e) * 64 + lane] = o[b][e];
+            }
+            __syncthreads();
+            if (team == 0) {
+                const float mi = to[lane], top = fmaxf(m, mi), base = top == -__builtin_inff() ? 0.f : top;
+                const float f = __builtin_amdgcn_exp2f((m - base) * unit), fi = __builtin_amdgcn_exp2f((mi - base) * unit);
+                l = l * f + to[64 + lane] * fi;
+                m = top;
+#pragma unroll
+                for (int b = 0; b < BLOCKS; ++b)
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) o[b][e] = o[b][e] * f + to[(2 + 16 * b + e) * 64 + lane] * fi;
+            }
+        }
+    }
+
+    __device__ __forceinline__ float whole_sum() const
+    {
+        float y, z;
+        swap_halves(l, &y, &z);
+        return y + z;
+    }
+
+    // Four dims each, or two.
+    template <typename F> __device__ __forceinline__ void each_dims(F f) const
+    {
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+            const int d = BLOCKS * (8 * (e >> 2) + 4 * (lane >> 5) + (e & 3));
+            if (d < a.dim) f(d, e);
+        }
+    }
+
+    __device__ __forceinline__ void write_out()
+    {
+        const float sum = whole_sum();
+        if (team != 0 || !valid) return;
+        const int32_t column = sub * kWideColumns + (lane & 31), token = column / a.job_heads;
+        const int64_t at = row.first + span.from + token;
+        const int32_t head = kv * a.group + block * a.job_heads + column - token * a.job_heads;
+        uint16_t* const out = static_cast<uint16_t*>(a.out) + at * a.out_stride + (int64_t)head * a.out_head_stride;
+        const float f = sum == 0.f ? 0.f : 1.f / sum;
+        each_dims([&](int d, int e) {
+            if constexpr (BLOCKS == 4) {
+                store4<uint16_t>(out + d, sum == 0.f ? V4f{0.f, 0.f, 0.f, 0.f} : V4f{o[0][e], o[1][e], o[2][e], o[3][e]} * f);
+            } else {
+                out[d] = rounded<uint16_t>(sum == 0.f ? 0.f : o[0][e] * f);
+                out[d + 1] = rounded<uint16_t>(sum == 0.f ? 0.f : o[1][e] * f);
+            }
+        });
+        if (lane < 32 && a.lse) a.lse[at * a.heads * a.group + head] = sum == 0.f ? -__builtin_inff() : m * fabsf(a.scale) + logf(sum);
+    }
+
+    // As the parts of the other kernels: a wave's maxima, sums and rows, here of two sets.
+    __device__ __forceinline__ void write_part(float* part)
+    {
+        const float sum = whole_sum();
+        if (team != 0) return;
+        float* const to = part + sub * tree_part_floats(2, a.dim);
+        const int column = lane & 31;
+        each_dims([&](int d, int e) {
+#pragma unroll
+            for (int b = 0; b < BLOCKS; ++b) to[64 + column * a.dim + d + b] = o[b][e];
+        });
+        if (lane < 32) {
+            to[column] = m == -__builtin_inff() ? m : m * fabsf(a.scale);
+            to[32 + column] = sum;
+        }
+    }
+};
+
+// Every row's tiles: a thread's share of them before, and after, its rows.
+template <int TILE> struct Line {
+    int32_t r0, r1;
+    int64_t mine, upto, tiles;
+
+    // All threads.
+    __device__ __forceinline__ Line(const TreeArgs& a, int64_t* s_sum)
+    {
+        const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+        const int32_t each = (a.rows + kThreads - 1) / kThreads;
+        r0 = min(a.rows, tid * each);
+        r1 = min(a.rows, r0 + each);
+        mine = 0;
+        for (int32_t r = r0; r < r1; ++r) mine += row_tiles<TILE>(a, row_at(a, r));
+        upto = mine;
+#pragma unroll
+        for (int d = 1; d < 64; d <<= 1) {
+            const int64_t y = __shfl_up(upto, d);
+            if (lane >= d) upto += y;
+        }
+        if (lane == 63) s_sum[wave] = upto;
+        __syncthreads();
+        tiles = 0;
+#pragma unroll
+        for (int w = 0; w < kWaves; ++w) {
+            if (w < wave) upto += s_sum[w];
+            tiles += s_sum[w];
+        }
+    }
+
+    // The thread that holds tile t of the rows' says in which of them it lies, and what is before that row.
+    __device__ __forceinline__ void find(const TreeArgs& a, int64_t t, int32_t* s_row, int64_t* s_before) const
+    {
+        if (t < upto - mine || t >= upto) return;
+        int64_t before = upto - mine;
+        int32_t r = r0;
+        for (; r < r1; ++r) {
+            const int64_t n = row_tiles<TILE>(a, row_at(a, r));
+            if (t < before + n) break;
+            before += n;
+        }
+        *s_row = r;
+        *s_before = before;
+    }
+};
+
+template <int DP> __global__ __launch_bounds__(kThreads, 2) void k_tree_wide(TreeArgs a)
+{
+    __shared__ alignas(16) WideShared<DP> s;
+    __shared__ int64_t s_sum[kWaves], s_before;
+    __shared__ int32_t s_row;
+    const Line<kWideTile> line(a, s_sum);
+    const int64_t units = line.tiles * a.heads * a.blocks;
+    const int32_t shares_n = (int32_t)max((int64_t)1, min((int64_t)a.groups, units / kWideShare)), me = blockIdx.x;
+    if (me >= shares_n || units == 0) return;
+    const Shares shares(units, shares_n);
+    const int64_t at = shares.begin(me), hh0 = quotient(at, line.tiles), t = at - hh0 * line.tiles;
+    line.find(a, t, &s_row, &s_before);
+    __syncthreads();
+    int64_t left = shares.begin(me + 1) - at;
+    Cursor cur;
+    cur.r = __builtin_amdgcn_readfirstlane(s_row);
+    cur.hh = __builtin_amdgcn_readfirstlane((int32_t)hh0);
+    cur.row = wave_row(a, cur.r);
+    int64_t in_row = t - s_before;
+    cur.piece = 0;
+    cur.span = span_at<kWideTile>(a, cur.row, 0);
+    while (in_row >= cur.span.tiles) {
+        in_row -= cur.span.tiles;
+        cur.span = span_at<kWideTile>(a, cur.row, ++cur.piece);
+    }
+    cur.piece = __builtin_amdgcn_readfirstlane(cur.piece);
+    cur.i = __builtin_amdgcn_readfirstlane((int32_t)in_row);
+    cur.span = span_at<kWideTile>(a, cur.row, cur.piece);
+    int64_t done = 0;
+    Wide<DP> work(a, s);
+#pragma unroll 1
+    while (left > 0) {
+        const int32_t take = (int32_t)min(left, (int64_t)(cur.span.tiles - cur.i));
+        const bool begins = cur.i == 0, turns = cur.i + take == cur.span.tiles;
+        work.begin(cur.row, cur.span, cur.hh);
+        work.run(cur.i, cur.i + take);
+        if (begins && threadIdx.x == 0)
+            // which shares hold the rest of it
+            a.joins[job_index(a, cur.r, cur.piece, cur.hh)] = int2{me, turns ? me : shares.of(at + done + cur.span.tiles - 1)};
+        if (begins && turns)
+            work.write_out();
+        else
+            work.write_part(a.parts + (2 * (int64_t)me + (begins ? 1 : 0)) * a.beside * tree_part_floats(2, a.dim));
+        done += take;
+        left -= take;
+        cur.i += take - 1;
+        if (left > 0) cur.next<kWideTile>(a);
+    }
+}
+
+template <int DP> __global__ __launch_bounds__(kThreads, 2) void k_tree_wide_jobs(TreeArgs a)
+{
+    __shared__ alignas(16) WideShared<DP> s;
+    const int32_t each = a.heads * a.blocks, hh = blockIdx.x % each;
+    const int64_t slots = gridDim.x / each;
+    int32_t r, piece;
+    // a row's last pieces see most: they begin first
+    if (!find_job(a, slots - 1 - blockIdx.x / each, &r, &piece)) return;
+    const Row row = wave_row(a, r);
+    if ((int64_t)piece * a.job_tokens >= row.tokens) return;
+    Wide<DP> work(a, s);
+    work.begin(row, span_at<kWideTile>(a, row, piece), hh);
+    work.run(0, work.span.tiles);
+    work.write_out();
 }
 
 // Joins the pieces of a job that lies in more than one share, as the join of one new
@@ -882,11 +1392,32 @@ template <typename T, int DP, bool kWhole> hipError_t tree_sets(const TreeArgs& 
 {
     if (a.sets == 1) return tree_as<T, DP, kWhole, 1>(a, s);
     if constexpr (DP == 256) return tree_as<T, DP, kWhole, 2>(a, s);
-    else return a.sets == 2 ? tree_as<T, DP, kWhole, 2>(a, s) : tree_as<T, DP, kWhole, 4>(a, s);
+    else if constexpr (std::is_same<T, uint16_t>::value) return tree_as<T, DP, kWhole, 2>(a, s);
+    else return tree_as<T, DP, kWhole, 2>(a, s);
+}
+
+template <int DP> hipError_t tree_wide(const TreeArgs& a, hipStream_t s)
+{
+    const int32_t each = a.heads * a.blocks;
+    const int64_t jobs = ((int64_t)a.tokens / a.job_tokens + a.rows) * each, most = most_tiles<kWideTile>(a);
+    if ((jobs >= 1024 || most <= 16) && jobs <= INT32_MAX / kThreads) {
+        hipLaunchKernelGGL(k_tree_wide_jobs<DP>, dim3((unsigned)jobs), dim3(kThreads), 0, s, a);
+        return hipGetLastError();
+    }
+    hipLaunchKernelGGL(k_tree_wide<DP>, dim3((unsigned)a.groups), dim3(kThreads), 0, s, a);
+    hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+    const int64_t all = (int64_t)a.rows * a.pieces * each;
+    hipLaunchKernelGGL(k_tree_join<uint16_t>, dim3((unsigned)std::min(all, kMaxGrid), (unsigned)std::min(a.columns, 16)), dim3(kThreads), 0,
+                       s, a);
+    return hipGetLastError();
 }
 
 template <typename T, int DP> hipError_t tree_dim(const TreeArgs& a, hipStream_t s)
 {
+    if constexpr (std::is_same<T, uint16_t>::value && DP <= 128)
+        if (a.wide) return tree_wide<DP>(a, s);
+
     return a.page_size % 16 == 0 ? tree_sets<T, DP, true>(a, s) : tree_sets<T, DP, false>(a, s);
 }
 
