@@ -786,16 +786,25 @@ __global__ __launch_bounds__(kThreads, DP == 256 || NQ > 1 ? 1 : 2) void k_tree_
 // queries, the next tile's are on their way in registers while one is worked on, and two
 // workgroups a CU let one's softmax run beside the other's products.
 typedef float V16f __attribute__((ext_vector_type(16)));
+typedef float V2f __attribute__((ext_vector_type(2)));
+typedef __bf16 V2bf __attribute__((ext_vector_type(2)));
+typedef short V4s __attribute__((ext_vector_type(4)));
 
 constexpr int kWideTile = 64;
 constexpr int kWideShare = 4;             // tiles of a workgroup's share at least
 constexpr int kWideColumns = 32;          // of a wave
+constexpr float kAhead = 4.f;
 
 template <int DP> struct WideShared {
     // A column of 16-byte pieces of the keys is read at once: their rows lie 16 bytes further apart than they are long.
     static constexpr int kRow = DP + 8;
     uint16_t keys[2][kWideTile * kRow];
+    // 16 dims of four positions are read at once, by 32 lanes twice that: a row's 64-byte pieces are swapped by its number.
     uint16_t values[2][kWideTile * DP];
+    static __device__ __forceinline__ int value(int r, int d)
+    {
+        return r * DP + (((d >> 5) ^ (DP == 128 ? r & 3 : r >> 1 & 1)) << 5) + (d & 31);
+    }
     uint32_t odd[2][2];                   // positions with values that are not finite, where not all queries see all of a tile
     Family<2> family[kWaves];
 };
@@ -815,7 +824,7 @@ template <int DP> struct Wide {
     V4u q[DP / 16];
     float unit;                           // of the scores, as powers of 2
     float m, l;                           // l is this lane's share
-    V16f o[BLOCKS];                       // o[b][i]: dim BLOCKS * (8 (i / 4) + 4 (lane / 32) + i % 4) + b
+    V16f o[BLOCKS];                       // o[b][i]: dim 32 b + 8 (i / 4) + 4 (lane / 32) + i % 4
 
     __device__ __forceinline__ Wide(const TreeArgs& args, WideShared<DP>& shared)
         : a(args), s(shared), tid(threadIdx.x), lane(threadIdx.x & 63), wave(__builtin_amdgcn_readfirstlane(threadIdx.x >> 6)),
@@ -943,7 +952,7 @@ template <int DP> struct Wide {
         for (int k = 0; k < LOADS; ++k) {
             const int r = tid / PIECES + k * ROWS;
             *reinterpret_cast<V4u*>(&s.keys[buffer][r * s.kRow + piece * 8]) = key[k];
-            *reinterpret_cast<V4u*>(&s.values[buffer][r * DP + piece * 8]) = val[k];
+            *reinterpret_cast<V4u*>(&s.values[buffer][s.value(r, piece * 8)]) = val[k];
         }
         if (edge) {
 #pragma unroll
@@ -981,22 +990,25 @@ template <int DP> struct Wide {
         for (int e = 1; e < 16; ++e) top = fmaxf(top, x[e]);
         float y, z;
         swap_halves(top, &y, &z);
-        const float most = fmaxf(m, fmaxf(y, z));
-        // nothing seen yet: any finite base gives weights of 0
-        const float shift = most == -__builtin_inff() ? 0.f : -most * unit;
-        const float keep = __builtin_amdgcn_exp2f(fmaf(m, unit, shift));
-        m = most;
-        float sum = 0.f;
-#pragma unroll
-        for (int e = 0; e < 16; ++e) {
-            x[e] = __builtin_amdgcn_exp2f(fmaf(x[e], unit, shift));
-            sum += x[e];
-        }
-        l = l * keep + sum;
-        if (__any(keep != 1.f)) {
+        top = fmaxf(y, z);
+        // weights may come to 2^kAhead: then only is the base moved, and what is there scaled
+        const bool moves = (top - m) * unit > kAhead;
+        if (__any(moves)) {
+            const float next = moves ? top : m, keep = moves ? __builtin_amdgcn_exp2f((m - next) * unit) : 1.f;
+            m = next;
+            l *= keep;
 #pragma unroll
             for (int b = 0; b < BLOCKS; ++b) o[b] *= keep;
         }
+        // nothing seen yet: any finite base gives weights of 0
+        const float shift = m == -__builtin_inff() ? 0.f : -m * unit;
+        float sum[2] = {0.f, 0.f};
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+            x[e] = __builtin_amdgcn_exp2f(fmaf(x[e], unit, shift));
+            sum[e & 1] += x[e];
+        }
+        l += sum[0] + sum[1];
         if (edge && __builtin_amdgcn_readfirstlane(s.odd[buffer][0] | s.odd[buffer][1])) {
             // values that are not finite: for the queries that see them only, and then no longer there
 #pragma unroll 1
@@ -1007,13 +1019,12 @@ template <int DP> struct Wide {
                 for (int e = 1; e < 16; ++e)
                     if (e == 4 * (r >> 3) + (r & 3)) w = x[e];
                 w = __shfl(w, (lane & 31) + 32 * (r >> 2 & 1));
-                const uint16_t* const p = &s.values[buffer][(r0 + r) * DP + 4 * BLOCKS * h];
                 if (seen >> r & 1) {
 #pragma unroll
                     for (int b = 0; b < BLOCKS; ++b)
 #pragma unroll
                         for (int e = 0; e < 16; ++e)
-                            o[b][e] = fmaf(w, __uint_as_float((uint32_t)p[BLOCKS * (8 * (e >> 2) + (e & 3)) + b] << 16), o[b][e]);
+                            o[b][e] = fmaf(w, __uint_as_float((uint32_t)s.values[buffer][s.value(r0 + r, 32 * b + 8 * (e >> 2) + 4 * h + (e & 3))] << 16), o[b][e]);
                 }
             }
             __syncthreads();
@@ -1024,39 +1035,38 @@ template <int DP> struct Wide {
             }
             __syncthreads();
         }
-        V8bf hi[2], lo[2];
+        V4u hi[2], lo[2];
 #pragma unroll
-        for (int e = 0; e < 16; ++e) {
-            hi[e >> 3][e & 7] = (__bf16)x[e];
-            lo[e >> 3][e & 7] = (__bf16)(x[e] - (float)hi[e >> 3][e & 7]);
+        for (int e = 0; e < 16; e += 2) {
+            const uint32_t both = pair(x[e], x[e + 1]);
+            hi[e >> 3][e >> 1 & 3] = both;
+            lo[e >> 3][e >> 1 & 3] = pair(x[e] - __uint_as_float(both << 16), x[e + 1] - __uint_as_float(both & 0xFFFF0000u));
         }
-        // positions 16 t + {0 .. 3, 8 .. 11} + 4 h of the half, dims BLOCKS (lane % 32) .. of each
-        const uint16_t* const vrow = &s.values[buffer][(r0 + 4 * h) * DP + BLOCKS * (lane & 31)];
+        // dim lane % 32 of each 32, positions 16 t + {0 .. 3, 8 .. 11} + 4 h of the half
+        const int in = lane >> 2 & 3;
 #pragma unroll
-        for (int t = 0; t < 2; ++t) {
-            uint32_t v[8][BLOCKS / 2];
+        for (int b = 0; b < BLOCKS; ++b) {
+            const uint16_t* const p = &s.values[buffer][s.value(r0 + 4 * h + in, 32 * b + (lane & 16) + 4 * (lane & 3))];
 #pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                const uint16_t* const p = vrow + (16 * t + 8 * (j >> 2) + (j & 3)) * DP;
-                if constexpr (BLOCKS == 4) {
-                    const V2u w = *reinterpret_cast<const V2u*>(p);
-                    v[j][0] = w[0];
-                    v[j][1] = w[1];
-                } else {
-                    v[j][0] = *reinterpret_cast<const uint32_t*>(p);
-                }
-            }
-#pragma unroll
-            for (int b = 0; b < BLOCKS; ++b) {
-                V4u w;
-#pragma unroll
-                for (int i = 0; i < 4; ++i)
-                    w[i] = __builtin_amdgcn_perm(v[2 * i + 1][b >> 1], v[2 * i][b >> 1], b & 1 ? 0x07060302u : 0x05040100u);
-                const V8bf v8 = __builtin_bit_cast(V8bf, w);
-                o[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v8, hi[t], o[b], 0, 0, 0);
-                o[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v8, lo[t], o[b], 0, 0, 0);
+            for (int t = 0; t < 2; ++t) {
+                const V2u v0 = turned(p + 16 * t * DP), v1 = turned(p + (16 * t + 8) * DP);
+                const V8bf v = __builtin_bit_cast(V8bf, V4u{v0[0], v0[1], v1[0], v1[1]});
+                o[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, __builtin_bit_cast(V8bf, hi[t]), o[b], 0, 0, 0);
+                o[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, __builtin_bit_cast(V8bf, lo[t]), o[b], 0, 0, 0);
             }
         }
+    }
+
+    static __device__ __forceinline__ uint32_t pair(float a, float b)
+    {
+        return __builtin_bit_cast(uint32_t, __builtin_convertvector(V2f{a, b}, V2bf));
+    }
+    // Four values of a position a lane: of 16 lanes, lane i gets the i-th value of what lanes i / 4, 4 + i / 4, .. name,
+    // i.e. a dim's four positions.
+    static __device__ __forceinline__ V2u turned(const uint16_t* p)
+    {
+        using At = __attribute__((address_space(3))) V4s*;
+        return __builtin_bit_cast(V2u, __builtin_amdgcn_ds_read_tr16_b64_v4i16((At)(p)));
     }
 
     // Tiles [first, last) of the job.
@@ -1128,14 +1138,15 @@ template <int DP> struct Wide {
         return y + z;
     }
 
-    // Four dims each, or two.
     template <typename F> __device__ __forceinline__ void each_dims(F f) const
     {
 #pragma unroll
-        for (int e = 0; e < 16; ++e) {
-            const int d = BLOCKS * (8 * (e >> 2) + 4 * (lane >> 5) + (e & 3));
-            if (d < a.dim) f(d, e);
-        }
+        for (int b = 0; b < BLOCKS; ++b)
+#pragma unroll
+            for (int e = 0; e < 16; e += 4) {
+                const int d = 32 * b + 2 * e + 4 * (lane >> 5);
+                if (d < a.dim) f(d, V4f{o[b][e], o[b][e + 1], o[b][e + 2], o[b][e + 3]});
+            }
     }
 
     __device__ __forceinline__ void write_out()
@@ -1147,14 +1158,7 @@ template <int DP> struct Wide {
         const int32_t head = kv * a.group + block * a.job_heads + column - token * a.job_heads;
         uint16_t* const out = static_cast<uint16_t*>(a.out) + at * a.out_stride + (int64_t)head * a.out_head_stride;
         const float f = sum == 0.f ? 0.f : 1.f / sum;
-        each_dims([&](int d, int e) {
-            if constexpr (BLOCKS == 4) {
-                store4<uint16_t>(out + d, sum == 0.f ? V4f{0.f, 0.f, 0.f, 0.f} : V4f{o[0][e], o[1][e], o[2][e], o[3][e]} * f);
-            } else {
-                out[d] = rounded<uint16_t>(sum == 0.f ? 0.f : o[0][e] * f);
-                out[d + 1] = rounded<uint16_t>(sum == 0.f ? 0.f : o[1][e] * f);
-            }
-        });
+        each_dims([&](int d, V4f v) { store4<uint16_t>(out + d, sum == 0.f ? V4f{0.f, 0.f, 0.f, 0.f} : v * f); });
         if (lane < 32 && a.lse) a.lse[at * a.heads * a.group + head] = sum == 0.f ? -__builtin_inff() : m * fabsf(a.scale) + logf(sum);
     }
 
@@ -1165,10 +1169,7 @@ template <int DP> struct Wide {
         if (team != 0) return;
         float* const to = part + sub * tree_part_floats(2, a.dim);
         const int column = lane & 31;
-        each_dims([&](int d, int e) {
-#pragma unroll
-            for (int b = 0; b < BLOCKS; ++b) to[64 + column * a.dim + d + b] = o[b][e];
-        });
+        each_dims([&](int d, V4f v) { *reinterpret_cast<V4f*>(to + 64 + column * a.dim + d) = v; });
         if (lane < 32) {
             to[column] = m == -__builtin_inff() ? m : m * fabsf(a.scale);
             to[32 + column] = sum;
