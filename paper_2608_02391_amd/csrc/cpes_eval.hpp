@@ -170,7 +170,7 @@ inline TreeShape tree_shape(bool bf16, int32_t longest, int32_t group, int32_t d
     t.wide = bf16 && dim <= 128 && queries > 32;
     t.sets = queries <= 16 ? 1 : 2;                     // what fits a wave's registers
     t.beside = 1;
-    while (t.beside < 4 && 16 * t.sets * t.beside < queries) t.beside *= 2;
+    while (t.beside < (t.wide ? 8 : 4) && 16 * t.sets * t.beside < queries) t.beside *= 2;
     t.columns = 16 * t.sets * t.beside;
     t.job_heads = group < t.columns ? group : t.columns;
     t.blocks = (group + t.job_heads - 1) / t.job_heads;
@@ -211,6 +211,7 @@ constexpr int kSampleLanes = 64;
 constexpr int kSampleWaves = 4;          // strips of a slice, where a row is cut into slices
 constexpr int kSampleBlocks = 256;       // blocks of such a row at most
 constexpr int kSampleRows = 1024;        // more rows are all cut alike
+constexpr int kSampleAtOnce = 8192;      // rows that a workspace holds
 
 // How a row of logits is cut: into slices of a workgroup (0: one wave does the row) and strips
 // of a wave; a strip into blocks of 2^shift steps, of which there are `slots`, and parts of

@@ -214,12 +214,13 @@ int check_attend(const cpes_cache* cache, int32_t layer, const cpes_pool* pool, 
 // Workgroups of the shares of trees: two per CU, one where a wave's state fills its SIMD's registers.
 int tree_groups(const cpes::TreeShape& t, int32_t head_dim)
 {
-    return t.wide || (head_dim <= 128 && t.sets == 1) ? 512 : 256;
+    return t.beside <= 4 && (t.wide || (head_dim <= 128 && t.sets == 1)) ? 512 : 256;
 }
 
 size_t tree_parts_bytes(const cpes::TreeShape& t, int32_t head_dim)
 {
-    return 2 * (size_t)tree_groups(t, head_dim) * cpes::kAttendWaves * cpes::tree_part_floats(t.sets, head_dim) * sizeof(float);
+    const size_t waves = std::max<size_t>(cpes::kAttendWaves, t.beside);
+    return 2 * (size_t)tree_groups(t, head_dim) * waves * cpes::tree_part_floats(t.sets, head_dim) * sizeof(float);
 }
 
 // Two partial results a wave, then the shares of every job.
@@ -241,6 +242,7 @@ size_t attend_bytes(int32_t rows, int32_t q_heads, int32_t kv_heads, int32_t hea
 
 size_t sample_bytes(int32_t rows, int32_t vocab, int dtype)
 {
+    rows = std::min(rows, cpes::kSampleAtOnce);
     const cpes::SampleSplit x = cpes::sample_split(rows, vocab, dtype);
     if (x.slices == 0) return 0;
     return rows * round16((size_t)x.strips() * (x.note_slots * 2 * cpes::kSampleLanes * sizeof(uint16_t) +
@@ -718,11 +720,9 @@ int cpes_sample(const void* x_dev, int dtype, int32_t rows, int32_t vocab, int64
     rc = check_workspace(workspace_dev, workspace_bytes, sample_bytes(rows, vocab, dtype), fn);
     if (rc || rows == 0) return rc;
     cpes::SampleArgs a;
-    a.x = x_dev;
-    a.uniforms = uniforms_dev;
-    a.tokens = tokens_dev;
-    a.logp = logp_dev;
-    const cpes::SampleSplit split = cpes::sample_split(rows, vocab, dtype);
+    int32_t at_once = std::min(rows, cpes::kSampleAtOnce);
+    const cpes::SampleSplit split = cpes::sample_split(at_once, vocab, dtype);
+    if (split.slices == 0) at_once = rows;                       // nothing in the workspace
     a.slices = split.slices;
     a.waves = split.waves;
     a.strip_steps = split.strip_steps;
@@ -731,21 +731,29 @@ int cpes_sample(const void* x_dev, int dtype, int32_t rows, int32_t vocab, int64
     a.note_shift = split.note_shift;
     a.note_slots = split.note_slots;
     a.group = split.group;
-    const size_t strips = (size_t)rows * split.strips(), notes = strips * split.note_slots * cpes::kSampleLanes;
+    const size_t strips = (size_t)at_once * split.strips(), notes = strips * split.note_slots * cpes::kSampleLanes;
     a.notes = static_cast<uint16_t*>(workspace_dev);            // 16 bytes at a time
     a.samples = a.notes + notes;
     a.sums = reinterpret_cast<double*>(a.samples + notes);
     a.refs = reinterpret_cast<float*>(a.sums + strips * split.slots);
     a.most = a.refs + strips * split.slots;
     a.stride = stride;
-    a.rows = rows;
     a.vocab = vocab;
     a.top_k = top_k >= vocab ? 0 : top_k;
     a.top_p = top_p;
     a.least = min_p > 0.f ? std::log((double)min_p) : -INFINITY;
     a.scale = scale;
     a.c = (double)scale * M_LOG2E;
-    return hip_status(cpes::launch_sample(dtype, a, (hipStream_t)stream), fn);
+    for (int32_t r = 0; r < rows && !rc; r += at_once) {
+        a.rows = std::min(at_once, rows - r);
+        a.x = static_cast<const char*>(x_dev) + (int64_t)r * stride * elem_size(dtype);
+        a.uniforms = uniforms_dev + r;
+        a.tokens = tokens_dev + r;
+        a.logp = logp_dev ? logp_dev + r : nullptr;
+        rc = hip_status(cpes::launch_sample(dtype, a, (hipStream_t)stream), fn);
+        if (rows - r <= at_once) break;                          // r may not pass 2^31
+    }
+    return rc;
 }
 
 }  // extern "C"

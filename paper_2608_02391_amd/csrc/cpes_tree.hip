@@ -795,25 +795,25 @@ constexpr int kWideShare = 4;             // tiles of a workgroup's share at lea
 constexpr int kWideColumns = 32;          // of a wave
 constexpr float kAhead = 4.f;
 
-template <int DP> struct WideShared {
-    // A column of 16-byte pieces of the keys is read at once: their rows lie 16 bytes further apart than they are long.
-    static constexpr int kRow = DP + 8;
-    uint16_t keys[2][kWideTile * kRow];
-    // 16 dims of four positions are read at once, by 32 lanes twice that: a row's 64-byte pieces are swapped by its number.
+template <int DP, int WAVES> struct WideShared {
+    // Rows in pieces of 16 bytes.  32 lanes read one piece each of as many keys, or 4 positions' values of 16 dims
+    // twice: which piece stands where in a row depends on its number, so that they lie in different banks.
+    uint16_t keys[2][kWideTile * DP];
     uint16_t values[2][kWideTile * DP];
-    static __device__ __forceinline__ int value(int r, int d)
-    {
-        return r * DP + (((d >> 5) ^ (DP == 128 ? r & 3 : r >> 1 & 1)) << 5) + (d & 31);
-    }
-    uint32_t odd[2][2];                   // positions with values that are not finite, where not all queries see all of a tile
-    Family<2> family[kWaves];
+    uint32_t odd[2];                      // positions with values that are not finite, where not all queries see all of a tile
+    Family<2> family[WAVES];
+
+    static __device__ __forceinline__ int key_swap(int r) { return DP == 128 ? r & 15 : r >> 1 & 7; }
+    static __device__ __forceinline__ int value_swap(int r) { return DP == 128 ? (r & 3) << 2 : (r >> 1 & 1) << 2; }
+    static __device__ __forceinline__ int value(int r, int d) { return r * DP + (((d >> 3) ^ value_swap(r)) << 3) + (d & 7); }
 };
 
-template <int DP> struct Wide {
-    static constexpr int PIECES = DP / 8, ROWS = kThreads / PIECES, LOADS = kWideTile / ROWS, BLOCKS = DP / 32;
+template <int DP, int WAVES> struct Wide {
+    static constexpr int PIECES = DP / 8, BLOCKS = DP / 32;
+    static constexpr int ROWS = 64 / PIECES, LOADS = kWideTile / ROWS / WAVES;     // of a wave's load, and how many of them
 
     const TreeArgs& a;
-    WideShared<DP>& s;
+    WideShared<DP, WAVES>& s;
     const int tid, lane, wave, sub, team, teams;
 
     Row row;
@@ -826,9 +826,9 @@ template <int DP> struct Wide {
     float m, l;                           // l is this lane's share
     V16f o[BLOCKS];                       // o[b][i]: dim 32 b + 8 (i / 4) + 4 (lane / 32) + i % 4
 
-    __device__ __forceinline__ Wide(const TreeArgs& args, WideShared<DP>& shared)
+    __device__ __forceinline__ Wide(const TreeArgs& args, WideShared<DP, WAVES>& shared)
         : a(args), s(shared), tid(threadIdx.x), lane(threadIdx.x & 63), wave(__builtin_amdgcn_readfirstlane(threadIdx.x >> 6)),
-          sub(wave % args.beside), team(wave / args.beside), teams(kWaves / args.beside)
+          sub(wave % args.beside), team(wave / args.beside), teams(WAVES / args.beside)
     {
     }
 
@@ -928,41 +928,49 @@ template <int DP> struct Wide {
         return id >= 0 && id < a.pages ? id * a.page_stride + (pos - at * a.page_size) * a.token_stride : -1;
     }
 
-    // A thread's pieces of a tile's rows; rows without a page are zeros.
-    V4u key[LOADS], val[LOADS];
-    __device__ __forceinline__ void load(int64_t at)
+    // A tile's rows that have a page go to a buffer, in 1 KiB a wave and load.  Written out, because the compiler would
+    // wait for them before any other read of shared memory; arrived() waits.
+    __device__ __forceinline__ void load(int buffer, int64_t at)
     {
-        const int piece = tid % PIECES;
+        typedef __attribute__((address_space(3))) uint16_t Lds;
+        const int in = lane / PIECES, piece = lane % PIECES;
 #pragma unroll
         for (int k = 0; k < LOADS; ++k) {
-            const int r = tid / PIECES + k * ROWS;
+            const int first = (wave + k * WAVES) * ROWS, r = first + in;
             const uint32_t lo = __shfl((uint32_t)(uint64_t)at, r), hi = __shfl((uint32_t)((uint64_t)at >> 32), r);
             const int64_t from = (int64_t)(((uint64_t)hi << 32) | lo);
-            key[k] = val[k] = V4u{0, 0, 0, 0};
-            if (from >= 0 && 8 * piece < a.dim) {
-                key[k] = *reinterpret_cast<const V4uAnywhere*>(keys_at() + from + 8 * piece);
-                val[k] = *reinterpret_cast<const V4uAnywhere*>(values_at() + from + 8 * piece);
-            }
+            const int kp = 8 * (piece ^ s.key_swap(r)), vp = 8 * (piece ^ s.value_swap(r));
+            const uint32_t key_to = (uint32_t)(uintptr_t)(Lds*)&s.keys[buffer][first * DP];
+            const uint32_t value_to = (uint32_t)(uintptr_t)(Lds*)&s.values[buffer][first * DP];
+            if (from >= 0 && kp < a.dim)
+                asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(key_to), "v"(keys_at() + from + kp)
+                             : "memory", "m0");
+            if (from >= 0 && vp < a.dim)
+                asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(value_to), "v"(values_at() + from + vp)
+                             : "memory", "m0");
         }
     }
-    __device__ __forceinline__ void store(int buffer, bool edge)
+    __device__ __forceinline__ void arrived()
     {
-        const int piece = tid % PIECES;
-#pragma unroll
-        for (int k = 0; k < LOADS; ++k) {
-            const int r = tid / PIECES + k * ROWS;
-            *reinterpret_cast<V4u*>(&s.keys[buffer][r * s.kRow + piece * 8]) = key[k];
-            *reinterpret_cast<V4u*>(&s.values[buffer][s.value(r, piece * 8)]) = val[k];
-        }
-        if (edge) {
-#pragma unroll
-            for (int k = 0; k < LOADS; ++k) {
-                bool odd = false;
-#pragma unroll
-                for (int e = 0; e < 4; ++e) odd |= (val[k][e] & 0x7F80u) == 0x7F80u || (val[k][e] & 0x7F800000u) == 0x7F800000u;
-                const int r = tid / PIECES + k * ROWS;
-                if (odd) atomicOr(&s.odd[buffer][r >> 5], 1u << (r & 31));
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    }
+
+    // Rows without a page become zeros, those with values that are not finite are marked.
+    __device__ __forceinline__ void clean(int buffer, uint64_t there)
+    {
+#pragma unroll 1
+        for (int i = tid; i < kWideTile * PIECES; i += 64 * WAVES) {
+            const int r = i / PIECES;
+            V4u* const v = reinterpret_cast<V4u*>(s.values[buffer]) + i;
+            if (!(there >> r & 1)) {
+                *v = V4u{0, 0, 0, 0};
+                reinterpret_cast<V4u*>(s.keys[buffer])[i] = V4u{0, 0, 0, 0};
+                continue;
             }
+            bool odd = false;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) odd |= ((*v)[e] & 0x7F80u) == 0x7F80u || ((*v)[e] & 0x7F800000u) == 0x7F800000u;
+            if (odd) atomicOr(&s.odd[r >> 5], 1u << (r & 31));
         }
     }
 
@@ -973,11 +981,12 @@ template <int DP> struct Wide {
         V16f x;
 #pragma unroll
         for (int e = 0; e < 16; ++e) x[e] = 0.f;
-        const uint16_t* const krow = &s.keys[buffer][(r0 + (lane & 31)) * s.kRow + 8 * h];
+        const int krow = (r0 + (lane & 31)) * DP + 8 * (h ^ s.key_swap(lane & 31));
 #pragma unroll
         for (int i = 0; i < DP / 16; ++i)
-            x = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(V8bf, *reinterpret_cast<const V4u*>(krow + 16 * i)),
-                                                        __builtin_bit_cast(V8bf, q[i]), x, 0, 0, 0);
+            x = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
+                __builtin_bit_cast(V8bf, *reinterpret_cast<const V4u*>(&s.keys[buffer][krow ^ (16 * i)])), __builtin_bit_cast(V8bf, q[i]),
+                x, 0, 0, 0);
         uint32_t seen = ~0u;
         if (edge) {
             seen = seen_from(pos0 + r0) & there;
@@ -1009,10 +1018,10 @@ template <int DP> struct Wide {
             sum[e & 1] += x[e];
         }
         l += sum[0] + sum[1];
-        if (edge && __builtin_amdgcn_readfirstlane(s.odd[buffer][0] | s.odd[buffer][1])) {
+        if (edge && __builtin_amdgcn_readfirstlane(s.odd[0] | s.odd[1])) {
             // values that are not finite: for the queries that see them only, and then no longer there
 #pragma unroll 1
-            for (uint32_t left = __builtin_amdgcn_readfirstlane(s.odd[buffer][part]); left; left &= left - 1) {
+            for (uint32_t left = __builtin_amdgcn_readfirstlane(s.odd[part]); left; left &= left - 1) {
                 const int r = __builtin_ctz(left);
                 float w = x[0];
 #pragma unroll
@@ -1029,9 +1038,9 @@ template <int DP> struct Wide {
             }
             __syncthreads();
 #pragma unroll 1
-            for (int i = tid; i < kWideTile * DP / 2; i += kThreads) {
+            for (int i = tid; i < kWideTile * DP / 2; i += 64 * WAVES) {
                 const int r = 2 * i / DP, its = teams == 1 ? part : r >> 5;
-                if (r >> 5 == its && (s.odd[buffer][its] >> (r & 31) & 1)) reinterpret_cast<uint32_t*>(s.values[buffer])[i] = 0;
+                if (r >> 5 == its && (s.odd[its] >> (r & 31) & 1)) reinterpret_cast<uint32_t*>(s.values[buffer])[i] = 0;
             }
             __syncthreads();
         }
@@ -1073,37 +1082,43 @@ template <int DP> struct Wide {
     __device__ __forceinline__ void run(int32_t first, int32_t last)
     {
         __syncthreads();                  // the buffers are no longer read
-        if (tid < 4) s.odd[tid >> 1][tid & 1] = 0;
+        if (tid < 2) s.odd[tid] = 0;
+        if (a.dim < DP) {
+            // what no load writes
+            for (int i = tid; i < 2 * kWideTile * PIECES; i += 64 * WAVES)
+                reinterpret_cast<V4u*>(s.keys)[i] = reinterpret_cast<V4u*>(s.values)[i] = V4u{0, 0, 0, 0};
+            __syncthreads();
+        }
         int32_t pos0 = span.at(first, kWideTile);
         int64_t at = place(ask(pos0), pos0);
-        load(at);
+        load(0, at);
         int32_t id = -1;
         if (first + 1 < last) id = ask(span.at(first + 1, kWideTile));
-        __syncthreads();
-        store(0, !whole(pos0));
-        uint64_t there = __ballot(at >= 0);
 #pragma unroll 1
         for (int32_t i = first; i < last; ++i) {
             const int buffer = (i - first) & 1;
-            const bool more = i + 1 < last;
-            const int32_t next = more ? span.at(i + 1, kWideTile) : 0;
-            __syncthreads();              // the tile is there, and the other buffer free
-            if (more) {
-                at = place(id, next);
-                load(at);
-                if (i + 2 < last) id = ask(span.at(i + 2, kWideTile));
-                if (tid < 2) s.odd[buffer ^ 1][tid] = 0;
-            }
+            const uint64_t there = __ballot(at >= 0);
             const bool edge = there != ~0ull || !whole(pos0);
+            arrived();
+            __syncthreads();              // the tile is there, and the other buffer free
+            int32_t next = 0;
+            if (i + 1 < last) {
+                next = span.at(i + 1, kWideTile);
+                at = place(id, next);
+                load(buffer ^ 1, at);
+                if (i + 2 < last) id = ask(span.at(i + 2, kWideTile));
+            }
+            if (edge) {
+                clean(buffer, there);
+                __syncthreads();
+            }
 #pragma unroll 1
             for (int part = team; part < 2; part += teams) fold(buffer, part, pos0, edge, (uint32_t)(there >> (32 * part)));
-            if (more) {
-                there = __ballot(at >= 0);
-                pos0 = next;
-                const bool odd_counts = there != ~0ull || !whole(pos0);
-                if (odd_counts) __syncthreads();          // the marks have been cleared
-                store(buffer ^ 1, odd_counts);
+            if (edge) {
+                __syncthreads();
+                if (tid < 2) s.odd[tid] = 0;
             }
+            pos0 = next;
         }
         // two waves with the same queries: the second hands its piece to the first
         if (teams == 2) {
@@ -1178,7 +1193,7 @@ template <int DP> struct Wide {
 };
 
 // Every row's tiles: a thread's share of them before, and after, its rows.
-template <int TILE> struct Line {
+template <int TILE, int WAVES> struct Line {
     int32_t r0, r1;
     int64_t mine, upto, tiles;
 
@@ -1186,7 +1201,7 @@ template <int TILE> struct Line {
     __device__ __forceinline__ Line(const TreeArgs& a, int64_t* s_sum)
     {
         const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-        const int32_t each = (a.rows + kThreads - 1) / kThreads;
+        const int32_t each = (a.rows + 64 * WAVES - 1) / (64 * WAVES);
         r0 = min(a.rows, tid * each);
         r1 = min(a.rows, r0 + each);
         mine = 0;
@@ -1201,7 +1216,7 @@ template <int TILE> struct Line {
         __syncthreads();
         tiles = 0;
 #pragma unroll
-        for (int w = 0; w < kWaves; ++w) {
+        for (int w = 0; w < WAVES; ++w) {
             if (w < wave) upto += s_sum[w];
             tiles += s_sum[w];
         }
@@ -1223,12 +1238,12 @@ template <int TILE> struct Line {
     }
 };
 
-template <int DP> __global__ __launch_bounds__(kThreads, 2) void k_tree_wide(TreeArgs a)
+template <int DP, int WAVES> __global__ __launch_bounds__(64 * WAVES, 2) void k_tree_wide(TreeArgs a)
 {
-    __shared__ alignas(16) WideShared<DP> s;
-    __shared__ int64_t s_sum[kWaves], s_before;
+    __shared__ alignas(256) WideShared<DP, WAVES> s;
+    __shared__ int64_t s_sum[WAVES], s_before;
     __shared__ int32_t s_row;
-    const Line<kWideTile> line(a, s_sum);
+    const Line<kWideTile, WAVES> line(a, s_sum);
     const int64_t units = line.tiles * a.heads * a.blocks;
     const int32_t shares_n = (int32_t)max((int64_t)1, min((int64_t)a.groups, units / kWideShare)), me = blockIdx.x;
     if (me >= shares_n || units == 0) return;
@@ -1252,7 +1267,7 @@ template <int DP> __global__ __launch_bounds__(kThreads, 2) void k_tree_wide(Tre
     cur.i = __builtin_amdgcn_readfirstlane((int32_t)in_row);
     cur.span = span_at<kWideTile>(a, cur.row, cur.piece);
     int64_t done = 0;
-    Wide<DP> work(a, s);
+    Wide<DP, WAVES> work(a, s);
 #pragma unroll 1
     while (left > 0) {
         const int32_t take = (int32_t)min(left, (int64_t)(cur.span.tiles - cur.i));
@@ -1273,9 +1288,9 @@ template <int DP> __global__ __launch_bounds__(kThreads, 2) void k_tree_wide(Tre
     }
 }
 
-template <int DP> __global__ __launch_bounds__(kThreads, 2) void k_tree_wide_jobs(TreeArgs a)
+template <int DP, int WAVES> __global__ __launch_bounds__(64 * WAVES, 2) void k_tree_wide_jobs(TreeArgs a)
 {
-    __shared__ alignas(16) WideShared<DP> s;
+    __shared__ alignas(256) WideShared<DP, WAVES> s;
     const int32_t each = a.heads * a.blocks, hh = blockIdx.x % each;
     const int64_t slots = gridDim.x / each;
     int32_t r, piece;
@@ -1283,7 +1298,7 @@ template <int DP> __global__ __launch_bounds__(kThreads, 2) void k_tree_wide_job
     if (!find_job(a, slots - 1 - blockIdx.x / each, &r, &piece)) return;
     const Row row = wave_row(a, r);
     if ((int64_t)piece * a.job_tokens >= row.tokens) return;
-    Wide<DP> work(a, s);
+    Wide<DP, WAVES> work(a, s);
     work.begin(row, span_at<kWideTile>(a, row, piece), hh);
     work.run(0, work.span.tiles);
     work.write_out();
@@ -1397,15 +1412,15 @@ template <typename T, int DP, bool kWhole> hipError_t tree_sets(const TreeArgs& 
     else return tree_as<T, DP, kWhole, 2>(a, s);
 }
 
-template <int DP> hipError_t tree_wide(const TreeArgs& a, hipStream_t s)
+template <int DP, int WAVES> hipError_t tree_wide(const TreeArgs& a, hipStream_t s)
 {
     const int32_t each = a.heads * a.blocks;
     const int64_t jobs = ((int64_t)a.tokens / a.job_tokens + a.rows) * each, most = most_tiles<kWideTile>(a);
-    if ((jobs >= 1024 || most <= 16) && jobs <= INT32_MAX / kThreads) {
-        hipLaunchKernelGGL(k_tree_wide_jobs<DP>, dim3((unsigned)jobs), dim3(kThreads), 0, s, a);
+    if ((jobs >= 1024 || most <= 16) && jobs <= INT32_MAX / (64 * WAVES)) {
+        hipLaunchKernelGGL((k_tree_wide_jobs<DP, WAVES>), dim3((unsigned)jobs), dim3(64 * WAVES), 0, s, a);
         return hipGetLastError();
     }
-    hipLaunchKernelGGL(k_tree_wide<DP>, dim3((unsigned)a.groups), dim3(kThreads), 0, s, a);
+    hipLaunchKernelGGL((k_tree_wide<DP, WAVES>), dim3((unsigned)a.groups), dim3(64 * WAVES), 0, s, a);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
     const int64_t all = (int64_t)a.rows * a.pieces * each;
@@ -1417,7 +1432,7 @@ template <int DP> hipError_t tree_wide(const TreeArgs& a, hipStream_t s)
 template <typename T, int DP> hipError_t tree_dim(const TreeArgs& a, hipStream_t s)
 {
     if constexpr (std::is_same<T, uint16_t>::value && DP <= 128)
-        if (a.wide) return tree_wide<DP>(a, s);
+        if (a.wide) return a.beside > 4 ? tree_wide<DP, 8>(a, s) : tree_wide<DP, 4>(a, s);
 
     return a.page_size % 16 == 0 ? tree_sets<T, DP, true>(a, s) : tree_sets<T, DP, false>(a, s);
 }

@@ -129,7 +129,7 @@ def test_workspaces_serve_smaller_calls():
     for vocab in (100, 8192, 50257, 151936, 1 << 20):
         sizes = [cp.cpes_sample_workspace_bytes(rows, vocab) for rows in range(600)]
         assert sizes == sorted(sizes)
-        assert cp.cpes_sample_workspace_bytes(1 << 20, vocab) == sizes[-1]
+        assert sizes[-1] <= cp.cpes_sample_workspace_bytes(8192, vocab) == cp.cpes_sample_workspace_bytes(2 ** 31 - 1, vocab) < 1 << 27
     for heads in ((8, 2, 64), (32, 8, 128), (33, 1, 256), (3, 1, 64), (300, 1, 128), (7, 7, 256), (20, 1, 40)):
         for longest in (1, 7, 60, 200):
             sizes = [cp.cpes_attend_tree_workspace_bytes(rows, 10000, longest, *heads) for rows in range(200)]
@@ -202,3 +202,10 @@ def test_plain_implementations():
     for n in (1, 2, 50):
         t = D.random_tree(n, rng)
         assert t[0] == -1 and all(0 <= a < i for i, a in enumerate(t) if i)
+
+
+def test_tree_workspace_holds_every_share():
+    """Where shares are of 256 queries of a KV head, 256 of them are resident, each with two partial results."""
+    for dim in (64, 128):
+        assert cp.cpes_attend_tree_workspace_bytes(1, 64, 64, 4, 1, dim) >= 2 * 256 * 256 * (2 + dim) * 4
+        assert cp.cpes_attend_tree_workspace_bytes(1, 4096, 4096, 8, 8, dim) >= 2 * 256 * 256 * (2 + dim) * 4

@@ -263,3 +263,12 @@ def test_many_logits():
     y[8, 99] = 40.0
     token, _ = run(y, torch.full((rows,), 0.5, device="cuda"))
     assert int(token[8]) == 99 and bool((token[:8] == vocab // 2).all())
+
+
+def test_more_rows_than_are_taken_at_once():
+    """8,192 rows are cut and kept together; the ones behind them draw from their own logits, strided."""
+    x, u = logits(8192 + 37, 8300, BF16, seed=12)
+    wide = torch.empty(8192 + 37, 8320, dtype=BF16, device="cuda")[:, :8300]
+    wide.copy_(x)
+    for f in (dict(), dict(top_k=20), dict(top_p=0.9)):
+        check(wide, u, rows=[0, 1, 4095, 8190, 8191, 8192, 8193, 8200, 8228], **f)
