@@ -982,11 +982,25 @@ template <int DP, int WAVES> struct Wide {
 #pragma unroll
         for (int e = 0; e < 16; ++e) x[e] = 0.f;
         const int krow = (r0 + (lane & 31)) * DP + 8 * (h ^ s.key_swap(lane & 31));
+        V4u k[DP / 16];
+#pragma unroll
+        for (int i = 0; i < DP / 16; ++i) k[i] = *reinterpret_cast<const V4u*>(&s.keys[buffer][krow ^ (16 * i)]);
+        __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
         for (int i = 0; i < DP / 16; ++i)
-            x = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
-                __builtin_bit_cast(V8bf, *reinterpret_cast<const V4u*>(&s.keys[buffer][krow ^ (16 * i)])), __builtin_bit_cast(V8bf, q[i]),
-                x, 0, 0, 0);
+            x = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(V8bf, k[i]), __builtin_bit_cast(V8bf, q[i]), x, 0, 0, 0);
+        // the values are on their way during the softmax: dim lane % 32 of each 32, positions 16 t + {0 .. 3, 8 .. 11} + 4 h of the half
+        V2u v[BLOCKS][4];
+        auto values = [&] {
+#pragma unroll
+            for (int b = 0; b < BLOCKS; ++b) {
+                const uint16_t* const p = &s.values[buffer][s.value(r0 + 4 * h + (lane >> 2 & 3), 32 * b + (lane & 16) + 4 * (lane & 3))];
+#pragma unroll
+                for (int t = 0; t < 4; ++t) v[b][t] = turned(p + 8 * t * DP);
+            }
+        };
+        values();
+        __builtin_amdgcn_sched_barrier(0);
         uint32_t seen = ~0u;
         if (edge) {
             seen = seen_from(pos0 + r0) & there;
@@ -1043,6 +1057,7 @@ template <int DP, int WAVES> struct Wide {
                 if (r >> 5 == its && (s.odd[its] >> (r & 31) & 1)) reinterpret_cast<uint32_t*>(s.values[buffer])[i] = 0;
             }
             __syncthreads();
+            values();
         }
         V4u hi[2], lo[2];
 #pragma unroll
@@ -1051,19 +1066,14 @@ template <int DP, int WAVES> struct Wide {
             hi[e >> 3][e >> 1 & 3] = both;
             lo[e >> 3][e >> 1 & 3] = pair(x[e] - __uint_as_float(both << 16), x[e + 1] - __uint_as_float(both & 0xFFFF0000u));
         }
-        // dim lane % 32 of each 32, positions 16 t + {0 .. 3, 8 .. 11} + 4 h of the half
-        const int in = lane >> 2 & 3;
 #pragma unroll
-        for (int b = 0; b < BLOCKS; ++b) {
-            const uint16_t* const p = &s.values[buffer][s.value(r0 + 4 * h + in, 32 * b + (lane & 16) + 4 * (lane & 3))];
+        for (int t = 0; t < 2; ++t)
 #pragma unroll
-            for (int t = 0; t < 2; ++t) {
-                const V2u v0 = turned(p + 16 * t * DP), v1 = turned(p + (16 * t + 8) * DP);
-                const V8bf v = __builtin_bit_cast(V8bf, V4u{v0[0], v0[1], v1[0], v1[1]});
-                o[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, __builtin_bit_cast(V8bf, hi[t]), o[b], 0, 0, 0);
-                o[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, __builtin_bit_cast(V8bf, lo[t]), o[b], 0, 0, 0);
+            for (int b = 0; b < BLOCKS; ++b) {
+                const V8bf v8 = __builtin_bit_cast(V8bf, V4u{v[b][2 * t][0], v[b][2 * t][1], v[b][2 * t + 1][0], v[b][2 * t + 1][1]});
+                o[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v8, __builtin_bit_cast(V8bf, hi[t]), o[b], 0, 0, 0);
+                o[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v8, __builtin_bit_cast(V8bf, lo[t]), o[b], 0, 0, 0);
             }
-        }
     }
 
     static __device__ __forceinline__ uint32_t pair(float a, float b)
