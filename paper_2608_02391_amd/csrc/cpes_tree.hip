@@ -808,17 +808,18 @@ template <int DP, int WAVES> struct WideShared {
     static __device__ __forceinline__ int value(int r, int d) { return r * DP + (((d >> 3) ^ value_swap(r)) << 3) + (d & 7); }
 };
 
-template <int DP, int WAVES> struct Wide {
+template <int DP, int WAVES, int TEAMS> struct Wide {
     static constexpr int PIECES = DP / 8, BLOCKS = DP / 32;
     static constexpr int ROWS = 64 / PIECES, LOADS = kWideTile / ROWS / WAVES;     // of a wave's load, and how many of them
 
     const TreeArgs& a;
     WideShared<DP, WAVES>& s;
-    const int tid, lane, wave, sub, team, teams;
+    const int tid, lane, wave, sub, team;
 
     Row row;
     Span span;
     int32_t kv, block;
+    bool busy;                            // the wave has queries of the job
     bool valid;                           // the lane's query: column sub * 32 + lane % 32
     int32_t low, high, every_low, every_high;
     V4u q[DP / 16];
@@ -828,7 +829,7 @@ template <int DP, int WAVES> struct Wide {
 
     __device__ __forceinline__ Wide(const TreeArgs& args, WideShared<DP, WAVES>& shared)
         : a(args), s(shared), tid(threadIdx.x), lane(threadIdx.x & 63), wave(__builtin_amdgcn_readfirstlane(threadIdx.x >> 6)),
-          sub(wave % args.beside), team(wave / args.beside), teams(WAVES / args.beside)
+          sub(wave % (WAVES / TEAMS)), team(wave / (WAVES / TEAMS))
     {
     }
 
@@ -847,6 +848,7 @@ template <int DP, int WAVES> struct Wide {
         const int32_t head = block * a.job_heads + column - token * a.job_heads;
         const int32_t i = span.from + min(token, span.count - 1);
         valid = token < span.count && head < a.group;
+        busy = sub * kWideColumns < span.count * a.job_heads;
         int32_t depth = i;
         if (tree) {
             wave_sync();                  // the last job's are no longer read
@@ -974,43 +976,63 @@ template <int DP, int WAVES> struct Wide {
         }
     }
 
-    // Folds half `part` of the tile in a buffer into the state.
-    __device__ __forceinline__ void fold(int buffer, int part, int32_t pos0, bool edge, uint32_t there)
+    // Folds the team's part of the tile in a buffer into the state: all of it, or a half.
+    __device__ __forceinline__ void fold(int buffer, int32_t pos0, bool edge, uint64_t there)
     {
-        const int h = lane >> 5, r0 = 32 * part;
-        V16f x;
-#pragma unroll
-        for (int e = 0; e < 16; ++e) x[e] = 0.f;
+        constexpr int PARTS = 2 / TEAMS;
+        const int h = lane >> 5, r0 = 32 * team;
+        V16f x[PARTS];
         const int krow = (r0 + (lane & 31)) * DP + 8 * (h ^ s.key_swap(lane & 31));
-        V4u k[DP / 16];
 #pragma unroll
-        for (int i = 0; i < DP / 16; ++i) k[i] = *reinterpret_cast<const V4u*>(&s.keys[buffer][krow ^ (16 * i)]);
-        __builtin_amdgcn_sched_barrier(0);
+        for (int p = 0; p < PARTS; ++p)
 #pragma unroll
-        for (int i = 0; i < DP / 16; ++i)
-            x = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(V8bf, k[i]), __builtin_bit_cast(V8bf, q[i]), x, 0, 0, 0);
-        // the values are on their way during the softmax: dim lane % 32 of each 32, positions 16 t + {0 .. 3, 8 .. 11} + 4 h of the half
-        V2u v[BLOCKS][4];
-        auto values = [&] {
+            for (int e = 0; e < 16; ++e) x[p][e] = 0.f;
+#pragma unroll
+        for (int i0 = 0; i0 < DP / 16; i0 += 8 / PARTS) {
+            // eight pieces of keys asked for at once: more do not fit the registers
+            V4u k[PARTS][8 / PARTS];
+#pragma unroll
+            for (int i = 0; i < 8 / PARTS; ++i)
+#pragma unroll
+                for (int p = 0; p < PARTS; ++p)
+                    if (i0 + i < DP / 16) k[p][i] = *reinterpret_cast<const V4u*>(&s.keys[buffer][(krow ^ (16 * (i0 + i))) + 32 * p * DP]);
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int i = 0; i < 8 / PARTS; ++i)
+#pragma unroll
+                for (int p = 0; p < PARTS; ++p)
+                    if (i0 + i < DP / 16)
+                        x[p] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(V8bf, k[p][i]), __builtin_bit_cast(V8bf, q[i0 + i]), x[p],
+                                                                       0, 0, 0);
+        }
+        // the values are on their way during the softmax: dim lane % 32 of each 32, positions 8 t + {0 .. 3} + 4 h of the part
+        V2u v[PARTS][BLOCKS][4];
+        auto values = [&](int p) {
 #pragma unroll
             for (int b = 0; b < BLOCKS; ++b) {
-                const uint16_t* const p = &s.values[buffer][s.value(r0 + 4 * h + (lane >> 2 & 3), 32 * b + (lane & 16) + 4 * (lane & 3))];
+                const uint16_t* const from = &s.values[buffer][s.value(r0 + 4 * h + (lane >> 2 & 3), 32 * b + (lane & 16) + 4 * (lane & 3))];
 #pragma unroll
-                for (int t = 0; t < 4; ++t) v[b][t] = turned(p + 8 * t * DP);
+                for (int t = 0; t < 4; ++t) v[p][b][t] = turned(from + (32 * p + 8 * t) * DP);
             }
         };
-        values();
+        values(0);
         __builtin_amdgcn_sched_barrier(0);
-        uint32_t seen = ~0u;
-        if (edge) {
-            seen = seen_from(pos0 + r0) & there;
+        uint32_t seen[PARTS];
 #pragma unroll
-            for (int e = 0; e < 16; ++e)
-                if (!(seen >> (8 * (e >> 2) + 4 * h + (e & 3)) & 1)) x[e] = -__builtin_inff();
+        for (int p = 0; p < PARTS; ++p) {
+            seen[p] = ~0u;
+            if (edge) {
+                seen[p] = seen_from(pos0 + r0 + 32 * p) & (uint32_t)(there >> (r0 + 32 * p));
+#pragma unroll
+                for (int e = 0; e < 16; ++e)
+                    if (!(seen[p] >> (8 * (e >> 2) + 4 * h + (e & 3)) & 1)) x[p][e] = -__builtin_inff();
+            }
         }
-        float top = x[0];
+        float top = x[0][0];
 #pragma unroll
-        for (int e = 1; e < 16; ++e) top = fmaxf(top, x[e]);
+        for (int p = 0; p < PARTS; ++p)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) top = fmaxf(top, x[p][e]);
         float y, z;
         swap_halves(top, &y, &z);
         top = fmaxf(y, z);
@@ -1025,55 +1047,66 @@ template <int DP, int WAVES> struct Wide {
         }
         // nothing seen yet: any finite base gives weights of 0
         const float shift = m == -__builtin_inff() ? 0.f : -m * unit;
-        float sum[2] = {0.f, 0.f};
-#pragma unroll
-        for (int e = 0; e < 16; ++e) {
-            x[e] = __builtin_amdgcn_exp2f(fmaf(x[e], unit, shift));
-            sum[e & 1] += x[e];
-        }
-        l += sum[0] + sum[1];
         if (edge && __builtin_amdgcn_readfirstlane(s.odd[0] | s.odd[1])) {
             // values that are not finite: for the queries that see them only, and then no longer there
+#pragma unroll
+            for (int p = 0; p < PARTS; ++p)
 #pragma unroll 1
-            for (uint32_t left = __builtin_amdgcn_readfirstlane(s.odd[part]); left; left &= left - 1) {
-                const int r = __builtin_ctz(left);
-                float w = x[0];
+                for (uint32_t left = __builtin_amdgcn_readfirstlane(s.odd[team + p]); left; left &= left - 1) {
+                    const int r = __builtin_ctz(left);
+                    float w = x[p][0];
 #pragma unroll
-                for (int e = 1; e < 16; ++e)
-                    if (e == 4 * (r >> 3) + (r & 3)) w = x[e];
-                w = __shfl(w, (lane & 31) + 32 * (r >> 2 & 1));
-                if (seen >> r & 1) {
+                    for (int e = 1; e < 16; ++e)
+                        if (e == 4 * (r >> 3) + (r & 3)) w = x[p][e];
+                    w = __builtin_amdgcn_exp2f(fmaf(__shfl(w, (lane & 31) + 32 * (r >> 2 & 1)), unit, shift));
+                    if (seen[p] >> r & 1) {
 #pragma unroll
-                    for (int b = 0; b < BLOCKS; ++b)
+                        for (int b = 0; b < BLOCKS; ++b)
 #pragma unroll
-                        for (int e = 0; e < 16; ++e)
-                            o[b][e] = fmaf(w, __uint_as_float((uint32_t)s.values[buffer][s.value(r0 + r, 32 * b + 8 * (e >> 2) + 4 * h + (e & 3))] << 16), o[b][e]);
+                            for (int e = 0; e < 16; ++e)
+                                o[b][e] = fmaf(w, __uint_as_float((uint32_t)s.values[buffer][s.value(r0 + 32 * p + r, 32 * b + 8 * (e >> 2) + 4 * h + (e & 3))] << 16), o[b][e]);
+                    }
                 }
+            clear_odd(buffer);
+            values(0);
+        }
+        float sum[2] = {0.f, 0.f};
+#pragma unroll
+        for (int p = 0; p < PARTS; ++p) {
+            if (p > 0) values(p);
+#pragma unroll
+            for (int e = 0; e < 16; ++e) {
+                x[p][e] = __builtin_amdgcn_exp2f(fmaf(x[p][e], unit, shift));
+                sum[e & 1] += x[p][e];
             }
-            __syncthreads();
+            V4u hi[2], lo[2];
+#pragma unroll
+            for (int e = 0; e < 16; e += 2) {
+                const uint32_t both = pair(x[p][e], x[p][e + 1]);
+                hi[e >> 3][e >> 1 & 3] = both;
+                lo[e >> 3][e >> 1 & 3] = pair(x[p][e] - __uint_as_float(both << 16), x[p][e + 1] - __uint_as_float(both & 0xFFFF0000u));
+            }
+#pragma unroll
+            for (int t = 0; t < 2; ++t)
+#pragma unroll
+                for (int b = 0; b < BLOCKS; ++b) {
+                    const V2u v0 = v[p][b][2 * t], v1 = v[p][b][2 * t + 1];
+                    const V8bf v8 = __builtin_bit_cast(V8bf, V4u{v0[0], v0[1], v1[0], v1[1]});
+                    o[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v8, __builtin_bit_cast(V8bf, hi[t]), o[b], 0, 0, 0);
+                    o[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v8, __builtin_bit_cast(V8bf, lo[t]), o[b], 0, 0, 0);
+                }
+        }
+        l += sum[0] + sum[1];
+    }
+
+    // All waves, when what the marked positions add has been added: their values become zeros.
+    __device__ __forceinline__ void clear_odd(int buffer)
+    {
+        __syncthreads();
 #pragma unroll 1
-            for (int i = tid; i < kWideTile * DP / 2; i += 64 * WAVES) {
-                const int r = 2 * i / DP, its = teams == 1 ? part : r >> 5;
-                if (r >> 5 == its && (s.odd[its] >> (r & 31) & 1)) reinterpret_cast<uint32_t*>(s.values[buffer])[i] = 0;
-            }
-            __syncthreads();
-            values();
-        }
-        V4u hi[2], lo[2];
-#pragma unroll
-        for (int e = 0; e < 16; e += 2) {
-            const uint32_t both = pair(x[e], x[e + 1]);
-            hi[e >> 3][e >> 1 & 3] = both;
-            lo[e >> 3][e >> 1 & 3] = pair(x[e] - __uint_as_float(both << 16), x[e + 1] - __uint_as_float(both & 0xFFFF0000u));
-        }
-#pragma unroll
-        for (int t = 0; t < 2; ++t)
-#pragma unroll
-            for (int b = 0; b < BLOCKS; ++b) {
-                const V8bf v8 = __builtin_bit_cast(V8bf, V4u{v[b][2 * t][0], v[b][2 * t][1], v[b][2 * t + 1][0], v[b][2 * t + 1][1]});
-                o[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v8, __builtin_bit_cast(V8bf, hi[t]), o[b], 0, 0, 0);
-                o[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v8, __builtin_bit_cast(V8bf, lo[t]), o[b], 0, 0, 0);
-            }
+        for (int i = tid; i < kWideTile * PIECES; i += 64 * WAVES)
+            if (s.odd[i / PIECES >> 5] >> (i / PIECES & 31) & 1) reinterpret_cast<V4u*>(s.values[buffer])[i] = V4u{0, 0, 0, 0};
+        __syncthreads();
     }
 
     static __device__ __forceinline__ uint32_t pair(float a, float b)
@@ -1122,8 +1155,10 @@ template <int DP, int WAVES> struct Wide {
                 clean(buffer, there);
                 __syncthreads();
             }
-#pragma unroll 1
-            for (int part = team; part < 2; part += teams) fold(buffer, part, pos0, edge, (uint32_t)(there >> (32 * part)));
+            if (busy)
+                fold(buffer, pos0, edge, there);
+            else if (edge && __builtin_amdgcn_readfirstlane(s.odd[0] | s.odd[1]))
+                clear_odd(buffer);
             if (edge) {
                 __syncthreads();
                 if (tid < 2) s.odd[tid] = 0;
@@ -1131,7 +1166,7 @@ template <int DP, int WAVES> struct Wide {
             pos0 = next;
         }
         // two waves with the same queries: the second hands its piece to the first
-        if (teams == 2) {
+        if constexpr (TEAMS == 2) {
             __syncthreads();
             float* const to = reinterpret_cast<float*>(&s) + sub * 64 * (16 * BLOCKS + 2);
             if (team == 1) {
@@ -1248,7 +1283,7 @@ template <int TILE, int WAVES> struct Line {
     }
 };
 
-template <int DP, int WAVES> __global__ __launch_bounds__(64 * WAVES, 2) void k_tree_wide(TreeArgs a)
+template <int DP, int WAVES, int TEAMS> __global__ __launch_bounds__(64 * WAVES, 2) void k_tree_wide(TreeArgs a)
 {
     __shared__ alignas(256) WideShared<DP, WAVES> s;
     __shared__ int64_t s_sum[WAVES], s_before;
@@ -1277,7 +1312,7 @@ template <int DP, int WAVES> __global__ __launch_bounds__(64 * WAVES, 2) void k_
     cur.i = __builtin_amdgcn_readfirstlane((int32_t)in_row);
     cur.span = span_at<kWideTile>(a, cur.row, cur.piece);
     int64_t done = 0;
-    Wide<DP, WAVES> work(a, s);
+    Wide<DP, WAVES, TEAMS> work(a, s);
 #pragma unroll 1
     while (left > 0) {
         const int32_t take = (int32_t)min(left, (int64_t)(cur.span.tiles - cur.i));
@@ -1298,7 +1333,7 @@ template <int DP, int WAVES> __global__ __launch_bounds__(64 * WAVES, 2) void k_
     }
 }
 
-template <int DP, int WAVES> __global__ __launch_bounds__(64 * WAVES, 2) void k_tree_wide_jobs(TreeArgs a)
+template <int DP, int WAVES, int TEAMS> __global__ __launch_bounds__(64 * WAVES, 2) void k_tree_wide_jobs(TreeArgs a)
 {
     __shared__ alignas(256) WideShared<DP, WAVES> s;
     const int32_t each = a.heads * a.blocks, hh = blockIdx.x % each;
@@ -1308,7 +1343,7 @@ template <int DP, int WAVES> __global__ __launch_bounds__(64 * WAVES, 2) void k_
     if (!find_job(a, slots - 1 - blockIdx.x / each, &r, &piece)) return;
     const Row row = wave_row(a, r);
     if ((int64_t)piece * a.job_tokens >= row.tokens) return;
-    Wide<DP, WAVES> work(a, s);
+    Wide<DP, WAVES, TEAMS> work(a, s);
     work.begin(row, span_at<kWideTile>(a, row, piece), hh);
     work.run(0, work.span.tiles);
     work.write_out();
@@ -1422,15 +1457,15 @@ template <typename T, int DP, bool kWhole> hipError_t tree_sets(const TreeArgs& 
     else return tree_as<T, DP, kWhole, 2>(a, s);
 }
 
-template <int DP, int WAVES> hipError_t tree_wide(const TreeArgs& a, hipStream_t s)
+template <int DP, int WAVES, int TEAMS> hipError_t tree_wide(const TreeArgs& a, hipStream_t s)
 {
     const int32_t each = a.heads * a.blocks;
     const int64_t jobs = ((int64_t)a.tokens / a.job_tokens + a.rows) * each, most = most_tiles<kWideTile>(a);
     if ((jobs >= 1024 || most <= 16) && jobs <= INT32_MAX / (64 * WAVES)) {
-        hipLaunchKernelGGL((k_tree_wide_jobs<DP, WAVES>), dim3((unsigned)jobs), dim3(64 * WAVES), 0, s, a);
+        hipLaunchKernelGGL((k_tree_wide_jobs<DP, WAVES, TEAMS>), dim3((unsigned)jobs), dim3(64 * WAVES), 0, s, a);
         return hipGetLastError();
     }
-    hipLaunchKernelGGL((k_tree_wide<DP, WAVES>), dim3((unsigned)a.groups), dim3(64 * WAVES), 0, s, a);
+    hipLaunchKernelGGL((k_tree_wide<DP, WAVES, TEAMS>), dim3((unsigned)a.groups), dim3(64 * WAVES), 0, s, a);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
     const int64_t all = (int64_t)a.rows * a.pieces * each;
@@ -1442,7 +1477,7 @@ template <int DP, int WAVES> hipError_t tree_wide(const TreeArgs& a, hipStream_t
 template <typename T, int DP> hipError_t tree_dim(const TreeArgs& a, hipStream_t s)
 {
     if constexpr (std::is_same<T, uint16_t>::value && DP <= 128)
-        if (a.wide) return a.beside > 4 ? tree_wide<DP, 8>(a, s) : tree_wide<DP, 4>(a, s);
+        if (a.wide) return a.beside > 4 ? tree_wide<DP, 8, 1>(a, s) : a.beside > 2 ? tree_wide<DP, 4, 1>(a, s) : tree_wide<DP, 4, 2>(a, s);
 
     return a.page_size % 16 == 0 ? tree_sets<T, DP, true>(a, s) : tree_sets<T, DP, false>(a, s);
 }
