@@ -808,7 +808,7 @@ template <int DP, int WAVES> struct WideShared {
     static __device__ __forceinline__ int value(int r, int d) { return r * DP + (((d >> 3) ^ value_swap(r)) << 3) + (d & 7); }
 };
 
-template <int DP, int WAVES, int TEAMS> struct Wide {
+template <int DP, int WAVES, int TEAMS, bool kLean> struct Wide {
     static constexpr int PIECES = DP / 8, BLOCKS = DP / 32;
     static constexpr int ROWS = 64 / PIECES, LOADS = kWideTile / ROWS / WAVES;     // of a wave's load, and how many of them
 
@@ -935,7 +935,10 @@ template <int DP, int WAVES, int TEAMS> struct Wide {
     __device__ __forceinline__ void load(int buffer, int64_t at)
     {
         typedef __attribute__((address_space(3))) uint16_t Lds;
-        const int in = lane / PIECES, piece = lane % PIECES;
+        // what follows from the lane is found again for each tile where the folding needs the registers
+        int again = lane;
+        if constexpr (kLean) asm volatile("" : "+v"(again));
+        const int in = again / PIECES, piece = again % PIECES;
 #pragma unroll
         for (int k = 0; k < LOADS; ++k) {
             const int first = (wave + k * WAVES) * ROWS, r = first + in;
@@ -1283,53 +1286,88 @@ template <int TILE, int WAVES> struct Line {
     }
 };
 
+// Where a workgroup is in its share.  Kept in shared memory: what it held in registers while tiles are folded would
+// cost the folding its own.
+struct Progress {
+    int64_t unit, end, units;
+    int32_t r, hh, piece, i;
+};
+
+__device__ __forceinline__ int32_t held(int32_t x) { return __builtin_amdgcn_readfirstlane(x); }
+
 template <int DP, int WAVES, int TEAMS> __global__ __launch_bounds__(64 * WAVES, 2) void k_tree_wide(TreeArgs a)
 {
     __shared__ alignas(256) WideShared<DP, WAVES> s;
     __shared__ int64_t s_sum[WAVES], s_before;
     __shared__ int32_t s_row;
-    const Line<kWideTile, WAVES> line(a, s_sum);
-    const int64_t units = line.tiles * a.heads * a.blocks;
-    const int32_t shares_n = (int32_t)max((int64_t)1, min((int64_t)a.groups, units / kWideShare)), me = blockIdx.x;
-    if (me >= shares_n || units == 0) return;
-    const Shares shares(units, shares_n);
-    const int64_t at = shares.begin(me), hh0 = quotient(at, line.tiles), t = at - hh0 * line.tiles;
-    line.find(a, t, &s_row, &s_before);
-    __syncthreads();
-    int64_t left = shares.begin(me + 1) - at;
-    Cursor cur;
-    cur.r = __builtin_amdgcn_readfirstlane(s_row);
-    cur.hh = __builtin_amdgcn_readfirstlane((int32_t)hh0);
-    cur.row = wave_row(a, cur.r);
-    int64_t in_row = t - s_before;
-    cur.piece = 0;
-    cur.span = span_at<kWideTile>(a, cur.row, 0);
-    while (in_row >= cur.span.tiles) {
-        in_row -= cur.span.tiles;
-        cur.span = span_at<kWideTile>(a, cur.row, ++cur.piece);
+    __shared__ Progress s_at[2];
+    const int32_t me = blockIdx.x;
+    auto number = [&](int64_t units) { return (int32_t)max((int64_t)1, min((int64_t)a.groups, units / kWideShare)); };
+    {
+        const Line<kWideTile, WAVES> line(a, s_sum);
+        Progress x;
+        x.units = line.tiles * a.heads * a.blocks;
+        if (me >= number(x.units) || x.units == 0) return;
+        const Shares shares(x.units, number(x.units));
+        x.unit = shares.begin(me);
+        x.end = shares.begin(me + 1);
+        x.hh = (int32_t)quotient(x.unit, line.tiles);
+        int64_t t = x.unit - x.hh * line.tiles;
+        line.find(a, t, &s_row, &s_before);
+        __syncthreads();
+        x.r = held(s_row);
+        x.piece = 0;
+        const Row row = wave_row(a, x.r);
+        t -= s_before;
+        for (int32_t n; t >= (n = span_at<kWideTile>(a, row, x.piece).tiles); ++x.piece) t -= n;
+        x.i = (int32_t)t;
+        if (threadIdx.x == 0) s_at[0] = x;
+        __syncthreads();
     }
-    cur.piece = __builtin_amdgcn_readfirstlane(cur.piece);
-    cur.i = __builtin_amdgcn_readfirstlane((int32_t)in_row);
-    cur.span = span_at<kWideTile>(a, cur.row, cur.piece);
-    int64_t done = 0;
-    Wide<DP, WAVES, TEAMS> work(a, s);
+    Wide<DP, WAVES, TEAMS, DP == 128> work(a, s);
 #pragma unroll 1
-    while (left > 0) {
-        const int32_t take = (int32_t)min(left, (int64_t)(cur.span.tiles - cur.i));
-        const bool begins = cur.i == 0, turns = cur.i + take == cur.span.tiles;
-        work.begin(cur.row, cur.span, cur.hh);
-        work.run(cur.i, cur.i + take);
-        if (begins && threadIdx.x == 0)
-            // which shares hold the rest of it
-            a.joins[job_index(a, cur.r, cur.piece, cur.hh)] = int2{me, turns ? me : shares.of(at + done + cur.span.tiles - 1)};
+    for (int slot = 0;; slot ^= 1) {
+        bool begins, turns;
+        {
+            const Progress& x = s_at[slot];
+            const Row row = wave_row(a, held(x.r));
+            const int32_t piece = held(x.piece), i = held(x.i), hh = held(x.hh);
+            const Span span = span_at<kWideTile>(a, row, piece);
+            const int32_t take = (int32_t)min(x.end - x.unit, (int64_t)(span.tiles - i));
+            begins = i == 0;
+            turns = i + take == span.tiles;
+            if (begins && threadIdx.x == 0) {
+                // which shares hold the rest of it
+                const int32_t last = turns ? me : Shares(x.units, number(x.units)).of(x.unit + span.tiles - 1);
+                a.joins[job_index(a, x.r, piece, hh)] = int2{me, last};
+            }
+            work.begin(row, span, hh);
+            work.run(i, held(i + take));
+        }
         if (begins && turns)
             work.write_out();
         else
             work.write_part(a.parts + (2 * (int64_t)me + (begins ? 1 : 0)) * a.beside * tree_part_floats(2, a.dim));
-        done += take;
-        left -= take;
-        cur.i += take - 1;
-        if (left > 0) cur.next<kWideTile>(a);
+        {
+            Progress x = s_at[slot];
+            Cursor cur;
+            cur.r = held(x.r);
+            cur.hh = held(x.hh);
+            cur.piece = held(x.piece);
+            cur.row = wave_row(a, cur.r);
+            cur.span = span_at<kWideTile>(a, cur.row, cur.piece);
+            const int32_t take = (int32_t)min(x.end - x.unit, (int64_t)(cur.span.tiles - x.i));
+            cur.i = held(x.i + take - 1);
+            x.unit += take;
+            if (x.unit >= x.end) return;
+            cur.template next<kWideTile>(a);
+            x.r = cur.r;
+            x.hh = cur.hh;
+            x.piece = cur.piece;
+            x.i = cur.i;
+            if (threadIdx.x == 0) s_at[slot ^ 1] = x;
+        }
+        __syncthreads();
     }
 }
 
@@ -1343,7 +1381,7 @@ template <int DP, int WAVES, int TEAMS> __global__ __launch_bounds__(64 * WAVES,
     if (!find_job(a, slots - 1 - blockIdx.x / each, &r, &piece)) return;
     const Row row = wave_row(a, r);
     if ((int64_t)piece * a.job_tokens >= row.tokens) return;
-    Wide<DP, WAVES, TEAMS> work(a, s);
+    Wide<DP, WAVES, TEAMS, false> work(a, s);
     work.begin(row, span_at<kWideTile>(a, row, piece), hh);
     work.run(0, work.span.tiles);
     work.write_out();
@@ -1421,6 +1459,12 @@ template <typename T> __global__ __launch_bounds__(kThreads) void k_tree_join(Tr
 }
 
 // Tiles a job has at most: its table's, or its window's and sinks'.
+// Workgroups for a job's columns: some thousands in all.
+unsigned join_columns(int64_t jobs, int32_t columns)
+{
+    return (unsigned)std::min<int64_t>(columns, std::max<int64_t>(16, 4096 / jobs));
+}
+
 template <int TILE> int64_t most_tiles(const TreeArgs& a)
 {
     const int64_t table = ((int64_t)a.width * a.page_size + TILE - 1) / TILE;
@@ -1444,7 +1488,7 @@ template <typename T, int DP, bool kWhole, int NQ> hipError_t tree_as(const Tree
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
     const int64_t all = (int64_t)a.rows * a.pieces * each;
-    hipLaunchKernelGGL(k_tree_join<T>, dim3((unsigned)std::min(all, kMaxGrid), (unsigned)std::min(a.columns, 16)), dim3(kThreads),
+    hipLaunchKernelGGL(k_tree_join<T>, dim3((unsigned)std::min(all, kMaxGrid), join_columns(all, a.columns)), dim3(kThreads),
                        0, s, a);
     return hipGetLastError();
 }
@@ -1469,7 +1513,7 @@ template <int DP, int WAVES, int TEAMS> hipError_t tree_wide(const TreeArgs& a, 
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
     const int64_t all = (int64_t)a.rows * a.pieces * each;
-    hipLaunchKernelGGL(k_tree_join<uint16_t>, dim3((unsigned)std::min(all, kMaxGrid), (unsigned)std::min(a.columns, 16)), dim3(kThreads), 0,
+    hipLaunchKernelGGL(k_tree_join<uint16_t>, dim3((unsigned)std::min(all, kMaxGrid), join_columns(all, a.columns)), dim3(kThreads), 0,
                        s, a);
     return hipGetLastError();
 }
