@@ -749,8 +749,9 @@ CPES_API size_t cpes_sample_workspace_bytes(int32_t rows, int32_t vocab);
  * token = the lowest v of those that stay with sum_{v' <= v} w_v' > u sum w, and
  * logp = ln(w_token / sum w), both sums over those that stay.  Weights and sums are in
  * 64 bits (of 37 bits and more; below 2^-52 of the largest one a weight counts as 0): a
- * token is off its place only where u is within their roundings of a border.  top_k = 1 takes the most likely token.  A u below 0 or NaN counts as 0, one
- * of 1 or more takes the last token that has a weight.
+ * token is off its place only where u is within their roundings of a border.  top_k = 1
+ * takes the most likely token.  A u below 0 or NaN counts as 0, one of 1 or more takes
+ * the last token that has a weight.
  * tokens_dev: device int64[rows]; logp_dev: NULL, or device float32[rows].
  * Logits of -inf are never chosen; a row of nothing but -inf has token -1 and logp
  * -inf, one with a NaN or +inf token -1 and logp NaN.

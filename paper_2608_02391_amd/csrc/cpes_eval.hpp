@@ -159,15 +159,15 @@ struct TreeArgs {
 
 // How jobs are cut, from what the host knows.
 struct TreeShape {
-    bool wide;                   // bf16 of up to 128 dims, more than 32 queries: through shared memory
+    bool wide;                   // more than 32 queries, up to 128 dims: through shared memory, where type and alignment let it
     int32_t sets, beside, columns, job_heads, blocks, job_tokens, pieces;
 };
 
-inline TreeShape tree_shape(bool bf16, int32_t longest, int32_t group, int32_t dim)
+inline TreeShape tree_shape(bool wide, int32_t longest, int32_t group, int32_t dim)
 {
     TreeShape t;
     const int64_t queries = (int64_t)longest * group;
-    t.wide = bf16 && dim <= 128 && queries > 32;
+    t.wide = wide && dim <= 128 && queries > 32;
     t.sets = queries <= 16 ? 1 : 2;                     // what fits a wave's registers
     t.beside = 1;
     while (t.beside < (t.wide ? 8 : 4) && 16 * t.sets * t.beside < queries) t.beside *= 2;

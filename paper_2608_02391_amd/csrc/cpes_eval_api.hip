@@ -590,9 +590,9 @@ size_t cpes_attend_tree_workspace_bytes(int32_t rows, int32_t tokens, int32_t lo
     if (rows < 0 || rows > CPES_MAX_SEQUENCES || tokens < 0 || (tokens > 0 && (longest < 1 || longest > tokens)) ||
         !check_heads(q_heads, kv_heads, head_dim))
         return 0;
-    size_t most = 0;             // either type's
-    for (bool bf16 : {false, true})
-        most = std::max(most, tree_bytes(rows, cpes::tree_shape(bf16, std::max(1, longest), q_heads / kv_heads, head_dim), kv_heads, head_dim));
+    size_t most = 0;             // either type's and alignment's
+    for (bool wide : {false, true})
+        most = std::max(most, tree_bytes(rows, cpes::tree_shape(wide, std::max(1, longest), q_heads / kv_heads, head_dim), kv_heads, head_dim));
     return most;
 }
 
@@ -614,12 +614,17 @@ int cpes_attend_tree(const cpes_cache* cache, int32_t layer, const cpes_pool* po
     if (!rc && tokens > 0 && parents_dev && longest > CPES_MAX_TREE)
         rc = fail(CPES_ERR_UNSUPPORTED, "%s: longest %d above CPES_MAX_TREE", fn, longest);
     if (rc) return rc;
-    const cpes::TreeShape shape = cpes::tree_shape(cache->dtype == CPES_BF16, std::max(1, longest), q_heads / cache->heads, cache->head_dim);
+    const char* const k = at_layer(cache, cache->k_dev, layer);
+    const char* const v = at_layer(cache, cache->v_dev, layer);
+    // straight into shared memory go 16 bytes that lie at a multiple of 16
+    const bool aligned = ((uintptr_t)k | (uintptr_t)v | (uintptr_t)((cache->page_stride | cache->head_stride | cache->token_stride) * 2)) % 16 == 0;
+    const cpes::TreeShape shape = cpes::tree_shape(cache->dtype == CPES_BF16 && aligned, std::max(1, longest), q_heads / cache->heads,
+                                                   cache->head_dim);
     rc = check_workspace(workspace_dev, workspace_bytes, tree_bytes(rows, shape, cache->heads, cache->head_dim), fn);
     if (rc || rows == 0 || tokens == 0) return rc;
     cpes::TreeArgs a;
-    a.k = at_layer(cache, cache->k_dev, layer);
-    a.v = at_layer(cache, cache->v_dev, layer);
+    a.k = k;
+    a.v = v;
     a.q = q_dev;
     a.out = out_dev;
     a.lse = lse_dev;

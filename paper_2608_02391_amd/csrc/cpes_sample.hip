@@ -10,21 +10,29 @@
 // Precision.  With V tokens there are V borders between 0 and 1, and sums that are off by
 // e put u on the wrong side of one with a probability of up to V e: 32-bit sums of
 // 151,936 logits would pick another token every few hundred rows.  Weights are
-// therefore 64-bit, of 40 bits and more (2^t from a table of 32 and a polynomial of degree 4),
-// and so are their sums, always taken in one order.
+// therefore 64-bit, right to 2^-37.5 (2^t from a table of 64 cells an octave and a short
+// polynomial), and so are their sums, always taken in one order.
 //
 // Split.  A row is cut into strips, one a wave, and these into blocks of 2^shift steps; a
 // step is four 16-byte vectors of each lane, in token order.  The one pass over the
-// logits leaves for each block its sum (where a sum over the whole row is needed: no
-// filter, or top_p of everything) and for each of its lanes the maximum of what it has
-// read.  What is behind that looks at little again:
+// logits (k_sample_read) leaves for each block its sum (where a sum over the whole row is
+// needed: no filter, or top_p of everything), and otherwise for each of its lanes the
+// maximum of what it has read, and one logit.  What is behind that (k_sample_join, a
+// workgroup a row) looks at little again:
 //   no filter:  the block in which u sum w lies, and in it the token;
 //   filters:    the tokens from a bound on that the lanes' maxima give: the k-th largest of
 //               them is reached by k tokens.  They are ranked, and what stays of them is known.
 //   Only where that is too much (flat rows, thousands of tokens in top_p) is the row read
-//   again, a few times: the bounding key is found by its digits, from histograms of weights.
-// A workgroup does a row; where there are few long rows, several read one, and a second
-// launch does the rest.
+//   again, a few times: the bounding key is found by its digits, from histograms of weights
+//   that begin where the logits that were noted put it.
+// Two launches, because they want other registers and other numbers of waves; rows of up to
+// four steps are one wave's, in one launch.
+//
+// What bounds it.  4,096 rows of 151,936 in bf16, 186 us of HBM: without a sum (top_k, min_p)
+// 263-274 us, the notes and the second launch's dozen dependent trips; with sums the vector
+// units, about 11 instructions a logit, 406 us; top_p of 0.95 where a seventh of the rows
+// is flat 1,045 us, of which reading those again takes most.  One row is two launches of
+// trips that wait for each other: 19-21 us, 49 where it is flat.
 #include <algorithm>
 #include <type_traits>
 
@@ -142,8 +150,8 @@ template <int K> __device__ __forceinline__ void fill_powers(double* powers)
 }
 
 // sum + 2^t for N exponents t = cells(j) / 64 + kLow.  The table's entries of the next four are asked for
-// before the last four are used: a wave waits for none of them (4,096 rows of 151,936: 385 us each on its
-// own, 345 so).
+// before the last four are used: a wave waits for none of them (the pass over 4,096 rows of 151,936: 385 us
+// with each asked for on its own, 345 so).
 template <int N, typename F> __device__ __forceinline__ double add_powers(double sum, const double* powers, F cells)
 {
     constexpr int G = 4;
@@ -175,7 +183,7 @@ template <int N, typename F> __device__ __forceinline__ double add_powers(double
 
 // The logits of a vector one after the other, so that a loop over them need not be unrolled: most
 // of what is behind the pass over the logits runs once a row, and what such code costs is its way
-// into the instruction cache (the whole of it unrolled: a row's rest in 27 us, so in 12).
+// into the instruction cache (one row's second launch: 27 us with all of it unrolled, 12 so).
 template <typename T> struct Logits {
     V4u w;
 

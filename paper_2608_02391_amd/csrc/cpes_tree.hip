@@ -8,18 +8,24 @@
 // reaches, and of the new ones its ancestors and itself: a bit each, found by walking up
 // the parents once.
 //
-// Tiles.  A wave takes 32 positions (16 in fp32) at a time and up to four sets of 16
-// queries, which all use the keys and values that it holds in registers in the layout of
-// cpes_attend.hpp: S^T = K Q^T leaves the weights where O^T = V^T P^T wants them.  So a
-// position costs one load whatever the number of queries, up to 64 a wave; with more, up to
-// four waves of a workgroup take the same positions and other queries, and the first one's
-// loads leave the others' in the caches.  The weights of a bf16 cache go in as a bf16 value
-// and its remainder, as there.
+// Tiles.  A wave takes 32 positions (16 in fp32) at a time and one or two sets of 16
+// queries, which use the keys and values that it holds in registers in the layout of
+// cpes_attend.hpp: S^T = K Q^T leaves the weights where O^T = V^T P^T wants them.  With more
+// queries up to four waves of a workgroup take the same positions and other queries, and
+// the first one's loads leave the others' in the caches.  Four sets a wave spilled (fp32, 32
+// nodes on 8,000 tokens: 2,512 us, 510 so).  Above 32 queries a bf16 cache goes through
+// shared memory (below, "many queries").  The weights of a bf16 cache go in as a bf16 value
+// and its remainder, as there: a bf16 weight alone is off by 2^-9, which the outputs of long
+// contexts would show.
 //
 // What a tile's queries see differs only where the new tokens are and at the edges of
 // windows.  Such tiles mask scores per query.  A value that one query sees and another does
 // not may be infinite or NaN, and 0 times it is not 0: where that is so, those positions
 // are left out of the matrix products and added by themselves.
+//
+// Work.  Either a workgroup does a job (the queries of a row's piece and KV head that go
+// together), or the jobs' tiles are laid in a line, cut into as many shares as workgroups are
+// resident, and what lies in several shares is joined by a second launch.
 #include <algorithm>
 #include <type_traits>
 
@@ -779,12 +785,25 @@ __global__ __launch_bounds__(kThreads, DP == 256 || NQ > 1 ? 1 : 2) void k_tree_
 }
 
 // ------------------------------------------------------------ many queries --
-// bf16, more than 32 queries a job: the workgroup's waves share a tile of 64 positions in
-// shared memory, 32 queries a wave, on the 32 x 32 matrix instruction.  With 64 queries two
-// waves take half of the tile each for the same queries and join at the end; with 128 every
-// wave takes all of it.  A key and a value are read from memory once for up to 128
-// queries, the next tile's are on their way in registers while one is worked on, and two
-// workgroups a CU let one's softmax run beside the other's products.
+// bf16, more than 32 queries a job: the workgroup's waves share tiles of 64 positions in
+// shared memory, 32 queries a wave, on the 32 x 32 matrix instruction.  A key and a value
+// are read from memory once for up to 256 queries: eight waves, a workgroup a CU.  Up to 128
+// queries four waves, two workgroups a CU; up to 64 of them two waves take a half of each
+// tile for the same queries, and join at the end.
+//
+// The next tile goes straight into the other buffer while one is folded (through registers
+// it took 32 of them, and as many instructions as the softmax).  A wave folds both halves of
+// a tile together: their products interleave, one base serves both, and one's weights are
+// taken beside the other's products (prompts 712 -> 656 us).  The values come out of shared
+// memory turned, four positions of a dim to a lane, so no lane sorts them (109 -> 87 us for
+// ragged trees of 12, with the next two).  The base of the weights moves only when it is 2^4
+// behind, which in most tiles it is not, and saves scaling the outputs.
+//
+// Bound: 24 products of 32 clocks and about 150 vector instructions of 4 a wave and half a
+// tile; a SIMD's two waves overlap them in part (matrix units 40 % busy, vector units 45 %).
+// 8 prompts of up to 4,095 tokens, 32 heads on 8 of 128: 656 us, 544 TFLOP/s of the scores' and
+// outputs' products, 820 with the remainders'.  4 rows of 65 - 131 thousand tokens with up to 64
+// nodes: 660 us, 2.4 TB/s and 430 TFLOP/s.
 typedef float V16f __attribute__((ext_vector_type(16)));
 typedef float V2f __attribute__((ext_vector_type(2)));
 typedef __bf16 V2bf __attribute__((ext_vector_type(2)));
@@ -793,7 +812,7 @@ typedef short V4s __attribute__((ext_vector_type(4)));
 constexpr int kWideTile = 64;
 constexpr int kWideShare = 4;             // tiles of a workgroup's share at least
 constexpr int kWideColumns = 32;          // of a wave
-constexpr float kAhead = 4.f;
+constexpr float kAhead = 4.f;             // powers of 2 that a weight may be above 1, and that the outputs' range is short of
 
 template <int DP, int WAVES> struct WideShared {
     // Rows in pieces of 16 bytes.  32 lanes read one piece each of as many keys, or 4 positions' values of 16 dims
@@ -881,7 +900,7 @@ template <int DP, int WAVES, int TEAMS, bool kLean> struct Wide {
             if (d >= a.dim || !valid) q[e] = V4u{0, 0, 0, 0};
             if (a.scale < 0.f) q[e] ^= 0x80008000u;       // of -q with -scale
         }
-        unit = fmaxf(fabsf(a.scale) * kLog2e, 1e-37f);    // -inf stays below all scores
+        unit = fmaxf(fabsf(a.scale) * kLog2e, 1.2e-38f);  // of 0: -inf stays below all scores, and others are as good as equal
         every_high = row.base < 0 ? 0 : tree ? row.base : row.base + span.from + 1;
         every_low = 0;
         if (a.window > 0 && row.base >= 0)

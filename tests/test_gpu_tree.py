@@ -314,6 +314,23 @@ def test_strides_alignment_and_order():
     assert torch.equal(again, out)
 
 
+@pytest.mark.parametrize("dim,extra,first", [(64, 1, 1), (128, 4, 0), (128, 8, 4), (72, 0, 8)])
+def test_caches_at_any_alignment(dim, extra, first):
+    """Keys and values whose rows, or whose first element, do not lie at multiples of 16 bytes."""
+    print(f"tree cache dim={dim} rows {extra} apart, first at {first}", flush=True)
+    for sizes in ([5, 8], [20, 13], [60, 33]):
+        c = Trees([50, 300], sizes, dim=dim, seed=dim + extra)
+        q = c.queries(8)
+        for name in ("k", "v"):
+            t = getattr(c, name)
+            room = torch.full((t.numel() // dim * (dim + extra) + first + dim,), math.nan, dtype=BF16, device="cuda")
+            moved = room[first:first + t.numel() // dim * (dim + extra)].view(*t.shape[:-1], dim + extra)[..., :dim]
+            moved.copy_(t)
+            setattr(c, name, moved)
+        c.bind()
+        c.check(q, *c.run(q))
+
+
 def test_captured_step_follows_lengths_and_trees():
     """A captured call reads lengths, starts and parents when it is replayed."""
     c = Trees([30, 2500], [9, 24], seed=17)
