@@ -1525,7 +1525,10 @@ template <typename T, int DP, bool kWhole, int NQ> hipError_t tree_as(const Tree
     // as many as find_job counts
     const int64_t jobs = ((int64_t)a.tokens / a.job_tokens + a.rows) * each;
     const int64_t most = most_tiles<Tile<T>::n>(a);
-    if ((jobs >= 1024 || most <= 32) && jobs <= INT32_MAX / kThreads) {
+    // Measured with a workgroup a job and with shares, trees of 5: one row of 500 tokens 19 and 25 us, of 1,000 25 and
+    // 25, of 2,000 38 and 30; 32 rows of 4,000 136 and 122, 64 of 8,000 421 and 402, 128 of 4,000 407 and 424, 256 of
+    // 100 - 8,000 499 and 524.  Prompts in fp32, 4 of 1,000 201 and 222, 8 of 2,000 517 and 763.
+    if ((jobs >= (a.parents ? 1024 : 512) || most <= 32) && jobs <= INT32_MAX / kThreads) {
         hipLaunchKernelGGL((k_tree_jobs<T, DP, kWhole, NQ>), dim3((unsigned)jobs), dim3(kThreads), 0, s, a);
         return hipGetLastError();
     }
@@ -1550,7 +1553,11 @@ template <int DP, int WAVES, int TEAMS> hipError_t tree_wide(const TreeArgs& a, 
 {
     const int32_t each = a.heads * a.blocks;
     const int64_t jobs = ((int64_t)a.tokens / a.job_tokens + a.rows) * each, most = most_tiles<kWideTile>(a);
-    if ((jobs >= 1024 || most <= 16) && jobs <= INT32_MAX / (64 * WAVES)) {
+    // Shares balance rows of any length, but each pays for its beginning and the join.  Measured with a workgroup a job
+    // and with shares: one prompt of 512 tokens 32 and 59 us, of 2,048 97 and 138, of 8,000 (1,000 jobs) 842 and
+    // 1,013; trees of 24 on 32 rows of up to 1,000 49 and 59, of 4,000 (256 jobs) 164 and 129, on 64 rows 246 and
+    // 238, on 128 426 and 430.  A prompt's many jobs are of all lengths, the longest first; a tree's job is a row.
+    if ((jobs >= (a.parents ? 4 : 2) * (int64_t)a.groups || most <= 32) && jobs <= INT32_MAX / (64 * WAVES)) {
         hipLaunchKernelGGL((k_tree_wide_jobs<DP, WAVES, TEAMS>), dim3((unsigned)jobs), dim3(64 * WAVES), 0, s, a);
         return hipGetLastError();
     }

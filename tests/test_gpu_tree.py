@@ -176,6 +176,22 @@ def test_prompts(dtype, dim, group):
     c.check(q, out, lse, skip={(r, i) for r in range(4) for i in range(c.sizes[r]) if i % 61 and i != c.sizes[r] - 1})
 
 
+@pytest.mark.parametrize("dim", [64, 128])
+@pytest.mark.parametrize("nodes", [10, 25, 50, 75])
+@pytest.mark.parametrize("chain", [False, True], ids=["tree", "chain"])
+def test_many_queries_over_long_contexts(dim, nodes, chain):
+    """40 to 300 queries a KV head, on contexts that several workgroups share; rows with fewer, and a window."""
+    print(f"tree shares dim={dim} nodes={nodes} chain={chain}", flush=True)
+    for window, sinks in ((0, 0), (2500, 70)):
+        c = Trees([5000, 40, 2911], [nodes, nodes // 3, 1 + nodes // 2], dim=dim, chain=chain, window=window, sinks=sinks, seed=nodes)
+        q = c.queries(8)
+        out, lse = c.run(q)
+        skip = {(r, i) for r in range(3) for i in range(c.sizes[r]) if i % 7 and i != c.sizes[r] - 1}
+        c.check(q, out, lse, skip=skip)
+        again, again_lse = c.run(q)
+        assert torch.equal(again, out) and torch.equal(again_lse, lse)
+
+
 def test_one_new_token_is_the_decode_attention():
     """Trees of one token: the same positions as cpes_attend, the same bounds; and a chain in two calls is one call's."""
     c = Trees([0, 40, 333, 2000], [1, 1, 1, 1], dim=128, seed=3)
