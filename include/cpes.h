@@ -649,6 +649,8 @@ CPES_API size_t cpes_attend_tree_workspace_bytes(int32_t rows, int32_t tokens, i
  * and rows behind one whose starts fall may be; what no row covers is left as it was.  The result of a token does not
  * depend on the contents of positions it does not see (other branches, too), nor on the
  * run.
+ * Any alignment of the cache will do; more than 32 queries of a row and KV head are
+ * fastest where its keys and values, and their strides, lie at multiples of 16 bytes.
  * workspace: as cpes_attend_tree_workspace_bytes, 16-byte aligned; needs no
  * particular contents, and calls that overlap in time need their own.
  * Errors: as cpes_attend; tokens < 0, longest outside [1, tokens] with tokens > 0 ->
