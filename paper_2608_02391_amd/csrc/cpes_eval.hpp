@@ -168,7 +168,7 @@ inline TreeShape tree_shape(bool wide, int32_t longest, int32_t group, int32_t d
     TreeShape t;
     const int64_t queries = (int64_t)longest * group;
     t.wide = wide && dim <= 128 && queries > 32;
-    t.sets = queries <= 16 ? 1 : 2;                     // what fits a wave's registers
+    t.sets = queries <= 16 || dim > 128 ? 1 : 2;        // what fits a wave's registers
     t.beside = 1;
     while (t.beside < (t.wide ? 8 : 4) && 16 * t.sets * t.beside < queries) t.beside *= 2;
     t.columns = 16 * t.sets * t.beside;

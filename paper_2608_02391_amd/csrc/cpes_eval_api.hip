@@ -211,7 +211,7 @@ int check_attend(const cpes_cache* cache, int32_t layer, const cpes_pool* pool, 
     return rc;
 }
 
-// Workgroups of the shares of trees: two per CU, one where a wave's state fills its SIMD's registers.
+// Workgroups of the shares of trees: two per CU, one of eight waves or where a wave's state fills its SIMD's registers.
 int tree_groups(const cpes::TreeShape& t, int32_t head_dim)
 {
     return t.beside <= 4 && (t.wide || (head_dim <= 128 && t.sets == 1)) ? 512 : 256;

@@ -13,7 +13,8 @@
 // cpes_attend.hpp: S^T = K Q^T leaves the weights where O^T = V^T P^T wants them.  With more
 // queries up to four waves of a workgroup take the same positions and other queries, and
 // the first one's loads leave the others' in the caches.  Four sets a wave spilled (fp32, 32
-// nodes on 8,000 tokens: 2,512 us, 510 so).  Above 32 queries a bf16 cache goes through
+// nodes on 8,000 tokens: 2,512 us, 510 so), and above 128 dims two (16 nodes of 256 in fp32:
+// 2,520 us, 520 with one).  Above 32 queries a bf16 cache goes through
 // shared memory (below, "many queries").  The weights of a bf16 cache go in as a bf16 value
 // and its remainder, as there: a bf16 weight alone is off by 2^-9, which the outputs of long
 // contexts would show.
@@ -1543,10 +1544,9 @@ template <typename T, int DP, bool kWhole, int NQ> hipError_t tree_as(const Tree
 
 template <typename T, int DP, bool kWhole> hipError_t tree_sets(const TreeArgs& a, hipStream_t s)
 {
-    if (a.sets == 1) return tree_as<T, DP, kWhole, 1>(a, s);
-    if constexpr (DP == 256) return tree_as<T, DP, kWhole, 2>(a, s);
-    else if constexpr (std::is_same<T, uint16_t>::value) return tree_as<T, DP, kWhole, 2>(a, s);
-    else return tree_as<T, DP, kWhole, 2>(a, s);
+    if constexpr (DP < 256)
+        if (a.sets == 2) return tree_as<T, DP, kWhole, 2>(a, s);
+    return tree_as<T, DP, kWhole, 1>(a, s);
 }
 
 template <int DP, int WAVES, int TEAMS> hipError_t tree_wide(const TreeArgs& a, hipStream_t s)
