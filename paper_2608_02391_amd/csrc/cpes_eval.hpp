@@ -163,12 +163,12 @@ struct TreeShape {
     int32_t sets, beside, columns, job_heads, blocks, job_tokens, pieces;
 };
 
-inline TreeShape tree_shape(bool wide, int32_t longest, int32_t group, int32_t dim)
+inline TreeShape tree_shape(bool bf16, bool aligned, int32_t longest, int32_t group, int32_t dim)
 {
     TreeShape t;
     const int64_t queries = (int64_t)longest * group;
-    t.wide = wide && dim <= 128 && queries > 32;
-    t.sets = queries <= 16 || dim > 128 ? 1 : 2;        // what fits a wave's registers
+    t.wide = bf16 && aligned && dim <= 128 && queries > 32;
+    t.sets = bf16 && dim <= 128 && queries > 16 ? 2 : 1;        // what fits a wave's registers
     t.beside = 1;
     while (t.beside < (t.wide ? 8 : 4) && 16 * t.sets * t.beside < queries) t.beside *= 2;
     t.columns = 16 * t.sets * t.beside;

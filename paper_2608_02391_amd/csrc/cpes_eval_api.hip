@@ -591,8 +591,8 @@ size_t cpes_attend_tree_workspace_bytes(int32_t rows, int32_t tokens, int32_t lo
         !check_heads(q_heads, kv_heads, head_dim))
         return 0;
     size_t most = 0;             // either type's and alignment's
-    for (bool wide : {false, true})
-        most = std::max(most, tree_bytes(rows, cpes::tree_shape(wide, std::max(1, longest), q_heads / kv_heads, head_dim), kv_heads, head_dim));
+    for (int way = 0; way < 3; ++way)
+        most = std::max(most, tree_bytes(rows, cpes::tree_shape(way > 0, way > 1, std::max(1, longest), q_heads / kv_heads, head_dim), kv_heads, head_dim));
     return most;
 }
 
@@ -618,7 +618,7 @@ int cpes_attend_tree(const cpes_cache* cache, int32_t layer, const cpes_pool* po
     const char* const v = at_layer(cache, cache->v_dev, layer);
     // straight into shared memory go 16 bytes that lie at a multiple of 16
     const bool aligned = ((uintptr_t)k | (uintptr_t)v | (uintptr_t)((cache->page_stride | cache->head_stride | cache->token_stride) * 2)) % 16 == 0;
-    const cpes::TreeShape shape = cpes::tree_shape(cache->dtype == CPES_BF16 && aligned, std::max(1, longest), q_heads / cache->heads,
+    const cpes::TreeShape shape = cpes::tree_shape(cache->dtype == CPES_BF16, aligned, std::max(1, longest), q_heads / cache->heads,
                                                    cache->head_dim);
     rc = check_workspace(workspace_dev, workspace_bytes, tree_bytes(rows, shape, cache->heads, cache->head_dim), fn);
     if (rc || rows == 0 || tokens == 0) return rc;

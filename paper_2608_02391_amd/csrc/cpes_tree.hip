@@ -12,12 +12,13 @@
 // queries, which use the keys and values that it holds in registers in the layout of
 // cpes_attend.hpp: S^T = K Q^T leaves the weights where O^T = V^T P^T wants them.  With more
 // queries up to four waves of a workgroup take the same positions and other queries, and
-// the first one's loads leave the others' in the caches.  Four sets a wave spilled (fp32, 32
-// nodes on 8,000 tokens: 2,512 us, 510 so), and above 128 dims two (16 nodes of 256 in fp32:
-// 2,520 us, 520 with one).  Above 32 queries a bf16 cache goes through
-// shared memory (below, "many queries").  The weights of a bf16 cache go in as a bf16 value
-// and its remainder, as there: a bf16 weight alone is off by 2^-9, which the outputs of long
-// contexts would show.
+// the first one's loads leave the others' in the caches.  Two sets are for bf16 up to 128 dims
+// (8 nodes on 64 rows of 8,000: 440 us, 476 with one).  In fp32 they leave room for one wave a
+// SIMD (32 nodes on 8 rows of 8,000: 505 us, 391 with one), and above 128 dims they spill (16
+// nodes of 256 in bf16 340 us and 215, in fp32 2,520 and 510).  Above 32 queries a bf16 cache
+// goes through shared memory (below, "many queries").  The weights of a bf16 cache go in as a
+// bf16 value and its remainder, as there: a bf16 weight alone is off by 2^-9, which the
+// outputs of long contexts would show.
 //
 // What a tile's queries see differs only where the new tokens are and at the edges of
 // windows.  Such tiles mask scores per query.  A value that one query sees and another does
@@ -1528,7 +1529,8 @@ template <typename T, int DP, bool kWhole, int NQ> hipError_t tree_as(const Tree
     const int64_t most = most_tiles<Tile<T>::n>(a);
     // Measured with a workgroup a job and with shares, trees of 5: one row of 500 tokens 19 and 25 us, of 1,000 25 and
     // 25, of 2,000 38 and 30; 32 rows of 4,000 136 and 122, 64 of 8,000 421 and 402, 128 of 4,000 407 and 424, 256 of
-    // 100 - 8,000 499 and 524.  Prompts in fp32, 4 of 1,000 201 and 222, 8 of 2,000 517 and 763.
+    // 100 - 8,000 499 and 524.  Prompts in fp32 (with two sets), 4 of 1,000 201 and 222, 8 of 2,000 517
+    // and 763.
     if ((jobs >= (a.parents ? 1024 : 512) || most <= 32) && jobs <= INT32_MAX / kThreads) {
         hipLaunchKernelGGL((k_tree_jobs<T, DP, kWhole, NQ>), dim3((unsigned)jobs), dim3(kThreads), 0, s, a);
         return hipGetLastError();
@@ -1544,7 +1546,7 @@ template <typename T, int DP, bool kWhole, int NQ> hipError_t tree_as(const Tree
 
 template <typename T, int DP, bool kWhole> hipError_t tree_sets(const TreeArgs& a, hipStream_t s)
 {
-    if constexpr (DP < 256)
+    if constexpr (std::is_same<T, uint16_t>::value && DP < 256)
         if (a.sets == 2) return tree_as<T, DP, kWhole, 2>(a, s);
     return tree_as<T, DP, kWhole, 1>(a, s);
 }
