@@ -37,6 +37,7 @@
 #include <type_traits>
 
 #include "cpes_eval.hpp"
+#include "cpes_powers.hpp"
 
 namespace cpes {
 
@@ -57,7 +58,6 @@ constexpr int kFewRows = 256;
 constexpr int kManyBlocks = 96;          // of a row among many
 constexpr int kManyParts = 32;           // and parts, of 64 lanes
 constexpr int kReadGroups = 1024;        // workgroups that read few rows
-constexpr double kExact = 2048.0;         // c x up to which the rounding of c max x, 2^-42, is let through
 constexpr double kFar = -52.0;           // weights below 2^kFar of the largest count as 0
 
 template <typename T> struct Vec { static constexpr int n = 16 / sizeof(T); };
@@ -139,9 +139,7 @@ __device__ __forceinline__ double power(double t, const double* table)
 // 1/64 octave from kLow on, whose beginnings are in a table that leaves no exponent to be put
 // together; in a cell 2^(r / 64) = 1 + a1 r + a2 r^2 + a3 r^3, r < 1, off by 2^-37.5 at most (a minimax
 // fit that is exact at 0).  The conversion takes what is below the table, -inf too, to its first entry,
-// which is 0, and the fraction's clamp takes -inf's NaN to 0.
-constexpr int kLow = -56, kRoom = 7, kCells = 64;
-constexpr int kPowers = (kRoom + 1 - kLow) * kCells;
+// which is 0, and the fraction's clamp takes -inf's NaN to 0.  What is above the table must not come here.
 
 template <int K> __device__ __forceinline__ void fill_powers(double* powers)
 {
@@ -309,9 +307,8 @@ __device__ float read_strip(const SampleArgs& a, const T* x0, int32_t strip, con
     const int32_t per = 1 << a.shift, per_part = 1 << a.note_shift;
     Notes note = {}, sample = {};
     const int32_t whole = (int32_t)max((int64_t)0, min((int64_t)s.steps, ((int64_t)a.vocab / N - s.first) / (kSampleLanes * kUnroll)));
-    float most = -__builtin_inff(), ref = -__builtin_inff(), noted = -__builtin_inff();
-    double sum = 0.0, base = 0.0;
-    const float room = (float)fmin(kRoom / a.c, 1e38);
+    float most = -__builtin_inff(), ref = -__builtin_inff(), last = -__builtin_inff(), noted = -__builtin_inff();
+    double sum = 0.0, start = 0.0;
     const double cells = a.c * kCells;
     V4u w[kUnroll];
     auto load = [&](int32_t step, int u) {
@@ -319,24 +316,29 @@ __device__ float read_strip(const SampleArgs& a, const T* x0, int32_t strip, con
             reinterpret_cast<const V4uAnywhere*>(x0 + (s.first + (int64_t)step * (kSampleLanes * kUnroll) + u * kSampleLanes + lane) * N);
         w[u] = NT ? __builtin_nontemporal_load(at) : *at;
     };
-    // the N logits of a vector
-    auto take = [&](const float* x) {
+    // the N logits of a vector, which may be changed
+    auto take = [&](float* x) {
         float top = x[0];
 #pragma unroll
         for (int j = 1; j < N; ++j) top = most_of(top, x[j]);
         noted = most_of(noted, top);
         if constexpr (kSums) {
-            if (__any(top > ref + room)) {
-                // a new base for all lanes; the block's sum so far moves to it
-                float high = top > -__builtin_inff() ? top : -__builtin_inff();
+            if (__any(!(top <= last))) {
+                // a new base for all lanes; the block's sum so far moves to it.  With a NaN or +inf the row has no
+                // token, and no logit beside it may reach the table's end: they count as nothing
+                const bool broken = !(top < __builtin_inff());
+                float high = broken ? -__builtin_inff() : top;
 #pragma unroll
                 for (int d = 1; d < 64; d <<= 1) high = fmaxf(high, __shfl_xor(high, d));
-                if (high < __builtin_inff()) {
+                if (high > last) {
                     const double t = a.c * ((double)ref - (double)high);
                     sum = t < 2 * kLow ? 0.0 : sum * power(t, table);
                     ref = high;
-                    base = cells * (double)ref + kLow * kCells;
+                    last = last_above(ref, a.c);
+                    start = start_of(ref, cells);
                 }
+#pragma unroll
+                for (int j = 0; j < N; ++j) x[j] = broken ? -__builtin_inff() : x[j];
             }
             auto add = [&](auto t) {
                 if constexpr (kQuick) {
@@ -347,10 +349,10 @@ __device__ float read_strip(const SampleArgs& a, const T* x0, int32_t strip, con
                         if (t(j) > 0.0) sum += power(t(j) / kCells + kLow, table);
                 }
             };
-            if (fabs(base) <= kExact * kCells) {
-                if (ref > -__builtin_inff()) add([&](int j) { return fma((double)x[j], cells, -base); });
+            if (start_is_near(start)) {
+                if (ref > -__builtin_inff()) add([&](int j) { return cells_near(x[j], cells, start); });
             } else {
-                add([&](int j) { return ((double)x[j] - (double)ref) * cells - kLow * kCells; });
+                add([&](int j) { return cells_far(x[j], ref, cells); });
             }
         }
     };

@@ -125,6 +125,43 @@ def test_values_close_together():
             check(x, u, **f)
 
 
+@pytest.mark.parametrize("scale", [1e5, 1e6, 1e7])
+@pytest.mark.parametrize("rows,vocab", [(48, 5000), (48, 40000), (300, 40000)])
+def test_neighbours_that_are_octaves_apart(rows, vocab, scale):
+    """fp32 logits a few steps of the type above those before them, which at a low temperature is octaves: the likelier
+    ones come later in the row, in the same step of a wave, in the next and much later."""
+    print(f"sample neighbours {rows}x{vocab} scale={scale}", flush=True)
+    g = torch.Generator().manual_seed(rows + vocab)
+    x = torch.randn(rows, vocab, generator=g)
+    for r in range(rows):
+        base = np.float32([10.0, 20.0, 31.0, 100.0, 600.0, -12.0, -100.0, 1000.0][r % 8])
+        for place, ulps in ((5, 0), (300, 1 + r // 8 % 3), (1100, 2 + r // 8 % 5), (4500, 1 + r // 8)):
+            y = base
+            for _ in range(ulps):
+                y = np.nextafter(y, np.float32(math.inf))
+            x[r, place] = float(y)
+        if base < 0:
+            x[r][x[r] > -10.0] = 2.0 * float(base)
+    x, u = x.cuda(), torch.rand(rows, generator=g).cuda()
+    for f in (dict(), dict(top_p=0.9), dict(top_p=0.9999), dict(top_k=3), dict(min_p=0.01)):
+        check(x, u, rows=range(min(rows, 48)), scale=scale, **f)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32], ids=["bf16", "fp32"])
+@pytest.mark.parametrize("rows", [12, 300])
+def test_infinite_logits_behind_a_finite_base(rows, dtype):
+    """A +inf, and one beside a NaN, long after the weights' base was found; the rows around are drawn as ever."""
+    x, u = logits(rows, 40000, dtype, seed=13)
+    x[1, 39000] = math.inf
+    x[2, 30000], x[2, 30001] = math.nan, math.inf
+    x[3, 30000], x[3, 30001] = math.inf, math.nan
+    x[4, 700:] = math.inf
+    x[5, 20000] = math.nan
+    for f in (dict(), dict(top_p=0.9), dict(top_p=0.95, scale=0.2), dict(scale=1e6)):
+        token, logp = check(x, u, rows=range(12), **f)
+        assert token[1:6].tolist() == [-1] * 5 and bool(torch.isnan(logp[1:6]).all())
+
+
 @pytest.mark.parametrize("dtype", [BF16, F32], ids=["bf16", "fp32"])
 @pytest.mark.parametrize("rows", [12, 300])
 def test_masks_and_broken_rows(dtype, rows):
