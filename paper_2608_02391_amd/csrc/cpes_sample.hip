@@ -585,8 +585,9 @@ template <typename T, typename S, int K> struct RowWork {
     {
         double x = 0.0, total;
         if (tid < blocks && s.sums[tid] > 0.0) {
+            // a block's largest weight may be above what its sum is relative to
             const double t = a.c * ((double)s.refs[tid] - (double)m);
-            if (t >= kFar) x = s.sums[tid] * power(t, s.table);
+            if (t >= kFar - (kRoom + 1)) x = s.sums[tid] * power(t, s.table);
         }
         const double upto = block_scan<K>(x, s.wave, &total);
         __syncthreads();
@@ -615,13 +616,19 @@ template <typename T, typename S, int K> struct RowWork {
             __syncthreads();
         }
         const double before = b ? s.sums[b - 1] : 0.0;
-        locate(block_begin(b), b + 1 < blocks ? block_begin(b + 1) : (int64_t)a.vocab, target - before, cut, cut.order ? s.ties[b] : 0);
+        const int64_t end = b + 1 < blocks ? block_begin(b + 1) : (int64_t)a.vocab;
+        locate(block_begin(b), end, target - before, cut, cut.order ? s.ties[b] : 0);
         __syncthreads();
-        // weights at the edge of what counts as 0 made that block: the first token that has one
+        // weights that count as 0 made that block's sum: the next token that has one, or else the last
         if (s.token < 0) {
             __syncthreads();
-            locate(0, a.vocab, 0.0, cut, 0);
+            locate(end, a.vocab, 0.0, cut, cut.order && b + 1 < blocks ? s.ties[b + 1] : 0);
             __syncthreads();
+            if (s.token < 0) {
+                __syncthreads();
+                locate(0, end, __builtin_inf(), cut, 0);
+                __syncthreads();
+            }
         }
     }
 

@@ -207,6 +207,37 @@ def test_ends_of_the_uniform_numbers(filters):
             assert int(token.min()) >= 2200 and int(token.max()) < 8000
 
 
+@pytest.mark.parametrize("dtype", [BF16, F32], ids=["bf16", "fp32"])
+@pytest.mark.parametrize("rows", [5, 300])
+def test_weights_at_the_edge_of_what_counts(rows, dtype):
+    """Weights between 2^-56 and 2^-52 of the largest count as 0: where the number given ends among them, a token on
+    either side is drawn, or the last; one of 2^-47 beside them is not lost."""
+    print(f"sample edge rows={rows} {dtype}", flush=True)
+    octave = math.log(2.0)
+
+    def token_of(x, u):
+        out, _ = run(x.to(dtype).repeat(rows, 1).cuda(), torch.full((rows,), u, device="cuda"))
+        assert bool((out == out[0]).all())
+        return int(out[0])
+
+    for vocab in (3500, 40000, 100000):
+        # nothing that counts lies between two pairs of the largest: half of the weight is in front of it
+        x = torch.full((1, vocab), -54.0 * octave)
+        x[0, 5] = x[0, 40] = x[0, vocab - 300] = x[0, vocab - 100] = 0.0
+        assert token_of(x, 0.5) in (40, vocab - 300)
+        assert token_of(x, 0.25) in (5, 40) and token_of(x, 0.75) in (vocab - 300, vocab - 100)
+        # nor behind the last of them
+        assert token_of(x, 1.0) == vocab - 100
+        x[0, vocab - 300] = x[0, vocab - 100] = -54.0 * octave
+        assert token_of(x, 1.0) == 40
+        # the first token that counts stands behind others within 7 octaves that do not
+        x = torch.full((1, vocab), -53.0 * octave)
+        x[0, 2100] = -47.0 * octave
+        x[0, vocab - 1] = 0.0
+        assert token_of(x, 0.0) == 2100
+        assert token_of(x, 2.0 ** -40) == vocab - 1
+
+
 @pytest.mark.parametrize("scale", [1e-30, 1e-6, 0.01, 30.0, 1e4, 1e20, 1.7e38])
 @pytest.mark.parametrize("dtype", [BF16, F32], ids=["bf16", "fp32"])
 def test_scales(scale, dtype):
