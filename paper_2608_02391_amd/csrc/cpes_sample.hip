@@ -597,7 +597,8 @@ template <typename T, typename S, int K> struct RowWork {
     }
 
     // From the blocks' sums up to each the token; s.ties holds the ties before each block where there is a cut.
-    __device__ void pick(double total, Cut cut)
+    // Inlined, because a call kept 240 bytes of its caller's state a lane in scratch where one wave does a row.
+    __device__ __forceinline__ void pick(double total, Cut cut)
     {
         const double target = uniform() * total;
         if (tid == 0) s.place = blocks;
@@ -615,19 +616,26 @@ template <typename T, typename S, int K> struct RowWork {
             b = s.place;
             __syncthreads();
         }
-        const double before = b ? s.sums[b - 1] : 0.0;
-        const int64_t end = b + 1 < blocks ? block_begin(b + 1) : (int64_t)a.vocab;
-        locate(block_begin(b), end, target - before, cut, cut.order ? s.ties[b] : 0);
-        __syncthreads();
-        // weights that count as 0 made that block's sum: the next token that has one, or else the last
-        if (s.token < 0) {
+        int64_t from = block_begin(b), to = b + 1 < blocks ? block_begin(b + 1) : (int64_t)a.vocab;
+        double rest = target - (b ? s.sums[b - 1] : 0.0);
+        int32_t ties = cut.order ? s.ties[b] : 0;
+#pragma unroll 1
+        for (int turn = 0;; ++turn) {
+            locate(from, to, rest, cut, ties);
             __syncthreads();
-            locate(end, a.vocab, 0.0, cut, cut.order && b + 1 < blocks ? s.ties[b + 1] : 0);
+            if (s.token >= 0 || turn == 2) break;
             __syncthreads();
-            if (s.token < 0) {
-                __syncthreads();
-                locate(0, end, __builtin_inf(), cut, 0);
-                __syncthreads();
+            // weights that count as 0 made that block's sum: the next token that has one, or else the last
+            if (turn == 0) {
+                from = to;
+                to = a.vocab;
+                rest = 0.0;
+                ties = cut.order && b + 1 < blocks ? s.ties[b + 1] : 0;
+            } else {
+                to = from;
+                from = 0;
+                rest = __builtin_inf();
+                ties = 0;
             }
         }
     }
@@ -876,31 +884,47 @@ template <typename T, typename S, int K> struct RowWork {
 
     // The cut that leaves the first `number` of the order (by_weight: as many as it takes to
     // reach `enough`), found by reading the row again: a histogram of what lies in [lo, hi] of
-    // the orders, and of the bin it ends in again, until that is one order.  Where it does
-    // not end in [lo, hi], everything is looked at.  *weight receives the weight that is left.
-    __device__ Cut search(uint32_t lo, uint32_t hi, int64_t number, double enough, bool by_weight, double* weight_left)
+    // the orders, and of the bin it ends in again, until that is one order.  Weights in bins of
+    // several orders are whole numbers, each off by up to half of 2^-44 of the heaviest, and 150,000 alike are off
+    // alike.  Where that could decide, what lies above is summed again in 64 bits (`exact`: from the beginning,
+    // for a caller who needs the weight): this says for certain whether the cut is in [lo, hi], and if not, the
+    // orders on that side are looked at.  (Summed again in every round, 256 flat rows took 285 us, 257 so.)
+    // *weight_left receives the weight that is left.
+    __device__ Cut search(uint32_t lo, uint32_t hi, int64_t number, double enough, bool by_weight, bool exact, double* weight_left)
     {
-        constexpr uint32_t kFirst = 0x00800000, kLast = 0xFF7FFFFF;            // finite numbers
+        constexpr uint32_t kFirst = 0x00800000;      // of finite numbers
         // bf16 logits have 16 bits of order, and a bin may be one of them, whose weight is its number of times one weight
         constexpr int kLeast = std::is_same<T, uint16_t>::value ? 16 : 0;
         const auto logit = [](uint32_t o) { return value_at(kLeast > 0 && o < 0x80000000u ? o | 0xFFFFu : o); };
         const int64_t vecs = ((int64_t)a.vocab + N - 1) / N;
         double* const masses = reinterpret_cast<double*>(s.mass);
-        bool above_known = false;
-        double above = 0.0;               // weight, and number, of what lies above hi
-        int64_t above_count = 0;
+        // the cut lies in [bottom, ceiling]; weight, and number, of what lies above that, and how far that weight may be off
+        const uint32_t highest = kLeast > 0 ? order_of(m) | 0xFFFFu : order_of(m);
+        uint32_t bottom = kFirst, ceiling = highest;
+        double above_ceiling = 0.0, doubt = 0.0;
+        int64_t count_ceiling = 0;
+        auto be_exact = [&] {
+            exact = true;
+            bottom = kFirst;
+            ceiling = highest;
+            above_ceiling = doubt = 0.0;
+            count_ceiling = 0;
+            __syncthreads();
+        };
 #pragma unroll 1
         while (true) {
+            hi = max(min(hi, ceiling), bottom);
+            lo = max(min(lo, hi), bottom);
             if (kLeast > 0) {
                 lo &= 0xFFFF0000u;
                 hi |= 0x0000FFFFu;
                 // nothing lies above hi where the bins reach that far
-                if (!above_known && (order_of(m) - lo) >> kLeast < kBins) hi = order_of(m) | 0xFFFFu;
+                if (count_ceiling == 0 && (ceiling - lo) >> kLeast < kBins) hi = ceiling;
             }
             int sh = kLeast;
             while (((hi - lo) >> sh) >= kBins) ++sh;
-            const bool alike = kLeast > 0 && sh == kLeast, above_before = above_known || hi < order_of(m);
-            const float least = value_at(lo), most = value_at(hi), known_from = above_known ? most : __builtin_inff();
+            const bool alike = sh == kLeast;          // a bin is one order
+            const float least = value_at(lo), most = value_at(hi), known_from = value_at(ceiling);
             // weights as whole numbers, so that their sums do not depend on the order: 2^units for the largest of them
             const int units = 62 - (32 - __clz((int)a.vocab));
             const double unit = (double)((uint64_t)1 << units) / fmax(weight(fminf(most, m)), 0x1p-100);
@@ -912,7 +936,7 @@ template <typename T, typename S, int K> struct RowWork {
             double mine = 0.0;
             uint32_t mine_count = 0;
             each_logit<K>(0, vecs, a.vocab, tid, [&](float x, uint32_t) {
-                if (!(x >= least) || x > known_from || x == -__builtin_inff()) return;
+                if (!(x >= least) || x > known_from) return;
                 if (x > most) {
                     mine += weight(x);
                     ++mine_count;
@@ -922,12 +946,12 @@ template <typename T, typename S, int K> struct RowWork {
                     atomicAdd(&s.count[bin], 1u);
                 }
             });
-            if (!above_known) {
-                uint32_t count;
-                block_scan<K>(mine, s.wave, &above);
-                block_scan<K>(mine_count, s.wave_count, &count);
-                above_count = count;
-            }
+            double above;                 // weight, and number, of what lies above hi
+            uint32_t more;
+            block_scan<K>(mine, s.wave, &above);
+            block_scan<K>(mine_count, s.wave_count, &more);
+            above += above_ceiling;
+            int64_t above_count = count_ceiling + more;
             __syncthreads();
             // from the top: the bin in which the number or the weight is reached
             constexpr int PER = kBins / K;
@@ -947,10 +971,23 @@ template <typename T, typename S, int K> struct RowWork {
             double mass_upto = block_scan<K>(mass, s.wave, &all_mass) - mass;
             uint32_t count_upto = block_scan<K>(count, s.wave_count, &all_count) - count;
             const auto reached = [&](double x, uint32_t n) { return by_weight ? !(above + x < enough) : above_count + n >= number; };
-            const bool inside = !reached(0.0, 0) && reached(all_mass, all_count);
-            if (!inside && !above_known && !(lo <= kFirst && hi >= order_of(m))) {
-                lo = kFirst;
-                hi = kLast;
+            const bool before = reached(0.0, 0), inside = !before && reached(all_mass, all_count), none_above = above_count == 0;
+            if (!inside && doubt > 0.0) {
+                be_exact();
+                continue;
+            }
+            if (before) {                 // above hi, which is below the ceiling
+                lo = bottom = hi + 1;
+                hi = ceiling;
+                __syncthreads();
+                continue;
+            }
+            ceiling = hi;
+            above_ceiling = above;
+            count_ceiling = above_count;
+            if (!inside && lo > bottom) {
+                hi = lo - 1;
+                lo = bottom;
                 __syncthreads();
                 continue;
             }
@@ -991,25 +1028,39 @@ template <typename T, typename S, int K> struct RowWork {
             block_scan<K>(count, s.wave_count, &all_count);
             above += all_mass;
             above_count += all_count;
-            above_known = true;
             __syncthreads();
             const uint32_t from = lo;
             hi = min(hi, lo + (bin << sh) + ((1u << sh) - 1));
             lo += bin << sh;
-            if (sh > kLeast) continue;
+            if (sh > kLeast) {
+                if (!exact) {
+                    ceiling = hi;
+                    above_ceiling = above;
+                    count_ceiling = above_count;
+                    doubt += 0.5 * all_count / unit;
+                }
+                continue;
+            }
             // `here` logits alike: as many of them as it takes, by the lowest tokens
             int64_t ties = here;
             if (inside) {
                 if (by_weight) {
                     const double w = weighs / here;
-                    if (w > 0.0) ties = (int64_t)fmin(ceil((enough - above) / w * (1 - 0x1p-50)), (double)here);
-                    ties = max(ties, (int64_t)1);
+                    auto needed = [&](double rest) {
+                        return w > 0.0 ? max((int64_t)1, (int64_t)fmin(ceil(rest / w * (1 - 0x1p-50)), (double)here)) : (int64_t)here;
+                    };
+                    ties = needed(enough - above);
+                    // one of them, or as many as there are, may stand for fewer or more
+                    if (doubt > 0.0 && (enough - above <= doubt || enough - above + doubt > weighs || needed(enough - above + doubt) != needed(enough - above - doubt))) {
+                        be_exact();
+                        continue;
+                    }
                 } else {
                     ties = max((int64_t)1, min((int64_t)here, number - above_count));
                 }
             }
             *weight_left = above + weighs * ((double)ties / here);
-            if (alike && !above_before) {
+            if (kLeast > 0 && none_above) {
                 // every token that stays lies in a bin: one weight each, for the sums that follow
                 weights_from = from;
 #pragma unroll 1
@@ -1186,7 +1237,7 @@ template <typename T, typename S, int K> struct RowWork {
                 __syncthreads();
                 if (a.top_k > 0) {
                     guess(order_of(m) + 1, a.top_k, a.vocab, false, &lo, &hi);
-                    cut = search(lo, hi, a.top_k, 0.0, false, &among);
+                    cut = search(lo, hi, a.top_k, 0.0, false, a.top_p < 1.0, &among);
                 }
                 if (a.top_p < 1.0) {
                     const double enough = a.top_p * among;
@@ -1195,7 +1246,7 @@ template <typename T, typename S, int K> struct RowWork {
                     else
                         guess(below, enough - weighs, total - weighs, true, &lo, &hi);
                     weights_from = 0;
-                    cut = cut.stricter(search(lo, hi, 0, enough, true, &ignored));
+                    cut = cut.stricter(search(lo, hi, 0, enough, true, false, &ignored));
                 }
                 total = sums_of(cut);
                 pick(total, cut);

@@ -114,6 +114,45 @@ def test_ties(vocab, dtype):
                 assert torch.equal(token, x.float().cpu().argmax(-1))
 
 
+def last_kept(x, top_p):
+    """(the last token that top_p of a row keeps, how near its border is, relative), of logits that fall with the token but
+    for equal ones."""
+    w = np.exp(x - x[0])
+    upto = np.concatenate([[0.0], np.cumsum(w.astype(np.longdouble)).astype(np.float64)])
+    enough = top_p * upto[-1]
+    return int((upto[:-1] < enough).sum()) - 1, float(np.abs(upto - enough).min() / upto[-1])
+
+
+@pytest.mark.parametrize("rows", [24, 260])
+@pytest.mark.parametrize("behind,top_k", [(0, 0), (50000, 0), (50000, 151935)])
+def test_a_cut_among_many_small_weights(behind, top_k, rows):
+    """One likely token in front of some 100,000 equal fp32 logits, and others behind those: where top_p ends, their sum has
+    to be right to its last bits, not each of them to as many as fit beside the likely one."""
+    print(f"sample cut among small weights behind={behind} top_k={top_k} rows={rows}", flush=True)
+    vocab = 151936
+    rng = np.random.default_rng(behind)
+    top_p = float(np.float32(0.9999 if behind else 0.93))
+    found = []
+    while len(found) < 24:
+        # rows whose border lies between what sums of 44 bits a weight and what the call promises tell apart
+        value = (-13.8 + 0.4 * rng.random(4000)).astype(np.float32)
+        if not behind:
+            # by the sum of equal ones, the candidates in the middle of that range
+            w = np.exp(value.astype(np.float64))
+            number = (top_p * (1 + (vocab - 1) * w) - 1) / w
+            value = value[np.abs(np.log2(np.abs(number - number.round()) * w) + 32) < 2.5]
+        x = np.full(vocab, value[0], dtype=np.float32)
+        x[0] = 0.0
+        if behind:
+            x[-behind:] = np.sort((-18.0 - rng.random(behind)).astype(np.float32))[::-1]
+        token, margin = last_kept(x.astype(np.float64)[:top_k or vocab], top_p)
+        if 2.0 ** -35 < margin < 2.0 ** -29:
+            found.append((x, token))
+    x = torch.from_numpy(np.stack([f[0] for f in found])).repeat(-(-rows // 24), 1)[:rows].cuda()
+    token, _ = run(x, torch.ones(rows, device="cuda"), top_p=top_p, top_k=top_k)
+    assert token.tolist() == ([f[1] for f in found] * -(-rows // 24))[:rows]
+
+
 def test_values_close_together():
     """fp32 logits that one bf16 number stands for."""
     g = torch.Generator().manual_seed(5)
