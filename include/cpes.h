@@ -607,7 +607,8 @@ CPES_API size_t cpes_attend_workspace_bytes(int32_t rows, int32_t q_heads, int32
  * empty sequence, an id out of range) gets out = 0 and lse = -inf, as does one
  * whose scores are all -inf; positions whose table entry names no page are not
  * seen.  The result does not depend on the contents of unseen positions, nor on
- * the run.
+ * the run.  Of a bf16 cache an infinite value that is seen comes out as an infinity or
+ * as NaN.
  * workspace: as cpes_attend_workspace_bytes, 16-byte aligned; needs no
  * particular contents, and calls that overlap in time need their own.
  * Errors: null pointers, rows < 0, q_heads not a positive multiple of the
@@ -648,7 +649,8 @@ CPES_API size_t cpes_attend_tree_workspace_bytes(int32_t rows, int32_t tokens, i
  * whose starts fall, lie outside [0, tokens] or more than `longest` apart is left out,
  * and rows behind one whose starts fall may be; what no row covers is left as it was.  The result of a token does not
  * depend on the contents of positions it does not see (other branches, too), nor on the
- * run.
+ * run.  A dim in which it sees an infinite value is infinite, and NaN where it sees a NaN
+ * or infinities of both signs, or where the infinite value's weight is 0 in 32 bits.
  * Any alignment of the cache will do; more than 32 queries of a row and KV head are
  * fastest where its keys and values, and their strides, lie at multiples of 16 bytes.
  * workspace: as cpes_attend_tree_workspace_bytes, 16-byte aligned; needs no
