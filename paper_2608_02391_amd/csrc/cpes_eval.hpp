@@ -159,15 +159,15 @@ struct TreeArgs {
 
 // How jobs are cut, from what the host knows.
 struct TreeShape {
-    bool wide;                   // more than 32 queries, up to 128 dims: through shared memory, where type and alignment let it
+    bool wide;                   // more than 32 queries, up to 128 dims: through shared memory, where the call lets it
     int32_t sets, beside, columns, job_heads, blocks, job_tokens, pieces;
 };
 
-inline TreeShape tree_shape(bool bf16, bool aligned, int32_t longest, int32_t group, int32_t dim)
+inline TreeShape tree_shape(bool bf16, bool shared, int32_t longest, int32_t group, int32_t dim)
 {
     TreeShape t;
     const int64_t queries = (int64_t)longest * group;
-    t.wide = bf16 && aligned && dim <= 128 && queries > 32;
+    t.wide = bf16 && shared && dim <= 128 && queries > 32;
     t.sets = bf16 && dim <= 128 && queries > 16 ? 2 : 1;        // what fits a wave's registers
     t.beside = 1;
     while (t.beside < (t.wide ? 8 : 4) && 16 * t.sets * t.beside < queries) t.beside *= 2;

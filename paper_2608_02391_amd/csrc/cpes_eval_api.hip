@@ -590,7 +590,7 @@ size_t cpes_attend_tree_workspace_bytes(int32_t rows, int32_t tokens, int32_t lo
     if (rows < 0 || rows > CPES_MAX_SEQUENCES || tokens < 0 || (tokens > 0 && (longest < 1 || longest > tokens)) ||
         !check_heads(q_heads, kv_heads, head_dim))
         return 0;
-    size_t most = 0;             // either type's and alignment's
+    size_t most = 0;             // either type's, through shared memory or not
     for (int way = 0; way < 3; ++way)
         most = std::max(most, tree_bytes(rows, cpes::tree_shape(way > 0, way > 1, std::max(1, longest), q_heads / kv_heads, head_dim), kv_heads, head_dim));
     return most;
@@ -618,8 +618,10 @@ int cpes_attend_tree(const cpes_cache* cache, int32_t layer, const cpes_pool* po
     const char* const v = at_layer(cache, cache->v_dev, layer);
     // straight into shared memory go 16 bytes that lie at a multiple of 16
     const bool aligned = ((uintptr_t)k | (uintptr_t)v | (uintptr_t)((cache->page_stride | cache->head_stride | cache->token_stride) * 2)) % 16 == 0;
-    const cpes::TreeShape shape = cpes::tree_shape(cache->dtype == CPES_BF16, aligned, std::max(1, longest), q_heads / cache->heads,
-                                                   cache->head_dim);
+    // that form takes scores times scale log2 e, which has to be a number with all its bits; the other takes them times scale first
+    const bool ordinary = std::fabs(scale) >= 1e-30f && std::fabs(scale) <= 1e30f;
+    const cpes::TreeShape shape = cpes::tree_shape(cache->dtype == CPES_BF16, aligned && ordinary, std::max(1, longest),
+                                                   q_heads / cache->heads, cache->head_dim);
     rc = check_workspace(workspace_dev, workspace_bytes, tree_bytes(rows, shape, cache->heads, cache->head_dim), fn);
     if (rc || rows == 0 || tokens == 0) return rc;
     cpes::TreeArgs a;

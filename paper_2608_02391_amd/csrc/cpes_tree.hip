@@ -912,7 +912,7 @@ template <int DP, int WAVES, int TEAMS, bool kLean> struct Wide {
             if (d >= a.dim || !valid) q[e] = V4u{0, 0, 0, 0};
             if (a.scale < 0.f) q[e] ^= 0x80008000u;       // of -q with -scale
         }
-        unit = fmaxf(fabsf(a.scale) * kLog2e, 1.2e-38f);  // of 0: -inf stays below all scores, and others are as good as equal
+        unit = fabsf(a.scale) * kLog2e;
         every_high = row.base < 0 ? 0 : tree ? row.base : row.base + span.from + 1;
         every_low = 0;
         if (a.window > 0 && row.base >= 0)

@@ -192,6 +192,44 @@ def test_many_queries_over_long_contexts(dim, nodes, chain):
         assert torch.equal(again, out) and torch.equal(again_lse, lse)
 
 
+def check_scaled(c, q, scale, step=1):
+    scale = float(torch.tensor(scale, dtype=torch.float32))
+    out, lse = c.run(q, scale=scale)
+    out, lse, group = out.double().cpu(), lse.cpu(), q.shape[1] // c.kv
+    for r in range(len(c.bases)):
+        for i in range(0, c.sizes[r], step):
+            at = c.starts[r] + i
+            for h in range(q.shape[1]):
+                ref, ref_lse, tol, tol_lse = H.attend(q[at, h].cpu(), c.keys[r][:, h // group], c.values[r][:, h // group], c.seen[r][i], scale)
+                off = (out[at, h] - ref).abs() - (tol + H.rounding(c.dtype) * (ref.abs() + tol) + 1e-38)
+                assert float(off.max()) <= 0, (r, i, h, scale, float(off.max()))
+                assert abs(float(lse[at, h]) - ref_lse) <= tol_lse, (r, i, h, scale, float(lse[at, h]), ref_lse)
+
+
+@pytest.mark.parametrize("scale", [-0.125, 0.0, -0.0, 1e-40, 1e-6, 1.0, -3.0])
+@pytest.mark.parametrize("dtype,dim,heads", [(BF16, 64, 1), (BF16, 64, 8), (BF16, 128, 32), (F32, 64, 4)])
+def test_scales(dtype, dim, heads, scale):
+    """Of either sign, none at all, and so small or large that all or one of the positions count."""
+    print(f"tree scale={scale} {dtype} dim={dim} heads={heads}", flush=True)
+    for bases, sizes, chain in (([0, 77, 3000], [5, 12, 1], False), ([4500], [9], False), ([20], [60], True)):
+        c = Trees(bases, sizes, kv_heads=1, dim=dim, dtype=dtype, seed=dim + heads, chain=chain)
+        check_scaled(c, c.queries(heads), scale, 1 if heads < 32 and max(sizes) < 60 else 5)
+
+
+@pytest.mark.parametrize("dtype,heads", [(BF16, 1), (BF16, 8), (F32, 4)])
+@pytest.mark.parametrize("scale", [2.0 ** 60, -(2.0 ** 101), 2.0 ** 127, 3e38, -3e38])
+def test_scales_near_the_largest_number(scale, dtype, heads):
+    """Scores that are ordinary numbers behind a scale whose product with log2 e may not be one."""
+    print(f"tree scale={scale} {dtype} heads={heads}", flush=True)
+    for bases, sizes in (([0, 77, 1000], [5, 12, 1]), ([2500], [9])):
+        c = Trees(bases, sizes, kv_heads=1, dtype=dtype, seed=heads)
+        q = c.queries(heads).float()
+        # one product a score, of numbers that have all their bits
+        q[..., 1:] = 0.0
+        q[..., 0] = (1.0 + q[..., 0].abs()) * 2.0 ** -math.floor(math.log2(abs(scale))) * q[..., 0].sign()
+        check_scaled(c, q.to(dtype), scale)
+
+
 def test_one_new_token_is_the_decode_attention():
     """Trees of one token: the same positions as cpes_attend, the same bounds; and a chain in two calls is one call's."""
     c = Trees([0, 40, 333, 2000], [1, 1, 1, 1], dim=128, seed=3)
