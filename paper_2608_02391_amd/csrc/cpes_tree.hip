@@ -559,6 +559,52 @@ __device__ __forceinline__ int64_t job_index(const TreeArgs& a, int32_t r, int32
     return ((int64_t)r * a.pieces + piece) * (a.heads * a.blocks) + hh;
 }
 
+// Every row's tiles: a thread's share of them before, and after, its rows.
+template <int TILE, int WAVES> struct Line {
+    int32_t r0, r1;
+    int64_t mine, upto, tiles;
+
+    // All threads.
+    __device__ __forceinline__ Line(const TreeArgs& a, int64_t* s_sum)
+    {
+        const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+        const int32_t each = (a.rows + 64 * WAVES - 1) / (64 * WAVES);
+        r0 = min(a.rows, tid * each);
+        r1 = min(a.rows, r0 + each);
+        mine = 0;
+        for (int32_t r = r0; r < r1; ++r) mine += row_tiles<TILE>(a, row_at(a, r));
+        upto = mine;
+#pragma unroll
+        for (int d = 1; d < 64; d <<= 1) {
+            const int64_t y = __shfl_up(upto, d);
+            if (lane >= d) upto += y;
+        }
+        if (lane == 63) s_sum[wave] = upto;
+        __syncthreads();
+        tiles = 0;
+#pragma unroll
+        for (int w = 0; w < WAVES; ++w) {
+            if (w < wave) upto += s_sum[w];
+            tiles += s_sum[w];
+        }
+    }
+
+    // The thread that holds tile t of the rows' says in which of them it lies, and what is before that row.
+    __device__ __forceinline__ void find(const TreeArgs& a, int64_t t, int32_t* s_row, int64_t* s_before) const
+    {
+        if (t < upto - mine || t >= upto) return;
+        int64_t before = upto - mine;
+        int32_t r = r0;
+        for (; r < r1; ++r) {
+            const int64_t n = row_tiles<TILE>(a, row_at(a, r));
+            if (t < before + n) break;
+            before += n;
+        }
+        *s_row = r;
+        *s_before = before;
+    }
+};
+
 // All jobs' tiles form one line, cut into equal shares, one for `beside` waves.
 template <typename T, int DP, bool kWhole, int NQ>
 __global__ __launch_bounds__(kThreads, DP == 256 || NQ > 1 ? 1 : 2) void k_tree(TreeArgs a)
@@ -571,25 +617,8 @@ __global__ __launch_bounds__(kThreads, DP == 256 || NQ > 1 ? 1 : 2) void k_tree(
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int teams = kWaves / a.beside, team = wave / a.beside, sub = wave - team * a.beside;
 
-    // every row's tiles, a thread to some rows
-    const int32_t each = (a.rows + kThreads - 1) / kThreads, r0 = min(a.rows, tid * each), r1 = min(a.rows, r0 + each);
-    int64_t mine = 0;
-    for (int32_t r = r0; r < r1; ++r) mine += row_tiles<TILE>(a, row_at(a, r));
-    int64_t upto = mine;
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) {
-        const int64_t y = __shfl_up(upto, d);
-        if (lane >= d) upto += y;
-    }
-    if (lane == 63) s_sum[wave] = upto;
-    __syncthreads();
-    int64_t tiles = 0;
-#pragma unroll
-    for (int w = 0; w < kWaves; ++w) {
-        if (w < wave) upto += s_sum[w];
-        tiles += s_sum[w];
-    }
-    const int64_t units = tiles * a.heads * a.blocks;
+    const Line<TILE, kWaves> line(a, s_sum);
+    const int64_t tiles = line.tiles, units = tiles * a.heads * a.blocks;
     constexpr int kShareTiles = 2 * NQ;
     const int32_t shares_n = (int32_t)max((int64_t)1, min((int64_t)a.groups * teams, units / kShareTiles));
     const bool apart = shares_n <= (int32_t)gridDim.x;
@@ -601,18 +630,8 @@ __global__ __launch_bounds__(kThreads, DP == 256 || NQ > 1 ? 1 : 2) void k_tree(
     for (int w = 0; w < teams; ++w) {
         const int32_t share = share0 + w * step;
         if (share >= shares_n) break;
-        const int64_t at = shares.begin(share), t = at - quotient(at, tiles) * tiles;
-        if (t >= upto - mine && t < upto) {
-            int64_t before = upto - mine;
-            int32_t r = r0;
-            for (; r < r1; ++r) {
-                const int64_t n = row_tiles<TILE>(a, row_at(a, r));
-                if (t < before + n) break;
-                before += n;
-            }
-            s_row[w] = r;
-            s_before[w] = before;
-        }
+        const int64_t at = shares.begin(share);
+        line.find(a, at - quotient(at, tiles) * tiles, &s_row[w], &s_before[w]);
     }
     __syncthreads();
     if (me >= shares_n) return;
@@ -1271,52 +1290,6 @@ template <int DP, int WAVES, int TEAMS, bool kLean> struct Wide {
     }
 };
 
-// Every row's tiles: a thread's share of them before, and after, its rows.
-template <int TILE, int WAVES> struct Line {
-    int32_t r0, r1;
-    int64_t mine, upto, tiles;
-
-    // All threads.
-    __device__ __forceinline__ Line(const TreeArgs& a, int64_t* s_sum)
-    {
-        const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-        const int32_t each = (a.rows + 64 * WAVES - 1) / (64 * WAVES);
-        r0 = min(a.rows, tid * each);
-        r1 = min(a.rows, r0 + each);
-        mine = 0;
-        for (int32_t r = r0; r < r1; ++r) mine += row_tiles<TILE>(a, row_at(a, r));
-        upto = mine;
-#pragma unroll
-        for (int d = 1; d < 64; d <<= 1) {
-            const int64_t y = __shfl_up(upto, d);
-            if (lane >= d) upto += y;
-        }
-        if (lane == 63) s_sum[wave] = upto;
-        __syncthreads();
-        tiles = 0;
-#pragma unroll
-        for (int w = 0; w < WAVES; ++w) {
-            if (w < wave) upto += s_sum[w];
-            tiles += s_sum[w];
-        }
-    }
-
-    // The thread that holds tile t of the rows' says in which of them it lies, and what is before that row.
-    __device__ __forceinline__ void find(const TreeArgs& a, int64_t t, int32_t* s_row, int64_t* s_before) const
-    {
-        if (t < upto - mine || t >= upto) return;
-        int64_t before = upto - mine;
-        int32_t r = r0;
-        for (; r < r1; ++r) {
-            const int64_t n = row_tiles<TILE>(a, row_at(a, r));
-            if (t < before + n) break;
-            before += n;
-        }
-        *s_row = r;
-        *s_before = before;
-    }
-};
-
 // Where a workgroup is in its share.  Kept in shared memory: what it held in registers while tiles are folded would
 // cost the folding its own.
 struct Progress {
@@ -1515,13 +1488,13 @@ template <typename T> __global__ __launch_bounds__(kThreads) void k_tree_join(Tr
     }
 }
 
-// Tiles a job has at most: its table's, or its window's and sinks'.
 // Workgroups for a job's columns: some thousands in all.
 unsigned join_columns(int64_t jobs, int32_t columns)
 {
     return (unsigned)std::min<int64_t>(columns, std::max<int64_t>(16, 4096 / jobs));
 }
 
+// Tiles a job has at most: its table's, or its window's and sinks'.
 template <int TILE> int64_t most_tiles(const TreeArgs& a)
 {
     const int64_t table = ((int64_t)a.width * a.page_size + TILE - 1) / TILE;
@@ -1537,10 +1510,11 @@ template <typename T, int DP, bool kWhole, int NQ> hipError_t tree_as(const Tree
     // as many as find_job counts
     const int64_t jobs = ((int64_t)a.tokens / a.job_tokens + a.rows) * each;
     const int64_t most = most_tiles<Tile<T>::n>(a);
-    // Measured with a workgroup a job and with shares, trees of 5: one row of 500 tokens 19 and 25 us, of 1,000 25 and
-    // 25, of 2,000 38 and 30; 32 rows of 4,000 136 and 122, 64 of 8,000 421 and 402, 128 of 4,000 407 and 424, 256 of
-    // 100 - 8,000 499 and 524.  Prompts in fp32 (with two sets), 4 of 1,000 201 and 222, 8 of 2,000 517
-    // and 763.
+    // Measured with a workgroup a job and with shares, bf16 trees of 5: one row of 500 tokens 18 and 24 us, of 1,000 24
+    // and 25, of 2,000 37 and 29; 32 rows of 4,000 134 and 118, 64 of 8,000 377 and 368, 128 of 4,000 350 and 388, 256 of
+    // 100 - 8,000 458 and 475.  Prompts in fp32, one of 1,000 (504 jobs) 149 and 173, of 2,000 427 and 533, 4 of 1,000 149
+    // and 213, 8 of 2,000 452 and 788; 500 tokens on each of 4 rows of up to 4,000 (520 jobs) 633 and 515.  fp32 trees of 5
+    // lose by it, 128 rows of 4,000 1,019 and 856, until jobs are more, 256 of 2,000 895 and 885.
     if ((jobs >= (a.parents ? 1024 : 512) || most <= 32) && jobs <= INT32_MAX / kThreads) {
         hipLaunchKernelGGL((k_tree_jobs<T, DP, kWhole, NQ>), dim3((unsigned)jobs), dim3(kThreads), 0, s, a);
         return hipGetLastError();
