@@ -234,7 +234,7 @@ struct SampleArgs {
     float* most;                 // [rows][strips]: maxima, NaN where there is one
     int64_t stride;
     int32_t rows, vocab;
-    int32_t slices, waves, strip_steps, shift, slots, note_shift, note_slots, group;
+    int32_t slices, strip_steps, shift, slots, note_shift, note_slots, group;
     bool notes_kept, samples_kept;
     int32_t top_k;               // 0: all
     double top_p;

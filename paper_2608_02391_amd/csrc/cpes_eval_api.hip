@@ -731,7 +731,6 @@ int cpes_sample(const void* x_dev, int dtype, int32_t rows, int32_t vocab, int64
     const cpes::SampleSplit split = cpes::sample_split(at_once, vocab, dtype);
     if (split.slices == 0) at_once = rows;                       // nothing in the workspace
     a.slices = split.slices;
-    a.waves = split.waves;
     a.strip_steps = split.strip_steps;
     a.shift = split.shift;
     a.slots = split.slots;
