@@ -1008,9 +1008,9 @@ template <typename T, typename S, int K> struct RowWork {
             }
             __syncthreads();
             const uint32_t found = inside && s.found ? s.found : s.place;
-            if (found == 0) {             // nothing that counts
+            if (found == 0) {             // nothing in [bottom, hi]: all that lies above stays
                 *weight_left = above;
-                return kEverything;
+                return bottom == kFirst ? kEverything : Cut{bottom, 0};
             }
             const uint32_t bin = found - 1, here = s.count[bin];
             const double weighs = masses[bin];
