@@ -86,6 +86,14 @@ def test_large_vocabulary(dtype, rows):
         check(x, u, rows=range(0, rows, max(1, rows // 12)), **f)
 
 
+@pytest.mark.parametrize("dtype", [BF16, F32], ids=["bf16", "fp32"])
+def test_a_vocabulary_of_a_million(dtype):
+    for rows in (1, 4):
+        x, u = logits(rows, 1 << 20, dtype, seed=rows, likely=200)
+        for f in (dict(), dict(top_k=50), dict(top_p=0.9), dict(top_p=0.95, scale=0.3), dict(top_k=2000, top_p=0.7), dict(min_p=0.02)):
+            check(x, u, **f)
+
+
 @pytest.mark.parametrize("filters", [dict(top_p=0.95), dict(top_k=400), dict(top_k=3000), dict(top_k=1000, top_p=0.7), dict(min_p=0.001),
                                      dict(top_p=0.999, min_p=1e-4), dict(top_p=0.5, scale=0.25), dict(top_k=20000, min_p=0.01)],
                          ids=lambda f: ",".join(f"{k}={v}" for k, v in f.items()))

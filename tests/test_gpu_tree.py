@@ -124,6 +124,16 @@ def test_page_sizes(page, order):
     c.check(q, *c.run(q))
 
 
+@pytest.mark.parametrize("dtype", [BF16, F32], ids=["bf16", "fp32"])
+@pytest.mark.parametrize("page", [96, 128, 1000])
+def test_large_pages(page, dtype):
+    """Pages of several tiles, and of more tokens than any row has."""
+    print(f"tree page={page} {dtype}", flush=True)
+    c = Trees(BASES, SIZES, page=page, dtype=dtype, seed=page)
+    q = c.queries(8)
+    c.check(q, *c.run(q))
+
+
 @pytest.mark.parametrize("kv,group", [(1, 1), (3, 1), (2, 5), (1, 16), (2, 17), (1, 33), (1, 70), (1, 300)])
 @pytest.mark.parametrize("dtype", [BF16, F32], ids=["bf16", "fp32"])
 def test_head_groups(kv, group, dtype):
