@@ -646,11 +646,14 @@ CPES_API size_t cpes_attend_tree_workspace_bytes(int32_t rows, int32_t tokens, i
  * token up to roundings.  Of a sequence the first 2^31 - 65 positions count.  The
  * tokens of a sequence that has fewer than T, or of an id out of range, get out = 0
  * and lse = -inf; positions whose table entry names no page are not seen.  A row
- * whose starts fall, lie outside [0, tokens] or more than `longest` apart is left out,
- * and rows behind one whose starts fall may be; what no row covers is left as it was.  The result of a token does not
+ * whose starts fall, lie outside [0, tokens] or more than `longest` apart is left out;
+ * where starts fall, tokens of other rows may be left out too, and tokens of two rows
+ * get either's result.  What no row covers is left as it was.  The result of a token does not
  * depend on the contents of positions it does not see (other branches, too), nor on the
  * run.  A dim in which it sees an infinite value is infinite, and NaN where it sees a NaN
  * or infinities of both signs, or where the infinite value's weight is 0 in 32 bits.
+ * Sums are of weights of up to 2^4 before they are divided: of n positions seen, values
+ * above 2^124 / n may come out infinite.
  * Any alignment of the cache will do; more than 32 queries of a row and KV head are
  * fastest where its keys and values, and their strides, lie at multiples of 16 bytes.
  * workspace: as cpes_attend_tree_workspace_bytes, 16-byte aligned; needs no
