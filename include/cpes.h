@@ -607,8 +607,7 @@ CPES_API size_t cpes_attend_workspace_bytes(int32_t rows, int32_t q_heads, int32
  * empty sequence, an id out of range) gets out = 0 and lse = -inf, as does one
  * whose scores are all -inf; positions whose table entry names no page are not
  * seen.  The result does not depend on the contents of unseen positions, nor on
- * the run.  Of a bf16 cache an infinite value that is seen comes out as an infinity or
- * as NaN.
+ * the run.
  * workspace: as cpes_attend_workspace_bytes, 16-byte aligned; needs no
  * particular contents, and calls that overlap in time need their own.
  * Errors: null pointers, rows < 0, q_heads not a positive multiple of the
@@ -650,8 +649,7 @@ CPES_API size_t cpes_attend_tree_workspace_bytes(int32_t rows, int32_t tokens, i
  * where starts fall, tokens of other rows may be left out too, and tokens of two rows
  * get either's result.  What no row covers is left as it was.  The result of a token does not
  * depend on the contents of positions it does not see (other branches, too), nor on the
- * run.  A dim in which it sees an infinite value is infinite, and NaN where it sees a NaN
- * or infinities of both signs, or where the infinite value's weight is 0 in 32 bits.
+ * run.
  * Sums are of weights of up to 2^4 before they are divided: of n positions seen, values
  * above 2^124 / n may come out infinite.
  * Any alignment of the cache will do; more than 32 queries of a row and KV head are

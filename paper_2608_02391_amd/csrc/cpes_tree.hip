@@ -18,9 +18,7 @@
 // nodes of 256 in bf16 340 us and 215, in fp32 2,520 and 510).  Above 32 queries a bf16 cache
 // goes through shared memory (below, "many queries").  The weights of a bf16 cache go in as a
 // bf16 value and its remainder, as there: a bf16 weight alone is off by 2^-9, which the
-// outputs of long contexts would show.  The value is the weight's first 8 bits and the remainder is
-// above 0 (a 2^-20th of the weight is added to it), so that both products of an infinite value
-// have its sign: with a remainder of 0 or below, inf comes out as NaN.  Right to 2^-16.
+// outputs of long contexts would show.
 //
 // What a tile's queries see differs only where the new tokens are and at the edges of
 // windows.  Such tiles mask scores per query.  A value that one query sees and another does
@@ -43,7 +41,6 @@ constexpr int kWaves = kAttendWaves;
 constexpr int kThreads = 64 * kWaves;
 constexpr int64_t kMaxGrid = 1 << 20;
 constexpr int kWords = kMaxTree / 32;
-constexpr float kOver = 1.f + 0x1p-20f;  // of a weight, so that its remainder is above 0
 
 // A row's sequence and new tokens.
 struct Row {
@@ -381,18 +378,6 @@ template <typename T, int DP, bool kWhole, int NQ> struct Work : Operands<T, DP,
         return __builtin_bit_cast(V8bf, v);
     }
 
-    // A weight as two bf16, both above 0.
-    __device__ __forceinline__ static void split(const float x[VROWS], V8bf* hi, V8bf* lo)
-    {
-        V4u first;
-#pragma unroll
-        for (int j = 0; j < 8; j += 2) first[j >> 1] = __builtin_amdgcn_perm(__float_as_uint(x[j + 1]), __float_as_uint(x[j]), 0x07060302u);
-        *hi = __builtin_bit_cast(V8bf, first);
-#pragma unroll
-        for (int j = 0; j < 8; ++j)
-            (*lo)[j] = (__bf16)fmaf(x[j], kOver, -__uint_as_float(__float_as_uint(x[j]) & 0xFFFF0000u));
-    }
-
     // Block b of the product of the values with set s's weights, added to o.
     __device__ __forceinline__ V4f product(int b, const float x[VROWS], V8bf hi, V8bf lo, V4f o) const
     {
@@ -441,7 +426,12 @@ template <typename T, int DP, bool kWhole, int NQ> struct Work : Operands<T, DP,
         V8bf hi[NQ], lo[NQ];
         if constexpr (std::is_same<T, uint16_t>::value) {
 #pragma unroll
-            for (int s = 0; s < NQ; ++s) split(x[s], &hi[s], &lo[s]);
+            for (int s = 0; s < NQ; ++s)
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    hi[s][j] = (__bf16)x[s][j];
+                    lo[s][j] = (__bf16)(x[s][j] - (float)hi[s][j]);
+                }
         }
 #pragma unroll
         for (int b = 0; b < DP / 16; ++b)
@@ -1135,9 +1125,9 @@ template <int DP, int WAVES, int TEAMS, bool kLean> struct Wide {
             V4u hi[2], lo[2];
 #pragma unroll
             for (int e = 0; e < 16; e += 2) {
-                const uint32_t w0 = __float_as_uint(x[p][e]), w1 = __float_as_uint(x[p][e + 1]);
-                hi[e >> 3][e >> 1 & 3] = __builtin_amdgcn_perm(w1, w0, 0x07060302u);
-                lo[e >> 3][e >> 1 & 3] = pair(fmaf(x[p][e], kOver, -__uint_as_float(w0 & 0xFFFF0000u)), fmaf(x[p][e + 1], kOver, -__uint_as_float(w1 & 0xFFFF0000u)));
+                const uint32_t both = pair(x[p][e], x[p][e + 1]);
+                hi[e >> 3][e >> 1 & 3] = both;
+                lo[e >> 3][e >> 1 & 3] = pair(x[p][e] - __uint_as_float(both << 16), x[p][e + 1] - __uint_as_float(both & 0xFFFF0000u));
             }
 #pragma unroll
             for (int t = 0; t < 2; ++t)
