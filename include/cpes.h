@@ -607,7 +607,8 @@ CPES_API size_t cpes_attend_workspace_bytes(int32_t rows, int32_t q_heads, int32
  * empty sequence, an id out of range) gets out = 0 and lse = -inf, as does one
  * whose scores are all -inf; positions whose table entry names no page are not
  * seen.  The result does not depend on the contents of unseen positions, nor on
- * the run.
+ * the run.  Where a value that is seen is infinite, its dim of out is that infinity or, of
+ * a bf16 cache (whose weights go in as two numbers, the second 0 or negative), NaN.
  * workspace: as cpes_attend_workspace_bytes, 16-byte aligned; needs no
  * particular contents, and calls that overlap in time need their own.
  * Errors: null pointers, rows < 0, q_heads not a positive multiple of the
@@ -647,11 +648,13 @@ CPES_API size_t cpes_attend_tree_workspace_bytes(int32_t rows, int32_t tokens, i
  * and lse = -inf; positions whose table entry names no page are not seen.  A row
  * whose starts fall, lie outside [0, tokens] or more than `longest` apart is left out;
  * where starts fall, tokens of other rows may be left out too, and tokens of two rows
- * get either's result.  What no row covers is left as it was.  The result of a token does not
- * depend on the contents of positions it does not see (other branches, too), nor on the
- * run.
- * Sums are of weights of up to 2^4 before they are divided: of n positions seen, values
- * above 2^124 / n may come out infinite.
+ * get either's result.  What no row covers is left as it was.
+ * The result of a token does not depend on the contents of positions it does not see
+ * (other branches, too), nor on the run.  Infinite values that it sees make their dims
+ * infinite or NaN, as in cpes_attend; which of them depends on the number of queries and
+ * the place in a tile, the other dims and lse on neither.  Sums are of weights of up to
+ * 2^4 before they are divided: of n positions seen, values above 2^124 / n may come out
+ * infinite.
  * Any alignment of the cache will do; more than 32 queries of a row and KV head are
  * fastest where its keys and values, and their strides, lie at multiples of 16 bytes.
  * workspace: as cpes_attend_tree_workspace_bytes, 16-byte aligned; needs no

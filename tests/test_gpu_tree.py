@@ -293,6 +293,57 @@ def test_a_broken_branch_stays_its_own(dtype, bad, base):
     assert not bool(torch.isfinite(out[6:].float()).all(-1).any())
 
 
+def expect_infinities(c, q, out, lse, rows, step=1):
+    """What is promised where values that are seen are not finite: a dim that sees an infinity is that or, of a bf16 cache,
+    NaN; one that sees a NaN or both signs is NaN; the others and the lse are as ever."""
+    out, lse, group, hit = out.float().cpu(), lse.cpu(), q.shape[1] // c.kv, [0, 0]
+    for r in rows:
+        for i in range(0, c.sizes[r], step):
+            at = c.starts[r] + i
+            for h in range(q.shape[1]):
+                k, v, seen = c.keys[r][:, h // group], c.values[r][:, h // group].double(), c.seen[r][i]
+                finite = torch.where(torch.isfinite(v), v, 0.0)
+                ref, ref_lse, tol, tol_lse = H.attend(q[at, h].cpu(), k, finite, seen, c.dim ** -0.5)
+                lost = torch.where(torch.isfinite(v) | ~seen[:len(v), None], 0.0, v).sum(0)
+                got = out[at, h].double()
+                odd = lost != 0
+                infinite = odd & ~lost.isnan()
+                as_promised = got[infinite] == lost[infinite]
+                if c.dtype == BF16:
+                    as_promised |= got[infinite].isnan()
+                assert bool(as_promised.all()), (r, i, h)
+                assert bool(got[lost.isnan()].isnan().all()), (r, i, h)
+                off = (got - ref).abs() - (tol + H.rounding(c.dtype) * (ref.abs() + tol) + 1e-38)
+                assert not bool((off[~odd] > 0).any()) and bool(torch.isfinite(got[~odd]).all()), (r, i, h)
+                assert abs(float(lse[at, h]) - ref_lse) <= tol_lse, (r, i, h)
+                hit[0] += int(odd.sum())
+                hit[1] += int(lost.isnan().sum())
+    return hit
+
+
+@pytest.mark.parametrize("dtype,dim,page", [(BF16, 64, 16), (BF16, 128, 16), (BF16, 128, 5), (BF16, 200, 16), (F32, 64, 16)])
+@pytest.mark.parametrize("heads", [1, 3, 8])
+def test_values_that_are_not_finite_and_seen(heads, dtype, dim, page):
+    """Infinities and NaN in the context and among the new tokens, in tiles that all see and in others, with one query a wave
+    or hundreds a workgroup, in one share or several: they stay in their dims."""
+    print(f"tree infinities {dtype} dim={dim} page={page} heads={heads}", flush=True)
+    for bases, sizes, chain in (([0, 40, 700, 5000], [9, 24, 2, 1], False), ([6000, 130], [70, 3], False), ([300, 0], [90, 33], True)):
+        c = Trees(bases, sizes, dim=dim, page=page, dtype=dtype, seed=dim + heads, chain=chain)
+        g = random.Random(heads)
+        for r, n in enumerate(c.lens):
+            for bad, d in ((math.inf, 3), (-math.inf, 17), (math.inf, 40), (-math.inf, 40), (math.nan, dim - 1)):
+                pos = g.randrange(n) if d != 3 else max(0, c.bases[r] - 1)
+                for kv in range(2):
+                    c.values[r][pos, kv, d] = bad
+                    c.v[1, int(c.table[r, pos // page]), kv, pos % page, d] = bad
+        q = c.queries(2 * heads) / 4
+        out, lse = c.run(q)
+        hit = expect_infinities(c, q, out, lse, range(len(bases)), 1 if max(sizes) < 60 else 9)
+        assert hit[0] > hit[1] > 0
+        again, again_lse = c.run(q)
+        assert torch.equal(again.isnan(), out.isnan()) and torch.equal(again.nan_to_num(), out.nan_to_num()) and torch.equal(again_lse, lse)
+
+
 def test_rows_that_do_not_fit():
     """Sequences without their tokens, unknown ids, starts that lie: zeros or nothing, and the others as ever."""
     c = Trees([60, 0, 100, 20], [5, 6, 7, 8], seed=13)
