@@ -608,7 +608,7 @@ CPES_API size_t cpes_attend_workspace_bytes(int32_t rows, int32_t q_heads, int32
  * whose scores are all -inf; positions whose table entry names no page are not
  * seen.  The result does not depend on the contents of unseen positions, nor on
  * the run.  Where a value that is seen is infinite, its dim of out is that infinity or, of
- * a bf16 cache (whose weights go in as two numbers, the second 0 or negative), NaN.
+ * a bf16 cache (whose weights go in as two numbers, the second of any sign), NaN.
  * workspace: as cpes_attend_workspace_bytes, 16-byte aligned; needs no
  * particular contents, and calls that overlap in time need their own.
  * Errors: null pointers, rows < 0, q_heads not a positive multiple of the

@@ -28,11 +28,12 @@
 // Two launches, because they want other registers and other numbers of waves; rows of up to
 // four steps are one wave's, in one launch.
 //
-// What bounds it.  4,096 rows of 151,936 in bf16, 186 us of HBM: without a sum (top_k, min_p)
-// 263-274 us, the notes and the second launch's dozen dependent trips; with sums the vector
-// units, about 11 instructions a logit, 406 us; top_p of 0.95 where a seventh of the rows
-// is flat 1,045 us, of which reading those again takes most.  One row is two launches of
-// trips that wait for each other: 19-21 us, 49 where it is flat.
+// What bounds it.  4,096 rows of 151,936 in bf16, 186 us of HBM: without a sum (top_k 20 or 50,
+// min_p) 272-292 us, the notes and the second launch's dozen dependent trips; with sums and no
+// filter the vector units, about 11 instructions a logit, 351 us; top_p of 0.95 where a seventh
+// of the rows is flat 1,022-1,049 us, of which reading those again takes most.  One row is two
+// launches of trips that wait for each other: 18-21 us, 50 where some hundred tokens stay and
+// 229 where most do.
 #include <algorithm>
 #include <type_traits>
 

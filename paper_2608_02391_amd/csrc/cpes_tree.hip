@@ -13,9 +13,9 @@
 // cpes_attend.hpp: S^T = K Q^T leaves the weights where O^T = V^T P^T wants them.  With more
 // queries up to four waves of a workgroup take the same positions and other queries, and
 // the first one's loads leave the others' in the caches.  Two sets are for bf16 up to 128 dims
-// (8 nodes on 64 rows of 8,000: 440 us, 476 with one).  In fp32 they leave room for one wave a
-// SIMD (32 nodes on 8 rows of 8,000: 505 us, 391 with one), and above 128 dims they spill (16
-// nodes of 256 in bf16 340 us and 215, in fp32 2,520 and 510).  Above 32 queries a bf16 cache
+// (8 nodes on 64 rows of 8,000, when they were chosen: 440 us, 476 with one; now 383).  In fp32 they
+// leave room for one wave a SIMD (32 nodes on 8 rows of 8,000: 505 us, 378 with one), and above 128
+// dims they spill (16 nodes of 256 in bf16 340 us and 203, in fp32 2,520 and 502).  Above 32 queries a bf16 cache
 // goes through shared memory (below, "many queries").  The weights of a bf16 cache go in as a
 // bf16 value and its remainder, as there: a bf16 weight alone is off by 2^-9, which the
 // outputs of long contexts would show.
@@ -821,10 +821,11 @@ __global__ __launch_bounds__(kThreads, DP == 256 || NQ > 1 ? 1 : 2) void k_tree_
 // behind, which in most tiles it is not, and saves scaling the outputs.
 //
 // Bound: 24 products of 32 clocks and about 150 vector instructions of 4 a wave and half a
-// tile; a SIMD's two waves overlap them in part (matrix units 40 % busy, vector units 45 %).
-// 8 prompts of up to 4,095 tokens, 32 heads on 8 of 128: 656 us, 544 TFLOP/s of the scores' and
-// outputs' products, 820 with the remainders'.  4 rows of 65 - 131 thousand tokens with up to 64
-// nodes: 660 us, 2.4 TB/s and 430 TFLOP/s.
+// tile; a SIMD's two waves overlap them in part (matrix units 36 - 41 % busy, vector units 41 - 45 %).
+// 8 prompts of up to 4,095 tokens, 32 heads on 8 of 128: 578 us, 617 TFLOP/s of the scores' and
+// outputs' products, 925 with the remainders'.  4 rows of 65 - 131 thousand tokens with up to 64
+// nodes: 571 us, of which the join is 15; 2.8 TB/s and 505 TFLOP/s.  Both vary by 5 % from one GPU to the
+// next, and by 15 % with its clock.
 typedef float V16f __attribute__((ext_vector_type(16)));
 typedef float V2f __attribute__((ext_vector_type(2)));
 typedef __bf16 V2bf __attribute__((ext_vector_type(2)));
