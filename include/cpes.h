@@ -655,8 +655,9 @@ CPES_API size_t cpes_attend_tree_workspace_bytes(int32_t rows, int32_t tokens, i
  * the place in a tile, the other dims and lse on neither.  Sums are of weights of up to
  * 2^4 before they are divided: of n positions seen, values above 2^124 / n may come out
  * infinite.
- * Any alignment of the cache will do; more than 32 queries of a row and KV head are
- * fastest where its keys and values, and their strides, lie at multiples of 16 bytes.
+ * Any alignment of the cache and any finite scale will do; more than 32 queries of a row
+ * and KV head are fastest where its keys and values, and their strides, lie at multiples
+ * of 16 bytes, and |scale| in [1e-30, 1e30].
  * workspace: as cpes_attend_tree_workspace_bytes, 16-byte aligned; needs no
  * particular contents, and calls that overlap in time need their own.
  * Errors: as cpes_attend; tokens < 0, longest outside [1, tokens] with tokens > 0 ->
